@@ -298,9 +298,9 @@ class _Layer:
         self.shape = B.make_shape(T, c["d"], E, k, c.get("f", 256), c.get("fs", 0))
         if c["op"] == "experts":
             self.plan = B.plan_bufs(*(st[n] for n in ("counts", "offsets", "perm", "route_pos")))
-            self.weights = B.i8_weights_struct(*(st.get(a + n) for a in ("W", "S") for n in ("g", "u", "d")),
+            self.weights = B.int_weights_struct(*(st.get(a + n) for a in ("W", "S") for n in ("g", "u", "d")),
                                                *(st.get(a + n) for a in ("W", "S") for n in ("gs", "us", "ds")))
-            self.ws = torch.empty(B.moe_i8_workspace_bytes(self.shape), dtype=torch.uint8, device=DEV)
+            self.ws = torch.empty(B.moe_int_workspace_bytes(self.shape), dtype=torch.uint8, device=DEV)
             self.Y = torch.empty(T, c["d"], dtype=BF, device=DEV)
             return
         self.routing = B.routing(c["score"], groups=c["groups"], top_groups=c["top_groups"],
@@ -327,7 +327,7 @@ def _own(st):
     if op == "route_grad":
         m.B.moe_score_backward(m.shape, m.routing, st["logits"], st["balance"], st["topk_idx"], st["dw"], m.dZ)
         return dict(dZ=m.dZ)
-    m.B.moe_forward_i8(m.shape, st["X"], m.weights, st["topk_idx"], st["topk_w"], m.plan, m.Y, m.ws)
+    m.B.moe_forward_int(m.shape, st["X"], m.weights, st["topk_idx"], st["topk_w"], m.plan, m.Y, m.ws)
     return dict(Y=m.Y)
 
 
