@@ -223,6 +223,58 @@ moe_status moe_route(const moe_shape *shape, const moe_bf16 *X, const moe_bf16 *
                      const float *bias, float *logits, int32_t *topk_idx, float *topk_w,
                      void *ws, size_t ws_bytes, moe_stream stream);
 
+/* Routing by scores: what moe_route does for routers that score their
+ * experts otherwise.  With Z = X W_r + bias as in moe_route, the score s_e of
+ * an expert is sigmoid(Z_e) or the softmax of Z over the row.  The k experts of
+ * a token are those with the largest s_e + balance_e (ties to the lower id);
+ * balance, which a trainer moves to even out the load, steers the choice and
+ * nothing else.  With groups > 1 the experts form groups of E / groups
+ * consecutive ids, and only the experts of the top_groups best groups can be
+ * chosen, a group being as good as its best expert or as the sum of its two
+ * best (ties to the lower group).  The weight of a chosen expert is
+ * scale * s_e, divided by the sum of the chosen experts' scores if renormalise
+ * is 1.  The values that are compared are held in 64 bits (without a balance
+ * and without sums over groups the logits are compared themselves), the
+ * weights in 32.
+ * An expert whose logit or balance is below -1e38 (-inf, and the lowest finite
+ * fp32 and bf16 values) or NaN is out of play: its score is 0, it is no part of
+ * a softmax or of a group's score, and it is chosen, with weight 0, only
+ * where the kept groups hold fewer than k others (lower ids first).  A logit
+ * above the largest finite fp32 value counts as that value. */
+typedef enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 } moe_score;
+typedef enum {
+    MOE_GROUP_MAX = 0,   /* a group's best expert */
+    MOE_GROUP_PAIR = 1   /* the sum of its two best (of its best, if it has no second) */
+} moe_group_score;
+typedef struct {
+    int32_t score;        /* moe_score */
+    int32_t groups;       /* 1 <= groups <= 64, divides E */
+    int32_t top_groups;   /* groups kept; their experts are at least k */
+    int32_t group_score;  /* moe_group_score */
+    int32_t renormalise;  /* 0 or 1 */
+    float scale;          /* finite */
+} moe_routing;
+
+/* Router with scores: arguments, outputs and workspace as moe_route;
+ *   balance [E] fp32 or NULL.
+ * MOE_EINVAL for a routing outside the ranges above, MOE_EUNSUPPORTED for more
+ * than 64 groups. */
+moe_status moe_route_scored(const moe_shape *shape, const moe_routing *routing, const moe_bf16 *X,
+                            const moe_bf16 *W_r, const float *bias, const float *balance,
+                            float *logits, int32_t *topk_idx, float *topk_w, void *ws,
+                            size_t ws_bytes, moe_stream stream);
+
+/* Gradient of moe_route_scored's weights, with the selection held fixed (which
+ * is all that balance takes part in):
+ *   logits [T, E], topk_idx [T, k] and balance as the forward had them,
+ *   dw [T, k] fp32 in: gradient wrt topk_w.
+ *   dZ [T, E] fp32 out: gradient wrt the logits.
+ * Experts out of play have gradient 0; an id outside [0, E) is left out; an id
+ * that a token lists twice counts twice. */
+moe_status moe_score_backward(const moe_shape *shape, const moe_routing *routing,
+                              const float *logits, const float *balance, const int32_t *topk_idx,
+                              const float *dw, float *dZ, moe_stream stream);
+
 /* Dispatch plan (§3.1, Algorithm 1 for one source rank: a stable counting
  * sort of the routes by expert; no host readback).
  *   topk_idx [T, k] int32 in.  plan: counts, offsets, perm, route_pos out.
@@ -490,6 +542,74 @@ moe_status moe_backward_ring(const moe_shape *shape, const moe_bf16 *dY, const m
                              const int32_t *topk_idx, const float *topk_w,
                              const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
                              int64_t ring_rows, void *ws, size_t ws_bytes, moe_stream stream);
+
+/* The backward passes of a layer that moe_route_scored routed: as the entry
+ * points above, with the router's gradient taken through the scores.
+ *   logits [T, E] of moe_route_scored; balance [E] or NULL as it had it. */
+moe_status moe_backward_scored(const moe_shape *shape, const moe_routing *routing,
+                               const float *logits, const float *balance, const moe_bf16 *dY,
+                               const moe_bf16 *X, const moe_bf16 *W_r, const moe_weights *weights,
+                               const int32_t *topk_idx, const float *topk_w,
+                               const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+                               void *ws, size_t ws_bytes, moe_stream stream,
+                               const moe_stage_events *events /* NULL = no timing */);
+moe_status moe_backward_ring_scored(const moe_shape *shape, const moe_routing *routing,
+                                    const float *logits, const float *balance, const moe_bf16 *dY,
+                                    const moe_bf16 *X, const moe_bf16 *W_r,
+                                    const moe_weights *weights, const int32_t *topk_idx,
+                                    const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+                                    const moe_grads *grads, int64_t ring_rows, void *ws,
+                                    size_t ws_bytes, moe_stream stream);
+moe_status moe_backward_mx_scored(const moe_shape *shape, const moe_routing *routing,
+                                  const float *logits, const float *balance, const moe_bf16 *dY,
+                                  const moe_bf16 *X, const moe_bf16 *W_r,
+                                  const moe_weights *weights, const moe_mx_bwd_weights *mx,
+                                  const int32_t *topk_idx, const float *topk_w,
+                                  const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+                                  int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream);
+
+/* Expert weights in 8-bit integers, routed (W) and shared (S), written once by
+ * moe_int_quantize_weights and read by moe_forward_int.  Codes are stored
+ * K-contiguous, i.e. transposed from the bf16 layout, with one fp32 scale per
+ * output channel:
+ *   Wg_q, Wu_q [E, f, d], Wg_s, Wu_s [E, f]      Sg_q, Su_q [f_shared, d], Sg_s, Su_s [f_shared]
+ *   Wd_q       [E, d, f], Wd_s       [E, d]      Sd_q       [d, f_shared], Sd_s       [d]
+ * The S pointers are NULL iff f_shared == 0.  Quantisation of a channel (or,
+ * for activations, of a token's row): scale s = amax / 127 in fp32, code =
+ * x / s rounded to fp32 and then to the nearest integer, ties to even.  A
+ * channel of zeros has scale 0; one that holds an infinity or a NaN has scale
+ * NaN, and whatever it contributes to is NaN. */
+typedef struct {
+    int8_t *Wg_q, *Wu_q, *Wd_q;
+    float *Wg_s, *Wu_s, *Wd_s;
+    int8_t *Sg_q, *Su_q, *Sd_q;
+    float *Sg_s, *Su_s, *Sd_s;
+} moe_int_weights;
+
+/* Quantises the routed and shared weights for moe_forward_int (once per weight
+ * update).  Reads every array of `weights`, writes every array of `i8`.  Extra
+ * limits of the int8 entry points: d, f, f_shared <= 131072; T*d, T*k*f,
+ * T*f_shared, E*f*d and f_shared*d below 2^32 (MOE_EUNSUPPORTED). */
+moe_status moe_int_quantize_weights(const moe_shape *shape, const moe_weights *weights,
+                                   const moe_int_weights *i8, moe_stream stream);
+
+/* Workspace bytes of moe_forward_int (it also serves moe_route,
+ * moe_route_scored and moe_plan); 0 for an invalid or unsupported shape.  Pure
+ * host function. */
+size_t moe_int_workspace_bytes(const moe_shape *shape);
+
+/* Forward of the layer with routed and shared experts in 8-bit integers
+ * (inference).  As moe_forward, except:
+ *   - X is quantised per token, and the up/gate products multiply int8 codes
+ *     with exact 32-bit integer sums, scaled by (token scale) * (channel scale);
+ *   - H = silu(A) * B is quantised per route (per token in the shared expert)
+ *     from fp32, and the down products run likewise;
+ *   - each expert's output is rounded to bf16 before the weighted sum.
+ * Y [T, d] bf16 out.  ws: at least moe_int_workspace_bytes(shape) bytes. */
+moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_int_weights *weights,
+                          const int32_t *topk_idx, const float *topk_w, const moe_plan_bufs *plan,
+                          moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream,
+                          const moe_stage_events *events /* NULL = no timing */);
 
 /* Static strings; never NULL. */
 const char *moe_status_string(moe_status status);

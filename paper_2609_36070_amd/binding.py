@@ -32,7 +32,9 @@ EXPORTS = ("moe_workspace_bytes", "moe_workspace_region", "moe_route", "moe_plan
            "moe_mx_workspace_region", "moe_forward_mx", "moe_ring_workspace_bytes",
            "moe_forward_ring", "moe_backward_ring", "moe_forward_fused",
            "moe_mx_quantize_weights_bwd", "moe_backward_mx", "moe_plan_noalloc", "moe_status_string",
-           "moe_version")
+           "moe_version", "moe_route_scored", "moe_score_backward", "moe_backward_scored",
+           "moe_backward_ring_scored", "moe_backward_mx_scored", "moe_int_quantize_weights",
+           "moe_int_workspace_bytes", "moe_forward_int")
 PLAN_NOALLOC_SCRATCH_BYTES = 4 << 20
 
 
@@ -51,6 +53,20 @@ class MoeMxWeights(ctypes.Structure):
 
 class MoeMxBwdWeights(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in ("Wg_q", "Wu_q", "Wd_q", "Wg_s", "Wu_s", "Wd_s")]
+
+
+class MoeIntWeights(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("Wg_q", "Wu_q", "Wd_q", "Wg_s", "Wu_s", "Wd_s",
+                                        "Sg_q", "Su_q", "Sd_q", "Sg_s", "Su_s", "Sd_s")]
+
+
+SCORES = ("softmax", "sigmoid")
+GROUP_SCORES = ("max", "pair")
+
+
+class MoeRouting(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("score", "groups", "top_groups", "group_score",
+                                              "renormalise")] + [("scale", ctypes.c_float)]
 
 
 class MoePlanBufs(ctypes.Structure):
@@ -133,11 +149,24 @@ def lib():
         L.moe_backward_ring.argtypes = [P(MoeShape), c_void_p, c_void_p, c_void_p, P(MoeWeights),
                                         c_void_p, c_void_p, P(MoePlanBufs), c_void_p, P(MoeGrads),
                                         ctypes.c_int64, c_void_p, c_size_t, c_void_p]
+        scored = [P(MoeShape), P(MoeRouting), c_void_p, c_void_p]   # ..., logits, balance
+        L.moe_route_scored.argtypes = [P(MoeShape), P(MoeRouting)] + [c_void_p] * 8 + [c_size_t, c_void_p]
+        L.moe_score_backward.argtypes = scored + [c_void_p] * 4
+        for fn in ("moe_backward", "moe_backward_ring", "moe_backward_mx"):
+            getattr(L, fn + "_scored").argtypes = scored + getattr(L, fn).argtypes[1:]
+        L.moe_int_quantize_weights.argtypes = [P(MoeShape), P(MoeWeights), P(MoeIntWeights), c_void_p]
+        L.moe_int_workspace_bytes.argtypes = [P(MoeShape)]
+        L.moe_int_workspace_bytes.restype = c_size_t
+        L.moe_forward_int.argtypes = [P(MoeShape), c_void_p, P(MoeIntWeights), c_void_p, c_void_p,
+                                     P(MoePlanBufs), c_void_p, c_void_p, c_size_t, c_void_p,
+                                     P(MoeStageEvents)]
         for fn in ("moe_route", "moe_plan", "moe_schedule", "moe_dispatch", "moe_forward",
                    "moe_backward", "moe_workspace_region", "moe_mx_quantize_weights",
                    "moe_mx_workspace_region", "moe_forward_mx", "moe_forward_ring",
                    "moe_backward_ring", "moe_forward_fused", "moe_mx_quantize_weights_bwd",
-                   "moe_backward_mx"):
+                   "moe_backward_mx", "moe_route_scored", "moe_score_backward", "moe_backward_scored",
+                   "moe_backward_ring_scored", "moe_backward_mx_scored", "moe_int_quantize_weights",
+                   "moe_forward_int"):
             getattr(L, fn).restype = c_int
         L.moe_status_string.argtypes = [c_int]
         L.moe_status_string.restype = ctypes.c_char_p
@@ -372,3 +401,89 @@ def moe_forward_fused(shape, X, weights: MoeWeights, topk_idx, topk_w, plan: Moe
                                  _p(topk_w), ctypes.byref(plan), _p(Y),
                                  int(bool(save_for_backward)), _p(ws), nbytes, _stream(stream))
     return _check("moe_forward_fused", st, raise_on_error)
+
+
+def routing(score="softmax", groups=1, top_groups=None, group_score="max", renormalise=True,
+            scale=1.0) -> MoeRouting:
+    """How moe_route_scored scores, chooses and weights experts (top_groups: None keeps every group)."""
+    return MoeRouting(SCORES.index(score), groups, groups if top_groups is None else top_groups,
+                      GROUP_SCORES.index(group_score), int(bool(renormalise)), scale)
+
+
+def moe_route_scored(shape, routing: MoeRouting, X, W_r, bias, balance, logits, topk_idx, topk_w, ws,
+                     ws_bytes=None, stream=None, raise_on_error=True):
+    nbytes = ws.nbytes if ws_bytes is None else ws_bytes
+    st = lib().moe_route_scored(ctypes.byref(shape), ctypes.byref(routing), _p(X), _p(W_r), _p(bias),
+                                _p(balance), _p(logits), _p(topk_idx), _p(topk_w), _p(ws), nbytes,
+                                _stream(stream))
+    return _check("moe_route_scored", st, raise_on_error)
+
+
+def moe_score_backward(shape, routing: MoeRouting, logits, balance, topk_idx, dw, dZ, stream=None,
+                       raise_on_error=True):
+    st = lib().moe_score_backward(ctypes.byref(shape), ctypes.byref(routing), _p(logits), _p(balance),
+                                  _p(topk_idx), _p(dw), _p(dZ), _stream(stream))
+    return _check("moe_score_backward", st, raise_on_error)
+
+
+def moe_backward_scored(shape, routing: MoeRouting, logits, balance, dY, X, W_r, weights: MoeWeights,
+                        topk_idx, topk_w, plan: MoePlanBufs, dX, grads: MoeGrads, ws, ws_bytes=None,
+                        stream=None, raise_on_error=True, events: MoeStageEvents = None):
+    nbytes = ws.nbytes if ws_bytes is None else ws_bytes
+    st = lib().moe_backward_scored(ctypes.byref(shape), ctypes.byref(routing), _p(logits), _p(balance),
+                                   _p(dY), _p(X), _p(W_r), ctypes.byref(weights), _p(topk_idx),
+                                   _p(topk_w), ctypes.byref(plan), _p(dX), ctypes.byref(grads), _p(ws),
+                                   nbytes, _stream(stream),
+                                   None if events is None else ctypes.byref(events))
+    return _check("moe_backward_scored", st, raise_on_error)
+
+
+def moe_backward_ring_scored(shape, routing: MoeRouting, logits, balance, dY, X, W_r,
+                             weights: MoeWeights, topk_idx, topk_w, plan: MoePlanBufs, dX,
+                             grads: MoeGrads, ring_rows, ws, ws_bytes=None, stream=None,
+                             raise_on_error=True):
+    nbytes = ws.nbytes if ws_bytes is None else ws_bytes
+    st = lib().moe_backward_ring_scored(ctypes.byref(shape), ctypes.byref(routing), _p(logits),
+                                        _p(balance), _p(dY), _p(X), _p(W_r), ctypes.byref(weights),
+                                        _p(topk_idx), _p(topk_w), ctypes.byref(plan), _p(dX),
+                                        ctypes.byref(grads), int(ring_rows), _p(ws), nbytes,
+                                        _stream(stream))
+    return _check("moe_backward_ring_scored", st, raise_on_error)
+
+
+def moe_backward_mx_scored(shape, routing: MoeRouting, logits, balance, dY, X, W_r, weights: MoeWeights,
+                           mx: MoeMxBwdWeights, topk_idx, topk_w, plan: MoePlanBufs, dX, grads: MoeGrads,
+                           ws, ws_bytes=None, stream=None, raise_on_error=True, wgrad_mxfp8=False):
+    nbytes = ws.nbytes if ws_bytes is None else ws_bytes
+    st = lib().moe_backward_mx_scored(ctypes.byref(shape), ctypes.byref(routing), _p(logits),
+                                      _p(balance), _p(dY), _p(X), _p(W_r), ctypes.byref(weights),
+                                      ctypes.byref(mx), _p(topk_idx), _p(topk_w), ctypes.byref(plan),
+                                      _p(dX), ctypes.byref(grads), int(wgrad_mxfp8), _p(ws), nbytes,
+                                      _stream(stream))
+    return _check("moe_backward_mx_scored", st, raise_on_error)
+
+
+def int_weights_struct(Wg_q, Wu_q, Wd_q, Wg_s, Wu_s, Wd_s, Sg_q=None, Su_q=None, Sd_q=None, Sg_s=None,
+                      Su_s=None, Sd_s=None) -> MoeIntWeights:
+    return MoeIntWeights(_p(Wg_q), _p(Wu_q), _p(Wd_q), _p(Wg_s), _p(Wu_s), _p(Wd_s),
+                        _p(Sg_q), _p(Su_q), _p(Sd_q), _p(Sg_s), _p(Su_s), _p(Sd_s))
+
+
+def moe_int_quantize_weights(shape, weights: MoeWeights, weights_int: MoeIntWeights, stream=None,
+                            raise_on_error=True):
+    st = lib().moe_int_quantize_weights(ctypes.byref(shape), ctypes.byref(weights), ctypes.byref(weights_int),
+                                       _stream(stream))
+    return _check("moe_int_quantize_weights", st, raise_on_error)
+
+
+def moe_int_workspace_bytes(shape: MoeShape) -> int:
+    return int(lib().moe_int_workspace_bytes(ctypes.byref(shape)))
+
+
+def moe_forward_int(shape, X, weights: MoeIntWeights, topk_idx, topk_w, plan: MoePlanBufs, Y, ws,
+                   ws_bytes=None, stream=None, raise_on_error=True, events: MoeStageEvents = None):
+    nbytes = ws.nbytes if ws_bytes is None else ws_bytes
+    st = lib().moe_forward_int(ctypes.byref(shape), _p(X), ctypes.byref(weights), _p(topk_idx),
+                              _p(topk_w), ctypes.byref(plan), _p(Y), _p(ws), nbytes, _stream(stream),
+                              None if events is None else ctypes.byref(events))
+    return _check("moe_forward_int", st, raise_on_error)

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <mutex>
@@ -281,6 +282,103 @@ moe_status check_mx_weights(const moe_shape *s, const moe_weights *w, const moe_
         return MOE_EINVAL;
     }
     return MOE_OK;
+}
+
+moe_status check_routing(const moe_shape *s, const moe_routing *r) {
+    if (!r) return MOE_EINVAL;
+    if (r->score != MOE_SCORE_SOFTMAX && r->score != MOE_SCORE_SIGMOID) return MOE_EINVAL;
+    if (r->group_score != MOE_GROUP_MAX && r->group_score != MOE_GROUP_PAIR) return MOE_EINVAL;
+    if (r->renormalise != 0 && r->renormalise != 1) return MOE_EINVAL;
+    if (!std::isfinite(r->scale)) return MOE_EINVAL;
+    if (r->groups < 1 || r->top_groups < 1 || r->top_groups > r->groups || s->E % r->groups)
+        return MOE_EINVAL;
+    if (r->top_groups * (s->E / r->groups) < s->k) return MOE_EINVAL;
+    if (r->groups > 64) return MOE_EUNSUPPORTED;
+    return MOE_OK;
+}
+
+ScoreArgs score_args(const moe_routing &r) {
+    ScoreArgs a;
+    a.sigmoid = r.score == MOE_SCORE_SIGMOID;
+    a.groups = r.groups;
+    a.top_groups = r.top_groups;
+    a.pair = r.group_score == MOE_GROUP_PAIR;
+    a.renorm = r.renormalise;
+    a.scale = r.scale;
+    return a;
+}
+
+// What a backward of a layer routed by scores needs beside moe_backward's
+// arguments.
+struct Scored {
+    const moe_routing *routing;
+    const float *logits, *balance;
+};
+
+moe_status check_scored(const moe_shape *shape, const Scored &sc) {
+    moe_status st = check_shape(shape);
+    if (st != MOE_OK) return st;
+    if ((st = check_routing(shape, sc.routing)) != MOE_OK) return st;
+    return ptr_ok(sc.logits) && opt_ok(sc.balance) ? MOE_OK : MOE_EINVAL;
+}
+
+// dg per plan row and dZ from the partials of the routed dgrad.
+hipError_t router_bwd(const Scored *sc, const float *dgpart, int nparts, const int *route_pos,
+                      const float *topk_w, const int *topk_idx, int T, int k, int E, float *dg, float *dZ,
+                      hipStream_t s) {
+    if (!sc) return launch_softmax_bwd(dgpart, nparts, route_pos, topk_w, topk_idx, T, k, E, dg, dZ, s);
+    return launch_score_bwd(sc->logits, sc->balance, topk_idx, nullptr, dgpart, nparts, route_pos, dg, dZ,
+                            T, E, k, score_args(*sc->routing), s);
+}
+
+// Int8 experts: every operand is addressed with 32-bit offsets, and a dot
+// product of 127^2 K stays below 2^31.
+moe_status check_i8_shape(const moe_shape *s) {
+    const int64_t lim = int64_t(1) << 32, kmax = int64_t(1) << 17;
+    if (s->d > kmax || s->f > kmax || s->f_shared > kmax) return MOE_EUNSUPPORTED;
+    if (s->T * s->d >= lim || s->T * s->k * s->f >= lim || s->E * s->f * s->d >= lim ||
+        s->T * s->f_shared >= lim || s->f_shared * s->d >= lim)
+        return MOE_EUNSUPPORTED;
+    return MOE_OK;
+}
+
+moe_status check_i8_weights(const moe_shape *s, const moe_int_weights *w) {
+    if (!w) return MOE_EINVAL;
+    if (!ptr_ok(w->Wg_q) || !ptr_ok(w->Wu_q) || !ptr_ok(w->Wd_q) || !ptr_ok(w->Wg_s) ||
+        !ptr_ok(w->Wu_s) || !ptr_ok(w->Wd_s))
+        return MOE_EINVAL;
+    if (s->f_shared > 0) {
+        if (!ptr_ok(w->Sg_q) || !ptr_ok(w->Su_q) || !ptr_ok(w->Sd_q) || !ptr_ok(w->Sg_s) ||
+            !ptr_ok(w->Su_s) || !ptr_ok(w->Sd_s))
+            return MOE_EINVAL;
+    } else if (w->Sg_q || w->Su_q || w->Sd_q || w->Sg_s || w->Su_s || w->Sd_s) {
+        return MOE_EINVAL;
+    }
+    return MOE_OK;
+}
+
+// Workspace of the int8 forward: the prefix of every layout, then its own.
+struct I8Layout {
+    size_t xq, xs, h, hq, hs, Yexp, hsh, hshq, hshs, Ysh, total;
+};
+
+I8Layout i8_layout(const moe_shape &s) {
+    const size_t T = s.T, d = s.d, f = s.f, fs = s.f_shared, R = T * (size_t)s.k;
+    I8Layout L{};
+    size_t o = make_layout(s).prefix_total;
+    auto take = [&](size_t bytes) { const size_t at = o; o += up(bytes > 0 ? bytes : 1); return at; };
+    L.xq = take(T * d);
+    L.xs = take(T * 4);
+    L.h = take(R * f * 4);
+    L.hq = take(R * f);
+    L.hs = take(R * 4);
+    L.Yexp = take(R * d * 2);
+    L.hsh = take(T * fs * 4);
+    L.hshq = take(T * fs);
+    L.hshs = take(fs ? T * 4 : 0);
+    L.Ysh = take(fs ? T * d * 2 : 0);
+    L.total = o;
+    return L;
 }
 
 // Records stage event i (if requested) on the stream.
@@ -885,6 +983,40 @@ moe_status moe_route(const moe_shape *shape, const moe_bf16 *X, const moe_bf16 *
     return MOE_OK;
 }
 
+moe_status moe_route_scored(const moe_shape *shape, const moe_routing *routing, const moe_bf16 *X,
+                            const moe_bf16 *W_r, const float *bias, const float *balance, float *logits,
+                            int32_t *topk_idx, float *topk_w, void *ws, size_t ws_bytes,
+                            moe_stream stream) {
+    moe_status st = check_shape(shape);
+    if (st != MOE_OK) return st;
+    if ((st = check_routing(shape, routing)) != MOE_OK) return st;
+    if (!ptr_ok(X) || !ptr_ok(W_r) || !opt_ok(bias) || !opt_ok(balance) || !ptr_ok(logits) ||
+        !ptr_ok(topk_idx) || !ptr_ok(topk_w))
+        return MOE_EINVAL;
+    if ((st = check_ws_prefix(shape, ws, ws_bytes)) != MOE_OK) return st;
+    const Layout L = make_layout(*shape);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int T = (int)shape->T, d = (int)shape->d, E = (int)shape->E, k = (int)shape->k;
+    float *part = at<float>(ws, L.rpart);
+    MOE_TRY(launch_route(X, W_r, bias, logits, nullptr, nullptr, at<uint16_t>(ws, L.wrt), part, T, d, E, k,
+                         s));
+    MOE_TRY(launch_score_select(part, route_partials(T, d, E, k), route_epad(E), bias, balance, logits,
+                                topk_idx, topk_w, T, E, k, score_args(*routing), s));
+    return MOE_OK;
+}
+
+moe_status moe_score_backward(const moe_shape *shape, const moe_routing *routing, const float *logits,
+                              const float *balance, const int32_t *topk_idx, const float *dw, float *dZ,
+                              moe_stream stream) {
+    const moe_status st = check_scored(shape, Scored{routing, logits, balance});
+    if (st != MOE_OK) return st;
+    if (!ptr_ok(topk_idx) || !ptr_ok(dw) || !ptr_ok(dZ)) return MOE_EINVAL;
+    MOE_TRY(launch_score_bwd(logits, balance, topk_idx, dw, nullptr, 0, nullptr, nullptr, dZ, (int)shape->T,
+                             (int)shape->E, (int)shape->k, score_args(*routing),
+                             static_cast<hipStream_t>(stream)));
+    return MOE_OK;
+}
+
 moe_status moe_plan(const moe_shape *shape, const int32_t *topk_idx, const moe_plan_bufs *plan,
                     void *ws, size_t ws_bytes, moe_stream stream) {
     moe_status st = check_shape(shape);
@@ -1046,11 +1178,11 @@ moe_status moe_forward_fused(const moe_shape *shape, const moe_bf16 *X, const mo
     return MOE_OK;
 }
 
-moe_status moe_backward(const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
-                        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
-                        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
-                        const moe_grads *grads, void *ws, size_t ws_bytes, moe_stream stream,
-                        const moe_stage_events *events) {
+static moe_status backward_run(const Scored *sc, const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
+        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
+        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+        const moe_grads *grads, void *ws, size_t ws_bytes, moe_stream stream,
+        const moe_stage_events *events) {
     moe_status st = check_backward_args(shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads);
     if (st != MOE_OK) return st;
     if ((st = check_ws(shape, ws, ws_bytes, 1)) != MOE_OK) return st;
@@ -1069,7 +1201,7 @@ moe_status moe_backward(const moe_shape *shape, const moe_bf16 *dY, const moe_bf
     MOE_TRY(mk.mark(1));
     MOE_TRY(routed_dgrad(*shape, L, ws, dY, weights, all, s));
     MOE_TRY(mk.mark(2));
-    MOE_TRY(launch_softmax_bwd(at<float>(ws, L.dgpart), L.dg_parts, plan->route_pos, topk_w, topk_idx,
+    MOE_TRY(router_bwd(sc, at<float>(ws, L.dgpart), L.dg_parts, plan->route_pos, topk_w, topk_idx,
                                T, k, E, at<float>(ws, L.dg), dZ, s));
     if (dense_routing(*shape)) {
         // dX in one product over every expert, the shared expert and the
@@ -1116,6 +1248,25 @@ moe_status moe_backward(const moe_shape *shape, const moe_bf16 *dY, const moe_bf
                                    dZ, W_r, plan->route_pos, T, d, k, E, nullptr, dX, s));
     MOE_TRY(mk.mark(11));
     return MOE_OK;
+}
+
+moe_status moe_backward(const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
+        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
+        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+        const moe_grads *grads, void *ws, size_t ws_bytes, moe_stream stream,
+        const moe_stage_events *events) {
+    return backward_run(nullptr, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ws, ws_bytes, stream, events);
+}
+
+moe_status moe_backward_scored(const moe_shape *shape, const moe_routing *routing, const float *logits,
+        const float *balance, const moe_bf16 *dY, const moe_bf16 *X,
+        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
+        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+        const moe_grads *grads, void *ws, size_t ws_bytes, moe_stream stream,
+        const moe_stage_events *events) {
+    const Scored sc{routing, logits, balance};
+    const moe_status st = check_scored(shape, sc);
+    return st != MOE_OK ? st : backward_run(&sc, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ws, ws_bytes, stream, events);
 }
 
 size_t moe_ring_workspace_bytes(const moe_shape *shape, int64_t ring_rows, int with_backward) {
@@ -1201,11 +1352,11 @@ moe_status moe_forward_ring(const moe_shape *shape, const moe_bf16 *X, const moe
     return MOE_OK;
 }
 
-moe_status moe_backward_ring(const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
-                             const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
-                             const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
-                             const moe_grads *grads, int64_t ring_rows, void *ws, size_t ws_bytes,
-                             moe_stream stream) {
+static moe_status backward_ring_run(const Scored *sc, const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
+        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
+        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+        const moe_grads *grads, int64_t ring_rows, void *ws, size_t ws_bytes,
+        moe_stream stream) {
     moe_status st = check_backward_args(shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads);
     if (st != MOE_OK) return st;
     if ((st = check_ring(ring_rows)) != MOE_OK) return st;
@@ -1262,7 +1413,7 @@ moe_status moe_backward_ring(const moe_shape *shape, const moe_bf16 *dY, const m
             // takes the shared expert's segments, the last the router term
             // (every dg is known once the last window's dgrad has run)
             if (m == nwin - 1) {
-                MOE_TRY(launch_softmax_bwd(at<float>(ws, L.dgpart), L.dg_parts, plan->route_pos, topk_w,
+                MOE_TRY(router_bwd(sc, at<float>(ws, L.dgpart), L.dg_parts, plan->route_pos, topk_w,
                                            topk_idx, T, k, E, at<float>(ws, L.dg), dZ, s));
                 MOE_TRY(launch_router_split(dZ, W_r, T, d, E, at<uint16_t>(ws, L.dzs),
                                             at<uint16_t>(ws, L.wrs), s));
@@ -1309,11 +1460,30 @@ moe_status moe_backward_ring(const moe_shape *shape, const moe_bf16 *dY, const m
         MOE_TRY(launch_dwr(X, dZ, T, d, E, at<float>(ws, L.dwr_part), grads->dW_r, s));
         return MOE_OK;
     }
-    MOE_TRY(launch_softmax_bwd(at<float>(ws, L.dgpart), L.dg_parts, plan->route_pos, topk_w, topk_idx,
+    MOE_TRY(router_bwd(sc, at<float>(ws, L.dgpart), L.dg_parts, plan->route_pos, topk_w, topk_idx,
                                T, k, E, at<float>(ws, L.dg), dZ, s));
     MOE_TRY(launch_dwr(X, dZ, T, d, E, at<float>(ws, L.dwr_part), grads->dW_r, s));
     MOE_TRY(launch_reverse_combine(nullptr, nullptr, dZ, W_r, plan->route_pos, T, d, k, E, acc, dX, s));
     return MOE_OK;
+}
+
+moe_status moe_backward_ring(const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
+        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
+        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+        const moe_grads *grads, int64_t ring_rows, void *ws, size_t ws_bytes,
+        moe_stream stream) {
+    return backward_ring_run(nullptr, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ring_rows, ws, ws_bytes, stream);
+}
+
+moe_status moe_backward_ring_scored(const moe_shape *shape, const moe_routing *routing, const float *logits,
+        const float *balance, const moe_bf16 *dY, const moe_bf16 *X,
+        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
+        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+        const moe_grads *grads, int64_t ring_rows, void *ws, size_t ws_bytes,
+        moe_stream stream) {
+    const Scored sc{routing, logits, balance};
+    const moe_status st = check_scored(shape, sc);
+    return st != MOE_OK ? st : backward_ring_run(&sc, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ring_rows, ws, ws_bytes, stream);
 }
 
 size_t moe_mx_workspace_bytes(const moe_shape *shape, int with_backward) {
@@ -1467,11 +1637,11 @@ moe_status moe_mx_quantize_weights_bwd(const moe_shape *shape, const moe_weights
     return MOE_OK;
 }
 
-moe_status moe_backward_mx(const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
-                           const moe_bf16 *W_r, const moe_weights *weights,
-                           const moe_mx_bwd_weights *mx, const int32_t *topk_idx, const float *topk_w,
-                           const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
-                           int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream) {
+static moe_status backward_mx_run(const Scored *sc, const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
+        const moe_bf16 *W_r, const moe_weights *weights,
+        const moe_mx_bwd_weights *mx, const int32_t *topk_idx, const float *topk_w,
+        const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+        int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream) {
     moe_status st = check_backward_args(shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads);
     if (st != MOE_OK) return st;
     if ((st = check_mx_shape(shape)) != MOE_OK) return st;
@@ -1520,7 +1690,7 @@ moe_status moe_backward_mx(const moe_shape *shape, const moe_bf16 *dY, const moe
         g.bs_bytes = (uint32_t)((long)E * f * d / 32);
         MOE_TRY(launch_gemm_mx_dgrad(g, R, E, s));
     }
-    MOE_TRY(launch_softmax_bwd(at<float>(ws, L.dgpart), L.dg_parts / 2, plan->route_pos, topk_w, topk_idx,
+    MOE_TRY(router_bwd(sc, at<float>(ws, L.dgpart), L.dg_parts / 2, plan->route_pos, topk_w, topk_idx,
                                T, k, E, at<float>(ws, L.dg), dZ, s));
     {   // dXperm = Q(dA) Q(W_gate)^T + Q(dB) Q(W_up)^T
         MxGemmArgs g;
@@ -1596,6 +1766,122 @@ moe_status moe_backward_mx(const moe_shape *shape, const moe_bf16 *dY, const moe
     MOE_TRY(launch_dwr(X, dZ, T, d, E, at<float>(ws, L.dwr_part), grads->dW_r, s));
     MOE_TRY(launch_reverse_combine(at<uint16_t>(ws, L.dXperm), shared ? at<uint16_t>(ws, L.dXsh) : nullptr,
                                    dZ, W_r, plan->route_pos, T, d, k, E, nullptr, dX, s));
+    return MOE_OK;
+}
+
+moe_status moe_backward_mx(const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
+        const moe_bf16 *W_r, const moe_weights *weights,
+        const moe_mx_bwd_weights *mx, const int32_t *topk_idx, const float *topk_w,
+        const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+        int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream) {
+    return backward_mx_run(nullptr, shape, dY, X, W_r, weights, mx, topk_idx, topk_w, plan, dX, grads, wgrad_mxfp8, ws, ws_bytes, stream);
+}
+
+moe_status moe_backward_mx_scored(const moe_shape *shape, const moe_routing *routing, const float *logits,
+        const float *balance, const moe_bf16 *dY, const moe_bf16 *X,
+        const moe_bf16 *W_r, const moe_weights *weights,
+        const moe_mx_bwd_weights *mx, const int32_t *topk_idx, const float *topk_w,
+        const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+        int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream) {
+    const Scored sc{routing, logits, balance};
+    const moe_status st = check_scored(shape, sc);
+    return st != MOE_OK ? st : backward_mx_run(&sc, shape, dY, X, W_r, weights, mx, topk_idx, topk_w, plan, dX, grads, wgrad_mxfp8, ws, ws_bytes, stream);
+}
+
+moe_status moe_int_quantize_weights(const moe_shape *shape, const moe_weights *weights,
+                                   const moe_int_weights *i8, moe_stream stream) {
+    moe_status st = check_shape(shape);
+    if (st != MOE_OK) return st;
+    if ((st = check_i8_shape(shape)) != MOE_OK) return st;
+    if ((st = check_weights(shape, weights)) != MOE_OK) return st;
+    if ((st = check_i8_weights(shape, i8)) != MOE_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int E = (int)shape->E, d = (int)shape->d, f = (int)shape->f, fs = (int)shape->f_shared;
+    auto quant = [&](const moe_bf16 *W, int n, int K, int N, int8_t *q, float *sc) {
+        return launch_i8_quant_weights(W, n, K, N, reinterpret_cast<uint8_t *>(q), sc, s);
+    };
+    MOE_TRY(quant(weights->W_gate, E, d, f, i8->Wg_q, i8->Wg_s));
+    MOE_TRY(quant(weights->W_up, E, d, f, i8->Wu_q, i8->Wu_s));
+    MOE_TRY(quant(weights->W_down, E, f, d, i8->Wd_q, i8->Wd_s));
+    if (fs > 0) {
+        MOE_TRY(quant(weights->Wg_s, 1, d, fs, i8->Sg_q, i8->Sg_s));
+        MOE_TRY(quant(weights->Wu_s, 1, d, fs, i8->Su_q, i8->Su_s));
+        MOE_TRY(quant(weights->Wd_s, 1, fs, d, i8->Sd_q, i8->Sd_s));
+    }
+    return MOE_OK;
+}
+
+size_t moe_int_workspace_bytes(const moe_shape *shape) {
+    if (check_shape(shape) != MOE_OK || check_i8_shape(shape) != MOE_OK) return 0;
+    return i8_layout(*shape).total;
+}
+
+moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_int_weights *weights,
+                          const int32_t *topk_idx, const float *topk_w, const moe_plan_bufs *plan,
+                          moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream,
+                          const moe_stage_events *events) {
+    moe_status st = check_shape(shape);
+    if (st != MOE_OK) return st;
+    if ((st = check_i8_shape(shape)) != MOE_OK) return st;
+    if (!ptr_ok(X) || !ptr_ok(topk_idx) || !ptr_ok(topk_w) || !ptr_ok(Y)) return MOE_EINVAL;
+    if ((st = check_i8_weights(shape, weights)) != MOE_OK) return st;
+    if ((st = check_plan(plan)) != MOE_OK) return st;
+    if (!ptr_ok(ws)) return MOE_EINVAL;
+    const I8Layout Q = i8_layout(*shape);
+    if (ws_bytes < Q.total) return MOE_ENOSPACE;
+    const Layout L = make_layout(*shape);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int T = (int)shape->T, d = (int)shape->d, E = (int)shape->E, k = (int)shape->k;
+    const int f = (int)shape->f, fs = (int)shape->f_shared, R = T * k;
+    const StageMarks mk{events, s};
+    auto bytes = [](const int8_t *p) { return reinterpret_cast<const uint8_t *>(p); };
+    uint8_t *xq = at<uint8_t>(ws, Q.xq), *hq = at<uint8_t>(ws, Q.hq), *hshq = at<uint8_t>(ws, Q.hshq);
+    float *xs = at<float>(ws, Q.xs), *hs = at<float>(ws, Q.hs), *hshs = at<float>(ws, Q.hshs);
+
+    I8GemmArgs up;
+    up.offsets = plan->offsets; up.rowidx = at<int>(ws, L.rowidx); up.E = E;
+    auto up_product = [&](const int8_t *g, const float *gs, const int8_t *u, const float *us, int n, int rows,
+                          int N, float *H) {
+        I8Product p;
+        p.A = xq; p.As = xs; p.a_nrows = T > 0 ? T : 1; p.a_bytes = (uint32_t)((long)p.a_nrows * d);
+        p.B = bytes(g); p.Bs = gs; p.B2 = bytes(u); p.Bs2 = us;
+        p.b_bytes = (uint32_t)((long)n * N * d);
+        p.rows = rows; p.K = d; p.N = N; p.H = H;
+        return p;
+    };
+    auto down_product = [&](const uint8_t *a, const float *as, const int8_t *w, const float *wsc, int n, int rows,
+                            int K, uint16_t *C) {
+        I8Product p;
+        p.A = a; p.As = as; p.a_nrows = rows > 0 ? rows : 1; p.a_bytes = (uint32_t)((long)p.a_nrows * K);
+        p.B = bytes(w); p.Bs = wsc; p.b_bytes = (uint32_t)((long)n * K * d);
+        p.rows = rows; p.K = K; p.N = d; p.C = C;
+        return p;
+    };
+    const moe_int_weights &w = *weights;
+    I8GemmArgs down = up;
+    up.routed = up_product(w.Wg_q, w.Wg_s, w.Wu_q, w.Wu_s, E, R, f, at<float>(ws, Q.h));
+    down.routed = down_product(hq, hs, w.Wd_q, w.Wd_s, E, R, f, at<uint16_t>(ws, Q.Yexp));
+    if (fs > 0) {
+        up.shared = up_product(w.Sg_q, w.Sg_s, w.Su_q, w.Su_s, 1, T, fs, at<float>(ws, Q.hsh));
+        down.shared = down_product(hshq, hshs, w.Sd_q, w.Sd_s, 1, T, fs, at<uint16_t>(ws, Q.Ysh));
+    }
+
+    MOE_TRY(mk.mark(0));
+    MOE_TRY(launch_prep(plan->perm, plan->offsets, E, topk_w, k, T, at<int>(ws, L.rowidx),
+                        at<float>(ws, L.wperm), at<uint16_t>(ws, L.zeros), s));
+    MOE_TRY(launch_i8_quant_rows(X, T, d, xq, xs, s));
+    MOE_TRY(mk.mark(1));
+    MOE_TRY(launch_gemm_i8_up(up, s));
+    MOE_TRY(mk.mark(2));
+    MOE_TRY(launch_i8_quant_rows_f32(up.routed.H, R, f, hq, hs, s));
+    if (fs > 0) MOE_TRY(launch_i8_quant_rows_f32(up.shared.H, T, fs, hshq, hshs, s));
+    MOE_TRY(mk.mark(3));
+    MOE_TRY(launch_gemm_i8_down(down, s));
+    MOE_TRY(mk.mark(4));
+    MOE_TRY(mk.mark(5));
+    MOE_TRY(launch_combine(at<uint16_t>(ws, Q.Yexp), fs > 0 ? at<uint16_t>(ws, Q.Ysh) : nullptr, topk_w,
+                           plan->route_pos, T, d, k, Y, s));
+    MOE_TRY(mk.mark(6));
     return MOE_OK;
 }
 

@@ -1,0 +1,171 @@
+// Quantisation to 8-bit integers (rule in i8_common.h):
+//
+//   i8_quant_rows:    one scale per row of a K-contiguous matrix: tokens of X
+//                     (bf16), rows of the gated activation (fp32).
+//   i8_quant_weights: [E][K][N] bf16 weights -> K-contiguous [E][N][K] codes
+//                     and one scale per channel [E][N], the operand layout of
+//                     the int8 products.
+#include "common.h"
+#include "i8_common.h"
+#include "kernels.h"
+
+namespace {
+
+DEV void load8(const uint16_t *p, float (&v)[8]) {
+    const u32x4_t w = ld_u32x4(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[2 * j] = bf_lo(w[j]);
+        v[2 * j + 1] = bf_hi(w[j]);
+    }
+}
+DEV void load8(const float *p, float (&v)[8]) {
+    const f32x8 w = ld_f32x8(p);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = w[j];
+}
+
+// Largest of a value over the 4 waves of a block.
+DEV uint32_t block_max(uint32_t x, uint32_t *red) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x = umax(x, (uint32_t)__shfl_xor((int)x, m, 64));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return umax(umax(red[0], red[1]), umax(red[2], red[3]));
+}
+
+// A block per row, 8 elements per thread and step.  Rows of up to 2048 NC
+// elements are held in registers between the two passes (NC = 0: read again).
+template <typename S, int NC>
+__global__ __launch_bounds__(256) void i8_quant_rows_kernel(const S *__restrict__ X, int K,
+                                                            uint8_t *__restrict__ q,
+                                                            float *__restrict__ sc) {
+    __shared__ uint32_t red[4];
+    const long row = blockIdx.x;
+    const S *x = X + row * K;
+    uint8_t *o = q + row * K;
+    const int n8 = K / 8;
+    float v[NC > 0 ? NC : 1][8];
+    uint32_t amax = 0;
+    auto put = [&](const float (&y)[8], const I8Scale &s, int c) {
+        *reinterpret_cast<u32x2_t *>(o + 8 * c) =
+            u32x2_t{pack_i8(s.code(y[0]), s.code(y[1]), s.code(y[2]), s.code(y[3])),
+                    pack_i8(s.code(y[4]), s.code(y[5]), s.code(y[6]), s.code(y[7]))};
+    };
+    if constexpr (NC > 0) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = threadIdx.x + 256 * i;
+            if (c < n8) load8(x + 8 * c, v[i]);
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) amax = umax(amax, abs_bits(v[i][j]));
+        const I8Scale s(block_max(amax, red));
+        if (threadIdx.x == 0) sc[row] = s.s;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = threadIdx.x + 256 * i;
+            if (c < n8) put(v[i], s, c);
+        }
+    } else {
+        for (int c = threadIdx.x; c < n8; c += 256) {
+            load8(x + 8 * c, v[0]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) amax = umax(amax, abs_bits(v[0][j]));
+        }
+        const I8Scale s(block_max(amax, red));
+        if (threadIdx.x == 0) sc[row] = s.s;
+        for (int c = threadIdx.x; c < n8; c += 256) {
+            load8(x + 8 * c, v[0]);
+            put(v[0], s, c);
+        }
+    }
+}
+
+// A block per 64 channels of an expert: the channels' largest magnitudes over
+// all K rows, then the codes, 128 rows at a time through LDS so that reads
+// (along n) and writes (along k) are whole 128-byte lines.  The second pass
+// reads what the first left in the caches.
+constexpr int QW_PITCH = 128 + 16;
+__global__ __launch_bounds__(256) void i8_quant_weights_kernel(const uint16_t *__restrict__ W, int K,
+                                                               int N, uint8_t *__restrict__ q,
+                                                               float *__restrict__ sc) {
+    __shared__ __attribute__((aligned(16))) uint8_t tile[64 * QW_PITCH];
+    __shared__ uint32_t red[32][64];
+    const int ntn = N / 64, e = blockIdx.x / ntn, n0 = blockIdx.x % ntn * 64;
+    const int r = threadIdx.x >> 3, c = 8 * (threadIdx.x & 7);
+    const uint16_t *src = W + (long)e * K * N + n0 + c;
+    uint32_t amax[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int k0 = 0; k0 < K; k0 += 128) {    // K is a multiple of 256
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load8(src + (long)(k0 + 32 * i + r) * N, v[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) amax[j] = umax(amax[j], abs_bits(v[i][j]));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) red[r][c + j] = amax[j];
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        uint32_t m = 0;
+        for (int i = 0; i < 32; ++i) m = umax(m, red[i][threadIdx.x]);
+        red[0][threadIdx.x] = m;
+        sc[(long)e * N + n0 + threadIdx.x] = I8Scale(m).s;
+    }
+    __syncthreads();
+    uint32_t top[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top[j] = red[0][c + j];
+    const int oc = threadIdx.x >> 2, ok = 32 * (threadIdx.x & 3);
+    uint8_t *dst = q + ((long)e * N + n0 + oc) * K + ok;
+    for (int k0 = 0; k0 < K; k0 += 128) {
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load8(src + (long)(k0 + 32 * i + r) * N, v[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const I8Scale s(top[j]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tile[(c + j) * QW_PITCH + 32 * i + r] = (uint8_t)s.code(v[i][j]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            st_u32x4(dst + k0 + 16 * h, ld_u32x4(tile + oc * QW_PITCH + ok + 16 * h));
+        __syncthreads();
+    }
+}
+
+template <typename S>
+hipError_t quant_rows(const S *X, long rows, int K, uint8_t *q, float *sc, hipStream_t st) {
+    if (rows <= 0) return hipSuccess;
+    const dim3 grid((unsigned)rows), block(256);
+    if (K <= 2048) i8_quant_rows_kernel<S, 1><<<grid, block, 0, st>>>(X, K, q, sc);
+    else if (K <= 4096) i8_quant_rows_kernel<S, 2><<<grid, block, 0, st>>>(X, K, q, sc);
+    else if (K <= 8192) i8_quant_rows_kernel<S, 4><<<grid, block, 0, st>>>(X, K, q, sc);
+    else i8_quant_rows_kernel<S, 0><<<grid, block, 0, st>>>(X, K, q, sc);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_i8_quant_rows(const uint16_t *X, long rows, int K, uint8_t *q, float *sc,
+                                hipStream_t st) {
+    return quant_rows(X, rows, K, q, sc, st);
+}
+hipError_t launch_i8_quant_rows_f32(const float *X, long rows, int K, uint8_t *q, float *sc,
+                                    hipStream_t st) {
+    return quant_rows(X, rows, K, q, sc, st);
+}
+hipError_t launch_i8_quant_weights(const uint16_t *W, int E, int K, int N, uint8_t *q, float *sc,
+                                   hipStream_t st) {
+    i8_quant_weights_kernel<<<dim3((unsigned)(E * (N / 64))), dim3(256), 0, st>>>(W, K, N, q, sc);
+    return hipGetLastError();
+}

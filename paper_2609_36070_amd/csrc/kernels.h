@@ -165,9 +165,31 @@ int route_epad(int E);
 // Scratch of the split router (many experts): fp32 partial logits of its d
 // slices; 0 for shapes on the one-pass router.
 size_t route_part_bytes(long T, int d, int E);
+// Slices of the d axis whose partial logits launch_route leaves in `part` when
+// it is not to select (topk_idx null); 0: it writes the logits.
+int route_partials(long T, int d, int E, int k);
 hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bias, float *logits,
                         int *topk_idx, float *topk_w, uint16_t *WrT, float *part, int T,
                         int d, int E, int k, hipStream_t st);
+
+// Selection by scores and its gradient (score.hip).
+struct ScoreArgs {
+    int sigmoid = 0;      // 0: softmax over the row
+    int groups = 1, top_groups = 1, pair = 0;
+    int renorm = 1;
+    float scale = 1.0f;
+};
+// part: fp32 partial logits of S slices [S][T][epad] that are added, with the
+// bias, into `logits`; S = 0: the logits are there.
+hipError_t launch_score_select(const float *part, int S, int epad, const float *bias,
+                               const float *balance, float *logits, int *topk_idx, float *topk_w, int T,
+                               int E, int k, const ScoreArgs &a, hipStream_t st);
+// The gradient of the routing weights: dw [T][k], or (dw null) the sums of the
+// nparts partials per plan row, which then go to dg_out as well.
+hipError_t launch_score_bwd(const float *logits, const float *balance, const int *topk_idx,
+                            const float *dw, const float *dgpart, int nparts, const int *route_pos,
+                            float *dg_out, float *dZ, int T, int E, int k, const ScoreArgs &a,
+                            hipStream_t st);
 
 int plan_nblocks(long R);
 hipError_t launch_plan(const int *topk_idx, int R, int E, int *counts, int *offsets, int *perm,
@@ -245,6 +267,35 @@ hipError_t launch_mx_quant_weights(const uint16_t *W, int E, int K, int N, uint8
 
 int sched_nchunks(long NK);
 int sched_rpad(int R);
+// Int8 experts (gemm_i8.hip): the product of one weight, for the plan's rows or
+// the shared expert's tokens.
+struct I8Product {
+    const uint8_t *A = nullptr;        // [a_nrows][K] codes
+    const float *As = nullptr;         // [a_nrows] scales
+    const uint8_t *B = nullptr;        // [E][N][K] codes (up product: gate rows), one scale per row
+    const float *Bs = nullptr;
+    const uint8_t *B2 = nullptr;       // up product: up rows
+    const float *Bs2 = nullptr;
+    int a_nrows = 1, rows = 0, K = 0, N = 0;
+    uint32_t a_bytes = 0, b_bytes = 0; // operand extents (< 4 GiB)
+    float *H = nullptr;                // up product: silu(gate) * up, fp32 [rows][N]
+    uint16_t *C = nullptr;             // down product: bf16 [rows][N]
+};
+struct I8GemmArgs {
+    I8Product routed, shared;          // shared.N = 0: no shared expert
+    const int *offsets = nullptr;      // [E+1] expert regions
+    const int *rowidx = nullptr;       // up product: token of each plan row
+    int E = 0;
+    int shared_grid = 0;               // set by the launcher
+};
+hipError_t launch_gemm_i8_up(const I8GemmArgs &a, hipStream_t st);
+hipError_t launch_gemm_i8_down(const I8GemmArgs &a, hipStream_t st);
+hipError_t launch_i8_quant_rows(const uint16_t *X, long rows, int K, uint8_t *q, float *sc,
+                                hipStream_t st);
+hipError_t launch_i8_quant_rows_f32(const float *X, long rows, int K, uint8_t *q, float *sc,
+                                    hipStream_t st);
+hipError_t launch_i8_quant_weights(const uint16_t *W, int E, int K, int N, uint8_t *q, float *sc,
+                                   hipStream_t st);
 hipError_t launch_schedule(const int *A, int R, int NK, int L, int c, int *M, int *S, int *phi,
                            long phi_rows, int *counts, int *flags, int *err, hipStream_t st);
 

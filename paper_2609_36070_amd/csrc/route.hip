@@ -15,6 +15,7 @@
 #include "common.h"
 #include "kernels.h"
 #include "rules.h"
+#include "topk.h"
 
 namespace {
 
@@ -73,47 +74,6 @@ DEV uint64_t pack_entry(uint32_t key, int id) {
     return ((uint64_t)key << 32) | (uint32_t)(0xffff - id);
 }
 DEV int entry_id(uint64_t v) { return 0xffff - (int)(uint32_t)v; }
-// put the better of a, b first
-DEV void order2(uint64_t &a, uint64_t &b) {
-    const bool sw = b > a;
-    const uint64_t x = a, y = b;
-    a = sw ? y : x;
-    b = sw ? x : y;
-}
-DEV uint64_t shfl_xor_u64(uint64_t v, int m) {
-    const int lo = __shfl_xor((int)(uint32_t)v, m, 64);
-    const int hi = __shfl_xor((int)(uint32_t)(v >> 32), m, 64);
-    return ((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo;
-}
-// Sort N entries best first (bitonic network, N a power of two).
-template <int N>
-DEV void sort_desc(uint64_t (&a)[N]) {
-#pragma unroll
-    for (int size = 2; size <= N; size <<= 1)
-#pragma unroll
-        for (int stride = size / 2; stride > 0; stride >>= 1)
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int j = i ^ stride;
-                if (j > i) {
-                    if ((i & size) == 0 || size == N) order2(a[i], a[j]);
-                    else order2(a[j], a[i]);
-                }
-            }
-}
-// a, b sorted best first: a becomes the best N of both, sorted (the
-// elementwise better of a and reversed b is bitonic; half-cleaners sort it).
-template <int N>
-DEV void merge_best(uint64_t (&a)[N], uint64_t (&b)[N]) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) order2(a[j], b[N - 1 - j]);
-#pragma unroll
-    for (int len = N / 2; len >= 1; len >>= 1)
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if ((j & len) == 0) order2(a[j], a[j + len]);
-}
-
 template <int EPAD, int KP>
 DEV void select_topk(const float *zs, int ld, int BT, int NW, int t0, int T, int E, int k,
                      int *__restrict__ topk_idx, float *__restrict__ topk_w) {
@@ -299,7 +259,8 @@ __global__ __launch_bounds__(64 * NW) void route_kernel(const uint16_t *__restri
 
     // top-k (ties to the lower expert id), ids ascending, renormalised
     // softmax weights; see select_topk.
-    select_block<EPAD>(&zs[0][0], EPAD + 1, BT, NW, t0, T, E, k, topk_idx, topk_w);
+    if (topk_idx)
+        select_block<EPAD>(&zs[0][0], EPAD + 1, BT, NW, t0, T, E, k, topk_idx, topk_w);
 }
 
 
@@ -454,7 +415,8 @@ __global__ __launch_bounds__(512) void route_split_kernel(const uint16_t *__rest
         zs[r * (EPAD + 1) + e] = z;
     }
     __syncthreads();
-    select_block<EPAD>(zs, EPAD + 1, RT, 8, t0, T, E, k, topk_idx, topk_w);
+    if (topk_idx)
+        select_block<EPAD>(zs, EPAD + 1, RT, 8, t0, T, E, k, topk_idx, topk_w);
 }
 
 
@@ -610,7 +572,8 @@ __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
         }
     }
     __syncthreads();
-    select_block<EPAD>(&zs[0][0], EPAD + 1, BT, NW, t0, T, E, k, topk_idx, topk_w);
+    if (topk_idx)
+        select_block<EPAD>(&zs[0][0], EPAD + 1, BT, NW, t0, T, E, k, topk_idx, topk_w);
 }
 
 }  // namespace
@@ -630,11 +593,18 @@ int route_split_slices(long T, int d, int E) {
     return S;
 }
 
+int route_partials(long T, int d, int E, int k) {
+    const int S = route_direct(T, d, E, k) ? 0 : route_split_slices(T, d, E);
+    return S > 1 ? S : 0;
+}
+
 size_t route_part_bytes(long T, int d, int E) {
     const int S = route_split_slices(T, d, E);
     return S > 1 ? (size_t)S * (size_t)T * (size_t)route_epad(E) * 4 : 0;
 }
 
+// topk_idx null: the logits alone, for a selection by scores (score.hip); with
+// route_partials(T, d, E, k) slices they stay fp32 partial sums in `part`.
 hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bias, float *logits,
                         int *topk_idx, float *topk_w, uint16_t *WrT, float *part, int T,
                         int d, int E, int k, hipStream_t st) {
@@ -671,7 +641,7 @@ hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bia
                 break;
             default: return hipErrorInvalidValue;
         }
-        if (S > 1) {
+        if (S > 1 && topk_idx) {
             const dim3 rg((unsigned)((T + RR_BT - 1) / RR_BT)), rb(256);
 #define ROUTE_REDUCE(EP, SL) \
     route_reduce_kernel<EP, SL><<<rg, rb, 0, st>>>(part, bias, logits, topk_idx, topk_w, T, E, k)

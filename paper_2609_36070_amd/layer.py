@@ -32,12 +32,16 @@ class DeviceLayer:
     """All tensors of one layer instance on the GPU, laid out as the C ABI expects."""
 
     def __init__(self, w: Workload, inputs: dict, device="cuda", with_backward=None, mx=False,
-                 ring_rows=None, mx_wgrad=False):
+                 ring_rows=None, mx_wgrad=False, routing=None, int8=False):
         """ring_rows: run forward/backward in bounded memory, with the per-route
         activations in a ring of that many rows (None: room for all T*k routes).
-        mx_wgrad: the MXFP8 backward computes its weight gradients in MXFP8."""
+        mx_wgrad: the MXFP8 backward computes its weight gradients in MXFP8.
+        routing: route by scores (a MoeRouting), with inputs["balance"] if given.
+        int8: the experts in 8-bit integers too (forward_int, step_int)."""
         self.w = w
         self.mx = mx
+        self.routing = routing
+        self.int8 = int8
         self.mx_wgrad = bool(mx_wgrad)
         self.ring_rows = ring_rows
         self.device = torch.device(device)
@@ -49,6 +53,10 @@ class DeviceLayer:
         self.W_r = _dev_bf16(inputs["W_r"], dev)
         self.bias = None if inputs.get("bias") is None else \
             torch.from_numpy(np.asarray(inputs["bias"], np.float32)).to(dev)
+        self.balance = None if inputs.get("balance") is None else \
+            torch.from_numpy(np.asarray(inputs["balance"], np.float32)).to(dev)
+        if routing is None and self.balance is not None:
+            raise ValueError("a balance belongs to routing by scores")
         self.W_gate = _dev_bf16(inputs["W_gate"], dev)
         self.W_up = _dev_bf16(inputs["W_up"], dev)
         self.W_down = _dev_bf16(inputs["W_down"], dev)
@@ -81,6 +89,13 @@ class DeviceLayer:
             if mx_bytes == 0:
                 raise ValueError(f"shape unsupported in MXFP8 {w}")
             nbytes = max(nbytes, mx_bytes)
+        if int8:
+            if ring_rows is not None:
+                raise ValueError("the int8 forward has no bounded-memory variant")
+            int_bytes = B.moe_int_workspace_bytes(self.shape)
+            if int_bytes == 0:
+                raise ValueError(f"shape unsupported in int8 {w}")
+            nbytes = max(nbytes, int_bytes)
         self.ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
         self.weights = B.weights_struct(self.W_gate, self.W_up, self.W_down,
                                         self.Wg_s, self.Wu_s, self.Wd_s)
@@ -123,8 +138,24 @@ class DeviceLayer:
                                                               self.Wg_scb, self.Wu_scb, self.Wd_scb)
             self.quantize_mx()
 
+        if int8:
+            q, sc = torch.int8, torch.float32
+            self.int_bufs = [torch.empty((E, f, d), dtype=q, device=dev), torch.empty((E, f, d), dtype=q, device=dev),
+                            torch.empty((E, d, f), dtype=q, device=dev), torch.empty((E, f), dtype=sc, device=dev),
+                            torch.empty((E, f), dtype=sc, device=dev), torch.empty((E, d), dtype=sc, device=dev)]
+            if fs:
+                self.int_bufs += [torch.empty((fs, d), dtype=q, device=dev), torch.empty((fs, d), dtype=q, device=dev),
+                                 torch.empty((d, fs), dtype=q, device=dev), torch.empty((fs,), dtype=sc, device=dev),
+                                 torch.empty((fs,), dtype=sc, device=dev), torch.empty((d,), dtype=sc, device=dev)]
+            self.int_weights = B.int_weights_struct(*self.int_bufs)
+            self.quantize_int()
+
     # -- the four calls of the path --------------------------------------
     def route(self, stream=None):
+        if self.routing is not None:
+            B.moe_route_scored(self.shape, self.routing, self.X, self.W_r, self.bias, self.balance,
+                               self.logits, self.topk_idx, self.topk_w, self.ws, stream=stream)
+            return
         B.moe_route(self.shape, self.X, self.W_r, self.bias, self.logits, self.topk_idx,
                     self.topk_w, self.ws, stream=stream)
 
@@ -155,9 +186,20 @@ class DeviceLayer:
         if self.ring_rows is not None:
             if events is not None:
                 raise ValueError("stage events are not recorded in bounded-memory execution")
+            if self.routing is not None:
+                B.moe_backward_ring_scored(self.shape, self.routing, self.logits, self.balance, self.dY,
+                                           self.X, self.W_r, self.weights, self.topk_idx, self.topk_w,
+                                           self.plan_bufs, self.dX, self.grads, self.ring_rows, self.ws,
+                                           stream=stream)
+                return
             B.moe_backward_ring(self.shape, self.dY, self.X, self.W_r, self.weights,
                                 self.topk_idx, self.topk_w, self.plan_bufs, self.dX, self.grads,
                                 self.ring_rows, self.ws, stream=stream)
+            return
+        if self.routing is not None:
+            B.moe_backward_scored(self.shape, self.routing, self.logits, self.balance, self.dY, self.X,
+                                  self.W_r, self.weights, self.topk_idx, self.topk_w, self.plan_bufs,
+                                  self.dX, self.grads, self.ws, stream=stream, events=events)
             return
         B.moe_backward(self.shape, self.dY, self.X, self.W_r, self.weights, self.topk_idx,
                        self.topk_w, self.plan_bufs, self.dX, self.grads, self.ws, stream=stream,
@@ -177,9 +219,29 @@ class DeviceLayer:
                          events=events, save_for_backward=save)
 
     def backward_mx(self, stream=None):
+        if self.routing is not None:
+            B.moe_backward_mx_scored(self.shape, self.routing, self.logits, self.balance, self.dY, self.X,
+                                     self.W_r, self.weights, self.mx_bwd_weights, self.topk_idx,
+                                     self.topk_w, self.plan_bufs, self.dX, self.grads, self.ws,
+                                     stream=stream, wgrad_mxfp8=self.mx_wgrad)
+            return
         B.moe_backward_mx(self.shape, self.dY, self.X, self.W_r, self.weights, self.mx_bwd_weights,
                           self.topk_idx, self.topk_w, self.plan_bufs, self.dX, self.grads, self.ws,
                           stream=stream, wgrad_mxfp8=self.mx_wgrad)
+
+    def quantize_int(self, stream=None):
+        """Quantise the routed and shared weights to int8 (once per weight update)."""
+        B.moe_int_quantize_weights(self.shape, self.weights, self.int_weights, stream=stream)
+
+    def forward_int(self, stream=None, events=None):
+        B.moe_forward_int(self.shape, self.X, self.int_weights, self.topk_idx, self.topk_w,
+                         self.plan_bufs, self.Y, self.ws, stream=stream, events=events)
+
+    def step_int(self, stream=None, fwd_events=None):
+        """Route, plan and the int8 forward."""
+        self.route(stream)
+        self.plan(stream)
+        self.forward_int(stream=stream, events=fwd_events)
 
     def step_mx(self, stream=None, fwd_events=None):
         """Route, plan, the MXFP8 forward (and the MXFP8 backward)."""

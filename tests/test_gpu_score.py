@@ -1,0 +1,307 @@
+"""Routing by scores on the GPU against the float64 oracle: the selection is
+exact on the GPU's own logits, the weights and gradients within the rounding of
+their 32-bit evaluation."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import moe_oracle as O
+from oracle import score_oracle as S
+from paper_2609_36070_amd import binding as B
+from paper_2609_36070_amd.layer import DeviceLayer
+from paper_2609_36070_amd.workloads import Workload, make_inputs, to_bf16
+from tests.parity import assert_close, say, to_np, weights_dict
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@dataclasses.dataclass(frozen=True)
+class Case:
+    T: int
+    d: int
+    E: int
+    k: int
+    score: str = "sigmoid"
+    groups: int = 1
+    top_groups: int = 1
+    group_score: str = "max"
+    renormalise: bool = True
+    scale: float = 1.0
+    balance: float = 0.1
+    bias: float = 0.0
+
+    @property
+    def sel(self):
+        return dict(score=self.score, groups=self.groups, top_groups=self.top_groups,
+                    group_score=self.group_score)
+
+    @property
+    def wts(self):
+        return dict(score=self.score, renormalise=self.renormalise, scale=self.scale)
+
+    def routing(self):
+        return B.routing(renormalise=self.renormalise, scale=self.scale, **self.sel)
+
+
+CASES = [
+    # one launch, a split d axis and the one-pass router; every number of lanes per token
+    Case(1, 256, 1, 1), Case(1, 7168, 256, 8, groups=8, top_groups=4, group_score="pair", scale=2.5),
+    Case(300, 256, 8, 2, "softmax"), Case(17, 512, 16, 16, "softmax", renormalise=False),
+    Case(33, 256, 20, 3, groups=5, top_groups=2), Case(65, 768, 33, 8, "softmax", balance=0.0),
+    Case(2500, 256, 60, 5, groups=5, top_groups=3, group_score="pair"),
+    Case(2100, 512, 64, 6, "softmax", groups=4, top_groups=4, renormalise=False, bias=0.5),
+    Case(257, 1024, 96, 6, "softmax", renormalise=False, balance=0.01),
+    Case(3000, 2048, 128, 8, groups=2, top_groups=1, scale=0.5),
+    Case(3001, 1280, 255, 7, groups=5, top_groups=3, group_score="pair"),
+    Case(2049, 512, 256, 16, "softmax", groups=64, top_groups=5, group_score="pair"),
+    Case(130, 6144, 200, 4, groups=8, top_groups=8, renormalise=False, balance=0.0),
+    Case(5, 256, 256, 1, "softmax", groups=32, top_groups=1, balance=0.0, bias=1.0),
+    Case(64, 256, 51, 9, groups=3, top_groups=2, group_score="pair", balance=0.0),
+    Case(64, 256, 8, 8, groups=8, top_groups=8, group_score="pair"),
+]
+IDS = ["-".join(str(v) for v in dataclasses.astuple(c)) for c in CASES]
+
+
+class Run:
+    """The router's buffers on the device, each with a guard of untouched rows behind it."""
+
+    def __init__(self, c, X, W_r, bias, balance):
+        self.c, self.shape, self.routing = c, B.make_shape(c.T, c.d, c.E, c.k, 256), c.routing()
+        up = lambda a, t: None if a is None else torch.from_numpy(np.ascontiguousarray(a)).to(t).to(DEV)  # noqa: E731
+        self.X, self.W_r = up(X, torch.bfloat16), up(W_r, torch.bfloat16)
+        self.bias, self.balance = up(bias, torch.float32), up(balance, torch.float32)
+        self.logits = torch.full((c.T + 3, c.E), 777.0, device=DEV)
+        self.idx = torch.full((c.T + 3, c.k), -7, dtype=torch.int32, device=DEV)
+        self.w = torch.full((c.T + 3, c.k), 777.0, device=DEV)
+        self.dZ = torch.full((c.T + 3, c.E), 777.0, device=DEV)
+        self.ws = torch.empty(B.moe_workspace_bytes(self.shape, False), dtype=torch.uint8, device=DEV)
+
+    def route(self, stream=None):
+        B.moe_route_scored(self.shape, self.routing, self.X, self.W_r, self.bias, self.balance, self.logits,
+                           self.idx, self.w, self.ws, stream=stream)
+
+    def grad(self, dw, stream=None):
+        B.moe_score_backward(self.shape, self.routing, self.logits, self.balance, self.idx, dw, self.dZ,
+                             stream=stream)
+
+    def outputs(self):
+        T = self.c.T
+        return [to_np(t)[:T] for t in (self.logits, self.idx, self.w, self.dZ)]
+
+    def check_guards(self):
+        T = self.c.T
+        assert (self.logits[T:] == 777).all() and (self.w[T:] == 777).all() and (self.idx[T:] == -7).all()
+        assert (self.dZ[T:] == 777).all()
+
+
+def inputs(c, seed=0):
+    rng = np.random.default_rng(seed)
+    X = to_bf16(rng.standard_normal((c.T, c.d), dtype=np.float32))
+    W_r = to_bf16(rng.standard_normal((c.d, c.E), dtype=np.float32) / np.float32(np.sqrt(c.d)))
+    bias = rng.standard_normal(c.E, dtype=np.float32) * np.float32(c.bias) if c.bias else None
+    balance = rng.standard_normal(c.E, dtype=np.float32) * np.float32(c.balance) if c.balance else None
+    return X, W_r, bias, balance
+
+
+def spread(Z, live):
+    """Largest |z - z'| of a row's experts in play, per token."""
+    z = np.clip(np.where(live, Z, np.nan).astype(np.float64), -1e4, 1e4)
+    top, low = np.where(np.isnan(z), -1e9, z).max(1), np.where(np.isnan(z), 1e9, z).min(1)
+    return np.maximum(top - low, 0.0)[:, None]
+
+
+def check(r, dw):
+    """Selection, weights and gradient of a finished run on its own logits."""
+    c = r.c
+    Z, idx, w, dZ = r.outputs()
+    bal = None if r.balance is None else to_np(r.balance)
+    assert np.array_equal(idx, S.select(Z, bal, c.k, **c.sel))
+    live = S.in_play(Z, bal)
+    # each weight: exponentials of differences of logits (rounded: 2^-24 of the
+    # difference, and about an ulp each), a sum of positive terms and a quotient
+    rel = (24 + 2 * np.minimum(spread(Z, live), 100.0)) * 2.0 ** -24
+    ref = S.weights(Z, bal, idx, **c.wts)
+    assert (np.abs(w - ref) <= rel * np.abs(ref) + 1e-37).all(), np.abs(w - ref).max()
+    g = to_np(dw).astype(np.float64)
+    ref = S.score_backward(Z, bal, idx, g, **c.wts)
+    # dw - sum u dw cancels: its error is that of the larger term
+    on = np.take_along_axis(live, idx, 1)
+    top = np.abs(np.where(on, g, 0)).max(1, keepdims=True)
+    u = S.unscaled_weights(Z, bal, idx, c.score, c.renormalise)
+    size = np.zeros(Z.shape)
+    np.put_along_axis(size, idx, np.abs(u), 1)
+    if c.score == "softmax" and not c.renormalise:
+        size = np.maximum(size, S.scores(Z, live, c.score))
+    tol = (3 * rel + (16 + c.k) * 2.0 ** -24) * c.scale * size * top
+    assert (np.abs(dZ - ref) <= tol + 1e-37).all(), (np.abs(dZ - ref) / (tol + 1e-37)).max()
+    r.check_guards()
+
+
+@pytest.mark.parametrize("c", CASES, ids=IDS)
+def test_route_and_gradient(c):
+    say(f"[gpu] {c}")
+    X, W_r, bias, balance = inputs(c)
+    r = Run(c, X, W_r, bias, balance)
+    r.route()
+    rng = np.random.default_rng(5)
+    dw = torch.from_numpy(rng.standard_normal((c.T, c.k), dtype=np.float32)).to(DEV)
+    r.grad(dw)
+    torch.cuda.synchronize()
+    Zo = O.router_logits(X, W_r, bias)
+    assert np.abs(to_np(r.logits)[:c.T] - Zo).max() <= 1e-4
+    check(r, dw)
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("renormalise", [True, False])
+@pytest.mark.parametrize("groups", [1, 4])
+def test_masks_infinities_and_ties(score, renormalise, groups):
+    """Rows of one-hot tokens against a router of chosen columns: logits of
+    exact ties, +-inf, the lowest finite values, NaN and nothing in play."""
+    E, d, k = 32, 256, 5
+    c = Case(24, d, E, k, score, groups, min(groups, 2), "pair", renormalise, 1.5, 0.05)
+    rng = np.random.default_rng(9)
+    W_r = np.zeros((d, E), np.float32)
+    W_r[:8] = to_bf16(rng.standard_normal((8, E), dtype=np.float32))
+    W_r[1] = 1.0                                    # all equal
+    W_r[2] = np.where(np.arange(E) % 3 == 0, 2.0, -2.0)
+    X = np.zeros((c.T, d), np.float32)
+    big = float(to_bf16(np.array([3e38], np.float32))[0])
+    for t in range(c.T):
+        X[t, t % 8] = big if t >= 16 else 30.0 if t >= 8 else 1.0   # logits to +-inf in the last rows
+    X[5] = 0.0
+    X[6, 0] = np.nan
+    bias = np.zeros(E, np.float32)
+    bias[[3, 9]] = -np.inf, np.finfo(np.float32).min
+    balance = (rng.standard_normal(E) * 0.05).astype(np.float32)
+    balance[[1, 12, 30]] = -np.inf, np.inf, np.nan
+    for bal, bi in ((balance, bias), (None, bias), (None, None),
+                    (np.zeros(E, np.float32), np.full(E, -np.inf, np.float32))):
+        r = Run(c, X, W_r, bi, bal)
+        r.route()
+        dw = torch.from_numpy(rng.standard_normal((c.T, k), dtype=np.float32)).to(DEV)
+        dw[3] = torch.where(r.w[3] == 0, torch.nan, dw[3])   # whatever a masked expert's gradient is
+        r.grad(dw)
+        torch.cuda.synchronize()
+        dw = torch.nan_to_num(dw)
+        assert torch.isfinite(r.w).all() and torch.isfinite(r.dZ).all()
+        check(r, dw)
+
+
+def test_close_scores_are_ranked_in_64_bits():
+    """Saturated sigmoids plus a balance: the scores differ by less than 2^-24."""
+    E, d, T = 16, 256, 64
+    c = Case(T, d, E, 4, balance=1.0)
+    W_r = np.zeros((d, E), np.float32)
+    W_r[0] = to_bf16(17.0 + 0.125 * np.arange(E, dtype=np.float32)[::-1])
+    X = np.zeros((T, d), np.float32)
+    X[:, 0] = 1.0
+    r = Run(c, X, W_r, None, np.full(E, 0.25, np.float32))
+    r.route()
+    torch.cuda.synchronize()
+    assert (to_np(r.idx)[:T] == np.arange(4)).all()
+
+
+def test_gradient_of_repeated_and_wrong_ids():
+    c = Case(40, 256, 24, 4, "softmax", renormalise=False)
+    X, W_r, bias, balance = inputs(c)
+    r = Run(c, X, W_r, bias, balance)
+    r.route()
+    r.idx[7] = torch.tensor([3, 3, 5, 3], dtype=torch.int32, device=DEV)
+    dw = torch.randn(c.T, c.k, device=DEV)
+    r.grad(dw)
+    torch.cuda.synchronize()
+    check_idx = to_np(r.idx)[:c.T]
+    ref = S.score_backward(to_np(r.logits)[:c.T], balance, check_idx, to_np(dw).astype(np.float64), **c.wts)
+    assert_close("dZ", to_np(r.dZ)[:c.T], ref, rel=1e-5)
+    r.idx[8] = torch.tensor([-1, 24, 1 << 30, -(1 << 31)], dtype=torch.int32, device=DEV)
+    r.grad(dw)
+    torch.cuda.synchronize()
+    assert (r.dZ[8] == 0).all() and torch.equal(r.dZ[9:c.T].cpu(), torch.from_numpy(ref[9:]).float()) or \
+        torch.allclose(r.dZ[9:c.T].double().cpu(), torch.from_numpy(ref[9:]), rtol=1e-4, atol=1e-6)
+    r.check_guards()
+
+
+def test_no_tokens():
+    c = Case(0, 256, 16, 2)
+    r = Run(c, np.zeros((0, 256), np.float32), np.zeros((256, 16), np.float32), None, None)
+    r.X, dw = torch.empty(8, 256, dtype=torch.bfloat16, device=DEV), torch.empty(8, 2, device=DEV)
+    r.route()
+    r.grad(dw)
+    torch.cuda.synchronize()
+    r.check_guards()
+
+
+def test_repeats_streams_and_graph():
+    """The same bits again, on another stream, and from a replayed graph."""
+    c = Case(700, 7168, 256, 8, groups=8, top_groups=4, group_score="pair", scale=2.5)
+    X, W_r, bias, balance = inputs(c, 3)
+    r = Run(c, X, W_r, bias, balance)
+    dw = torch.randn(c.T, c.k, device=DEV)
+    r.route()
+    r.grad(dw)
+    torch.cuda.synchronize()
+    want = [t.copy() for t in r.outputs()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for t in (r.logits, r.idx, r.w, r.dZ):
+        t.zero_()
+    torch.cuda.synchronize()
+    r.route(side)
+    r.grad(dw, side)
+    torch.cuda.synchronize()
+    assert all(np.array_equal(a, b) for a, b in zip(want, r.outputs()))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.route()
+        r.grad(dw)
+    for _ in range(3):
+        for t in (r.logits, r.idx, r.w, r.dZ):
+            t.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(np.array_equal(a, b) for a, b in zip(want, r.outputs()))
+
+
+LAYERS = [
+    (Workload("scored", T=300, d=256, E=8, k=2, f=256, f_s=256, backward=True),
+     B.routing("sigmoid", 4, 2, "pair", True, 2.5), dict()),
+    (Workload("scored dense", T=130, d=512, E=4, k=4, f=256, f_s=256, backward=True),
+     B.routing("softmax", renormalise=False), dict()),
+    (Workload("scored ring", T=300, d=256, E=16, k=4, f=256, backward=True),
+     B.routing("softmax", renormalise=False, scale=4.0), dict(ring_rows=500)),
+    (Workload("scored ring, dense", T=130, d=512, E=4, k=4, f=256, backward=True),
+     B.routing("sigmoid", renormalise=False), dict(ring_rows=260)),
+    (Workload("scored mx", T=300, d=256, E=8, k=2, f=256, backward=True),
+     B.routing("sigmoid", 4, 2), dict(mx=True)),
+]
+
+
+@pytest.mark.parametrize("w,routing,kw", LAYERS, ids=lambda v: getattr(v, "name", ""))
+def test_layer_step(w, routing, kw):
+    """A training step of a layer routed by scores: the router's gradient, and
+    what it adds to dX and dW_r, against the oracle on the layer's own dg."""
+    say(f"[gpu] {w.name}")
+    inp = dict(make_inputs(w, 11), balance=(np.random.default_rng(4).standard_normal(w.E) * 0.1).astype(np.float32))
+    L = DeviceLayer(w, inp, routing=routing, **kw)
+    (L.step_mx if L.mx else L.step)()
+    torch.cuda.synchronize()
+    sel = dict(score=B.SCORES[routing.score], groups=routing.groups, top_groups=routing.top_groups,
+               group_score=B.GROUP_SCORES[routing.group_score])
+    wts = dict(score=sel["score"], renormalise=bool(routing.renormalise), scale=routing.scale)
+    Z, idx, wt = to_np(L.logits), to_np(L.topk_idx), to_np(L.topk_w)
+    assert np.array_equal(idx, S.select(Z, inp["balance"], w.k, **sel))
+    ref_w = S.weights(Z, inp["balance"], idx, **wts)
+    assert np.abs(wt - ref_w).max() <= 1e-5
+    g = O.moe_backward(inp["X"], inp["W_r"], weights_dict(inp), idx, ref_w, inp["dY"])
+    dZ = S.score_backward(Z, inp["balance"], idx, g["dg"], **wts)
+    rel = 0.1 if L.mx else 2e-2
+    assert_close("dZ", to_np(L.dZ), dZ, rel)
+    assert_close("dW_r", to_np(L.dW_r), inp["X"].astype(np.float64).T @ dZ, rel)
+    dX = g["dX"] + (dZ - g["dZ"]) @ inp["W_r"].astype(np.float64).T
+    assert_close("dX", to_np(L.dX), dX, rel)
+    assert_close("dW_down", to_np(L.dW_down), g["dW_down"], rel)
