@@ -1000,7 +1000,7 @@ moe_status moe_route_scored(const moe_shape *shape, const moe_routing *routing, 
     float *part = at<float>(ws, L.rpart);
     MOE_TRY(launch_route(X, W_r, bias, logits, nullptr, nullptr, at<uint16_t>(ws, L.wrt), part, T, d, E, k,
                          s));
-    MOE_TRY(launch_score_select(part, route_partials(T, d, E, k), route_epad(E), bias, balance, logits,
+    MOE_TRY(launch_score_select(part, route_partials(T, d, E), route_epad(E), bias, balance, logits,
                                 topk_idx, topk_w, T, E, k, score_args(*routing), s));
     return MOE_OK;
 }

@@ -167,7 +167,7 @@ int route_epad(int E);
 size_t route_part_bytes(long T, int d, int E);
 // Slices of the d axis whose partial logits launch_route leaves in `part` when
 // it is not to select (topk_idx null); 0: it writes the logits.
-int route_partials(long T, int d, int E, int k);
+int route_partials(long T, int d, int E);
 hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bias, float *logits,
                         int *topk_idx, float *topk_w, uint16_t *WrT, float *part, int T,
                         int d, int E, int k, hipStream_t st);

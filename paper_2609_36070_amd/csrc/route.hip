@@ -497,8 +497,8 @@ constexpr int rd_waves(int EPAD) { return EPAD <= 64 ? 16 : 8; }
 template <int EPAD>
 __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
         const uint16_t *__restrict__ X, const uint16_t *__restrict__ Wr, const float *__restrict__ bias,
-        float *__restrict__ logits, int *__restrict__ topk_idx, float *__restrict__ topk_w, int T, int d,
-        int E, int k) {
+        float *__restrict__ logits, int *__restrict__ topk_idx, float *__restrict__ topk_w,
+        float *__restrict__ part, int T, int d, int E, int k, int S) {
     constexpr int NW = rd_waves(EPAD), BT = 16;
     constexpr int CPL = EPAD / 16, VW = CPL < 8 ? CPL : 8, NV = CPL / VW;
     constexpr int U = EPAD <= 32 ? 8 : EPAD <= 128 ? 4 : 2;   // steps in flight per wave
@@ -507,8 +507,9 @@ __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
     __shared__ float zs[BT][EPAD + 1];
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
     const int g = l >> 4, r = l & 15;
-    const int t0 = blockIdx.x * BT;
-    const int nsteps = d / 32;
+    const int t0 = blockIdx.x / S * BT;
+    // this block's slice of the d axis (S > 1: its sums go to `part`)
+    const int ks = blockIdx.x % S, s_first = d / 32 * ks / S, nsteps = d / 32 * (ks + 1) / S;
 
     // columns past the experts re-read the last ones; their logits are not used
     int col[NV];
@@ -519,7 +520,7 @@ __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
     f32x4_t acc[CPL];
 #pragma unroll
     for (int i = 0; i < CPL; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int s0 = w; s0 < nsteps; s0 += NW * U) {
+    for (int s0 = s_first + w; s0 < nsteps; s0 += NW * U) {
         wvec wv[U][8][NV];
         u32x4_t xv[U];
 #pragma unroll
@@ -565,12 +566,15 @@ __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
         float z = red[0][tt][ecol] + red[1][tt][ecol];
 #pragma unroll
         for (int v = 2; v < NW; ++v) z = z + red[v][tt][ecol];
-        if (ecol < E) {
+        if (S > 1) {
+            if (t0 + tt < T) part[((long)ks * T + t0 + tt) * EPAD + ecol] = z;
+        } else if (ecol < E) {
             if (bias) z = z + bz;
             if (t0 + tt < T) logits[(long)(t0 + tt) * E + ecol] = z;
             zs[tt][ecol] = z;
         }
     }
+    if (S > 1) return;
     __syncthreads();
     if (topk_idx)
         select_block<EPAD>(&zs[0][0], EPAD + 1, BT, NW, t0, T, E, k, topk_idx, topk_w);
@@ -593,26 +597,41 @@ int route_split_slices(long T, int d, int E) {
     return S;
 }
 
-int route_partials(long T, int d, int E, int k) {
-    const int S = route_direct(T, d, E, k) ? 0 : route_split_slices(T, d, E);
-    return S > 1 ? S : 0;
+// The same for the logits alone, whose slices are added by the selection that
+// follows: any divisor up to 8, the one whose rounds of the 256 CUs end first.
+static int route_logits_slices(long T, int d, int E) {
+    if (route_epad(E) < ROUTE_SPLIT_MIN) return 0;
+    const long ntiles = (T + RT - 1) / RT;
+    int best = 1;
+    for (int S = 2; S <= 8; ++S)
+        if ((d / 64) % S == 0 && (ntiles * S + 255) / 256 * best < (ntiles * best + 255) / 256 * S) best = S;
+    return best;
+}
+
+int route_partials(long T, int d, int E) {
+    const int S = (int)route_slices(T, d, E);
+    const int n = S > 0 ? S : route_logits_slices(T, d, E);
+    return n > 1 ? n : 0;
 }
 
 size_t route_part_bytes(long T, int d, int E) {
     const int S = route_split_slices(T, d, E);
-    return S > 1 ? (size_t)S * (size_t)T * (size_t)route_epad(E) * 4 : 0;
+    const size_t logits = std::max(route_logits_slices(T, d, E) > 1 ? (size_t)8 * (size_t)T : 0,
+                                   (size_t)route_slice_rows(T, d, E));
+    return std::max(S > 1 ? (size_t)S * (size_t)T : 0, logits) * (size_t)route_epad(E) * 4;
 }
 
-// topk_idx null: the logits alone, for a selection by scores (score.hip); with
-// route_partials(T, d, E, k) slices they stay fp32 partial sums in `part`.
 hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bias, float *logits,
                         int *topk_idx, float *topk_w, uint16_t *WrT, float *part, int T,
                         int d, int E, int k, hipStream_t st) {
     const int EPAD = route_epad(E);
-    if (route_direct(T, d, E, k)) {
-        const dim3 grid((unsigned)((T + 15) / 16)), block(64 * rd_waves(EPAD));
-#define ROUTE_DIRECT(EP) \
-    route_direct_kernel<EP><<<grid, block, 0, st>>>(X, W_r, bias, logits, topk_idx, topk_w, T, d, E, k)
+    const int slices = topk_idx ? 0 : (int)route_slices(T, d, E);
+    if (slices > 0 || (topk_idx && route_direct(T, d, E, k))) {
+        const int S = slices > 1 ? slices : 1;
+        const dim3 grid((unsigned)((T + 15) / 16 * S)), block(64 * rd_waves(EPAD));
+#define ROUTE_DIRECT(EP)                                                                                   \
+    route_direct_kernel<EP><<<grid, block, 0, st>>>(X, W_r, bias, logits, topk_idx, topk_w, part, T, d, E, \
+                                                    k, S)
         switch (EPAD) {
             case 16: ROUTE_DIRECT(16); break;
             case 32: ROUTE_DIRECT(32); break;
@@ -624,7 +643,7 @@ hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bia
 #undef ROUTE_DIRECT
         return hipGetLastError();
     }
-    const int S = route_split_slices(T, d, E);
+    const int S = topk_idx ? route_split_slices(T, d, E) : route_logits_slices(T, d, E);
     wr_transpose_kernel<<<dim3((unsigned)((d + 31) / 32), (unsigned)((EPAD + 63) / 64)), dim3(256), 0,
                           st>>>(W_r, WrT, d, E, EPAD);
     if (T == 0) return hipGetLastError();

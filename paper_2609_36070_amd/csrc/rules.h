@@ -156,6 +156,28 @@ inline bool route_direct(long T, long d, long E, long k) {
     return d <= top + (k >= 16 || (k >= 4 && T * E <= ROUTE_DIRECT_ROWS) ? 512 : 0);
 }
 
+// Logits for a selection by scores (score.hip), few tokens: the one-launch
+// router's blocks on slices of the d axis, so that about all CUs read W_r; the
+// selection adds the slices.  0: the other routers.
+constexpr long ROUTE_SLICE_MAX = 512, ROUTE_SLICE_BLOCKS = 256;
+
+inline long route_slice_steps(long d, long E) {      // slices of one step of 32 rows per wave
+    const long nw = route_padded(E) <= 64 ? 16 : 8;
+    const long s = d / 32 / nw;
+    return s > 1 ? s : 1;
+}
+inline long route_slices(long T, long d, long E) {
+    const long ep = route_padded(E), cols = ep / 16 < 8 ? ep / 16 : 8;
+    if (T <= 0 || T > ROUTE_SLICE_MAX || E % cols) return 0;
+    const long fill = ROUTE_SLICE_BLOCKS / ((T + 15) / 16), most = route_slice_steps(d, E);
+    return fill < most ? fill : most;
+}
+// Rows of partial logits of any batch of up to T tokens.
+inline long route_slice_rows(long T, long d, long E) {
+    const long t = T < ROUTE_SLICE_MAX ? T : ROUTE_SLICE_MAX;
+    return std::min(t * route_slice_steps(d, E), 16 * ROUTE_SLICE_BLOCKS);
+}
+
 // The third LDS stage of B in a row product of `rows` rows over `groups` experts
 // (DEEP in gemm.hip) pays while an expert's weights serve few m-tiles and costs
 // a little where they serve many (its loads then hit in L2 either way, and more

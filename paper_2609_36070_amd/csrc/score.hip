@@ -2,13 +2,22 @@
 // among the best groups of experts and weighted by their scores s_e (sigmoid
 // or softmax of the logits), and the gradient of those weights.
 //
-// Choosing has to be right next to a border, where two experts' scores differ
-// in the last bits: the ranking value c_e = s_e + balance_e is held in 64 bits
-// and ranked on its sign, exponent and the upper 44 bits of its mantissa; the
-// 8 bits below hold 255 - e, so rank order, ties to the lower id, is plain
-// order of unsigned 64-bit entries (and 2^-44 is far below the rounding of
-// any logit).  Where the balance is null and no group adds scores, the order
-// of the scores is that of the logits, which are ranked as they are.
+// Choosing has to be right next to a border, where two experts' values differ
+// in the last bits, and the values that are ranked, c_e = s_e + balance_e, are
+// defined in 64 bits (without a balance and without sums over groups the order
+// is that of the logits, which are ranked as they are).  The selection runs in
+// 32 bits first: c_e is computed in fp32 and laid on 24 bits between the row's
+// smallest and largest, 8 bits below hold 255 - e, and the entries go through
+// sorting networks of integer maxima and minima.  The first expert left out and
+// the last one taken then say whether the errors of the fp32 values could have
+// swapped them, and likewise the groups; only where they could (a few tokens in
+// 100000, and rows of exact ties) the experts that the errors reach, mostly two,
+// are ranked again by 64-bit values, in compact loops.  A selection in 64 bits throughout spent 25-50 us, most of it
+// on fetching its unrolled code (30 us for a single token).
+//
+// 64-bit entries hold sign, exponent and the upper 44 bits of the mantissa
+// above the 8 bits of 255 - e: rank order, ties to the lower id, is plain order
+// of the entries (2^-44 is far below the rounding of any logit).
 //
 // Out-of-play experts (logit or balance below MASKED or NaN) have score 0 and
 // rank after every other expert of the kept groups, lower ids first.  Logits
@@ -32,168 +41,399 @@ DEV uint64_t rank_key(double v) {
     return ((b >> 63) ? ~b : (b | (1ull << 63))) & ~0xffull;
 }
 constexpr uint64_t MASKED_KEY = 0x100;   // below every rank_key, above the padding 0
+constexpr uint32_t MASKED_Q = 1, FIRST_Q = 3;   // 24-bit places: masked; in play, from
 
-// exp(z - m) / ... of a chosen expert; the scores are computed in 32 bits.
 DEV float sigmoid32(float z) { return 1.0f / (1.0f + expf(-z)); }
+DEV uint32_t umax32(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+template <int N> struct Int { static constexpr int value = N; };
+
+// The value of a lane at distance M, for exchanges that run M = 1, 2, 4, ... and
+// leave the lanes below M equal: a mirrored half row or row then serves as
+// well as the xor, and DPP moves take a few cycles where a shuffle goes through
+// the LDS unit.
+template <int M>
+DEV uint32_t peer(uint32_t v) {
+    if constexpr (M == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);    // quad 1,0,3,2
+    else if constexpr (M == 2) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);   // 2,3,0,1
+    else if constexpr (M == 4) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true);  // half mirror
+    else if constexpr (M == 8) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true);  // mirror
+    else return (uint32_t)__shfl_xor((int)v, M, 64);
+}
+template <int M>
+DEV float peer_f(float v) { return __uint_as_float(peer<M>(__float_as_uint(v))); }
+// f<M>() for M = 1, 2, ... below L (and below `most`)
+template <int L, typename F>
+DEV void exchanges(int most, F f) {
+    if constexpr (L > 1) { if (1 < most) f(Int<1>{}); }
+    if constexpr (L > 2) { if (2 < most) f(Int<2>{}); }
+    if constexpr (L > 4) { if (4 < most) f(Int<4>{}); }
+    if constexpr (L > 8) { if (8 < most) f(Int<8>{}); }
+    if constexpr (L > 16) { if (16 < most) f(Int<16>{}); }
+    if constexpr (L > 32) { if (32 < most) f(Int<32>{}); }
+}
 
 constexpr int PE = 16;   // experts per lane at most
 
-// L lanes share a token.  The groups of experts are dealt to lanes, `lpg` lanes
-// to a group, each lane taking every lpg-th expert of its group, so that the
-// lanes of a load read neighbouring logits and a group's best scores meet in
-// log2 lpg exchanges.  Each lane sorts its entries best first in groups of KP
-// (k rounded up to a power of two); the lanes' lists are merged in log2 L
-// rounds, after which every lane of the token has its best KP.  Then lane j
-// finishes the j-th best expert: its place in ascending id and its weight.
+// The 64-bit side of a token's selection: its logits, balance and row maximum.
+struct Exact {
+    const float *zt, *sbal;
+    bool by_score, sigmoid;
+    float zmax;
+    double sum;
+    DEV double value(int id) const {
+        double v = (double)fminf(zt[id], FLT_MAX);
+        if (by_score) {
+            const double x = exp(sigmoid ? -v : v - (double)zmax);
+            v = (sigmoid ? 1.0 / (1.0 + x) : x / sum) + (double)sbal[id];
+        }
+        return v;
+    }
+};
+// The softmax's denominator.
+template <int L>
+DEV void exact_sum(Exact &x, uint32_t live, int first, int lpg) {
+    x.sum = 0.0;
+    if (!x.by_score || x.sigmoid) return;
+#pragma unroll 4
+    for (int i = 0; i < PE; ++i) {
+        const bool on = (live >> i) & 1;
+        const double v = exp((double)fminf(x.zt[on ? first + lpg * i : 0], FLT_MAX) - (double)x.zmax);
+        x.sum += on ? v : 0.0;
+    }
+#pragma unroll 1
+    for (int m = 1; m < L; m <<= 1) x.sum += shfl_xor_d(x.sum, m);
+}
+
+// The groups near the border by their 64-bit values: those surely in (`sure` >
+// 0) rank before, those surely out (< 0) after all of them.  Returns whether
+// this lane's group is kept.
+template <int L>
+DEV bool groups_64(Exact x, uint32_t live, int grp, int first, int lpg, int sure, const ScoreArgs &a) {
+    exact_sum<L>(x, live, first, lpg);
+    double b1 = -INFINITY, b2 = -INFINITY;
+    if (sure == 0) {
+#pragma unroll 4
+        for (int i = 0; i < PE; ++i) {
+            const bool on = (live >> i) & 1;
+            const double v = on ? x.value(first + lpg * i) : -INFINITY;
+            b2 = fmax(b2, fmin(b1, v));
+            b1 = fmax(b1, v);
+        }
+    }
+#pragma unroll 1
+    for (int m = 1; m < lpg; m <<= 1) {
+        const double o1 = shfl_xor_d(b1, m), o2 = shfl_xor_d(b2, m);
+        b2 = fmax(fmin(b1, o1), fmax(b2, o2));
+        b1 = fmax(b1, o1);
+    }
+    double gs = a.pair && b2 > -INFINITY ? b1 + b2 : b1;
+    uint64_t gk = sure > 0 ? ~0xffull : sure < 0 ? 0ull : rank_key(gs);
+    gk = grp < a.groups ? gk | (uint64_t)(255 - grp) : 0ull;
+    int better = 0;
+#pragma unroll 1
+    for (int o = 0; o < a.groups; ++o) {
+        const int lo = __shfl((int)(uint32_t)gk, o * lpg, L);
+        const int hi = __shfl((int)(uint32_t)(gk >> 32), o * lpg, L);
+        better += (((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo) > gk ? 1 : 0;
+    }
+    return better < a.top_groups;
+}
+
+// Places `from` .. k - 1 of the token's chosen experts: the best, by their
+// 64-bit values, of the candidates (bits of `cand` for this lane's experts).
+// kb: room for this lane's entries, at stride 256.
+template <int L, int KP>
+DEV void select_64(Exact x, uint64_t *kb, uint32_t live, uint32_t cand, int first, int lpg, int from,
+                   int k, uint32_t (&bk)[KP]) {
+    exact_sum<L>(x, live, first, lpg);
+#pragma unroll 1
+    for (uint32_t m = cand; m; m &= m - 1) {
+        const int i = __builtin_ctz(m), id = first + lpg * i;
+        kb[256 * i] = rank_key(x.value(id)) | (uint64_t)(255 - id);
+    }
+#pragma unroll 1
+    for (int r = from; r < k; ++r) {
+        uint64_t best = 0;
+        int at = 0;
+#pragma unroll 1
+        for (uint32_t m = cand; m; m &= m - 1) {
+            const int i = __builtin_ctz(m);
+            const uint64_t key = kb[256 * i];
+            if (key > best) {
+                best = key;
+                at = i;
+            }
+        }
+        const uint64_t mine = best;
+#pragma unroll 1
+        for (int m = 1; m < L; m <<= 1) {
+            const uint64_t o = shfl_xor_u64(best, m);
+            best = o > best ? o : best;
+        }
+        if (mine == best) cand &= ~(1u << at);   // ids differ, so one lane's
+        const uint32_t e = (FIRST_Q << 8) | (uint32_t)(best & 0xff);
+#pragma unroll
+        for (int j = 0; j < KP; ++j)
+            if (j == r) bk[j] = e;
+    }
+}
+
+// The block's 256 / L tokens go through LDS: their logits, or the partial
+// logits of S slices added in slice order, 16 bytes per load.  Then L lanes
+// share a token.  The groups of experts are dealt to lanes, `lpg` lanes to a
+// group, each lane taking every lpg-th expert of its group, so that a group's
+// best values meet in log2 lpg exchanges.  Each lane sorts its entries best
+// first in groups of KP (k rounded up to a power of two); the lanes' lists are
+// merged in log2 L rounds, after which every lane of the token has its best KP
+// and the best entry that was left out.  Then lane j finishes the j-th best
+// expert: its place in ascending id and its weight.
 template <int L, int KP>
 __global__ __launch_bounds__(256) void score_select_kernel(
         const float *__restrict__ part, int S, int epad, const float *__restrict__ bias,
         const float *__restrict__ balance, float *__restrict__ logits, int *__restrict__ topk_idx,
         float *__restrict__ topk_w, int T, int E, int k, int lpg, ScoreArgs a) {
-    __shared__ float zs[256 * PE];           // the block's logits, clamped, by token and expert
-    const int sub = threadIdx.x % L;
-    const long tk = (long)blockIdx.x * (256 / L) + threadIdx.x / L;
-    const int t = (int)(tk < T ? tk : T - 1);
-    const bool store = tk < T;
-    const int grp = sub / lpg, lane0 = sub % lpg, n = E / a.groups;
-    float *const ztok = zs + (threadIdx.x / L) * (L * PE);
-
-    // ---------------- logits ----------------
-    float z[PE];
-    uint32_t in = 0, live = 0;               // bit i: expert i of the lane exists, is in play
-#pragma unroll
-    for (int i = 0; i < PE; ++i) {
-        const int off = lane0 + lpg * i, id = grp * n + off;
-        z[i] = 0.f;
-        if (grp < a.groups && off < n) {
-            in |= 1u << i;
-            if (S == 0) z[i] = logits[(long)t * E + id];
-        }
-    }
-    if (S > 0) {
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-            for (int i = 0; i < PE; ++i)
-                if ((in >> i) & 1) {
-                    const float v = part[((long)s * T + t) * epad + grp * n + lane0 + lpg * i];
-                    z[i] = s == 0 ? v : z[i] + v;
-                }
-#pragma unroll
-        for (int i = 0; i < PE; ++i)
-            if ((in >> i) & 1) {
-                const int id = grp * n + lane0 + lpg * i;
-                if (bias) z[i] = z[i] + bias[id];
-                if (store) logits[(long)t * E + id] = z[i];
+    constexpr int TB = 256 / L;
+    __shared__ __attribute__((aligned(16))) float zs[256 * PE];   // TB rows of E <= L PE
+    __shared__ uint64_t keys[256 * PE];      // room for select_64
+    __shared__ float sbal[256];
+    if ((int)threadIdx.x < E) sbal[threadIdx.x] = balance ? balance[threadIdx.x] : 0.f;
+    const long t0 = (long)blockIdx.x * TB;
+    const int nt = (int)(T - t0 < TB ? T - t0 : TB);
+    float *zrow = logits + t0 * E;           // 16-byte aligned: TB is a multiple of 4
+    if (S == 0) {
+        for (int i = 4 * threadIdx.x; i < nt * E; i += 1024) {
+            if (i + 3 < nt * E) {
+                *reinterpret_cast<f32x4_t *>(zs + i) = *reinterpret_cast<const f32x4_t *>(zrow + i);
+            } else {
+                for (int q = i; q < nt * E; ++q) zs[q] = zrow[q];
             }
+        }
+    } else {
+        // pieces of 4 logits, two at a time; NB slices of each in flight
+        const int ch = epad / 4, pieces = nt * ch;
+        const long pitch = (long)T * epad;
+        auto add = [&](auto nb, int i0) {
+            constexpr int NB = decltype(nb)::value;
+            const float *p[2];
+            f32x4_t v[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = min(i0 + 256 * h, pieces - 1);
+                p[h] = part + (t0 + i / ch) * epad + 4 * (i % ch);
+                v[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+            for (int s = 0; s < S; s += NB) {
+                f32x4_t u[2][NB];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+                        u[h][j] = *reinterpret_cast<const f32x4_t *>(p[h] + min(s + j, S - 1) * pitch);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+                        if (s + j < S)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) v[h][q] = v[h][q] + u[h][j][q];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = i0 + 256 * h, c = 4 * (i % ch);
+                if (i >= pieces) break;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (c + q < E) zs[i / ch * E + c + q] = bias ? v[h][q] + bias[c + q] : v[h][q];
+            }
+        };
+        for (int i = threadIdx.x; i < pieces; i += 512) {
+            if (S <= 2) add(Int<2>{}, i);
+            else if (S <= 8) add(Int<8>{}, i);
+            else add(Int<14>{}, i);
+        }
     }
+    __syncthreads();
+    if (S > 0) {
+        for (int i = 4 * threadIdx.x; i < nt * E; i += 1024) {
+            if (i + 3 < nt * E) {
+                *reinterpret_cast<f32x4_t *>(zrow + i) = *reinterpret_cast<const f32x4_t *>(zs + i);
+            } else {
+                for (int q = i; q < nt * E; ++q) zrow[q] = zs[q];
+            }
+        }
+    }
+
+    // ---------------- this lane's experts ----------------
+    const int sub = threadIdx.x % L, tok = threadIdx.x / L;
+    const bool store = tok < nt;
+    const int grp = sub / lpg, lane0 = sub % lpg, n = E / a.groups;
+    const float *zt = zs + (store ? tok : nt - 1) * E;
     const bool by_score = balance || (a.groups > 1 && a.pair);
-    float bal[PE];
-#pragma unroll
-    for (int i = 0; i < PE; ++i) {
-        bal[i] = 0.f;
-        if ((in >> i) & 1) {
-            const int id = grp * n + lane0 + lpg * i;
-            if (balance) bal[i] = balance[id];
-            if (z[i] >= MASKED && bal[i] >= MASKED) live |= 1u << i;
-            z[i] = fminf(z[i], FLT_MAX);
-            ztok[id] = z[i];
-        }
-    }
-
-    // ---------------- softmax over the row ----------------
+    const bool row_sum = !a.sigmoid && (by_score || !a.renorm);
+    float c[PE], bal[PE];
+    uint32_t in = 0, live = 0;               // bit i: expert i of the lane exists, is in play
     float zmax = -INFINITY;
-    double sum = 0.0;
-    if (!a.sigmoid && (by_score || !a.renorm)) {
-#pragma unroll
-        for (int i = 0; i < PE; ++i)
-            if ((live >> i) & 1) zmax = fmaxf(zmax, z[i]);
-#pragma unroll
-        for (int m = 1; m < L; m <<= 1) zmax = fmaxf(zmax, shfl_xor_f(zmax, m));
-    }
-
-    // ---------------- ranking values ----------------
-    double v[PE];
+    // selects, no branches, here and below: the arrays stay in their registers
 #pragma unroll
     for (int i = 0; i < PE; ++i) {
-        v[i] = (double)z[i];
-        if (a.sigmoid) {
-            if (by_score) v[i] = 1.0 / (1.0 + exp(-v[i]));
-        } else if (by_score || !a.renorm) {
-            const double x = ((live >> i) & 1) ? exp(v[i] - (double)zmax) : 0.0;
-            sum += x;
-            if (by_score) v[i] = x;
+        const int off = lane0 + lpg * i;
+        const bool is = grp < a.groups && off < n;
+        const int id = is ? grp * n + off : 0;
+        const float z = zt[id];
+        bal[i] = sbal[id];
+        const bool on = is && z >= MASKED && bal[i] >= MASKED;
+        in |= is ? 1u << i : 0u;
+        live |= on ? 1u << i : 0u;
+        c[i] = on ? fminf(z, FLT_MAX) : 0.f;
+        zmax = fmaxf(zmax, on ? c[i] : -INFINITY);
+    }
+
+    // ---------------- ranking values in 32 bits ----------------
+    float sum = 0.f, smax = 0.f;
+    if (row_sum) {
+        exchanges<L>(L, [&](auto m) { zmax = fmaxf(zmax, peer_f<m.value>(zmax)); });
+#pragma unroll
+        for (int i = 0; i < PE; ++i) {
+            const float x = (live >> i) & 1 ? __builtin_amdgcn_exp2f((c[i] - zmax) * 1.4426950408889634f) : 0.f;
+            sum = sum + x;
+            c[i] = by_score ? x : c[i];
+        }
+        exchanges<L>(L, [&](auto m) { sum = sum + peer_f<m.value>(sum); });
+    }
+    if (by_score) {
+        const float inv = a.sigmoid ? 1.f : __builtin_amdgcn_rcpf(sum);
+#pragma unroll
+        for (int i = 0; i < PE; ++i) {
+            const float s = a.sigmoid ? sigmoid_f(c[i]) : c[i] * inv;
+            smax = fmaxf(smax, (live >> i) & 1 ? s : 0.f);
+            c[i] = s + bal[i];
         }
     }
-    if (!a.sigmoid && (by_score || !a.renorm)) {
+    float hi = -INFINITY, lo = INFINITY;
+    float b1 = -INFINITY, b2 = -INFINITY;    // the group's two largest
 #pragma unroll
-        for (int m = 1; m < L; m <<= 1) sum += shfl_xor_d(sum, m);
+    for (int i = 0; i < PE; ++i) {
+        const bool on = (live >> i) & 1;
+        const float x = on ? c[i] : -INFINITY;
+        lo = fminf(lo, on ? c[i] : INFINITY);
+        b2 = fmaxf(b2, fminf(b1, x));
+        b1 = fmaxf(b1, x);
     }
-    double b1 = -INFINITY, b2 = -INFINITY;   // the group's two largest
-    uint64_t key[PE];
+    hi = b1;
+    exchanges<L>(L, [&](auto m) {
+        hi = fmaxf(hi, peer_f<m.value>(hi));
+        lo = fminf(lo, peer_f<m.value>(lo));
+        smax = fmaxf(smax, peer_f<m.value>(smax));
+    });
+    // Bound of a value's error.  Sigmoid: the exponential's argument rounds to
+    // 1.5 2^-24 of itself, and |z| s (1 - s) < 0.23; an ulp each for exponential
+    // (times s (1 - s) <= 1/4), sum and reciprocal.  Softmax: |x| exp(-|x|) < 0.4
+    // times the same, an ulp each for exponential, sum, reciprocal and product,
+    // relative to the row's largest score.  Then the addition of the balance.
+    // The 24-bit places below add two units each.
+    const float top = fmaxf(fabsf(hi), fabsf(lo));
+    const float err = by_score ? smax * (a.sigmoid ? 0x1.8p-22f : 0x1p-21f) + top * 0x1p-24f : 0.f;
+    const float range = hi - lo;
+    const bool fits = range > 1e-30f && range < 1e30f;
+    const float unit = fits ? 16777200.0f / range : 0.f;
+    uint32_t key[PE];
 #pragma unroll
     for (int i = 0; i < PE; ++i) {
         const int id = grp * n + lane0 + lpg * i;
-        key[i] = 0;
-        if (!((in >> i) & 1)) continue;
-        key[i] = MASKED_KEY | (uint64_t)(255 - id);
-        if (!((live >> i) & 1)) continue;
-        if (by_score) {
-            if (!a.sigmoid) v[i] = v[i] / sum;
-            v[i] = v[i] + (double)bal[i];
-        }
-        key[i] = rank_key(v[i]) | (uint64_t)(255 - id);
-        b2 = fmax(b2, fmin(b1, v[i]));
-        b1 = fmax(b1, v[i]);
+        const uint32_t q = (live >> i) & 1 ? FIRST_Q + (uint32_t)((c[i] - lo) * unit) : MASKED_Q;
+        key[i] = (in >> i) & 1 ? (q << 8) | (uint32_t)(255 - id) : 0u;
     }
 
     // ---------------- the lane's best KP, sorted ----------------
-    uint64_t bk[KP];
+    uint32_t bk[KP], out = 0;                // out: the best entry left out
     constexpr int G = PE < KP ? PE : KP;
 #pragma unroll
     for (int g0 = 0; g0 < PE; g0 += G) {
-        uint64_t w[KP];
+        uint32_t w[KP];
 #pragma unroll
-        for (int j = 0; j < KP; ++j) w[j] = j < G ? key[g0 + j] : 0ull;
+        for (int j = 0; j < KP; ++j) w[j] = j < G ? key[g0 + j] : 0u;
         sort_desc<KP>(w);
         if (g0 == 0) {
 #pragma unroll
             for (int j = 0; j < KP; ++j) bk[j] = w[j];
         } else {
             merge_best<KP>(bk, w);
+#pragma unroll
+            for (int j = 0; j < KP; ++j) out = umax32(out, w[j]);
         }
     }
 
+    const Exact ex{zt, sbal, by_score, a.sigmoid != 0, zmax, 0.0};
+    const int first = grp * n + lane0;
+
     // ---------------- groups ----------------
+    bool kept = true;
     if (a.groups > 1) {
-        for (int m = 1; m < lpg; m <<= 1) {
-            const double o1 = shfl_xor_d(b1, m), o2 = shfl_xor_d(b2, m);
-            b2 = fmax(fmin(b1, o1), fmax(b2, o2));
-            b1 = fmax(b1, o1);
-        }
-        const double gs = a.pair && b2 > -INFINITY ? b1 + b2 : b1;
-        const uint64_t gk = grp < a.groups ? rank_key(gs) | (uint64_t)(255 - grp) : 0ull;
+        exchanges<L>(lpg, [&](auto m) {
+            const float o1 = peer_f<m.value>(b1), o2 = peer_f<m.value>(b2);
+            b2 = fmaxf(fminf(b1, o1), fmaxf(b2, o2));
+            b1 = fmaxf(b1, o1);
+        });
+        const float gs = a.pair && b2 > -INFINITY ? b1 + b2 : b1;
         int better = 0;
         for (int o = 0; o < a.groups; ++o) {
-            const int lo = __shfl((int)(uint32_t)gk, o * lpg, L);
-            const int hi = __shfl((int)(uint32_t)(gk >> 32), o * lpg, L);
-            const uint64_t og = ((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo;
-            better += og > gk ? 1 : 0;
+            const float og = __shfl(gs, o * lpg, L);
+            better += og > gs || (og == gs && o < grp) ? 1 : 0;
         }
-        if (better >= a.top_groups) {
+        kept = better < a.top_groups && grp < a.groups;
+        if (by_score) {
+            // the worst kept group and the best one left out: could errors (of
+            // two values and a sum on either side) have swapped them?
+            float worst = kept ? gs : INFINITY, next = kept || grp >= a.groups ? -INFINITY : gs;
+            exchanges<L>(L, [&](auto m) {
+                worst = fminf(worst, peer_f<m.value>(worst));
+                next = fmaxf(next, peer_f<m.value>(next));
+            });
+            const float gerr = 4.f * err + 4.f * top * 0x1p-24f;
+            if (next > -INFINITY && !(worst - next > gerr)) {
+                const int sure = gs > next + gerr ? 1 : gs < worst - gerr ? -1 : 0;
+                kept = groups_64<L>(ex, live, grp, first, lpg, sure, a) && grp < a.groups;
+            }
+        }
 #pragma unroll
-            for (int j = 0; j < KP; ++j) bk[j] = 0;
-        }
+        for (int j = 0; j < KP; ++j) bk[j] = kept ? bk[j] : 0u;
+        out = kept ? out : 0u;
     }
 
     // ---------------- the token's best KP ----------------
+    exchanges<L>(L, [&](auto m) {
+        uint32_t o[KP];
 #pragma unroll
-    for (int m = 1; m < L; m <<= 1) {
-        uint64_t o[KP];
-#pragma unroll
-        for (int j = 0; j < KP; ++j) o[j] = shfl_xor_u64(bk[j], m);
+        for (int j = 0; j < KP; ++j) o[j] = peer<m.value>(bk[j]);
+        out = umax32(out, peer<m.value>(out));
         merge_best<KP>(bk, o);
+#pragma unroll
+        for (int j = 0; j < KP; ++j) out = umax32(out, o[j]);
+    });
+    uint32_t last = 0;
+#pragma unroll
+    for (int j = 0; j < KP; ++j) {
+        if (j == k - 1) last = bk[j];
+        if (j >= k) out = umax32(out, bk[j]);
     }
-    __syncthreads();                         // ztok is written
+    // An expert in play was left out: those that its errors, and the last
+    // chosen one's, reach are ranked again.  Values that do not fit 24 bits are
+    // ranked again all together.
+    const float tol = fits ? fminf(2.f * err * unit + 5.f, 3e7f) : 3e7f;
+    if ((out >> 8) >= FIRST_Q && (float)(last >> 8) - (float)(out >> 8) <= tol) {
+        const float from_q = (float)(last >> 8) - tol, to_q = (float)(out >> 8) + tol;
+        uint32_t cand = 0;
+#pragma unroll
+        for (int i = 0; i < PE; ++i) {
+            const float q = (float)(key[i] >> 8);
+            cand |= kept && ((live >> i) & 1) && q >= from_q && q <= to_q ? 1u << i : 0u;
+        }
+        int from = 0;
+#pragma unroll
+        for (int j = 0; j < KP; ++j) from += j < k && (float)(bk[j] >> 8) > to_q ? 1 : 0;
+        select_64<L, KP>(ex, keys + threadIdx.x, live, cand, first, lpg, from, k, bk);
+    }
 
     // ---------------- ids and weights of the chosen ----------------
     constexpr int JN = (KP + L - 1) / L;     // slots per lane
@@ -204,7 +444,7 @@ __global__ __launch_bounds__(256) void score_select_kernel(
 #pragma unroll
     for (int q = 0; q < JN; ++q) {
         const int j = q * L + sub;
-        uint64_t en = 0;
+        uint32_t en = 0;
 #pragma unroll
         for (int i = 0; i < KP; ++i)
             if (i == j) en = bk[i];
@@ -212,17 +452,16 @@ __global__ __launch_bounds__(256) void score_select_kernel(
         at[q] = 0;
 #pragma unroll
         for (int i = 0; i < KP; ++i)
-            if (i < k && 255 - (int)(bk[i] & 0xff) < id[q]) ++at[q];
-        on[q] = j < k && (en >> 8) > (MASKED_KEY >> 8);
-        zc[q] = on[q] ? ztok[id[q]] : 0.f;
+            if (i < k && (bk[i] & 0xff) > (en & 0xff)) ++at[q];
+        on[q] = j < k && (en >> 8) >= FIRST_Q;
+        zc[q] = on[q] ? fminf(zt[id[q]], FLT_MAX) : 0.f;
         if (on[q]) m = fmaxf(m, a.sigmoid ? fminf(zc[q], 0.f) : zc[q]);
     }
     float u[JN], total = 1.0f;
     if (a.renorm) {
         // ratios of scores, taken to the largest of them: scores that underflow
         // together keep their ratio
-#pragma unroll
-        for (int x = 1; x < L; x <<= 1) m = fmaxf(m, shfl_xor_f(m, x));
+        exchanges<L>(L, [&](auto x) { m = fmaxf(m, peer_f<x.value>(m)); });
         total = 0.f;
 #pragma unroll
         for (int q = 0; q < JN; ++q) {
@@ -231,20 +470,19 @@ __global__ __launch_bounds__(256) void score_select_kernel(
                 u[q] = a.sigmoid ? expf(fminf(zc[q], 0.f) - m) / (1.0f + expf(-fabsf(zc[q]))) : expf(zc[q] - m);
             total = total + u[q];
         }
-#pragma unroll
-        for (int x = 1; x < L; x <<= 1) total = total + shfl_xor_f(total, x);
+        exchanges<L>(L, [&](auto x) { total = total + peer_f<x.value>(total); });
     } else {
 #pragma unroll
         for (int q = 0; q < JN; ++q) {
             u[q] = 0.f;
-            if (on[q]) u[q] = a.sigmoid ? sigmoid32(zc[q]) : expf(zc[q] - zmax) / (float)sum;
+            if (on[q]) u[q] = a.sigmoid ? sigmoid32(zc[q]) : expf(zc[q] - zmax) / sum;
         }
     }
 #pragma unroll
     for (int q = 0; q < JN; ++q)
         if (store && q * L + sub < k) {
-            topk_idx[(long)t * k + at[q]] = id[q];
-            topk_w[(long)t * k + at[q]] = u[q] > 0.f ? a.scale * (u[q] / total) : 0.f;
+            topk_idx[(t0 + tok) * k + at[q]] = id[q];
+            topk_w[(t0 + tok) * k + at[q]] = u[q] > 0.f ? a.scale * (u[q] / total) : 0.f;
         }
 }
 

@@ -1,5 +1,5 @@
-// Sorting networks over packed 64-bit (rank key, expert id) entries, shared by
-// the routers' selections.  A larger entry ranks higher; 0 is padding.
+// Sorting networks over packed (rank key, expert id) entries of 64 or 32 bits,
+// shared by the routers' selections.  A larger entry ranks higher; 0 is padding.
 #pragma once
 
 #include "common.h"
@@ -11,14 +11,21 @@ DEV void order2(uint64_t &a, uint64_t &b) {
     a = sw ? y : x;
     b = sw ? x : y;
 }
+// 32-bit entries: one maximum and one minimum, where 64-bit ones take a compare
+// and four selects
+DEV void order2(uint32_t &a, uint32_t &b) {
+    const uint32_t x = a, y = b;
+    a = x > y ? x : y;
+    b = x > y ? y : x;
+}
 DEV uint64_t shfl_xor_u64(uint64_t v, int m) {
     const int lo = __shfl_xor((int)(uint32_t)v, m, 64);
     const int hi = __shfl_xor((int)(uint32_t)(v >> 32), m, 64);
     return ((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo;
 }
 // Sort N entries best first (bitonic network, N a power of two).
-template <int N>
-DEV void sort_desc(uint64_t (&a)[N]) {
+template <int N, typename V>
+DEV void sort_desc(V (&a)[N]) {
 #pragma unroll
     for (int size = 2; size <= N; size <<= 1)
 #pragma unroll
@@ -34,8 +41,9 @@ DEV void sort_desc(uint64_t (&a)[N]) {
 }
 // a, b sorted best first: a becomes the best N of both, sorted (the
 // elementwise better of a and reversed b is bitonic; half-cleaners sort it).
-template <int N>
-DEV void merge_best(uint64_t (&a)[N], uint64_t (&b)[N]) {
+// `b` is left with the others, in no order.
+template <int N, typename V>
+DEV void merge_best(V (&a)[N], V (&b)[N]) {
 #pragma unroll
     for (int j = 0; j < N; ++j) order2(a[j], b[N - 1 - j]);
 #pragma unroll
