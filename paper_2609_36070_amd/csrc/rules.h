@@ -87,6 +87,13 @@ inline int skinny_kslices(long T, long k, long E, long d, long f, long fs, long 
     return (int)best;
 }
 
+// Small batches in int8 (skinny_i8.hip): the same tiles, and whether a product
+// of up to 16 rows per tile quantises its own activations, rows of K values.
+constexpr long SI_QUANT_LDS = 48 * 1024;
+inline bool skinny_i8_quantises(long T, long K, long Ks) {
+    return T <= 16 && T * ((K > Ks ? K : Ks) + 16) <= SI_QUANT_LDS;
+}
+
 // Dense routing on few token tiles: the folded down product has one workgroup
 // per 256 x 256 tile of Y and a K loop over every expert, so a short batch
 // leaves most CUs idle (200 tokens at d 7168: 28 workgroups of 288 K steps).
