@@ -296,7 +296,8 @@ struct I8SkinnyArgs {
     const uint16_t *X = nullptr;
     const int *offsets = nullptr, *perm = nullptr;
     int E = 0, T = 0, k = 1;
-    int bm = 16, nshared = 0;          // set by the launcher: rows per tile, shared tiles
+    int bm = 16, nshared = 0;          // set by the launcher: rows per tile, shared tiles,
+    int nw = 0, dense = 0;             //   waves of weights, columns dealt over all experts
 };
 hipError_t launch_skinny_i8_up(const I8SkinnyArgs &a, int tt, bool quantise, hipStream_t st);
 hipError_t launch_skinny_i8_down(const I8SkinnyArgs &a, int tt, bool quantise, hipStream_t st);

@@ -87,11 +87,33 @@ inline int skinny_kslices(long T, long k, long E, long d, long f, long fs, long 
     return (int)best;
 }
 
-// Small batches in int8 (skinny_i8.hip): the same tiles, and whether a product
-// of up to 16 rows per tile quantises its own activations, rows of K values.
-constexpr long SI_QUANT_LDS = 48 * 1024;
+// Small batches in int8 (skinny_i8.hip): the same tiles; whether a product
+// quantises its own activations, rows of up to SI_QUANT_K values.
+constexpr long SI_QUANT_T = 1, SI_QUANT_LDS = 48 * 1024;
 inline bool skinny_i8_quantises(long T, long K, long Ks) {
-    return T <= 16 && T * ((K > Ks ? K : Ks) + 16) <= SI_QUANT_LDS;
+    return T <= SI_QUANT_T && T * ((K > Ks ? K : Ks) + 16) <= SI_QUANT_LDS;
+}
+
+// Waves of a streaming workgroup, `wc` columns each.  A CU's time is the lines
+// it fetches, its waves' weights (16 rows) and the tile's bm rows of
+// activations, in whole rounds of the 256 CUs.  Columns of an expert are a
+// multiple of 256 and go in equal parts, over all experts (dense) in any.
+constexpr long SX_MAX_WAVES = 15;
+inline long skinny_i8_waves(long T, long k, long E, long N, long Ns, long bm, long wc, bool dense) {
+    const long R = T * k, tiles = std::max(std::min(R, E), R / bm);
+    long best = 4;
+    double cost = 0;
+    for (long nw = 4; nw <= SX_MAX_WAVES; ++nw) {
+        if (!dense && nw != 4 && nw != 8) continue;
+        const long units = dense ? (E * N + Ns + wc * nw - 1) / (wc * nw)
+                                 : tiles * (N / (wc * nw)) + (T + bm - 1) / bm * (Ns / (wc * nw));
+        const double c = (double)((units + 255) / 256) * (16 * nw + bm);
+        if (cost == 0 || c < cost) {
+            cost = c;
+            best = nw;
+        }
+    }
+    return best;
 }
 
 // Dense routing on few token tiles: the folded down product has one workgroup

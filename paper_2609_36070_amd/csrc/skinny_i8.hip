@@ -32,11 +32,46 @@ enum { SI_UP = 0, SI_DOWN = 1 };
 constexpr int SI_NW = 4;             // waves per workgroup, each 1/4 of K
 constexpr int SI_PIECE = 128;        // bytes of a row per wave and step
 
-DEV void lds_barrier() {             // LDS writes visible, loads from memory still in flight
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+DEV void barrier_no_fence() {
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
+DEV void lds_barrier() {             // LDS writes visible, loads from memory still in flight
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier_no_fence();
+}
+
+// The expert of tile slot `slot` and the tile's number in it, -1 past the last
+// tile: every wave scans the plan's offsets.
+DEV int find_tile(const I8SkinnyArgs &a, int slot, int lane, int &within) {
+    int found = -1, cum = 0;
+    within = 0;
+    for (int base = 0; base < a.E && found < 0; base += 64) {
+        const int ee = base + lane;
+        const int cnt = ee < a.E ? a.offsets[ee + 1] - a.offsets[ee] : 0;
+        const int tiles = cnt > 0 ? (cnt + a.bm - 1) / a.bm : 0;
+        int x = tiles;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int y = __shfl_up(x, off, 64);
+            if (lane >= off) x += y;
+        }
+        const int excl = cum + x - tiles;
+        const unsigned long long m = __ballot(slot >= excl && slot < excl + tiles);
+        if (m) {
+            const int src = __builtin_ctzll(m);
+            found = base + src;
+            within = slot - __shfl(excl, src, 64);
+        }
+        cum += __shfl(x, 63, 64);
+    }
+    within = __builtin_amdgcn_readfirstlane(within);
+    return __builtin_amdgcn_readfirstlane(found);
+}
+// Whether lane group g4 of an accumulator holds up channels (the up product's
+// second 8 rows).
+DEV bool up_half(int g4) { return g4 >= 2; }
 
 DEV void load8(const uint16_t *p, float (&v)[8]) {
     const u32x4_t w = ld_u32x4(p);
@@ -113,31 +148,10 @@ __global__ __launch_bounds__(64 * SI_NW, 2) void skinny_i8_kernel(I8SkinnyArgs a
     } else {
         const int slot = (b - a.nshared) / ncol;
         ntile = (b - a.nshared) % ncol;
-        // the expert of tile slot `slot`: every wave scans the plan's offsets
-        int found = -1, within = 0, cum = 0;
-        for (int base = 0; base < a.E && found < 0; base += 64) {
-            const int ee = base + lane;
-            const int cnt = ee < a.E ? a.offsets[ee + 1] - a.offsets[ee] : 0;
-            const int tiles = cnt > 0 ? (cnt + a.bm - 1) / a.bm : 0;
-            int x = tiles;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const int y = __shfl_up(x, off, 64);
-                if (lane >= off) x += y;
-            }
-            const int excl = cum + x - tiles;
-            const unsigned long long m = __ballot(slot >= excl && slot < excl + tiles);
-            if (m) {
-                const int src = __builtin_ctzll(m);
-                found = base + src;
-                within = slot - __shfl(excl, src, 64);
-            }
-            cum += __shfl(x, 63, 64);
-        }
-        found = __builtin_amdgcn_readfirstlane(found);
-        if (found < 0) return;
-        e = found;
-        row0 = a.offsets[e] + __builtin_amdgcn_readfirstlane(within) * a.bm;
+        int within = 0;
+        e = find_tile(a, slot, lane, within);
+        if (e < 0) return;
+        row0 = a.offsets[e] + within * a.bm;
         row_end = a.offsets[e + 1];
     }
     row_end = min(row_end, row0 + a.bm);
@@ -274,13 +288,216 @@ hipError_t launch(I8SkinnyArgs a, hipStream_t st) {
     return hipGetLastError();
 }
 
+// ---------------------------------------------------------------------------
+// The same products without a split of K, for calls with tiles enough: what
+// bounds a CU is then the lines it can have on their way, of weights and of
+// activations alike (7 TB/s in all, whatever the tile), so the activations are
+// fetched once per workgroup and its channels are many.
+//
+// NW waves own 16 channels each (up product: 8 gate rows and the up rows of
+// the same columns) over all of K, their codes straight into registers, D
+// pieces of 128 bytes per row in flight.  One more wave fetches the rows'
+// codes, a piece of 16 TT rows at a time, into a ring of SX_D pieces in LDS by
+// direct loads (whole 128-byte lines, chunk XOR (row >> 1) & 7); it is a wave of
+// its own because loads return in order, and the activations, from L2, would
+// wait for weights asked for long before.  One barrier per piece.
+//
+// With dense routing every expert's rows are the tokens, so a workgroup's
+// columns may belong to two experts, or to the shared one, and NW is what deals
+// the columns evenly to the CUs (skinny_i8_waves).
+constexpr int SX_D = 4, SX_WAVES = 15;
+
+#define LDS_AS __attribute__((address_space(3)))
+template <int N>
+DEV void wait_vmcnt() {
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+}
+
+DEV void load_lds16(const uint8_t *src, uint8_t *dst) {
+    __builtin_amdgcn_global_load_lds(src, (LDS_AS void *)dst, 16, 0, 0);
+}
+
+template <int MODE, int TT, int D>
+__global__ __launch_bounds__(64 * (SX_WAVES + 1)) void stream_i8_kernel(I8SkinnyArgs a) {
+    constexpr bool UP = MODE == SI_UP;
+    constexpr int STAGE = 16 * TT * SI_PIECE, NXL = STAGE / 1024;
+    __shared__ __attribute__((aligned(16))) uint8_t ring[SX_D * STAGE];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), NW = a.nw;
+    const int r = lane & 15, g4 = lane >> 4;
+    constexpr int WC = UP ? 8 : 16;                    // output columns per wave
+
+    // ---------------- which rows, which channels ----------------
+    const int b = (int)blockIdx.x;
+    bool sh = b < a.nshared;         // the shared expert's tiles come first
+    int e = 0, row0, row_end, col;   // col: the wave's first output column
+    bool idle = wave >= NW;
+    if (UP && a.dense) {
+        row0 = 0;
+        row_end = a.T;
+        const int c = (b * NW + min(wave, NW - 1)) * WC, routed = a.E * a.routed.N;
+        sh = c >= routed;
+        e = sh ? 0 : c / a.routed.N;
+        col = sh ? c - routed : c - e * a.routed.N;
+        if (sh && col >= a.shared.N) {   // past the last column: along for the barriers
+            idle = true;
+            sh = false;
+            e = col = 0;
+        }
+    } else {
+        const int ncol = (sh ? a.shared.N : a.routed.N) / (WC * NW);
+        if (sh) {
+            row0 = b / ncol * a.bm;
+            row_end = a.T;
+            col = b % ncol;
+        } else {
+            const int slot = (b - a.nshared) / ncol;
+            col = (b - a.nshared) % ncol;
+            int within = 0;
+            e = find_tile(a, slot, lane, within);
+            if (e < 0) return;
+            row0 = a.offsets[e] + within * a.bm;
+            row_end = a.offsets[e + 1];
+        }
+        col = (col * NW + min(wave, NW - 1)) * WC;
+    }
+    row_end = min(row_end, row0 + a.bm);
+    const I8Product &g = sh ? a.shared : a.routed;
+    const int K = g.K, pieces = K / SI_PIECE;
+    const bool tokens = UP && (a.dense || sh);         // the rows are the tokens in order
+    auto source_row = [&](int p) {
+        p = min(p, row_end - 1);
+        if (UP && !tokens) {
+            const int j = a.perm[min(max(p, 0), a.routed.rows - 1)];
+            p = (j >= 0 && j < a.routed.rows) ? j / a.k : 0;
+        }
+        return min(max(p, 0), g.a_nrows - 1);
+    };
+
+    if (wave == NW) {
+        // ---------------- the activations ----------------
+        const uint8_t *xp[NXL];
+#pragma unroll
+        for (int i = 0; i < NXL; ++i) {
+            const int row = 8 * i + (lane >> 3);
+            xp[i] = g.A + (long)source_row(row0 + row) * K + 16 * ((lane & 7) ^ ((row >> 1) & 7));
+        }
+        auto issue = [&](int st) {
+#pragma unroll
+            for (int i = 0; i < NXL; ++i) {
+                load_lds16(xp[i], ring + st * STAGE + i * 1024);
+                xp[i] += SI_PIECE;
+            }
+        };
+        for (int u = 0; u < SX_D - 1 && u < pieces; ++u) issue(u);
+        for (int u = 0; u < pieces; ++u) {
+            // piece u has arrived; after the barrier nobody reads u - 1
+            if (u + SX_D - 1 <= pieces) wait_vmcnt<NXL * (SX_D - 2)>();
+            else wait_vmcnt<0>();
+            barrier_no_fence();
+            if (u + SX_D - 1 < pieces) issue((u + SX_D - 1) % SX_D);
+        }
+        return;
+    }
+
+    // ---------------- the weights ----------------
+    const bool up = UP && r >= 8;
+    const uint8_t *wp = (up ? g.B2 : g.B) + ((long)e * g.N + col + (UP ? r & 7 : r)) * K + 16 * g4;
+    u32x4_t w[D][2];
+    auto load = [&](int s, int u) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[s][h] = ld_u32x4(wp + SI_PIECE * u + 64 * h);
+    };
+    i32x4_t acc[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) acc[t] = i32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < D; ++s)
+        if (s < pieces) load(s, s);
+    __builtin_amdgcn_sched_barrier(0);
+    for (int u0 = 0; u0 < pieces; u0 += D) {
+#pragma unroll
+        for (int s = 0; s < D; ++s) {
+            const int u = u0 + s;
+            if (u < pieces) {
+                barrier_no_fence();
+                const uint8_t *x = ring + u % SX_D * STAGE;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int t = 0; t < TT; ++t) {
+                        const int row = 16 * t + r;
+                        const u32x4_t xv = ld_u32x4(x + row * SI_PIECE + 16 * ((4 * h + g4) ^ ((row >> 1) & 7)));
+                        acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                            __builtin_bit_cast(i32x4_t, w[s][h]), __builtin_bit_cast(i32x4_t, xv), acc[t], 0, 0, 0);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+                if (u + D < pieces) load(s, u + D);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+    if (idle) return;
+
+    // ---------------- epilogue ----------------
+    // lane (g4, r), register q: channel row 4 g4 + q of the wave (up product:
+    // rows 0..7 gate, 8..15 up), for row r of the tile
+    const long ch = (long)e * g.N + col;
+    const int first = UP && a.dense && !sh ? a.offsets[e] : 0;   // dense: plan row of token 0
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        const int row = row0 + 16 * t + r;
+        const bool live = row < row_end;
+        const float rs = g.As[source_row(row)];
+        if constexpr (UP) {
+            const f32x4_t sc = *reinterpret_cast<const f32x4_t *>((up_half(g4) ? g.Bs2 : g.Bs) + ch + 4 * (g4 & 1));
+            float v[4];
+            f32x4_t h;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = rs * ((float)acc[t][q] * sc[q]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) h[q] = silu_f(v[q]) * shfl_xor_f(v[q], 32);
+            // a dense plan row that a malformed plan would push past the buffer is left out
+            const int p = first + row;
+            if (live && !up_half(g4) && p >= 0 && p < g.rows)
+                *reinterpret_cast<f32x4_t *>(g.H + (long)p * g.N + col + 4 * g4) = h;
+        } else if (live) {
+            const f32x4_t sc = *reinterpret_cast<const f32x4_t *>(g.Bs + ch + 4 * g4);
+            float y[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = rs * ((float)acc[t][q] * sc[q]);
+            *reinterpret_cast<u32x2_t *>(g.C + (long)row * g.N + col + 4 * g4) =
+                u32x2_t{pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3])};
+        }
+    }
+}
+
+template <int MODE, int TT, int D>
+hipError_t launch_stream(I8SkinnyArgs a, hipStream_t st) {
+    constexpr int WC = MODE == SI_UP ? 8 : 16;
+    a.bm = 16 * TT;
+    a.dense = MODE == SI_UP && a.k == a.E && a.T <= a.bm;
+    a.nw = (int)skinny_i8_waves(a.T, a.k, a.E, a.routed.N, a.shared.N, a.bm, WC, a.dense);
+    long grid;
+    if (a.dense) {
+        a.nshared = 0;
+        grid = ((long)a.E * a.routed.N + a.shared.N + WC * a.nw - 1) / (WC * a.nw);
+    } else {
+        a.nshared = a.shared.N > 0 ? (a.T + a.bm - 1) / a.bm * (a.shared.N / (WC * a.nw)) : 0;
+        grid = a.nshared + skinny_slots(a.routed.rows, a.E, a.bm) * (a.routed.N / (WC * a.nw));
+    }
+    if (grid <= 0) return hipSuccess;
+    stream_i8_kernel<MODE, TT, D><<<dim3((unsigned)grid), dim3(64 * (a.nw + 1)), 0, st>>>(a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_skinny_i8_up(const I8SkinnyArgs &a, int tt, bool quantise, hipStream_t st) {
-    if (tt > 1) return launch<SI_UP, 4, 4, 2, false>(a, st);
-    return quantise ? launch<SI_UP, 1, 2, 4, true>(a, st) : launch<SI_UP, 1, 2, 4, false>(a, st);
+    if (quantise) return launch<SI_UP, 1, 2, 4, true>(a, st);
+    return tt > 1 ? launch_stream<SI_UP, 4, 6>(a, st) : launch_stream<SI_UP, 1, 6>(a, st);
 }
 hipError_t launch_skinny_i8_down(const I8SkinnyArgs &a, int tt, bool quantise, hipStream_t st) {
-    if (tt > 1) return launch<SI_DOWN, 4, 4, 2, false>(a, st);
-    return quantise ? launch<SI_DOWN, 1, 2, 4, true>(a, st) : launch<SI_DOWN, 1, 2, 4, false>(a, st);
+    if (quantise) return launch<SI_DOWN, 1, 2, 4, true>(a, st);
+    return tt > 1 ? launch_stream<SI_DOWN, 4, 6>(a, st) : launch_stream<SI_DOWN, 1, 6>(a, st);
 }
