@@ -1866,28 +1866,36 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
         down.shared = down_product(hshq, hshs, w.Sd_q, w.Sd_s, 1, T, fs, at<uint16_t>(ws, Q.Ysh));
     }
 
-    const int tt = skinny_tiles(T, k, E, f, fs);
-    const bool own_x = tt == 1 && skinny_i8_quantises(T, d, d), own_h = tt == 1 && skinny_i8_quantises(T, f, fs);
+    I8SkinnyArgs small;
+    small.offsets = plan->offsets; small.perm = plan->perm;
+    small.E = E; small.T = T; small.k = k;
+    small.routed = up.routed; small.shared = up.shared;
     MOE_TRY(mk.mark(0));
+    if (token_i8(T, d, k, f, fs)) {
+        small.X = X; small.topk_idx = topk_idx;
+        MOE_TRY(mk.mark(1));
+        MOE_TRY(launch_token_i8_up(small, s));
+        MOE_TRY(mk.mark(2));
+        small.routed = down.routed; small.shared = down.shared;
+        small.routed.Hin = up.routed.H; small.shared.Hin = up.shared.H;
+        MOE_TRY(mk.mark(3));
+        MOE_TRY(launch_token_i8_down(small, topk_w, Y, s));
+        for (int i = 4; i <= 6; ++i) MOE_TRY(mk.mark(i));
+        return MOE_OK;
+    }
+    const int tt = skinny_tiles(T, k, E, f, fs);
     if (!tt)
         MOE_TRY(launch_prep(plan->perm, plan->offsets, E, topk_w, k, T, at<int>(ws, L.rowidx),
                             at<float>(ws, L.wperm), at<uint16_t>(ws, L.zeros), s));
-    if (!own_x) MOE_TRY(launch_i8_quant_rows(X, T, d, xq, xs, s));
+    MOE_TRY(launch_i8_quant_rows(X, T, d, xq, xs, s));
     MOE_TRY(mk.mark(1));
-    I8SkinnyArgs small;
-    small.X = X; small.offsets = plan->offsets; small.perm = plan->perm;
-    small.E = E; small.T = T; small.k = k;
-    small.routed = up.routed; small.shared = up.shared;
-    MOE_TRY(tt ? launch_skinny_i8_up(small, tt, own_x, s) : launch_gemm_i8_up(up, s));
+    MOE_TRY(tt ? launch_skinny_i8_up(small, tt, s) : launch_gemm_i8_up(up, s));
     MOE_TRY(mk.mark(2));
-    if (!own_h) {
-        MOE_TRY(launch_i8_quant_rows_f32(up.routed.H, R, f, hq, hs, s));
-        if (fs > 0) MOE_TRY(launch_i8_quant_rows_f32(up.shared.H, T, fs, hshq, hshs, s));
-    }
+    MOE_TRY(launch_i8_quant_rows_f32(up.routed.H, R, f, hq, hs, s));
+    if (fs > 0) MOE_TRY(launch_i8_quant_rows_f32(up.shared.H, T, fs, hshq, hshs, s));
     MOE_TRY(mk.mark(3));
     small.routed = down.routed; small.shared = down.shared;
-    small.routed.Hin = up.routed.H; small.shared.Hin = up.shared.H;
-    MOE_TRY(tt ? launch_skinny_i8_down(small, tt, own_h, s) : launch_gemm_i8_down(down, s));
+    MOE_TRY(tt ? launch_skinny_i8_down(small, tt, s) : launch_gemm_i8_down(down, s));
     MOE_TRY(mk.mark(4));
     MOE_TRY(mk.mark(5));
     MOE_TRY(launch_combine(at<uint16_t>(ws, Q.Yexp), fs > 0 ? at<uint16_t>(ws, Q.Ysh) : nullptr, topk_w,

@@ -279,7 +279,7 @@ struct I8Product {
     int a_nrows = 1, rows = 0, K = 0, N = 0;
     uint32_t a_bytes = 0, b_bytes = 0; // operand extents (< 4 GiB)
     float *H = nullptr;                // up product: silu(gate) * up, fp32 [rows][N]
-    const float *Hin = nullptr;        // down product of a small batch that quantises it: [rows][K]
+    const float *Hin = nullptr;        // down product of one token, which quantises it: [rows][K]
     uint16_t *C = nullptr;             // down product: bf16 [rows][N]
 };
 struct I8GemmArgs {
@@ -289,18 +289,21 @@ struct I8GemmArgs {
     int E = 0;
     int shared_grid = 0;               // set by the launcher
 };
-// The same for small batches (skinny_i8.hip); `quantise`: from X and Hin
-// instead of the codes A.
+// The same for small batches (skinny_i8.hip).
 struct I8SkinnyArgs {
     I8Product routed, shared;
-    const uint16_t *X = nullptr;
     const int *offsets = nullptr, *perm = nullptr;
+    const uint16_t *X = nullptr;       // one token: it, and its experts
+    const int *topk_idx = nullptr;
     int E = 0, T = 0, k = 1;
     int bm = 16, nshared = 0;          // set by the launcher: rows per tile, shared tiles,
     int nw = 0, dense = 0;             //   waves of weights, columns dealt over all experts
 };
-hipError_t launch_skinny_i8_up(const I8SkinnyArgs &a, int tt, bool quantise, hipStream_t st);
-hipError_t launch_skinny_i8_down(const I8SkinnyArgs &a, int tt, bool quantise, hipStream_t st);
+hipError_t launch_skinny_i8_up(const I8SkinnyArgs &a, int tt, hipStream_t st);
+hipError_t launch_skinny_i8_down(const I8SkinnyArgs &a, int tt, hipStream_t st);
+// One token (token_i8): quantising X and Hin themselves; the second sums into Y.
+hipError_t launch_token_i8_up(const I8SkinnyArgs &a, hipStream_t st);
+hipError_t launch_token_i8_down(const I8SkinnyArgs &a, const float *topk_w, uint16_t *Y, hipStream_t st);
 hipError_t launch_gemm_i8_up(const I8GemmArgs &a, hipStream_t st);
 hipError_t launch_gemm_i8_down(const I8GemmArgs &a, hipStream_t st);
 hipError_t launch_i8_quant_rows(const uint16_t *X, long rows, int K, uint8_t *q, float *sc,

@@ -87,11 +87,11 @@ inline int skinny_kslices(long T, long k, long E, long d, long f, long fs, long 
     return (int)best;
 }
 
-// Small batches in int8 (skinny_i8.hip): the same tiles; whether a product
-// quantises its own activations, rows of up to SI_QUANT_K values.
-constexpr long SI_QUANT_T = 1, SI_QUANT_LDS = 48 * 1024;
-inline bool skinny_i8_quantises(long T, long K, long Ks) {
-    return T <= SI_QUANT_T && T * ((K > Ks ? K : Ks) + 16) <= SI_QUANT_LDS;
+// Int8, one token (skinny_i8.hip): rows whose codes fit the workgroups' LDS.
+constexpr long TOKEN_I8_K = 8192, TOKEN_I8_LDS = 56 * 1024;
+inline bool token_i8(long T, long d, long k, long f, long fs) {
+    const long routes = k + (fs > 0), waves = routes < 16 ? routes : 16;
+    return T == 1 && d <= TOKEN_I8_K && waves * ((f > fs ? f : fs) + 16) <= TOKEN_I8_LDS;
 }
 
 // Waves of a streaming workgroup, `wc` columns each.  A CU's time is the lines

@@ -1,24 +1,8 @@
 // Int8 expert products of small batches (decoding): few rows per expert, so a
 // product is a stream of the experts' codes from HBM, as in skinny.hip, at half
-// the bytes.
-//
-// The codes are K-contiguous, one row per output channel, which is the row
-// operand of v_mfma_i32_16x16x64_i8 as it lies: lane (g, r) takes 16 bytes of
-// row r at k 16 g.  A workgroup owns up to 16 TT rows (tokens) of one expert and
-// 16 NR channels (up product: half of them gate rows, half the up rows of the
-// same f range); its 4 waves take every fourth 128-byte piece of K, so together
-// they walk each row through neighbouring memory, whole 128-byte lines each.
-// A wave keeps D pieces in flight (D 2 NR loads of 16 bytes per lane), straight
-// into registers: no two waves need the same codes.  The tokens' codes are the
-// column operand, 16 tokens each, from L2 or LDS.  The waves' 32-bit integer
-// sums are added through LDS (in any order: they are exact), then come the
-// scales and the SwiGLU.
-//
-// Up to 16 tokens the products quantise their own activations where they fit
-// LDS (QF): the codes of the tile's rows, in every workgroup again, while the
-// first pieces of the weights are on their way; two launches less, of the five
-// that a call of one token would have.  The shared expert's tiles ride in the
-// same launch.
+// the bytes.  The codes are K-contiguous, one row per output channel, which is
+// the row operand of v_mfma_i32_16x16x64_i8 as it lies: lane (g, r) takes 16
+// bytes of row r at k 16 g.  The activations' codes are the column operand.
 #include "common.h"
 #include "i8_common.h"
 #include "kernels.h"
@@ -29,7 +13,6 @@ namespace {
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 
 enum { SI_UP = 0, SI_DOWN = 1 };
-constexpr int SI_NW = 4;             // waves per workgroup, each 1/4 of K
 constexpr int SI_PIECE = 128;        // bytes of a row per wave and step
 
 DEV void barrier_no_fence() {
@@ -86,213 +69,234 @@ DEV void load8(const float *p, float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = w[j];
 }
-
-// Codes and scales of `rows` rows of K values (row i at src + at(i)) into LDS,
-// rows at pitch K + 16 (16 rows read side by side touch different banks).
-template <typename S, typename F>
-DEV void quantise_tile(const S *__restrict__ src, F at, int rows, int K, uint8_t *codes, float *scale,
-                       uint32_t (*amax)[SI_NW]) {
-    const int tid = threadIdx.x;
-    for (int i = 0; i < rows; ++i) {
-        const S *x = src + at(i);
-        uint32_t m = 0;
-        for (int c = tid; c < K / 8; c += 64 * SI_NW) {
-            float v[8];
-            load8(x + 8 * c, v);
+DEV uint32_t max8(const float (&v)[8]) {
+    uint32_t m = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) m = umax(m, abs_bits(v[j]));
-        }
-#pragma unroll
-        for (int s = 1; s < 64; s <<= 1) m = umax(m, (uint32_t)__shfl_xor((int)m, s, 64));
-        if ((tid & 63) == 0) amax[i][tid >> 6] = m;
-    }
-    lds_barrier();
-    for (int i = 0; i < rows; ++i) {
-        const S *x = src + at(i);
-        const I8Scale s(umax(umax(amax[i][0], amax[i][1]), umax(amax[i][2], amax[i][3])));
-        if (tid == 0) scale[i] = s.s;
-        for (int c = tid; c < K / 8; c += 64 * SI_NW) {
-            float v[8];
-            load8(x + 8 * c, v);
-            *reinterpret_cast<u32x2_t *>(codes + i * (K + 16) + 8 * c) =
-                u32x2_t{pack_i8(s.code(v[0]), s.code(v[1]), s.code(v[2]), s.code(v[3])),
-                        pack_i8(s.code(v[4]), s.code(v[5]), s.code(v[6]), s.code(v[7]))};
-        }
-    }
-    lds_barrier();
+    for (int j = 0; j < 8; ++j) m = umax(m, abs_bits(v[j]));
+    return m;
 }
-
-template <int MODE, int TT, int NR, int D, bool QF>
-__global__ __launch_bounds__(64 * SI_NW, 2) void skinny_i8_kernel(I8SkinnyArgs a) {
-    constexpr bool UP = MODE == SI_UP;
-    constexpr int GR = UP ? NR / 2 : NR;               // groups of 16 output columns
-    static_assert(!QF || TT == 1, "rows quantised in LDS: one tile of 16");
-    __shared__ __attribute__((aligned(16))) i32x4_t red[SI_NW][TT * NR][64];
-    __shared__ float row_scale[16];
-    __shared__ uint32_t amax[16][SI_NW];
-    extern __shared__ __attribute__((aligned(16))) uint8_t codes[];   // QF: [bm][K + 16]
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int r = lane & 15, g4 = lane >> 4;
-
-    // ---------------- which rows, which channels ----------------
-    const int b = (int)blockIdx.x;
-    const bool sh = b < a.nshared;   // the shared expert's tiles come first
-    const I8Product &g = sh ? a.shared : a.routed;
-    const int ncol = g.N / (16 * GR);
-    int e = 0, row0, row_end, ntile;
-    if (sh) {
-        row0 = b / ncol * a.bm;
-        row_end = a.T;
-        ntile = b % ncol;
-    } else {
-        const int slot = (b - a.nshared) / ncol;
-        ntile = (b - a.nshared) % ncol;
-        int within = 0;
-        e = find_tile(a, slot, lane, within);
-        if (e < 0) return;
-        row0 = a.offsets[e] + within * a.bm;
-        row_end = a.offsets[e + 1];
-    }
-    row_end = min(row_end, row0 + a.bm);
-    const int K = g.K, n0 = ntile * 16 * GR;
-    // row of the activations that plan row p reads (rows past the tile repeat its last)
-    auto source_row = [&](int p) {
-        p = min(p, row_end - 1);
-        if (UP && !sh) {
-            const int j = a.perm[min(max(p, 0), a.routed.rows - 1)];
-            p = (j >= 0 && j < a.routed.rows) ? j / a.k : 0;
-        }
-        return min(max(p, 0), g.a_nrows - 1);
-    };
-
-    // ---------------- operands ----------------
-    const int pieces = K / SI_PIECE;
-    const uint8_t *wp[NR];
+DEV uint32_t wave_max(uint32_t m) {
 #pragma unroll
-    for (int j = 0; j < NR; ++j) {
-        const bool up = UP && j >= GR;
-        wp[j] = (up ? g.B2 : g.B) + ((long)e * g.N + n0 + 16 * (up ? j - GR : j) + r) * K + 16 * g4;
-    }
-    uint32_t xo[TT];                 // element offsets (the rows span under 2^32)
-    if constexpr (!QF) {
-#pragma unroll
-        for (int t = 0; t < TT; ++t) xo[t] = (uint32_t)source_row(row0 + 16 * t + r) * (uint32_t)K + 16u * g4;
-    }
-    u32x4_t w[D][NR][2], x[D][TT][2];
-    auto load = [&](int s, int u) {
-        const int k0 = SI_PIECE * u;
-        if constexpr (!QF) {
-#pragma unroll
-            for (int t = 0; t < TT; ++t)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) x[s][t][h] = ld_u32x4(g.A + (xo[t] + (uint32_t)(k0 + 64 * h)));
-        }
-#pragma unroll
-        for (int j = 0; j < NR; ++j)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) w[s][j][h] = ld_u32x4(wp[j] + k0 + 64 * h);
-    };
-    i32x4_t acc[TT][NR];
-#pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int j = 0; j < NR; ++j) acc[t][j] = i32x4_t{0, 0, 0, 0};
-
-#pragma unroll
-    for (int s = 0; s < D; ++s)
-        if (wave + SI_NW * s < pieces) load(s, wave + SI_NW * s);
-    __builtin_amdgcn_sched_barrier(0);
-    const int rows = row_end - row0;
-    if constexpr (QF) {
-        if constexpr (UP) quantise_tile(a.X, [&](int i) { return (long)source_row(row0 + i) * K; }, rows, K, codes, row_scale, amax);
-        else quantise_tile(g.Hin, [&](int i) { return (long)source_row(row0 + i) * K; }, rows, K, codes, row_scale, amax);
-    }
-    const uint8_t *cr = codes + min(r, rows - 1) * (K + 16) + 16 * g4;
-    auto mul = [&](int s, int u) {
-        if constexpr (QF) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) x[s][0][h] = ld_u32x4(cr + SI_PIECE * u + 64 * h);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < NR; ++j)
-#pragma unroll
-                for (int t = 0; t < TT; ++t)
-                    acc[t][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-                        __builtin_bit_cast(i32x4_t, w[s][j][h]), __builtin_bit_cast(i32x4_t, x[s][t][h]),
-                        acc[t][j], 0, 0, 0);
-    };
-    for (int u = wave; u < pieces;) {
-#pragma unroll
-        for (int s = 0; s < D; ++s) {
-            if (u < pieces) {
-                mul(s, u);
-                __builtin_amdgcn_sched_barrier(0);
-                if (u + SI_NW * D < pieces) load(s, u + SI_NW * D);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            u += SI_NW;
-        }
-    }
-
-    // ---------------- sum over the waves, epilogue ----------------
-    // accumulator layout: lane (g4, r), register q holds channel 4 g4 + q of its
-    // group, for row r
-#pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int j = 0; j < NR; ++j) red[wave][t * NR + j][lane] = acc[t][j];
-    __syncthreads();
-    for (int o = wave; o < TT * GR; o += SI_NW) {
-        const int t = o / GR, j = o % GR, p = row0 + 16 * t + r;
-        auto total = [&](int i) {
-            i32x4_t v = red[0][i][lane];
-#pragma unroll
-            for (int q = 1; q < SI_NW; ++q) v += red[q][i][lane];
-            return v;
-        };
-        if (p >= row_end) continue;
-        const float rs = QF ? row_scale[r] : g.As[source_row(p)];
-        const long col = n0 + 16 * j + 4 * g4, ch = (long)e * g.N + col;
-        const f32x4_t s1 = *reinterpret_cast<const f32x4_t *>(g.Bs + ch);
-        const i32x4_t v = total(t * NR + j);
-        if constexpr (UP) {
-            const f32x4_t s2 = *reinterpret_cast<const f32x4_t *>(g.Bs2 + ch);
-            const i32x4_t u = total(t * NR + GR + j);
-            f32x4_t h;
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                h[q] = silu_f(rs * ((float)v[q] * s1[q])) * (rs * ((float)u[q] * s2[q]));
-            *reinterpret_cast<f32x4_t *>(g.H + (long)p * g.N + col) = h;
-        } else {
-            float y[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) y[q] = rs * ((float)v[q] * s1[q]);
-            *reinterpret_cast<u32x2_t *>(g.C + (long)p * g.N + col) =
-                u32x2_t{pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3])};
-        }
-    }
+    for (int s = 1; s < 64; s <<= 1) m = umax(m, (uint32_t)__shfl_xor((int)m, s, 64));
+    return m;
 }
-
-template <int MODE, int TT, int NR, int D, bool QF>
-hipError_t launch(I8SkinnyArgs a, hipStream_t st) {
-    const int cols = 16 * (MODE == SI_UP ? NR / 2 : NR);
-    a.bm = TT > 1 ? 16 * TT : (a.T < 16 ? a.T : 16);
-    a.nshared = a.shared.N > 0 ? (a.T + a.bm - 1) / a.bm * (a.shared.N / cols) : 0;
-    const long grid = a.nshared + skinny_slots(a.routed.rows, a.E, a.bm) * (a.routed.N / cols);
-    if (grid <= 0) return hipSuccess;
-    const size_t lds = QF ? (size_t)a.bm * ((a.shared.N > 0 && a.shared.K > a.routed.K ? a.shared.K : a.routed.K) + 16) : 0;
-    skinny_i8_kernel<MODE, TT, NR, D, QF><<<dim3((unsigned)grid), dim3(64 * SI_NW), lds, st>>>(a);
-    return hipGetLastError();
+DEV void put8(uint8_t *codes, const float (&v)[8], const I8Scale &s) {
+    *reinterpret_cast<u32x2_t *>(codes) =
+        u32x2_t{pack_i8(s.code(v[0]), s.code(v[1]), s.code(v[2]), s.code(v[3])),
+                pack_i8(s.code(v[4]), s.code(v[5]), s.code(v[6]), s.code(v[7]))};
 }
 
 // ---------------------------------------------------------------------------
-// The same products without a split of K, for calls with tiles enough: what
-// bounds a CU is then the lines it can have on their way, of weights and of
-// activations alike (7 TB/s in all, whatever the tile), so the activations are
-// fetched once per workgroup and its channels are many.
+// One token: two launches in all, without the plan (the experts are the
+// token's own list).  What counts is latency: every load that a wave will need
+// goes out at once, and the workgroups quantise the activations for
+// themselves, each the same row again, under the weights' round trip.
+//
+// Up product: a workgroup owns 16 columns of f of one of the token's experts (or
+// of the shared one); its 4 waves take every fourth 128-byte piece of K.
+constexpr int TK_NW = 4, TK_D = 4;
+constexpr int TK_HELD = TOKEN_I8_K / 8 / (64 * TK_NW);   // 8-value chunks of the token per thread
+
+__global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
+    __shared__ __attribute__((aligned(16))) uint8_t codes[TOKEN_I8_K];
+    __shared__ int red[TK_NW][2][16];
+    __shared__ uint32_t amax[TK_NW];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g4 = lane >> 4;
+    const int ns = a.shared.N / 16, b = (int)blockIdx.x - ns;
+    const bool sh = b < 0;
+    const I8Product &g = sh ? a.shared : a.routed;
+    const int slot = sh ? 0 : b / (g.N / 16);
+    const int n0 = 16 * (sh ? b + ns : b % (g.N / 16));
+    const int e = sh ? 0 : __builtin_amdgcn_readfirstlane(a.topk_idx[slot]);
+    if (e < 0 || e >= a.E) return;   // routes outside the experts are left out
+    const int K = g.K, pieces = K / SI_PIECE;
+
+    // loads return in order: the token first, then the weights
+    float v[TK_HELD][8];
+#pragma unroll
+    for (int i = 0; i < TK_HELD; ++i) {
+        const int c = tid + 64 * TK_NW * i;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+        if (c < K / 8) load8(a.X + 8 * c, v[i]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const long ch = (long)e * g.N + n0 + r;
+    const uint8_t *wp[2] = {g.B + ch * K + 16 * g4, g.B2 + ch * K + 16 * g4};
+    u32x4_t w[TK_D][2][2];
+    auto load = [&](int s, int u) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) w[s][j][h] = ld_u32x4(wp[j] + SI_PIECE * u + 64 * h);
+    };
+#pragma unroll
+    for (int s = 0; s < TK_D; ++s)
+        if (wave + TK_NW * s < pieces) load(s, wave + TK_NW * s);
+    __builtin_amdgcn_sched_barrier(0);
+
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < TK_HELD; ++i) m = umax(m, max8(v[i]));
+    m = wave_max(m);
+    if (lane == 0) amax[wave] = m;
+    lds_barrier();
+    const I8Scale xs(umax(umax(amax[0], amax[1]), umax(amax[2], amax[3])));
+#pragma unroll
+    for (int i = 0; i < TK_HELD; ++i) {
+        const int c = tid + 64 * TK_NW * i;
+        if (c < K / 8) put8(codes + 8 * c, v[i], xs);
+    }
+    lds_barrier();
+
+    i32x4_t acc[2] = {i32x4_t{0, 0, 0, 0}, i32x4_t{0, 0, 0, 0}};
+    for (int u = wave; u < pieces;) {
+#pragma unroll
+        for (int s = 0; s < TK_D; ++s) {
+            if (u < pieces) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    // every column of the product is the token
+                    const u32x4_t x = ld_u32x4(codes + SI_PIECE * u + 64 * h + 16 * g4);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                            __builtin_bit_cast(i32x4_t, w[s][j][h]), __builtin_bit_cast(i32x4_t, x), acc[j], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (u + TK_NW * TK_D < pieces) load(s, u + TK_NW * TK_D);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            u += TK_NW;
+        }
+    }
+    // lane (g4, r), register q: channel 4 g4 + q, whatever r
+    if (r == 0)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) red[wave][j][4 * g4 + q] = acc[j][q];
+    __syncthreads();
+    if (tid < 16) {
+        int gate = 0, up = 0;
+#pragma unroll
+        for (int q = 0; q < TK_NW; ++q) {
+            gate += red[q][0][tid];
+            up += red[q][1][tid];
+        }
+        const long c = (long)e * g.N + n0 + tid;
+        g.H[(long)slot * g.N + n0 + tid] =
+            silu_f(xs.s * ((float)gate * g.Bs[c])) * (xs.s * ((float)up * g.Bs2[c]));
+    }
+}
+
+// Down product and the sum over the token's experts: a workgroup owns 16
+// columns of Y, a wave of it one of the token's routes (the shared expert
+// first): the route's row of H to LDS as codes, 16 channels over all of f, and
+// the weighted result to LDS in fp32.  The sum runs in the routes' order and is
+// rounded once.
+constexpr int TK_DD = 6;
+__global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const float *__restrict__ topk_w,
+                                                          uint16_t *__restrict__ Y, int pitch) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t codes_all[];   // [waves][pitch]
+    __shared__ float y[32][16];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
+    const int r = lane & 15, g4 = lane >> 4;
+    const int n0 = 16 * (int)blockIdx.x, nsh = a.shared.N > 0 ? 1 : 0, routes = a.k + nsh;
+    uint8_t *codes = codes_all + wave * pitch;
+    for (int s0 = wave; s0 < routes; s0 += nw) {
+        const bool sh = s0 < nsh;
+        const I8Product &g = sh ? a.shared : a.routed;
+        const int slot = s0 - nsh, e = sh ? 0 : __builtin_amdgcn_readfirstlane(a.topk_idx[slot]);
+        if (e < 0 || e >= a.E) {
+            if (lane < 16) y[s0][lane] = 0.f;
+            continue;
+        }
+        const int K = g.K, pieces = K / SI_PIECE;
+        const float *h = g.Hin + (sh ? 0 : (long)slot * K);
+        // the row's largest value: the first 2048 values stay in registers
+        float v[4][8];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = lane + 64 * i;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+            if (c < K / 8) load8(h + 8 * c, v[i]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const uint8_t *wp = g.B + ((long)e * g.N + n0 + r) * K + 16 * g4;
+        u32x4_t w[TK_DD][2];
+        auto load = [&](int s, int u) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) w[s][q] = ld_u32x4(wp + SI_PIECE * u + 64 * q);
+        };
+#pragma unroll
+        for (int s = 0; s < TK_DD; ++s)
+            if (s < pieces) load(s, s);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = umax(m, max8(v[i]));
+        for (int c = lane + 256; c < K / 8; c += 64) {
+            float u[8];
+            load8(h + 8 * c, u);
+            m = umax(m, max8(u));
+        }
+        const I8Scale hs(wave_max(m));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = lane + 64 * i;
+            if (c < K / 8) put8(codes + 8 * c, v[i], hs);
+        }
+        for (int c = lane + 256; c < K / 8; c += 64) {
+            float u[8];
+            load8(h + 8 * c, u);
+            put8(codes + 8 * c, u, hs);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wave's own codes
+        i32x4_t acc = i32x4_t{0, 0, 0, 0};
+        for (int u0 = 0; u0 < pieces; u0 += TK_DD) {
+#pragma unroll
+            for (int s = 0; s < TK_DD; ++s) {
+                const int u = u0 + s;
+                if (u < pieces) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const u32x4_t x = ld_u32x4(codes + SI_PIECE * u + 64 * q + 16 * g4);
+                        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, w[s][q]),
+                                                                    __builtin_bit_cast(i32x4_t, x), acc, 0, 0, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (u + TK_DD < pieces) load(s, u + TK_DD);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        if (r == 0) {
+            const float wt = sh ? 1.0f : topk_w[slot];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = 4 * g4 + q;
+                y[s0][c] = wt * (hs.s * ((float)acc[q] * g.Bs[(long)e * g.N + n0 + c]));
+            }
+        }
+    }
+    __syncthreads();
+    if (tid < 16) {
+        float sum = 0.f;
+        for (int s = 0; s < routes; ++s) sum = sum + y[s][tid];
+        Y[n0 + tid] = f2bf(sum);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Several tokens: up to 16 TT rows of one expert per workgroup.  What bounds a CU
+// here is the lines it can have on their way, of weights and of activations
+// alike (7 TB/s in all, whatever the tile), so the activations are fetched once
+// per workgroup and its channels are many.
 //
 // NW waves own 16 channels each (up product: 8 gate rows and the up rows of
 // the same columns) over all of K, their codes straight into registers, D
@@ -493,11 +497,22 @@ hipError_t launch_stream(I8SkinnyArgs a, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_skinny_i8_up(const I8SkinnyArgs &a, int tt, bool quantise, hipStream_t st) {
-    if (quantise) return launch<SI_UP, 1, 2, 4, true>(a, st);
-    return tt > 1 ? launch_stream<SI_UP, 4, 6>(a, st) : launch_stream<SI_UP, 1, 6>(a, st);
+hipError_t launch_skinny_i8_up(const I8SkinnyArgs &a, int tt, hipStream_t st) {
+    return tt > 1 ? launch_stream<SI_UP, 4, 4>(a, st) : launch_stream<SI_UP, 1, 4>(a, st);
 }
-hipError_t launch_skinny_i8_down(const I8SkinnyArgs &a, int tt, bool quantise, hipStream_t st) {
-    if (quantise) return launch<SI_DOWN, 1, 2, 4, true>(a, st);
-    return tt > 1 ? launch_stream<SI_DOWN, 4, 6>(a, st) : launch_stream<SI_DOWN, 1, 6>(a, st);
+hipError_t launch_skinny_i8_down(const I8SkinnyArgs &a, int tt, hipStream_t st) {
+    return tt > 1 ? launch_stream<SI_DOWN, 4, 4>(a, st) : launch_stream<SI_DOWN, 1, 4>(a, st);
+}
+
+hipError_t launch_token_i8_up(const I8SkinnyArgs &a, hipStream_t st) {
+    const int grid = a.shared.N / 16 + a.k * (a.routed.N / 16);
+    token_up_kernel<<<dim3((unsigned)grid), dim3(64 * TK_NW), 0, st>>>(a);
+    return hipGetLastError();
+}
+hipError_t launch_token_i8_down(const I8SkinnyArgs &a, const float *topk_w, uint16_t *Y, hipStream_t st) {
+    const int routes = a.k + (a.shared.N > 0), nw = routes < 16 ? routes : 16;
+    const int pitch = (a.shared.K > a.routed.K ? a.shared.K : a.routed.K) + 16;
+    token_down_kernel<<<dim3((unsigned)(a.routed.N / 16)), dim3(64 * nw), (size_t)nw * pitch, st>>>(a, topk_w, Y,
+                                                                                               pitch);
+    return hipGetLastError();
 }
