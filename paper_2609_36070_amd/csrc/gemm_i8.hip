@@ -14,6 +14,11 @@
 // global->LDS loads (128-byte rows, chunk XOR (row >> 1) & 7), 8 waves of 128 x 64
 // (two per SIMD), tiles rastered XCD-aware.  The MFMA takes 16 consecutive
 // bytes of row l % 32 from lane l, at k 16 (l / 32) of its 32.
+//
+// One workgroup per CU runs tile after tile.  A tile of K = 768 is six steps, and
+// its first loads and its epilogue's stores together take as long: the next
+// tile's first step is asked for before the epilogue, whose stores then drain
+// behind the next tile's products.
 #include "common.h"
 #include "i8_common.h"
 #include "kernels.h"
@@ -27,11 +32,16 @@ typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int BM = 256, BN = 256, BK = 128;
-constexpr int WAVES_M = 2, WAVES_N = 4, NWAVES = WAVES_M * WAVES_N;
+constexpr int WAVES_M = 2, WAVES_N = 4, NWAVES = WAVES_M * WAVES_N;   // XW
 constexpr int NTHREADS = 64 * NWAVES;
 constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 32, TN = WN / 32;
 constexpr int TILE = BM * BK;                      // bytes per operand per stage
 constexpr int LD_PER_OP = TILE / 1024 / NWAVES;    // 1 KB direct loads per operand per wave per step
+
+constexpr int SP = WN + 4;                         // pitch of an epilogue scratch row
+constexpr int STORES = 4 * TM;                     // 16-byte stores per lane and tile
+constexpr int NT = 2;                              // buffer stores past the L2 (non-temporal)
+static_assert(TN == 2, "a gate and an up group of 32 columns per wave");
 
 enum I8Mode { I8_UP = 0, I8_DOWN = 1 };
 
@@ -41,6 +51,16 @@ DEV int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // Raw buffer resource over [p, p + bytes) (gfx9 word 3: 32-bit data format).
 DEV __amdgpu_buffer_rsrc_t make_rsrc(const void *p, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, (int)bytes, 0x00020000);
+}
+// 16 bytes per lane from [p, p + bytes) at voff + soff (zeros past the end) to
+// LDS, consecutive lanes to consecutive places from dst
+DEV void load_lds16(const uint8_t *p, uint32_t bytes, uint8_t *dst, uint32_t voff, uint32_t soff) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(p, bytes), (LDSP void *)dst, 16, voff, soff, 0, 0);
+}
+// 16 bytes per lane to [p, p + bytes) at off, dropped past the end
+template <int AUX>
+DEV void store_b128(u32x4_t v, void *p, uint32_t bytes, uint32_t off) {
+    __builtin_amdgcn_raw_buffer_store_b128(v, make_rsrc(p, bytes), off, 0, AUX);
 }
 DEV void barrier_no_fence() {
     asm volatile("" ::: "memory");
@@ -58,194 +78,284 @@ DEV i32x4_t frag(const uint8_t *t, int r0, int ks, int lane) {
     return __builtin_bit_cast(i32x4_t, ld_u32x4(t + r * BK + 16 * swz(r, 2 * ks + h)));
 }
 
+// One tile: its expert's region and place in it.
+struct I8Tile {
+    int sh, e, row0, row_end, ntile;
+};
+
 template <int MODE>
 __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds_all[4 * TILE];
-    __shared__ float sc_a[BM], sc_b[BN];     // scales of the tile's rows and columns
+    // An array per stage and operand, named where it is used: the compiler lets
+    // direct loads into one of them pass reads of another.  With one array for
+    // all stages it waits for every load in flight before any read of it, so
+    // the loads of step k + 1 had to arrive before step k began (16384 tokens,
+    // 32 experts of 1536, d 4096: up 1770 us, down 1107).
+    __shared__ __attribute__((aligned(16))) uint8_t lds_a0[TILE], lds_b0[TILE], lds_a1[TILE], lds_b1[TILE];
+    // scales of a tile's rows and columns, by parity of the tile, and the waves'
+    // epilogue scratch
+    __shared__ __attribute__((aligned(16))) float epi[2 * (BM + BN) + NWAVES * 8 * SP];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = uniform(tid >> 6);
     const int wm = wave / WAVES_N, wn = wave % WAVES_N;
+    constexpr int COLS = (MODE == I8_UP) ? BN / 2 : BN;     // output columns per tile
 
-    // ---------------- tile: expert region and rows ----------------
-    const bool sh = (int)blockIdx.x < args.shared_grid;   // the shared expert's tiles come first
-    const I8Product &g = sh ? args.shared : args.routed;
-    int e = 0, row0 = 0, row_end = 0, ntile = 0;
-    const int ntn = (MODE == I8_UP) ? g.N / (BN / 2) : g.N / BN;
-    if (sh) {
-        int mt = 0;
-        if (!map_tile(blockIdx.x, (g.rows + BM - 1) / BM, ntn, mt, ntile)) return;
-        row0 = mt * BM;
-        row_end = g.rows;
-    } else {
-        int within = 0;
-        if (!place_tile<BM>(args.offsets, args.E, (int)blockIdx.x - args.shared_grid, ntn, lane, e, within, ntile))
-            return;
-        row0 = uniform(args.offsets[e]) + within * BM;
-        row_end = uniform(args.offsets[e + 1]);
-    }
-    const int n0 = ntile * ((MODE == I8_UP) ? BN / 2 : BN);
-    const bool gather = MODE == I8_UP && !sh;
-
-    // physical A row of tile row r (rows past the region's end repeat its last
-    // row; their results are never stored)
-    auto a_phys = [&](int r) {
-        const int p = min(row0 + r, row_end - 1);
-        const int phys = gather ? args.rowidx[min(max(p, 0), args.routed.rows - 1)] : p;
-        return min(max(phys, 0), g.a_nrows - 1);
+    // ---------------- tiles of this workgroup ----------------
+    // slots blockIdx, blockIdx + 256, ... of the raster (the shared expert's
+    // come first), some of them empty; the experts' tile counts stay in registers
+    ExpertTiles<BM> ex;
+    ex.scan(args.offsets, args.E, lane);
+    const int slots = args.shared_grid + args.routed_grid;
+    int slot = (int)blockIdx.x - (int)gridDim.x;
+    auto next_tile = [&](I8Tile &t) {        // leaves t alone where there is none
+        for (slot += (int)gridDim.x; slot < slots; slot += (int)gridDim.x) {
+            const int sh = slot < args.shared_grid;
+            const I8Product &g = sh ? args.shared : args.routed;
+            const int mtiles = sh ? (g.rows + BM - 1) / BM : ex.total;
+            int mt = 0, n = 0;
+            if (!map_tile(sh ? slot : slot - args.shared_grid, mtiles, g.N / COLS, mt, n)) continue;
+            int e = 0, within = mt;
+            if (!sh) e = ex.find(mt, within);
+            const int first = sh ? 0 : uniform(args.offsets[e]);
+            t = I8Tile{sh, e, first + within * BM, sh ? g.rows : uniform(args.offsets[e + 1]), n};
+            return true;
+        }
+        return false;
+    };
+    // physical A row of a tile's row r (rows past the region's end repeat its
+    // last row; their results are never stored), in two parts: the plan's
+    // entry, then the row's number
+    auto a_entry = [&](const I8Tile &t, int r) {
+        const int p = min(t.row0 + r, t.row_end - 1);
+        return MODE == I8_UP && !t.sh ? args.rowidx[min(max(p, 0), args.routed.rows - 1)] : p;
+    };
+    auto a_row = [&](const I8Tile &t, int entry) {
+        return min(max(entry, 0), (t.sh ? args.shared.a_nrows : args.routed.a_nrows) - 1);
     };
     // MODE I8_UP: tile columns 64 c + 0..31 are gate, 64 c + 32..63 the up columns of the same f
-    auto b_col = [&](int c) { return (MODE == I8_UP) ? n0 + (c >> 6) * 32 + (c & 31) : n0 + c; };
-    if (tid < BM) {
-        sc_a[tid] = g.As[a_phys(tid)];
-    } else {
-        const int c = tid - BM;
-        const float *s = (MODE == I8_UP) && (c & 32) ? g.Bs2 : g.Bs;
-        sc_b[c] = s[(long)e * g.N + b_col(c)];
-    }
+    auto b_col = [&](const I8Tile &t, int c) {
+        return t.ntile * COLS + ((MODE == I8_UP) ? (c >> 6) * 32 + (c & 31) : c);
+    };
 
-    // ---------------- direct-load set-up ----------------
+    // ---------------- loads ----------------
     // Tile load i of wave w is wave instruction q = LD_PER_OP w + i: 1 KB = 8
     // rows of 128 bytes; lane -> row 8 q + lane / 8, physical chunk
     // (lane & 7) ^ ((4 (q & 1) + lane / 16) & 7).
     const int l8 = lane >> 3;
     const uint32_t col_even = 16u * (uint32_t)((lane & 7) ^ ((l8 >> 1) & 7));
     const uint32_t col_odd = 16u * (uint32_t)((lane & 7) ^ ((4 + (l8 >> 1)) & 7));
-    const uint32_t K = (uint32_t)g.K;
-    const uint32_t b_lane_even = (uint32_t)l8 * K + col_even, b_lane_odd = (uint32_t)l8 * K + col_odd;
-    uint32_t a_off[LD_PER_OP];
-#pragma unroll
-    for (int i = 0; i < LD_PER_OP; ++i) {
-        const int q = LD_PER_OP * wave + i;
-        a_off[i] = (uint32_t)a_phys(8 * q + l8) * K + ((q & 1) ? col_odd : col_even);
-    }
-    const int nk = g.K / BK;
-    auto issue_a = [&](int kt, uint8_t *la) {
-#pragma unroll
-        for (int i = 0; i < LD_PER_OP; ++i) {
-            const int q = LD_PER_OP * wave + i;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(g.A, g.a_bytes), (LDSP void *)(la + q * 1024),
-                                                     16, a_off[i], (uint32_t)kt * BK, 0, 0);
-        }
+    struct Loads {
+        uint32_t a[LD_PER_OP];               // lane offsets of A's loads
+        uint32_t scale;                      // row of this thread's scale
     };
-    auto issue_b = [&](int kt, uint8_t *lb) {
+    auto ask_loads = [&](const I8Tile &t, Loads &l) {
+#pragma unroll
+        for (int i = 0; i < LD_PER_OP; ++i) l.a[i] = (uint32_t)a_entry(t, 8 * (LD_PER_OP * wave + i) + l8);
+        l.scale = (uint32_t)a_entry(t, tid & (BM - 1));
+    };
+    auto set_loads = [&](const I8Tile &t, Loads &l) {
+        const uint32_t K = (uint32_t)(t.sh ? args.shared.K : args.routed.K);
+#pragma unroll
+        for (int i = 0; i < LD_PER_OP; ++i)
+            l.a[i] = (uint32_t)a_row(t, (int)l.a[i]) * K + (((LD_PER_OP * wave + i) & 1) ? col_odd : col_even);
+        l.scale = (uint32_t)a_row(t, (int)l.scale);
+    };
+    auto issue_a = [&](const I8Tile &t, const Loads &l, int kt, uint8_t *la) {
+        const I8Product &g = t.sh ? args.shared : args.routed;
+#pragma unroll
+        for (int i = 0; i < LD_PER_OP; ++i)
+            load_lds16(g.A, g.a_bytes, la + (LD_PER_OP * wave + i) * 1024, l.a[i], (uint32_t)kt * BK);
+    };
+    auto issue_b = [&](const I8Tile &t, int kt, uint8_t *lb) {
+        const I8Product &g = t.sh ? args.shared : args.routed;
+        const uint32_t K = (uint32_t)g.K;
 #pragma unroll
         for (int i = 0; i < LD_PER_OP; ++i) {
             const int q = LD_PER_OP * wave + i;
             const bool up = (MODE == I8_UP) && ((q >> 2) & 1);
-            const uint32_t brow = (uint32_t)(e * g.N + b_col(8 * q));
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(up ? g.B2 : g.B, g.b_bytes),
-                                                     (LDSP void *)(lb + q * 1024), 16,
-                                                     (q & 1) ? b_lane_odd : b_lane_even,
-                                                     brow * K + (uint32_t)kt * BK, 0, 0);
+            const uint32_t brow = (uint32_t)(t.e * g.N + b_col(t, 8 * q));
+            load_lds16(up ? g.B2 : g.B, g.b_bytes, lb + q * 1024, (uint32_t)l8 * K + ((q & 1) ? col_odd : col_even),
+                       brow * K + (uint32_t)kt * BK);
         }
     };
+    // thread tid's scale of a tile: row tid, or column tid - BM
+    static_assert(NTHREADS == BM + BN && BM % 64 == 0, "a scale per thread, rows and columns in waves of their own");
+    // (gate and up channels alternate by 32 lanes: a wave of columns reads both arrays)
+    auto scale_at = [&](const I8Tile &t, const Loads &l) {
+        const I8Product &g = t.sh ? args.shared : args.routed;
+        const int c = (tid - BM) & (BN - 1);
+        return tid < BM ? g.As + l.scale
+                        : ((MODE == I8_UP) && (c & 32) ? g.Bs2 : g.Bs) + ((long)t.e * g.N + b_col(t, c));
+    };
 
-    i32x16_t acc[TM][TN];
+    I8Tile t, nt;
+    Loads ld, nld;
+    if (!next_tile(t)) return;
+    nt = t;
+    ask_loads(t, ld);
+    set_loads(t, ld);
+    nld = ld;
+    float scale = *scale_at(t, ld);
+    issue_b(t, 0, lds_b0);
+    issue_a(t, ld, 0, lds_a0);
+    // in the place of a previous tile's stores, as many that an empty range drops
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
+    for (int i = 0; i < STORES; ++i) store_b128<0>(u32x4_t{0, 0, 0, 0}, args.routed.H, 0, 0);
+    issue_a(t, ld, 1, lds_a1);               // K is a multiple of 256: steps come in pairs
+    issue_b(t, 1, lds_b1);
 
-    // Fragments one step ahead of their MFMAs.
-    constexpr int KS = BK / 32;
-    i32x4_t bfr[TN], a_cur;
-    auto compute_ks = [&](const uint8_t *la, const uint8_t *lb, int ks) {
-        if (ks == 0) {
+    constexpr int KS = BK / 32, LPS = 2 * LD_PER_OP;
+    const int lrow = lane & 31, lhalf = lane >> 5;
+    float *const scr = epi + 2 * (BM + BN) + wave * 8 * SP;
+    for (int parity = 0;; parity ^= 1) {
+        epi[parity * (BM + BN) + tid] = scale;
+        i32x16_t acc[TM][TN];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) bfr[j] = frag(lb, wn * WN + 32 * j, 0, lane);
-            a_cur = frag(la, wm * WM, 0, lane);
-        }
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            i32x4_t a_nxt = a_cur;
-            if (i + 1 < TM) a_nxt = frag(la, wm * WM + 32 * (i + 1), ks, lane);
-            else if (ks + 1 < KS) a_nxt = frag(la, wm * WM, ks + 1, lane);
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a_cur, bfr[j], acc[i][j], 0, 0, 0);
-                if (i == TM - 1 && ks + 1 < KS) bfr[j] = frag(lb, wn * WN + 32 * j, ks + 1, lane);
+                for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
+        // Fragments one step ahead of their MFMAs.
+        i32x4_t bfr[TN], a_cur;
+        auto compute_ks = [&](const uint8_t *la, const uint8_t *lb, int ks) {
+            if (ks == 0) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) bfr[j] = frag(lb, wn * WN + 32 * j, 0, lane);
+                a_cur = frag(la, wm * WM, 0, lane);
             }
-            a_cur = a_nxt;
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                i32x4_t a_nxt = a_cur;
+                if (i + 1 < TM) a_nxt = frag(la, wm * WM + 32 * (i + 1), ks, lane);
+                else if (ks + 1 < KS) a_nxt = frag(la, wm * WM, ks + 1, lane);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a_cur, bfr[j], acc[i][j], 0, 0, 0);
+                    if (i == TM - 1 && ks + 1 < KS) bfr[j] = frag(lb, wn * WN + 32 * j, ks + 1, lane);
+                }
+                a_cur = a_nxt;
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
 
-    issue_a(0, lds_all);
-    issue_b(0, lds_all + 2 * TILE);
-    int cur = 0;
-#pragma clang loop unroll(disable)
-    for (int kt = 0; kt < nk; ++kt) {
+        // Step 0 of a tile is asked for at the last step of the tile before (the
+        // last tile's own again where there is none after it: one sequence of loads
+        // and stores, whose waits are known counts), ahead of that tile's stores,
+        // step 1 behind them, step kt + 1 at step kt from then on.  What the next
+        // tile is, is asked three steps before the end; its rows' numbers are there
+        // a step later.
+        const int nk = (t.sh ? args.shared.K : args.routed.K) / BK;
+        bool more = false;
+        auto ask_next = [&] {
+            more = next_tile(nt);
+            if (more) ask_loads(nt, nld);
+        };
+        auto set_next = [&] {
+            if (more) {
+                set_loads(nt, nld);
+                scale = *scale_at(nt, nld);
+            }
+        };
+        // the second step of a pair, and the loads of the step after it
+        auto odd_step = [&](int kt) {
+            const bool last = kt + 1 == nk;
+            const I8Tile &lt = last ? nt : t;
+            const Loads &ll = last ? nld : ld;
+            const int lk = last ? 0 : kt + 1;
+            issue_b(lt, lk, lds_b0);
+            asm volatile("" ::: "memory");
+            compute_ks(lds_a1, lds_b1, 0);
+            compute_ks(lds_a1, lds_b1, 1);
+            asm volatile("" ::: "memory");
+            issue_a(lt, ll, lk, lds_a0);
+            asm volatile("" ::: "memory");
+            compute_ks(lds_a1, lds_b1, 2);
+            compute_ks(lds_a1, lds_b1, 3);
+        };
+        wait_vmcnt<LPS + STORES>();
+        barrier_no_fence();
+        if (nk == 2) {
+            ask_next();
+            set_next();
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) compute_ks(lds_a0, lds_b0, ks);
         wait_vmcnt<0>();
         barrier_no_fence();
-        const int nxt = uniform(cur ^ 1);
-        const uint8_t *la = lds_all + cur * TILE, *lb = lds_all + (2 + cur) * TILE;
-        if (kt + 1 < nk) issue_b(kt + 1, lds_all + (2 + nxt) * TILE);
-        asm volatile("" ::: "memory");
-        compute_ks(la, lb, 0);
-        compute_ks(la, lb, 1);
-        if (kt + 1 < nk) {
+        if (nk == 4) ask_next();
+        odd_step(1);
+#pragma clang loop unroll(disable)
+        for (int kt = 2; kt < nk; kt += 2) {
+            wait_vmcnt<0>();
+            barrier_no_fence();
+            if (kt + 2 == nk) set_next();
+            issue_b(t, kt + 1, lds_b1);
             asm volatile("" ::: "memory");
-            issue_a(kt + 1, lds_all + nxt * TILE);
+            compute_ks(lds_a0, lds_b0, 0);
+            compute_ks(lds_a0, lds_b0, 1);
             asm volatile("" ::: "memory");
+            issue_a(t, ld, kt + 1, lds_a1);
+            asm volatile("" ::: "memory");
+            compute_ks(lds_a0, lds_b0, 2);
+            compute_ks(lds_a0, lds_b0, 3);
+            wait_vmcnt<0>();
+            barrier_no_fence();
+            if (kt + 4 == nk) ask_next();
+            odd_step(kt + 1);
         }
-        compute_ks(la, lb, 2);
-        compute_ks(la, lb, 3);
-        cur = nxt;
+        // ---------------- epilogue ----------------
+        // accumulator layout: lane l, register q -> row 8 (q / 4) + 4 (l / 32) + q % 4,
+        // column l % 32.  8 rows at a time go through a scratch of the wave's own
+        // (8 x WN fp32), one 16-byte store per lane each; rows past the region lie
+        // past the end of the stores' resource and are dropped there, so that
+        // every tile has the same number of stores.
+        const I8Product &g = t.sh ? args.shared : args.routed;
+        const float *sc = epi + parity * (BM + BN);
+        float sb[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sb[j] = sc[BM + wn * WN + 32 * j + lrow];
+        const int rows = t.row_end - t.row0, er = lane >> 3, ec = lane & 7;
+        constexpr uint32_t ELEM = (MODE == I8_UP) ? 4 : 2;
+        void *const out = (MODE == I8_UP) ? (void *)(g.H + (long)t.row0 * g.N) : (void *)(g.C + (long)t.row0 * g.N);
+        const uint32_t out_bytes = (uint32_t)min(rows, BM) * (uint32_t)g.N * ELEM;
+        const int n0 = t.ntile * COLS;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int qg = 0; qg < 4; ++qg) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        scr[(4 * lhalf + q) * SP + 32 * j + lrow] = (float)acc[i][j][4 * qg + q] * sb[j];
+                const int rl = wm * WM + 32 * i + 8 * qg + er;
+                const float sr = sc[rl];
+                if constexpr (MODE == I8_UP) {
+                    const f32x4_t ga = *reinterpret_cast<const f32x4_t *>(scr + er * SP + 4 * ec);
+                    const f32x4_t ub = *reinterpret_cast<const f32x4_t *>(scr + er * SP + 32 + 4 * ec);
+                    f32x4_t h;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) h[k] = silu_f(sr * ga[k]) * (sr * ub[k]);
+                    store_b128<0>(__builtin_bit_cast(u32x4_t, h), out, out_bytes,
+                                  (uint32_t)(rl * g.N + n0 + wn * 32 + 4 * ec) * ELEM);
+                } else {
+                    f32x8 v = ld_f32x8(scr + er * SP + 8 * ec);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = sr * v[k];
+                    store_b128<NT>(pack_bf8(v), out, out_bytes,
+                                   (uint32_t)(rl * g.N + n0 + wn * WN + 8 * ec) * ELEM);
+                }
+            }
+        // every wave is done with the last step's stage by now
+        barrier_no_fence();
+        if (!more) break;
+        t = nt;
+        ld = nld;
+        issue_a(t, ld, 1, lds_a1);
+        issue_b(t, 1, lds_b1);
     }
-    __syncthreads();
-
-    // ---------------- epilogue ----------------
-    // accumulator layout: lane l, register q -> row 8 (q / 4) + 4 (l / 32) + q % 4,
-    // column l % 32; rows go through a per-wave LDS scratch (32 x WN fp32)
-    const int lrow = lane & 31, lhalf = lane >> 5;
-    constexpr int SP = WN + 4;
-    static_assert(NWAVES * 32 * SP * 4 <= 4 * TILE, "epilogue scratch fits the stages");
-    float *scr = reinterpret_cast<float *>(lds_all) + wave * 32 * SP;
-    float sb[TN];
-#pragma unroll
-    for (int j = 0; j < TN; ++j) sb[j] = sc_b[wn * WN + 32 * j + lrow];
-    auto stage = [&](int i) {
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const int row = 8 * (q >> 2) + 4 * lhalf + (q & 3);
-                scr[row * SP + 32 * j + lrow] = (float)acc[i][j][q] * sb[j];
-            }
-    };
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        stage(i);
-        if constexpr (MODE == I8_UP) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int row = (lane >> 2) + 16 * t, c = 8 * (lane & 3);
-                const int rl = wm * WM + 32 * i + row, p = row0 + rl;
-                const float sr = sc_a[rl];
-                const f32x8 ga = ld_f32x8(scr + row * SP + c), ub = ld_f32x8(scr + row * SP + 32 + c);
-                f32x8 h;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) h[k] = silu_f(sr * ga[k]) * (sr * ub[k]);
-                if (p < row_end) st_f32x8(g.H + (long)p * g.N + n0 + wn * 32 + c, h);
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int row = (lane >> 3) + 8 * t, c = 8 * (lane & 7);
-                const int rl = wm * WM + 32 * i + row, p = row0 + rl;
-                const float sr = sc_a[rl];
-                f32x8 v = ld_f32x8(scr + row * SP + c);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = sr * v[k];
-                if (p < row_end)
-                    __builtin_nontemporal_store(pack_bf8(v), reinterpret_cast<u32x4_t *>(
-                                                                 g.C + (long)p * g.N + n0 + wn * WN + c));
-            }
-        }
-    }
+    wait_vmcnt<0>();                         // no load into LDS outlives the workgroup
 }
 
 template <int MODE>
@@ -256,7 +366,9 @@ hipError_t launch_i8_mode(I8GemmArgs a, hipStream_t st) {
     const long rt = a.routed.rows > 0 ? raster_grid(a.routed.rows / BM + a.E, a.routed.N / cols) : 0;
     if (sh + rt <= 0) return hipSuccess;
     a.shared_grid = (int)sh;
-    gemm_i8_kernel<MODE><<<dim3((unsigned)(sh + rt)), dim3(NTHREADS), 0, st>>>(a);
+    a.routed_grid = (int)rt;
+    // one workgroup per CU (the rasters' grids are multiples of 256)
+    gemm_i8_kernel<MODE><<<dim3(256), dim3(NTHREADS), 0, st>>>(a);
     return hipGetLastError();
 }
 

@@ -287,7 +287,7 @@ struct I8GemmArgs {
     const int *offsets = nullptr;      // [E+1] expert regions
     const int *rowidx = nullptr;       // up product: token of each plan row
     int E = 0;
-    int shared_grid = 0;               // set by the launcher
+    int shared_grid = 0, routed_grid = 0;   // set by the launcher: slots of the rasters
 };
 // The same for small batches (skinny_i8.hip).
 struct I8SkinnyArgs {
