@@ -65,8 +65,9 @@ def moe_forward_int(X, Wq, idx, w, extra=0.0):
         near = tie_codes(a, h, hs, extra)
         flip = near.astype(np.float64) @ np.abs(dn[0]).T.astype(np.float64)
         off = flip * hs[:, None].astype(np.float64) * dn[1].astype(np.float64)
-        # the scale hs carries the error of the largest value, the output rounds to bf16
-        off += np.abs(y) * (2.0 ** -8 + 200 * 2.0 ** -24)
+        # the scale hs carries the error of the largest value; the output rounds to
+        # bf16: half a step of the computed value, which is at most |y| + off
+        off += (np.abs(y) + off) * (2.0 ** -8 + 200 * 2.0 ** -24)
         Y[t] += wt[:, None] * y
         tol[t] += np.abs(wt)[:, None] * off
 
@@ -76,4 +77,4 @@ def moe_forward_int(X, Wq, idx, w, extra=0.0):
             add(t, w[t, s].astype(np.float64), Wq["g"][e], Wq["u"][e], Wq["d"][e])
     if "gs" in Wq:
         add(np.arange(T), np.ones(T), Wq["gs"], Wq["us"], Wq["ds"])
-    return Y, tol + np.abs(Y) * 2.0 ** -8 + 1e-30
+    return Y, tol + (np.abs(Y) + tol) * 2.0 ** -8 + 1e-30

@@ -39,7 +39,8 @@ constexpr int TILE = BM * BK;                      // bytes per operand per stag
 constexpr int LD_PER_OP = TILE / 1024 / NWAVES;    // 1 KB direct loads per operand per wave per step
 
 constexpr int SP = WN + 4;                         // pitch of an epilogue scratch row
-constexpr int STORES = 4 * TM;                     // 16-byte stores per lane and tile
+// stores per lane and tile: up product one per value of H, down product 8 rows at a time
+template <int MODE> constexpr int STORES = MODE == 0 ? 16 * TM : 4 * TM;
 constexpr int NT = 2;                              // buffer stores past the L2 (non-temporal)
 static_assert(TN == 2, "a gate and an up group of 32 columns per wave");
 
@@ -57,10 +58,13 @@ DEV __amdgpu_buffer_rsrc_t make_rsrc(const void *p, uint32_t bytes) {
 DEV void load_lds16(const uint8_t *p, uint32_t bytes, uint8_t *dst, uint32_t voff, uint32_t soff) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(p, bytes), (LDSP void *)dst, 16, voff, soff, 0, 0);
 }
-// 16 bytes per lane to [p, p + bytes) at off, dropped past the end
-template <int AUX>
+// 16 or 4 bytes per lane to [p, p + bytes), dropped past the end; the first past
+// the L2, which holds the operand panels
 DEV void store_b128(u32x4_t v, void *p, uint32_t bytes, uint32_t off) {
-    __builtin_amdgcn_raw_buffer_store_b128(v, make_rsrc(p, bytes), off, 0, AUX);
+    __builtin_amdgcn_raw_buffer_store_b128(v, make_rsrc(p, bytes), off, 0, NT);
+}
+DEV void store_b32(float v, void *p, uint32_t bytes, uint32_t voff, uint32_t soff) {
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), make_rsrc(p, bytes), voff, soff, 0);
 }
 DEV void barrier_no_fence() {
     asm volatile("" ::: "memory");
@@ -197,13 +201,10 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
     float scale = *scale_at(t, ld);
     issue_b(t, 0, lds_b0);
     issue_a(t, ld, 0, lds_a0);
-    // in the place of a previous tile's stores, as many that an empty range drops
-#pragma unroll
-    for (int i = 0; i < STORES; ++i) store_b128<0>(u32x4_t{0, 0, 0, 0}, args.routed.H, 0, 0);
     issue_a(t, ld, 1, lds_a1);               // K is a multiple of 256: steps come in pairs
     issue_b(t, 1, lds_b1);
-
     constexpr int KS = BK / 32, LPS = 2 * LD_PER_OP;
+    wait_vmcnt<LPS>();
     const int lrow = lane & 31, lhalf = lane >> 5;
     float *const scr = epi + 2 * (BM + BN) + wave * 8 * SP;
     for (int parity = 0;; parity ^= 1) {
@@ -273,7 +274,8 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
             compute_ks(lds_a1, lds_b1, 2);
             compute_ks(lds_a1, lds_b1, 3);
         };
-        wait_vmcnt<LPS + STORES>();
+        // (the counter ends at 63: with more behind them, the first stores too)
+        wait_vmcnt<LPS + STORES<MODE> < 63 ? LPS + STORES<MODE> : 63>();
         barrier_no_fence();
         if (nk == 2) {
             ask_next();
@@ -306,47 +308,57 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
         }
         // ---------------- epilogue ----------------
         // accumulator layout: lane l, register q -> row 8 (q / 4) + 4 (l / 32) + q % 4,
-        // column l % 32.  8 rows at a time go through a scratch of the wave's own
-        // (8 x WN fp32), one 16-byte store per lane each; rows past the region lie
-        // past the end of the stores' resource and are dropped there, so that
-        // every tile has the same number of stores.
+        // column l % 32.  Rows past the region lie past the end of the stores'
+        // resource and are dropped there, so that every tile has the same number
+        // of stores.
         const I8Product &g = t.sh ? args.shared : args.routed;
         const float *sc = epi + parity * (BM + BN);
         float sb[TN];
 #pragma unroll
         for (int j = 0; j < TN; ++j) sb[j] = sc[BM + wn * WN + 32 * j + lrow];
-        const int rows = t.row_end - t.row0, er = lane >> 3, ec = lane & 7;
-        constexpr uint32_t ELEM = (MODE == I8_UP) ? 4 : 2;
-        void *const out = (MODE == I8_UP) ? (void *)(g.H + (long)t.row0 * g.N) : (void *)(g.C + (long)t.row0 * g.N);
-        const uint32_t out_bytes = (uint32_t)min(rows, BM) * (uint32_t)g.N * ELEM;
-        const int n0 = t.ntile * COLS;
+        const int rows = min(t.row_end - t.row0, BM), n0 = t.ntile * COLS;
+        if constexpr (MODE == I8_UP) {
+            // a lane has gate and up of the same column: H needs no exchange, and
+            // the 32 lanes of a row store a whole line
+            float *const out = g.H + (long)t.row0 * g.N;
+            const uint32_t bytes = (uint32_t)rows * (uint32_t)g.N * 4u, pitch = (uint32_t)g.N * 4u;
+            const uint32_t lane_off = (uint32_t)(4 * lhalf) * pitch + (uint32_t)(n0 + wn * 32 + lrow) * 4u;
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+            for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int qg = 0; qg < 4; ++qg) {
+                for (int qg = 0; qg < 4; ++qg) {
+                    const int rl = wm * WM + 32 * i + 8 * qg;
+                    const f32x4_t sr = *reinterpret_cast<const f32x4_t *>(sc + rl + 4 * lhalf);
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
+                    for (int q = 0; q < 4; ++q) {
+                        const float ga = sr[q] * ((float)acc[i][0][4 * qg + q] * sb[0]);
+                        const float ub = sr[q] * ((float)acc[i][1][4 * qg + q] * sb[1]);
+                        store_b32(silu_f(ga) * ub, out, bytes, lane_off, (uint32_t)(rl + q) * pitch);
+                    }
+                }
+        } else {
+            // 8 rows at a time through a scratch of the wave's own (8 x WN fp32),
+            // one 16-byte store per lane
+            const int er = lane >> 3, ec = lane & 7;
+            uint16_t *const out = g.C + (long)t.row0 * g.N;
+            const uint32_t bytes = (uint32_t)rows * (uint32_t)g.N * 2u;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        scr[(4 * lhalf + q) * SP + 32 * j + lrow] = (float)acc[i][j][4 * qg + q] * sb[j];
-                const int rl = wm * WM + 32 * i + 8 * qg + er;
-                const float sr = sc[rl];
-                if constexpr (MODE == I8_UP) {
-                    const f32x4_t ga = *reinterpret_cast<const f32x4_t *>(scr + er * SP + 4 * ec);
-                    const f32x4_t ub = *reinterpret_cast<const f32x4_t *>(scr + er * SP + 32 + 4 * ec);
-                    f32x4_t h;
+            for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) h[k] = silu_f(sr * ga[k]) * (sr * ub[k]);
-                    store_b128<0>(__builtin_bit_cast(u32x4_t, h), out, out_bytes,
-                                  (uint32_t)(rl * g.N + n0 + wn * 32 + 4 * ec) * ELEM);
-                } else {
+                for (int qg = 0; qg < 4; ++qg) {
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            scr[(4 * lhalf + q) * SP + 32 * j + lrow] = (float)acc[i][j][4 * qg + q] * sb[j];
+                    const int rl = wm * WM + 32 * i + 8 * qg + er;
+                    const float sr = sc[rl];
                     f32x8 v = ld_f32x8(scr + er * SP + 8 * ec);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] = sr * v[k];
-                    store_b128<NT>(pack_bf8(v), out, out_bytes,
-                                   (uint32_t)(rl * g.N + n0 + wn * WN + 8 * ec) * ELEM);
+                    store_b128(pack_bf8(v), out, bytes, (uint32_t)(rl * g.N + n0 + wn * WN + 8 * ec) * 2u);
                 }
-            }
+        }
         // every wave is done with the last step's stage by now
         barrier_no_fence();
         if (!more) break;
