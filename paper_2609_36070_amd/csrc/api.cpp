@@ -1884,15 +1884,14 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
         return MOE_OK;
     }
     const int tt = skinny_tiles(T, k, E, f, fs);
-    if (!tt)
-        MOE_TRY(launch_prep(plan->perm, plan->offsets, E, topk_w, k, T, at<int>(ws, L.rowidx),
-                            at<float>(ws, L.wperm), at<uint16_t>(ws, L.zeros), s));
-    MOE_TRY(launch_i8_quant_rows(X, T, d, xq, xs, s));
+    if (tt)
+        MOE_TRY(launch_i8_quant_tokens(X, T, d, xq, xs, s));
+    else
+        MOE_TRY(launch_i8_prologue(X, T, d, xq, xs, plan->perm, plan->offsets, E, k, at<int>(ws, L.rowidx), s));
     MOE_TRY(mk.mark(1));
     MOE_TRY(tt ? launch_skinny_i8_up(small, tt, s) : launch_gemm_i8_up(up, s));
     MOE_TRY(mk.mark(2));
-    MOE_TRY(launch_i8_quant_rows_f32(up.routed.H, R, f, hq, hs, s));
-    if (fs > 0) MOE_TRY(launch_i8_quant_rows_f32(up.shared.H, T, fs, hshq, hshs, s));
+    MOE_TRY(launch_i8_quant_h(up.routed.H, R, f, hq, hs, up.shared.H, fs > 0 ? T : 0, fs, hshq, hshs, s));
     MOE_TRY(mk.mark(3));
     small.routed = down.routed; small.shared = down.shared;
     MOE_TRY(tt ? launch_skinny_i8_down(small, tt, s) : launch_gemm_i8_down(down, s));

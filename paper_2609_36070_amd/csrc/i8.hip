@@ -11,6 +11,8 @@
 
 namespace {
 
+template <int N> struct Chunks { static constexpr int value = N; };
+
 DEV void load8(const uint16_t *p, float (&v)[8]) {
     const u32x4_t w = ld_u32x4(p);
 #pragma unroll
@@ -34,17 +36,23 @@ DEV uint32_t block_max(uint32_t x, uint32_t *red) {
     return umax(umax(red[0], red[1]), umax(red[2], red[3]));
 }
 
-// A block per row, 8 elements per thread and step.  Rows of up to 2048 NC
-// elements are held in registers between the two passes (NC = 0: read again).
+// Rows of a matrix to quantise.
+template <typename S>
+struct QuantRows {
+    const S *X;
+    uint8_t *q;
+    float *sc;
+    long rows;
+    int K;
+};
+
+// Row `row`, 8 elements per thread and step.  Rows of up to 2048 NC elements are
+// held in registers between the two passes (NC = 0: read again).
 template <typename S, int NC>
-__global__ __launch_bounds__(256) void i8_quant_rows_kernel(const S *__restrict__ X, int K,
-                                                            uint8_t *__restrict__ q,
-                                                            float *__restrict__ sc) {
-    __shared__ uint32_t red[4];
-    const long row = blockIdx.x;
-    const S *x = X + row * K;
-    uint8_t *o = q + row * K;
-    const int n8 = K / 8;
+DEV void quant_row(const QuantRows<S> &m, long row, uint32_t *red) {
+    const S *x = m.X + row * m.K;
+    uint8_t *o = m.q + row * m.K;
+    const int n8 = m.K / 8;
     float v[NC > 0 ? NC : 1][8];
     uint32_t amax = 0;
     auto put = [&](const float (&y)[8], const I8Scale &s, int c) {
@@ -66,7 +74,7 @@ __global__ __launch_bounds__(256) void i8_quant_rows_kernel(const S *__restrict_
 #pragma unroll
             for (int j = 0; j < 8; ++j) amax = umax(amax, abs_bits(v[i][j]));
         const I8Scale s(block_max(amax, red));
-        if (threadIdx.x == 0) sc[row] = s.s;
+        if (threadIdx.x == 0) m.sc[row] = s.s;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = threadIdx.x + 256 * i;
@@ -79,12 +87,39 @@ __global__ __launch_bounds__(256) void i8_quant_rows_kernel(const S *__restrict_
             for (int j = 0; j < 8; ++j) amax = umax(amax, abs_bits(v[0][j]));
         }
         const I8Scale s(block_max(amax, red));
-        if (threadIdx.x == 0) sc[row] = s.s;
+        if (threadIdx.x == 0) m.sc[row] = s.s;
         for (int c = threadIdx.x; c < n8; c += 256) {
             load8(x + 8 * c, v[0]);
             put(v[0], s, c);
         }
     }
+}
+
+// A block per row of one matrix, then of another.
+template <typename S, int NC>
+__global__ __launch_bounds__(256) void i8_quant_rows_kernel(QuantRows<S> m0, QuantRows<S> m1) {
+    __shared__ uint32_t red[4];
+    const long b = blockIdx.x;
+    if (b < m0.rows) quant_row<S, NC>(m0, b, red);
+    else quant_row<S, NC>(m1, b - m0.rows, red);
+}
+
+// The tile products' prologue in one launch: the tokens' rows, and the token of
+// every position of the plan (0 where the plan has none), 256 per block.
+template <int NC>
+__global__ __launch_bounds__(256) void i8_prologue_kernel(QuantRows<uint16_t> x, const int *__restrict__ perm,
+                                                          const int *__restrict__ offsets, int E, int k, int R,
+                                                          int *__restrict__ rowidx) {
+    __shared__ uint32_t red[4];
+    const long b = blockIdx.x;
+    if (b < x.rows) {
+        quant_row<uint16_t, NC>(x, b, red);
+        return;
+    }
+    const int p = (int)(b - x.rows) * 256 + threadIdx.x;
+    if (p >= R) return;
+    const int j = p < offsets[E] ? perm[p] : -1;
+    rowidx[p] = j >= 0 && j < R ? j / k : 0;
 }
 
 // A block per 64 channels of an expert: the channels' largest magnitudes over
@@ -143,26 +178,43 @@ __global__ __launch_bounds__(256) void i8_quant_weights_kernel(const uint16_t *_
     }
 }
 
-template <typename S>
-hipError_t quant_rows(const S *X, long rows, int K, uint8_t *q, float *sc, hipStream_t st) {
-    if (rows <= 0) return hipSuccess;
-    const dim3 grid((unsigned)rows), block(256);
-    if (K <= 2048) i8_quant_rows_kernel<S, 1><<<grid, block, 0, st>>>(X, K, q, sc);
-    else if (K <= 4096) i8_quant_rows_kernel<S, 2><<<grid, block, 0, st>>>(X, K, q, sc);
-    else if (K <= 8192) i8_quant_rows_kernel<S, 4><<<grid, block, 0, st>>>(X, K, q, sc);
-    else i8_quant_rows_kernel<S, 0><<<grid, block, 0, st>>>(X, K, q, sc);
+// f(NC) for rows of K elements: chunks of 2048 in registers
+template <typename F>
+hipError_t with_chunks(int K, F f) {
+    if (K <= 2048) f(Chunks<1>{});
+    else if (K <= 4096) f(Chunks<2>{});
+    else if (K <= 8192) f(Chunks<4>{});
+    else f(Chunks<0>{});
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_i8_quant_rows(const uint16_t *X, long rows, int K, uint8_t *q, float *sc,
-                                hipStream_t st) {
-    return quant_rows(X, rows, K, q, sc, st);
+hipError_t launch_i8_quant_tokens(const uint16_t *X, long rows, int K, uint8_t *q, float *sc, hipStream_t st) {
+    if (rows <= 0) return hipSuccess;
+    const QuantRows<uint16_t> m{X, q, sc, rows, K};
+    return with_chunks(K, [&](auto nc) {
+        i8_quant_rows_kernel<uint16_t, decltype(nc)::value><<<dim3((unsigned)rows), dim3(256), 0, st>>>(
+            m, QuantRows<uint16_t>{});
+    });
 }
-hipError_t launch_i8_quant_rows_f32(const float *X, long rows, int K, uint8_t *q, float *sc,
-                                    hipStream_t st) {
-    return quant_rows(X, rows, K, q, sc, st);
+hipError_t launch_i8_prologue(const uint16_t *X, int T, int d, uint8_t *q, float *sc, const int *perm,
+                              const int *offsets, int E, int k, int *rowidx, hipStream_t st) {
+    if (T <= 0) return hipSuccess;
+    const QuantRows<uint16_t> m{X, q, sc, T, d};
+    const int R = T * k;
+    return with_chunks(d, [&](auto nc) {
+        i8_prologue_kernel<decltype(nc)::value><<<dim3((unsigned)(T + (R + 255) / 256)), dim3(256), 0, st>>>(
+            m, perm, offsets, E, k, R, rowidx);
+    });
+}
+hipError_t launch_i8_quant_h(const float *H, long rows, int f, uint8_t *q, float *sc, const float *Hs,
+                             long rows_s, int fs, uint8_t *qs, float *scs, hipStream_t st) {
+    if (rows + rows_s <= 0) return hipSuccess;
+    const QuantRows<float> m{H, q, sc, rows, f}, ms{Hs, qs, scs, rows_s, fs};
+    return with_chunks(rows_s > 0 && fs > f ? fs : f, [&](auto nc) {
+        i8_quant_rows_kernel<float, decltype(nc)::value><<<dim3((unsigned)(rows + rows_s)), dim3(256), 0, st>>>(m, ms);
+    });
 }
 hipError_t launch_i8_quant_weights(const uint16_t *W, int E, int K, int N, uint8_t *q, float *sc,
                                    hipStream_t st) {

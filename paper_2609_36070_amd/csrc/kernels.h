@@ -306,10 +306,13 @@ hipError_t launch_token_i8_up(const I8SkinnyArgs &a, hipStream_t st);
 hipError_t launch_token_i8_down(const I8SkinnyArgs &a, const float *topk_w, uint16_t *Y, hipStream_t st);
 hipError_t launch_gemm_i8_up(const I8GemmArgs &a, hipStream_t st);
 hipError_t launch_gemm_i8_down(const I8GemmArgs &a, hipStream_t st);
-hipError_t launch_i8_quant_rows(const uint16_t *X, long rows, int K, uint8_t *q, float *sc,
-                                hipStream_t st);
-hipError_t launch_i8_quant_rows_f32(const float *X, long rows, int K, uint8_t *q, float *sc,
-                                    hipStream_t st);
+// X to codes; the same with the token of every plan position (tile products);
+// H of the routed experts' rows and of the shared expert's (rows_s of them).
+hipError_t launch_i8_quant_tokens(const uint16_t *X, long rows, int K, uint8_t *q, float *sc, hipStream_t st);
+hipError_t launch_i8_prologue(const uint16_t *X, int T, int d, uint8_t *q, float *sc, const int *perm,
+                              const int *offsets, int E, int k, int *rowidx, hipStream_t st);
+hipError_t launch_i8_quant_h(const float *H, long rows, int f, uint8_t *q, float *sc, const float *Hs,
+                             long rows_s, int fs, uint8_t *qs, float *scs, hipStream_t st);
 hipError_t launch_i8_quant_weights(const uint16_t *W, int E, int K, int N, uint8_t *q, float *sc,
                                    hipStream_t st);
 hipError_t launch_schedule(const int *A, int R, int NK, int L, int c, int *M, int *S, int *phi,

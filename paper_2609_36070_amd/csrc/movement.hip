@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const uint16_t *__restrict
                 wt[s] = topk_w[(long)t * k + s];
             }
         }
-        for (int c = threadIdx.x; c < nc; c += 256) {
+        for (int c = threadIdx.x + 256 * blockIdx.y; c < nc; c += 256 * gridDim.y) {
             // every load first (slots past k or without a position read row 0
             // and are not added), so they are in flight together
             u32x4_t rows[16];
@@ -682,7 +682,9 @@ hipError_t launch_prep(const int *perm, const int *offsets, int E, const float *
 hipError_t launch_combine(const uint16_t *Yexp, const uint16_t *Ysh, const float *topk_w,
                           const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st) {
     if (T == 0) return hipSuccess;
-    combine_kernel<<<dim3(rows_grid(T)), dim3(256), 0, st>>>(Yexp, Ysh, topk_w, route_pos, T, d, k,
+    // few tokens: a block per 2048 columns of one (61 tokens, 9 rows of 7168 each, 8.8 -> REPLACE_CMB us)
+    const unsigned cols = T <= 256 ? (unsigned)((d + 2047) / 2048) : 1;
+    combine_kernel<<<dim3(rows_grid(T), cols), dim3(256), 0, st>>>(Yexp, Ysh, topk_w, route_pos, T, d, k,
                                                               T * k, Y);
     return hipGetLastError();
 }
