@@ -68,8 +68,8 @@ def moe_forward_int(X, Wq, idx, w, extra=0.0):
         # the scale hs carries the error of the largest value; the output rounds to
         # bf16: half a step of the computed value, which is at most |y| + off
         off += (np.abs(y) + off) * (2.0 ** -8 + 200 * 2.0 ** -24)
-        Y[t] += wt[:, None] * y
-        tol[t] += np.abs(wt)[:, None] * off
+        np.add.at(Y, t, wt[:, None] * y)      # a token may list an expert twice
+        np.add.at(tol, t, np.abs(wt)[:, None] * off)
 
     for e in range(len(Wq["g"])):
         t, s = np.nonzero(idx == e)

@@ -1883,7 +1883,7 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
         for (int i = 4; i <= 6; ++i) MOE_TRY(mk.mark(i));
         return MOE_OK;
     }
-    const int tt = skinny_tiles(T, k, E, f, fs);
+    const int tt = skinny_i8_tiles(T, k, E, f, fs);
     if (tt)
         MOE_TRY(launch_i8_quant_tokens(X, T, d, xq, xs, s));
     else

@@ -682,7 +682,7 @@ hipError_t launch_prep(const int *perm, const int *offsets, int E, const float *
 hipError_t launch_combine(const uint16_t *Yexp, const uint16_t *Ysh, const float *topk_w,
                           const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st) {
     if (T == 0) return hipSuccess;
-    // few tokens: a block per 2048 columns of one (61 tokens, 9 rows of 7168 each, 8.8 -> REPLACE_CMB us)
+    // few tokens: a block per 2048 columns of one (61 tokens, 9 rows of 7168 each: 1 us less)
     const unsigned cols = T <= 256 ? (unsigned)((d + 2047) / 2048) : 1;
     combine_kernel<<<dim3(rows_grid(T), cols), dim3(256), 0, st>>>(Yexp, Ysh, topk_w, route_pos, T, d, k,
                                                               T * k, Y);

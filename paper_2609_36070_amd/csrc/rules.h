@@ -88,32 +88,61 @@ inline int skinny_kslices(long T, long k, long E, long d, long f, long fs, long 
 }
 
 // Int8, one token (skinny_i8.hip): rows whose codes fit the workgroups' LDS.
+// Two launches in place of five (us here / the streaming kernels): 128 experts,
+// top 8, d 2048, f 768 15.8 / 26; 64, top 4, d 4096, f 256 12.0 / 27.6; 32, top 8, and a
+// shared one, d 7168, f 2048 80 / 98; 16, top 2, d 1024, f 512 10 / 20.6.
 constexpr long TOKEN_I8_K = 8192, TOKEN_I8_LDS = 56 * 1024;
 inline bool token_i8(long T, long d, long k, long f, long fs) {
     const long routes = k + (fs > 0), waves = routes < 16 ? routes : 16;
     return T == 1 && d <= TOKEN_I8_K && waves * ((f > fs ? f : fs) + 16) <= TOKEN_I8_LDS;
 }
 
-// Waves of a streaming workgroup, `wc` columns each.  A CU's time is the lines
-// it fetches, its waves' weights (16 rows) and the tile's bm rows of
-// activations, in whole rounds of the 256 CUs.  Columns of an expert are a
-// multiple of 256 and go in equal parts, over all experts (dense) in any.
+// Int8: 16-row tiles of the streaming products, or 0 for the tile products.  The
+// two cross where the bf16 ones do if the up product's 256 x 256 tiles fill the
+// CUs (us here / there): 128 experts of 768, d 2048, 48 rows each 191 / 205, 64 216
+// / 210; 32 of 1536, d 4096, 48 175 / 199, 64 202 / 199, 96 244 / 210; 16 of 2048, d 7168,
+// 64 209 / 213, 96 266 / 220.  With fewer tiles a launch of them is one round,
+// whatever their rows: 8 of 1536, d 4096, 96 rows 87 / 91, 128 95.5 / 94; 16 of 768, d
+// 2048, 96 52 / 58, 128 60.5 / 60.3; later where every expert has the same rows: 8 and
+// a shared one of 2048, d 7168, 128 172 / 239, 192 223 / 246, 256 303 / 254; 12 of
+// 512, d 5120, 192 101 / 173; 8 of 768, d 2048, 256 48 / 56, 384 65 / 58.
+inline int skinny_i8_tiles(long T, long k, long E, long f, long fs) {
+    const int t = skinny_tiles(T, k, E, f, fs);
+    if (t || (E * f + fs) / 128 >= 256) return t;
+    const long rows = k == E ? 192 : 96;
+    return T > 0 && T * k <= rows * E && T * fs <= rows * E * f ? 4 : 0;
+}
+
+// Waves of a streaming workgroup, 8 columns of f (up product) or 16 of d each.
+// Four, unless
+// - dense routing: the columns of all experts are dealt in any parts, and a CU's
+//   time is the lines it fetches, its waves' weights (16 rows) and the tile's bm
+//   rows of activations, in whole rounds of the 256 CUs (8 experts and a shared
+//   one, d 7168, f 2048, up to 64 tokens: 91-106 us so, 100-129 with four, 111-131
+//   with eight);
+// - the up product of 64-row tiles, at most six workgroups of four to a CU: eight
+//   halve the activations' lines (us with eight / four, 40 tokens to 8 of 48 of 1024:
+//   d 2048 79 / 88, d 5120 166 / 178; 28 of 1536: 74 / 82, 158 / 162; 48 of 768: 73 /
+//   76, 146 / 140; past that, 64 of 1024: 102 / 97, 203 / 208; 128 of 768, d 2048, 64
+//   tokens 148 / 140; 16-row tiles, 14 tokens to 48 of 768: 61 / 58, 130 / 120).
+//   The down product with eight: 3 us slower to 3 faster over the same shapes.
 constexpr long SX_MAX_WAVES = 15;
-inline long skinny_i8_waves(long T, long k, long E, long N, long Ns, long bm, long wc, bool dense) {
-    const long R = T * k, tiles = std::max(std::min(R, E), R / bm);
-    long best = 4;
-    double cost = 0;
-    for (long nw = 4; nw <= SX_MAX_WAVES; ++nw) {
-        if (!dense && nw != 4 && nw != 8) continue;
-        const long units = dense ? (E * N + Ns + wc * nw - 1) / (wc * nw)
-                                 : tiles * (N / (wc * nw)) + (T + bm - 1) / bm * (Ns / (wc * nw));
-        const double c = (double)((units + 255) / 256) * (16 * nw + bm);
-        if (cost == 0 || c < cost) {
-            cost = c;
-            best = nw;
+inline long skinny_i8_waves(long T, long k, long E, long N, long Ns, long bm, bool up, bool dense) {
+    if (dense) {
+        long best = 4, cost = 0;
+        for (long nw = 4; nw <= SX_MAX_WAVES; ++nw) {
+            const long units = (E * N + Ns + 8 * nw - 1) / (8 * nw);
+            const long c = (units + 255) / 256 * (16 * nw + bm);
+            if (cost == 0 || c < cost) {
+                cost = c;
+                best = nw;
+            }
         }
+        return best;
     }
-    return best;
+    const long R = T * k, tiles = std::max(std::min(R, E), R / bm);
+    const long units = tiles * (N / 32) + (T + bm - 1) / bm * (Ns / 32);
+    return up && bm > 16 && units <= 6 * 256 ? 8 : 4;
 }
 
 // Dense routing on few token tiles: the folded down product has one workgroup
@@ -187,8 +216,13 @@ inline bool route_direct(long T, long d, long E, long k) {
 
 // Logits for a selection by scores (score.hip), few tokens: the one-launch
 // router's blocks on slices of the d axis, so that about all CUs read W_r; the
-// selection adds the slices.  0: the other routers.
-constexpr long ROUTE_SLICE_MAX = 512, ROUTE_SLICE_BLOCKS = 256;
+// selection adds the slices.  0: the other routers.  A block reads its slice
+// of W_r for 16 tokens, so the two cross by T d E (us with the selection, here /
+// the others): 256 experts, d 7168, 1 token 13.7 / 26.4, 512 25.4 / 33, 1024 30.6 / 32.8,
+// 2048 45 / 37; 128, d 7168, 2048 23.5 / 24.4, 3000 32 / 26.6; d 2048, 4096 18.4 / 23.9; 64,
+// d 7168, 1024 17 / 44, 4096 30 / 46; 32, d 4096, 1 token 8.5 / 16, 4096 17 / 22.5; at most
+// one slice is left past that: 32, d 4096, 8192 24 / 30, 16384 51 / 43.
+constexpr long ROUTE_SLICE_MAX = 4096, ROUTE_SLICE_BLOCKS = 256, ROUTE_SLICE_READS = 1L << 31;
 
 inline long route_slice_steps(long d, long E) {      // slices of one step of 32 rows per wave
     const long nw = route_padded(E) <= 64 ? 16 : 8;
@@ -197,7 +231,7 @@ inline long route_slice_steps(long d, long E) {      // slices of one step of 32
 }
 inline long route_slices(long T, long d, long E) {
     const long ep = route_padded(E), cols = ep / 16 < 8 ? ep / 16 : 8;
-    if (T <= 0 || T > ROUTE_SLICE_MAX || E % cols) return 0;
+    if (T <= 0 || T > ROUTE_SLICE_MAX || T * d * ep > ROUTE_SLICE_READS || E % cols) return 0;
     const long fill = ROUTE_SLICE_BLOCKS / ((T + 15) / 16), most = route_slice_steps(d, E);
     return fill < most ? fill : most;
 }

@@ -92,23 +92,26 @@ DEV void put8(uint8_t *codes, const float (&v)[8], const I8Scale &s) {
 // goes out at once, and the workgroups quantise the activations for
 // themselves, each the same row again, under the weights' round trip.
 //
-// Up product: a workgroup owns 16 columns of f of one of the token's experts (or
-// of the shared one); its 4 waves take every fourth 128-byte piece of K.
-constexpr int TK_NW = 4, TK_D = 4;
+// Up product: a workgroup owns 8 columns of f of one of the token's experts (or
+// of the shared one), 8 gate and 8 up rows in one operand; its 4 waves take every
+// fourth 128-byte piece of K.  (16 columns: half as many workgroups, uneven over
+// the CUs; with them one token to 8 of 128 experts of 768, d 2048, took 16.05 us in
+// both launches, so 15.75.)
+constexpr int TK_NW = 4, TK_D = 8;
 constexpr int TK_HELD = TOKEN_I8_K / 8 / (64 * TK_NW);   // 8-value chunks of the token per thread
 
 __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t codes[TOKEN_I8_K];
-    __shared__ int red[TK_NW][2][16];
+    __shared__ int red[TK_NW][16];
     __shared__ uint32_t amax[TK_NW];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g4 = lane >> 4;
-    const int ns = a.shared.N / 16, b = (int)blockIdx.x - ns;
+    const int ns = a.shared.N / 8, b = (int)blockIdx.x - ns;
     const bool sh = b < 0;
     const I8Product &g = sh ? a.shared : a.routed;
-    const int slot = sh ? 0 : b / (g.N / 16);
-    const int n0 = 16 * (sh ? b + ns : b % (g.N / 16));
+    const int slot = sh ? 0 : b / (g.N / 8);
+    const int n0 = 8 * (sh ? b + ns : b % (g.N / 8));
     const int e = sh ? 0 : __builtin_amdgcn_readfirstlane(a.topk_idx[slot]);
     if (e < 0 || e >= a.E) return;   // routes outside the experts are left out
     const int K = g.K, pieces = K / SI_PIECE;
@@ -123,14 +126,11 @@ __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
         if (c < K / 8) load8(a.X + 8 * c, v[i]);
     }
     __builtin_amdgcn_sched_barrier(0);
-    const long ch = (long)e * g.N + n0 + r;
-    const uint8_t *wp[2] = {g.B + ch * K + 16 * g4, g.B2 + ch * K + 16 * g4};
-    u32x4_t w[TK_D][2][2];
+    const uint8_t *wp = (r < 8 ? g.B : g.B2) + ((long)e * g.N + n0 + (r & 7)) * K + 16 * g4;
+    u32x4_t w[TK_D][2];
     auto load = [&](int s, int u) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) w[s][j][h] = ld_u32x4(wp[j] + SI_PIECE * u + 64 * h);
+        for (int h = 0; h < 2; ++h) w[s][h] = ld_u32x4(wp + SI_PIECE * u + 64 * h);
     };
 #pragma unroll
     for (int s = 0; s < TK_D; ++s)
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
     }
     lds_barrier();
 
-    i32x4_t acc[2] = {i32x4_t{0, 0, 0, 0}, i32x4_t{0, 0, 0, 0}};
+    i32x4_t acc = i32x4_t{0, 0, 0, 0};
     for (int u = wave; u < pieces;) {
 #pragma unroll
         for (int s = 0; s < TK_D; ++s) {
@@ -160,10 +160,8 @@ __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
                 for (int h = 0; h < 2; ++h) {
                     // every column of the product is the token
                     const u32x4_t x = ld_u32x4(codes + SI_PIECE * u + 64 * h + 16 * g4);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-                            __builtin_bit_cast(i32x4_t, w[s][j][h]), __builtin_bit_cast(i32x4_t, x), acc[j], 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, w[s][h]),
+                                                                __builtin_bit_cast(i32x4_t, x), acc, 0, 0, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (u + TK_NW * TK_D < pieces) load(s, u + TK_NW * TK_D);
@@ -172,19 +170,17 @@ __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
             u += TK_NW;
         }
     }
-    // lane (g4, r), register q: channel 4 g4 + q, whatever r
+    // lane (g4, r), register q: row 4 g4 + q, whatever r
     if (r == 0)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) red[wave][j][4 * g4 + q] = acc[j][q];
+        for (int q = 0; q < 4; ++q) red[wave][4 * g4 + q] = acc[q];
     __syncthreads();
-    if (tid < 16) {
+    if (tid < 8) {
         int gate = 0, up = 0;
 #pragma unroll
         for (int q = 0; q < TK_NW; ++q) {
-            gate += red[q][0][tid];
-            up += red[q][1][tid];
+            gate += red[q][tid];
+            up += red[q][8 + tid];
         }
         const long c = (long)e * g.N + n0 + tid;
         g.H[(long)slot * g.N + n0 + tid] =
@@ -192,12 +188,13 @@ __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
     }
 }
 
-// Down product and the sum over the token's experts: a workgroup owns 16
-// columns of Y, a wave of it one of the token's routes (the shared expert
-// first): the route's row of H to LDS as codes, 16 channels over all of f, and
-// the weighted result to LDS in fp32.  The sum runs in the routes' order and is
-// rounded once.
+// Down product and the sum over the token's experts: a workgroup owns COLS
+// columns of Y (8 where 16 would leave CUs without one), a wave of it one of the
+// token's routes (the shared expert first): the route's row of H to LDS as
+// codes, its channels over all of f, and the weighted result to LDS in fp32.  The
+// sum runs in the routes' order and is rounded once.
 constexpr int TK_DD = 6;
+template <int COLS>
 __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const float *__restrict__ topk_w,
                                                           uint16_t *__restrict__ Y, int pitch) {
     extern __shared__ __attribute__((aligned(16))) uint8_t codes_all[];   // [waves][pitch]
@@ -205,7 +202,7 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
     const int r = lane & 15, g4 = lane >> 4;
-    const int n0 = 16 * (int)blockIdx.x, nsh = a.shared.N > 0 ? 1 : 0, routes = a.k + nsh;
+    const int n0 = COLS * (int)blockIdx.x, nsh = a.shared.N > 0 ? 1 : 0, routes = a.k + nsh;
     uint8_t *codes = codes_all + wave * pitch;
     for (int s0 = wave; s0 < routes; s0 += nw) {
         const bool sh = s0 < nsh;
@@ -228,7 +225,7 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
             if (c < K / 8) load8(h + 8 * c, v[i]);
         }
         __builtin_amdgcn_sched_barrier(0);
-        const uint8_t *wp = g.B + ((long)e * g.N + n0 + r) * K + 16 * g4;
+        const uint8_t *wp = g.B + ((long)e * g.N + n0 + (r & (COLS - 1))) * K + 16 * g4;
         u32x4_t w[TK_DD][2];
         auto load = [&](int s, int u) {
 #pragma unroll
@@ -275,7 +272,7 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
                 }
             }
         }
-        if (r == 0) {
+        if (r == 0 && 4 * g4 < COLS) {
             const float wt = sh ? 1.0f : topk_w[slot];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -285,7 +282,7 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
         }
     }
     __syncthreads();
-    if (tid < 16) {
+    if (tid < COLS) {
         float sum = 0.f;
         for (int s = 0; s < routes; ++s) sum = sum + y[s][tid];
         Y[n0 + tid] = f2bf(sum);
@@ -481,7 +478,7 @@ hipError_t launch_stream(I8SkinnyArgs a, hipStream_t st) {
     constexpr int WC = MODE == SI_UP ? 8 : 16;
     a.bm = 16 * TT;
     a.dense = MODE == SI_UP && a.k == a.E && a.T <= a.bm;
-    a.nw = (int)skinny_i8_waves(a.T, a.k, a.E, a.routed.N, a.shared.N, a.bm, WC, a.dense);
+    a.nw = (int)skinny_i8_waves(a.T, a.k, a.E, a.routed.N, a.shared.N, a.bm, MODE == SI_UP, a.dense);
     long grid;
     if (a.dense) {
         a.nshared = 0;
@@ -505,14 +502,18 @@ hipError_t launch_skinny_i8_down(const I8SkinnyArgs &a, int tt, hipStream_t st) 
 }
 
 hipError_t launch_token_i8_up(const I8SkinnyArgs &a, hipStream_t st) {
-    const int grid = a.shared.N / 16 + a.k * (a.routed.N / 16);
+    const int grid = a.shared.N / 8 + a.k * (a.routed.N / 8);
     token_up_kernel<<<dim3((unsigned)grid), dim3(64 * TK_NW), 0, st>>>(a);
     return hipGetLastError();
 }
 hipError_t launch_token_i8_down(const I8SkinnyArgs &a, const float *topk_w, uint16_t *Y, hipStream_t st) {
     const int routes = a.k + (a.shared.N > 0), nw = routes < 16 ? routes : 16;
     const int pitch = (a.shared.K > a.routed.K ? a.shared.K : a.routed.K) + 16;
-    token_down_kernel<<<dim3((unsigned)(a.routed.N / 16)), dim3(64 * nw), (size_t)nw * pitch, st>>>(a, topk_w, Y,
-                                                                                               pitch);
+    const dim3 block(64 * nw);
+    const size_t lds = (size_t)nw * pitch;
+    if (a.routed.N / 16 < 256)
+        token_down_kernel<8><<<dim3((unsigned)(a.routed.N / 8)), block, lds, st>>>(a, topk_w, Y, pitch);
+    else
+        token_down_kernel<16><<<dim3((unsigned)(a.routed.N / 16)), block, lds, st>>>(a, topk_w, Y, pitch);
     return hipGetLastError();
 }

@@ -9,10 +9,11 @@ from oracle import int_oracle as I
 from paper_2609_36070_amd import binding as B
 from paper_2609_36070_amd.layer import DeviceLayer
 from paper_2609_36070_amd.workloads import Workload, make_inputs, to_bf16
+from tests import dispatch, score_int_rules as R
 from tests.parity import say, to_np
 
 pytestmark = pytest.mark.gpu
-NAMES = ("Wg", "Wu", "Wd")
+EXTRA_CODES = 0.0     # codes that a different rounding of H could move beyond the oracle's own count
 
 
 def oracle_weights(w, inp):
@@ -51,8 +52,6 @@ def parity(w, seed=0, inp=None, codes=True):
     return L, inp
 
 
-EXTRA_CODES = 0.0
-
 SHAPES = [
     Workload("one token", T=1, d=256, E=8, k=2, f=256),
     Workload("one token, one expert", T=1, d=512, E=1, k=1, f=256),
@@ -76,6 +75,76 @@ SHAPES = [
 @pytest.mark.parametrize("w", SHAPES, ids=lambda w: w.name)
 def test_forward(w):
     parity(w, seed=2)
+
+
+PATHS = [
+    # (what the rules say, checked where a host compiler is there)
+    (Workload("token, longest row", T=1, d=8192, E=4, k=2, f=256, f_s=256), dict(token=1)),
+    (Workload("token, 17 routes", T=1, d=256, E=32, k=16, f=256, f_s=512), dict(token=1)),
+    (Workload("token, f past the registers", T=1, d=256, E=3, k=2, f=2816, f_s=2304), dict(token=1)),
+    (Workload("token, wide Y", T=1, d=4352, E=3, k=3, f=256), dict(token=1)),
+    (Workload("one long token", T=1, d=8448, E=4, k=2, f=256, f_s=256), dict(token=0, tiles=1)),
+    (Workload("one token, long f", T=1, d=256, E=16, k=16, f=3584), dict(token=0, tiles=1)),
+    (Workload("dense, uneven waves", T=16, d=512, E=12, k=12, f=768, f_s=256), dict(up_dense=1, up_waves=5)),
+    (Workload("dense, waves across experts", T=33, d=256, E=8, k=8, f=1280, f_s=256), dict(up_dense=1, up_waves=6)),
+    (Workload("dense, two tiles of rows", T=100, d=256, E=4, k=4, f=512, f_s=256), dict(up_dense=0, tiles=4)),
+    (Workload("dense, 192 rows", T=192, d=256, E=3, k=3, f=256), dict(up_dense=0, tiles=4)),
+    (Workload("dense, tiles", T=193, d=256, E=3, k=3, f=256), dict(tiles=0)),
+    (Workload("eight waves", T=60, d=256, E=12, k=4, f=512, f_s=256), dict(tiles=4, up_waves=8)),
+    (Workload("four waves", T=60, d=256, E=64, k=8, f=1024), dict(tiles=4, up_waves=4)),
+    (Workload("sixteen on one", T=16, d=256, E=8, k=1, f=256, bias_std=9.0), dict(tiles=1, up_waves=4)),
+    (Workload("many up tiles", T=600, d=256, E=16, k=8, f=1280, bias_std=0.5), dict(tiles=0)),
+    (Workload("many down tiles", T=600, d=2560, E=16, k=8, f=256, f_s=512), dict(tiles=0)),
+    (Workload("shared and hot", T=1500, d=512, E=8, k=1, f=256, f_s=768, bias_std=2.0), dict(tiles=0)),
+]
+
+
+@pytest.mark.parametrize("w,path", PATHS, ids=lambda v: getattr(v, "name", ""))
+def test_paths(w, path):
+    """Shapes at the edges of every path, and several tiles per workgroup."""
+    if dispatch.HAVE_CXX:
+        assert {n: R.layer(n, w) for n in path} == path
+    parity(w, seed=3, codes=False)
+
+
+@pytest.mark.parametrize("T", [1, 9, 40, 700])
+def test_an_expert_listed_twice(T):
+    """A token may list an expert twice: it counts twice, each with its weight."""
+    w = Workload("twice", T=T, d=256, E=6, k=3, f=256, f_s=256)
+    inp = make_inputs(w, 14)
+    L = DeviceLayer(w, inp, int8=True)
+    L.route()
+    L.topk_idx[0] = torch.tensor([4, 4, 1], dtype=torch.int32, device="cuda")
+    L.topk_idx[T - 1] = torch.tensor([2, 2, 2], dtype=torch.int32, device="cuda")
+    L.plan()
+    L.forward_int()
+    torch.cuda.synchronize()
+    Y, tol = I.moe_forward_int(inp["X"], oracle_weights(w, inp), to_np(L.topk_idx), to_np(L.topk_w),
+                               extra=EXTRA_CODES)
+    assert (np.abs(to_np(L.Y) - Y) <= tol).all()
+
+
+def test_one_workspace_under_two_graphs():
+    """Two captured layers that share a workspace, replayed in turn on one
+    stream, with eager work on the same workspace between."""
+    w = Workload("shared ws", T=24, d=256, E=8, k=2, f=256, f_s=256)
+    layers = [DeviceLayer(w, make_inputs(w, s), int8=True) for s in (1, 2)]
+    layers[1].ws = layers[0].ws
+    want, graphs = [], []
+    for L in layers:
+        L.step_int()
+        torch.cuda.synchronize()
+        want.append(L.Y.clone())
+    for L in layers:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            L.step_int()
+    for i in (0, 1, 0, 1, 1, 0):
+        layers[i].Y.zero_()
+        layers[1 - i].step_int()
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(layers[i].Y, want[i]) and torch.equal(layers[1 - i].Y, want[1 - i])
 
 
 def test_special_values():

@@ -61,6 +61,12 @@ CASES = [
     Case(5, 256, 256, 1, "softmax", groups=32, top_groups=1, balance=0.0, bias=1.0),
     Case(64, 256, 51, 9, groups=3, top_groups=2, group_score="pair", balance=0.0),
     Case(64, 256, 8, 8, groups=8, top_groups=8, group_score="pair"),
+    # past the sliced router, one slice of it, and groups of every width
+    Case(4097, 256, 16, 2, "softmax"), Case(4096, 512, 32, 4, groups=32, top_groups=4),
+    Case(4096, 7168, 64, 4, "softmax", groups=16, top_groups=3, group_score="pair"),
+    Case(2049, 7168, 128, 8, groups=64, top_groups=9, group_score="pair"), Case(1025, 7168, 256, 2, "softmax"),
+    Case(5000, 256, 100, 11, groups=50, top_groups=20), Case(4500, 256, 250, 13, groups=2, top_groups=1),
+    Case(3, 16384, 64, 1, groups=64, top_groups=64),
 ]
 IDS = ["-".join(str(v) for v in dataclasses.astuple(c)) for c in CASES]
 
