@@ -11,7 +11,7 @@
 
 namespace {
 
-template <int N> struct Chunks { static constexpr int value = N; };
+template <int N> struct Const { static constexpr int value = N; };
 
 DEV void load8(const uint16_t *p, float (&v)[8]) {
     const u32x4_t w = ld_u32x4(p);
@@ -27,10 +27,12 @@ DEV void load8(const float *p, float (&v)[8]) {
     for (int j = 0; j < 8; ++j) v[j] = w[j];
 }
 
-// Largest of a value over the 4 waves of a block.
-DEV uint32_t block_max(uint32_t x, uint32_t *red) {
+// Largest of a value over a wave, or over the 4 waves of a block.
+template <int W>
+DEV uint32_t row_max(uint32_t x, uint32_t *red) {
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) x = umax(x, (uint32_t)__shfl_xor((int)x, m, 64));
+    if constexpr (W == 1) return x;
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
     __syncthreads();
     return umax(umax(red[0], red[1]), umax(red[2], red[3]));
@@ -46,13 +48,14 @@ struct QuantRows {
     int K;
 };
 
-// Row `row`, 8 elements per thread and step.  Rows of up to 2048 NC elements are
-// held in registers between the two passes (NC = 0: read again).
-template <typename S, int NC>
+// Row `row` by W waves, 8 elements per thread and step.  Rows of up to 512 W NC
+// elements are held in registers between the two passes (NC = 0: read again).
+template <typename S, int NC, int W>
 DEV void quant_row(const QuantRows<S> &m, long row, uint32_t *red) {
+    constexpr int TH = 64 * W;
     const S *x = m.X + row * m.K;
     uint8_t *o = m.q + row * m.K;
-    const int n8 = m.K / 8;
+    const int n8 = m.K / 8, tid = threadIdx.x % TH;
     float v[NC > 0 ? NC : 1][8];
     uint32_t amax = 0;
     auto put = [&](const float (&y)[8], const I8Scale &s, int c) {
@@ -63,7 +66,7 @@ DEV void quant_row(const QuantRows<S> &m, long row, uint32_t *red) {
     if constexpr (NC > 0) {
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int c = threadIdx.x + 256 * i;
+            const int c = tid + TH * i;
             if (c < n8) load8(x + 8 * c, v[i]);
             else
 #pragma unroll
@@ -73,50 +76,54 @@ DEV void quant_row(const QuantRows<S> &m, long row, uint32_t *red) {
         for (int i = 0; i < NC; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) amax = umax(amax, abs_bits(v[i][j]));
-        const I8Scale s(block_max(amax, red));
-        if (threadIdx.x == 0) m.sc[row] = s.s;
+        const I8Scale s(row_max<W>(amax, red));
+        if (tid == 0) m.sc[row] = s.s;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int c = threadIdx.x + 256 * i;
+            const int c = tid + TH * i;
             if (c < n8) put(v[i], s, c);
         }
     } else {
-        for (int c = threadIdx.x; c < n8; c += 256) {
+        for (int c = tid; c < n8; c += TH) {
             load8(x + 8 * c, v[0]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) amax = umax(amax, abs_bits(v[0][j]));
         }
-        const I8Scale s(block_max(amax, red));
-        if (threadIdx.x == 0) m.sc[row] = s.s;
-        for (int c = threadIdx.x; c < n8; c += 256) {
+        const I8Scale s(row_max<W>(amax, red));
+        if (tid == 0) m.sc[row] = s.s;
+        for (int c = tid; c < n8; c += TH) {
             load8(x + 8 * c, v[0]);
             put(v[0], s, c);
         }
     }
 }
 
-// A block per row of one matrix, then of another.
-template <typename S, int NC>
+// Rows of one matrix, then of another, 4 / W per block.
+template <typename S, int NC, int W>
 __global__ __launch_bounds__(256) void i8_quant_rows_kernel(QuantRows<S> m0, QuantRows<S> m1) {
     __shared__ uint32_t red[4];
-    const long b = blockIdx.x;
-    if (b < m0.rows) quant_row<S, NC>(m0, b, red);
-    else quant_row<S, NC>(m1, b - m0.rows, red);
+    constexpr int RB = 4 / W;
+    const long n0 = (m0.rows + RB - 1) / RB, b = blockIdx.x;
+    const bool first = b < n0;
+    const long row = RB * (first ? b : b - n0) + threadIdx.x / (64 * W);
+    if (row < (first ? m0.rows : m1.rows)) quant_row<S, NC, W>(first ? m0 : m1, row, red);
 }
 
 // The tile products' prologue in one launch: the tokens' rows, and the token of
 // every position of the plan (0 where the plan has none), 256 per block.
-template <int NC>
+template <int NC, int W>
 __global__ __launch_bounds__(256) void i8_prologue_kernel(QuantRows<uint16_t> x, const int *__restrict__ perm,
                                                           const int *__restrict__ offsets, int E, int k, int R,
                                                           int *__restrict__ rowidx) {
     __shared__ uint32_t red[4];
-    const long b = blockIdx.x;
-    if (b < x.rows) {
-        quant_row<uint16_t, NC>(x, b, red);
+    constexpr int RB = 4 / W;
+    const long n0 = (x.rows + RB - 1) / RB, b = blockIdx.x;
+    if (b < n0) {
+        const long row = RB * b + threadIdx.x / (64 * W);
+        if (row < x.rows) quant_row<uint16_t, NC, W>(x, row, red);
         return;
     }
-    const int p = (int)(b - x.rows) * 256 + threadIdx.x;
+    const int p = (int)(b - n0) * 256 + threadIdx.x;
     if (p >= R) return;
     const int j = p < offsets[E] ? perm[p] : -1;
     rowidx[p] = j >= 0 && j < R ? j / k : 0;
@@ -178,24 +185,37 @@ __global__ __launch_bounds__(256) void i8_quant_weights_kernel(const uint16_t *_
     }
 }
 
-// f(NC) for rows of K elements: chunks of 2048 in registers
+// f(NC, W) for rows of K elements, which stay in registers up to 8192: a block per
+// row, or a wave if a block's threads would have no more than one chunk each and
+// there are rows for every CU (whole forward, us by waves / by blocks: 65536 rows of
+// 768 555 / 591; 32768 of 256 85 / 105; 131072 of 1536 2850 / 2867; 8000 of 1536 260.4 /
+// 260.2; 488 of 2048 108.6 / 107.2; 128 of 1536 139 / 137).  They move 5.2 TB/s from
+// 131072 rows of 1536 (188 us), and few rows take a launch's time (5 us).
+constexpr long QUANT_WAVE_ROWS = 2048;
 template <typename F>
-hipError_t with_chunks(int K, F f) {
-    if (K <= 2048) f(Chunks<1>{});
-    else if (K <= 4096) f(Chunks<2>{});
-    else if (K <= 8192) f(Chunks<4>{});
-    else f(Chunks<0>{});
+hipError_t with_chunks(long rows, int K, F f) {
+    if (rows >= QUANT_WAVE_ROWS && K <= 2048) {
+        if (K <= 512) f(Const<1>{}, Const<1>{});
+        else if (K <= 1024) f(Const<2>{}, Const<1>{});
+        else if (K <= 1536) f(Const<3>{}, Const<1>{});
+        else f(Const<4>{}, Const<1>{});
+    }
+    else if (K <= 2048) f(Const<1>{}, Const<4>{});
+    else if (K <= 4096) f(Const<2>{}, Const<4>{});
+    else if (K <= 8192) f(Const<4>{}, Const<4>{});
+    else f(Const<0>{}, Const<4>{});
     return hipGetLastError();
 }
+unsigned row_blocks(long rows, int W) { return (unsigned)((rows + 4 / W - 1) / (4 / W)); }
 
 }  // namespace
 
 hipError_t launch_i8_quant_tokens(const uint16_t *X, long rows, int K, uint8_t *q, float *sc, hipStream_t st) {
     if (rows <= 0) return hipSuccess;
     const QuantRows<uint16_t> m{X, q, sc, rows, K};
-    return with_chunks(K, [&](auto nc) {
-        i8_quant_rows_kernel<uint16_t, decltype(nc)::value><<<dim3((unsigned)rows), dim3(256), 0, st>>>(
-            m, QuantRows<uint16_t>{});
+    return with_chunks(rows, K, [&](auto nc, auto w) {
+        i8_quant_rows_kernel<uint16_t, decltype(nc)::value, decltype(w)::value>
+            <<<dim3(row_blocks(rows, w.value)), dim3(256), 0, st>>>(m, QuantRows<uint16_t>{});
     });
 }
 hipError_t launch_i8_prologue(const uint16_t *X, int T, int d, uint8_t *q, float *sc, const int *perm,
@@ -203,8 +223,9 @@ hipError_t launch_i8_prologue(const uint16_t *X, int T, int d, uint8_t *q, float
     if (T <= 0) return hipSuccess;
     const QuantRows<uint16_t> m{X, q, sc, T, d};
     const int R = T * k;
-    return with_chunks(d, [&](auto nc) {
-        i8_prologue_kernel<decltype(nc)::value><<<dim3((unsigned)(T + (R + 255) / 256)), dim3(256), 0, st>>>(
+    return with_chunks(T, d, [&](auto nc, auto w) {
+        const dim3 grid(row_blocks(T, w.value) + (unsigned)((R + 255) / 256));
+        i8_prologue_kernel<decltype(nc)::value, decltype(w)::value><<<grid, dim3(256), 0, st>>>(
             m, perm, offsets, E, k, R, rowidx);
     });
 }
@@ -212,8 +233,9 @@ hipError_t launch_i8_quant_h(const float *H, long rows, int f, uint8_t *q, float
                              long rows_s, int fs, uint8_t *qs, float *scs, hipStream_t st) {
     if (rows + rows_s <= 0) return hipSuccess;
     const QuantRows<float> m{H, q, sc, rows, f}, ms{Hs, qs, scs, rows_s, fs};
-    return with_chunks(rows_s > 0 && fs > f ? fs : f, [&](auto nc) {
-        i8_quant_rows_kernel<float, decltype(nc)::value><<<dim3((unsigned)(rows + rows_s)), dim3(256), 0, st>>>(m, ms);
+    return with_chunks(rows + rows_s, rows_s > 0 && fs > f ? fs : f, [&](auto nc, auto w) {
+        const dim3 grid(row_blocks(rows, w.value) + row_blocks(rows_s, w.value));
+        i8_quant_rows_kernel<float, decltype(nc)::value, decltype(w)::value><<<grid, dim3(256), 0, st>>>(m, ms);
     });
 }
 hipError_t launch_i8_quant_weights(const uint16_t *W, int E, int K, int N, uint8_t *q, float *sc,

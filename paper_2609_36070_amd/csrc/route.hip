@@ -472,6 +472,191 @@ __global__ __launch_bounds__(256) void route_reduce_kernel(const float *__restri
 
 
 // ---------------------------------------------------------------------------
+// The split router's tiles for logits alone (a selection by scores follows and
+// adds the slices): W_r is read as it lies, [64][EPAD] per chunk, and its
+// fragments come from the transposing ds_read_b64_tr_b16, so that the launch
+// which transposes W_r falls away (4099 tokens to 256 experts, d 7168, with the
+// selection 45 -> 42 us; 16384 to 128, d 2048, 34 -> 32; 3000 to 128, d 7168, 24 -> 22).  Rows of W_r must be whole
+// 16-byte pieces.  What bounds it are the lines a CU can have on their way: the
+// first of these loads 177 MB in 25 us, 7 TB/s; tiles of 256 tokens would load a
+// third less and write as much more in partial sums.
+//
+// LDS: X as in the split router; W_r's 64-byte blocks of a row XOR k & 3, so that
+// the four k rows a transposing read touches are at different banks.  Every
+// stage is an array of its own and every step issues the same number of
+// loads (past the last chunk of one line), so that the compiler sees that
+// reading X's stage waits for none of the loads on their way.  It does not see
+// that for the transposing reads, and waited for all of them before the first:
+// they are written out, with their own wait.
+
+// Experts 32 j + (lane & 31) of the wave's half at k 16 KS + 8 (lane / 32) + 0..7: two
+// reads of 4 k rows each, at[j] the lane's address at KS = 0.
+template <int EPAD, int KS>
+DEV void r_frags(const uint32_t (&at)[EPAD / 64], bf16x8_t (&b)[EPAD / 64]) {
+    constexpr int LO = 16 * KS * EPAD * 2, HI = LO + 4 * EPAD * 2;
+    u32x2_t lo[EPAD / 64], hi[EPAD / 64];
+    if constexpr (EPAD == 256)
+        asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %4, %8 offset:%13\n\t"
+                     "ds_read_b64_tr_b16 %1, %9 offset:%12\n\tds_read_b64_tr_b16 %5, %9 offset:%13\n\t"
+                     "ds_read_b64_tr_b16 %2, %10 offset:%12\n\tds_read_b64_tr_b16 %6, %10 offset:%13\n\t"
+                     "ds_read_b64_tr_b16 %3, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(lo[0]), "=&v"(lo[1]), "=&v"(lo[2]), "=&v"(lo[3]), "=&v"(hi[0]), "=&v"(hi[1]),
+                       "=&v"(hi[2]), "=&v"(hi[3])
+                     : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(LO), "n"(HI)
+                     : "memory");
+    else
+        asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %2, %4 offset:%7\n\t"
+                     "ds_read_b64_tr_b16 %1, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(lo[0]), "=&v"(lo[1]), "=&v"(hi[0]), "=&v"(hi[1])
+                     : "v"(at[0]), "v"(at[1]), "n"(LO), "n"(HI)
+                     : "memory");
+#pragma unroll
+    for (int j = 0; j < EPAD / 64; ++j)
+        b[j] = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[j][0], lo[j][1], hi[j][0], hi[j][1]});
+}
+
+template <int EPAD>
+__global__ __launch_bounds__(512) void route_logits_kernel(const uint16_t *__restrict__ X,
+                                                           const uint16_t *__restrict__ Wr,
+                                                           const float *__restrict__ bias,
+                                                           float *__restrict__ logits,
+                                                           float *__restrict__ part, int T, int d, int E,
+                                                           int S) {
+    static_assert(EPAD == 128 || EPAD == 256, "128 or 256 padded experts");
+    constexpr int TN = EPAD / 64;                         // 32-wide expert tiles per wave
+    constexpr int XT = RT * 64, WT = EPAD * 64;           // stage elements (bf16)
+    constexpr int NST = EPAD == 128 ? 4 : 3;              // as many as 160 KiB of LDS hold
+    constexpr int LPC = 2 + TN;                           // loads per wave and chunk
+    __shared__ __attribute__((aligned(16))) uint16_t x0[XT], x1[XT], x2[XT], x3[NST > 3 ? XT : 8];
+    __shared__ __attribute__((aligned(16))) uint16_t w0[WT], w1[WT], w2[WT], w3[NST > 3 ? WT : 8];
+
+    const int tile = blockIdx.x / S, slice = blockIdx.x % S;
+    const int t0 = tile * RT;
+    const int dS = d / S, k0 = slice * dS, nch = dS / 64;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave >> 1, wc = wave & 1;
+
+    // direct loads of 1024 bytes: 8 rows of X's chunk, 2 or 4 of W_r's
+    long xoff[2], woff[TN];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = 8 * (2 * wave + i) + (lane >> 3);
+        const int t = min(t0 + r, T - 1);          // rows past the batch load its last token
+        xoff[i] = (long)t * d + k0 + 8 * r_swz(r, lane & 7);
+    }
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+        constexpr int LPR = EPAD / 8;              // lanes per row
+        const int r = 64 / LPR * (TN * wave + i) + lane / LPR, p = lane % LPR;
+        const int c = 4 * ((p >> 2) ^ (r & 3)) + (p & 3);
+        // columns past the experts re-read the last ones; their logits are not used
+        woff[i] = (long)(k0 + r) * E + min(8 * c, E - 8);
+    }
+    auto issue = [&](int c, uint16_t *x, uint16_t *w) {
+        uint32_t live = c < nch ? ~0u : 0u;
+        asm volatile("" : "+v"(live));             // no branch: every path issues the same loads
+        const long mask = (long)(int)live;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) r_load_lds16(X + ((xoff[i] + 64 * c) & mask), x + (2 * wave + i) * 512);
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+            r_load_lds16(Wr + ((woff[i] + (long)64 * E * c) & mask), w + (TN * wave + i) * 512);
+    };
+
+    f32x16_t acc[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[j][q] = 0.f;
+
+    const int arow = 32 * wr + (lane & 31);
+    uint32_t wat[TN];   // byte addresses of the lane's fragments in a stage
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int i = lane & 15, k = 8 * (lane >> 5) + (i >> 2);
+        wat[j] = 2 * (k * EPAD + 32 * ((TN * wc + j) ^ (k & 3)) + 16 * ((lane >> 4) & 1) + 4 * (i & 3));
+    }
+    // chunk c, in stage (x, w); chunk c + NST - 1 goes to the stage of chunk c - 1,
+    // which every wave has read
+    auto step = [&](int c, const uint16_t *x, const uint16_t *w, uint16_t *xn, uint16_t *wn) {
+        r_wait_vmcnt<(NST - 2) * LPC>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        r_barrier();
+        issue(c + NST - 1, xn, wn);
+        uint32_t at[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) at[j] = wat[j] + (uint32_t)(uintptr_t)(LDS_AS const uint16_t *)w;
+        bf16x8_t av[4], b[TN];
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+            av[ks] = __builtin_bit_cast(
+                bf16x8_t, ld_u32x4(x + arow * 64 + 8 * r_swz(arow, 2 * ks + (lane >> 5))));
+        auto multiply = [&](const bf16x8_t &a) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b[j], acc[j], 0, 0, 0);
+        };
+        r_frags<EPAD, 0>(at, b);
+        multiply(av[0]);
+        r_frags<EPAD, 1>(at, b);
+        multiply(av[1]);
+        r_frags<EPAD, 2>(at, b);
+        multiply(av[2]);
+        r_frags<EPAD, 3>(at, b);
+        multiply(av[3]);
+    };
+    issue(0, x0, w0);
+    issue(1, x1, w1);
+    if constexpr (NST > 3) issue(2, x2, w2);
+    // whole rounds of the stages, then the rest (a loop left from its middle
+    // would look to the compiler like a way back to its start)
+    int c = 0;
+    for (; c + NST <= nch; c += NST) {
+        if constexpr (NST > 3) {
+            step(c, x0, w0, x3, w3);
+            step(c + 1, x1, w1, x0, w0);
+            step(c + 2, x2, w2, x1, w1);
+            step(c + 3, x3, w3, x2, w2);
+        } else {
+            step(c, x0, w0, x2, w2);
+            step(c + 1, x1, w1, x0, w0);
+            step(c + 2, x2, w2, x1, w1);
+        }
+    }
+    if (c < nch) {
+        if constexpr (NST > 3) step(c, x0, w0, x3, w3);
+        else step(c, x0, w0, x2, w2);
+        if (c + 1 < nch) {
+            step(c + 1, x1, w1, x0, w0);
+            if constexpr (NST > 3)
+                if (c + 2 < nch) step(c + 2, x2, w2, x1, w1);
+        }
+    }
+
+    // 32x32 accumulator layout: lane l, register q -> row 8 (q / 4) + 4 (l / 32) + q % 4, column l % 32
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int e = (EPAD / 2) * wc + 32 * j + (lane & 31);
+        const int t1 = t0 + 32 * wr + 4 * (lane >> 5);
+        if (S > 1) {
+            float *out = part + ((long)slice * T + t1) * EPAD + e;
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                if (t1 + 8 * (q >> 2) + (q & 3) < T) out[(8 * (q >> 2) + (q & 3)) * EPAD] = acc[j][q];
+        } else if (e < E) {
+            const float bz = bias ? bias[e] : 0.f;
+            float *out = logits + (long)t1 * E + e;
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                if (t1 + 8 * (q >> 2) + (q & 3) < T) out[(8 * (q >> 2) + (q & 3)) * E] = acc[j][q] + bz;
+        }
+    }
+    r_wait_vmcnt<0>();   // the loads past the last chunk, before the LDS is another block's
+}
+
+// ---------------------------------------------------------------------------
 // Router of small batches: one launch, no transposed copy of W_r.  A call of
 // a few tokens is a chain of latencies (the transpose's launch and round trip,
 // then the loads of a block, then the selection), so the block reads W_r as it
@@ -644,6 +829,15 @@ hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bia
         return hipGetLastError();
     }
     const int S = topk_idx ? route_split_slices(T, d, E) : route_logits_slices(T, d, E);
+    if (!topk_idx && S > 0 && E % 8 == 0) {
+        if (T == 0) return hipSuccess;
+        const dim3 grid((unsigned)(((T + RT - 1) / RT) * S)), block(512);
+        if (EPAD == 128)
+            route_logits_kernel<128><<<grid, block, 0, st>>>(X, W_r, bias, logits, part, T, d, E, S);
+        else
+            route_logits_kernel<256><<<grid, block, 0, st>>>(X, W_r, bias, logits, part, T, d, E, S);
+        return hipGetLastError();
+    }
     wr_transpose_kernel<<<dim3((unsigned)((d + 31) / 32), (unsigned)((EPAD + 63) / 64)), dim3(256), 0,
                           st>>>(W_r, WrT, d, E, EPAD);
     if (T == 0) return hipGetLastError();

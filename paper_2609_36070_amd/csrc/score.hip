@@ -73,8 +73,6 @@ DEV void exchanges(int most, F f) {
     if constexpr (L > 32) { if (32 < most) f(Int<32>{}); }
 }
 
-constexpr int PE = 16;   // experts per lane at most
-
 // The 64-bit side of a token's selection: its logits, balance and row maximum.
 struct Exact {
     const float *zt, *sbal;
@@ -91,7 +89,7 @@ struct Exact {
     }
 };
 // The softmax's denominator.
-template <int L>
+template <int PE, int L>
 DEV void exact_sum(Exact &x, uint32_t live, int first, int lpg) {
     x.sum = 0.0;
     if (!x.by_score || x.sigmoid) return;
@@ -108,9 +106,9 @@ DEV void exact_sum(Exact &x, uint32_t live, int first, int lpg) {
 // The groups near the border by their 64-bit values: those surely in (`sure` >
 // 0) rank before, those surely out (< 0) after all of them.  Returns whether
 // this lane's group is kept.
-template <int L>
+template <int PE, int L>
 DEV bool groups_64(Exact x, uint32_t live, int grp, int first, int lpg, int sure, const ScoreArgs &a) {
-    exact_sum<L>(x, live, first, lpg);
+    exact_sum<PE, L>(x, live, first, lpg);
     double b1 = -INFINITY, b2 = -INFINITY;
     if (sure == 0) {
 #pragma unroll 4
@@ -143,10 +141,10 @@ DEV bool groups_64(Exact x, uint32_t live, int grp, int first, int lpg, int sure
 // Places `from` .. k - 1 of the token's chosen experts: the best, by their
 // 64-bit values, of the candidates (bits of `cand` for this lane's experts).
 // kb: room for this lane's entries, at stride 256.
-template <int L, int KP>
+template <int PE, int L, int KP>
 DEV void select_64(Exact x, uint64_t *kb, uint32_t live, uint32_t cand, int first, int lpg, int from,
                    int k, uint32_t (&bk)[KP]) {
-    exact_sum<L>(x, live, first, lpg);
+    exact_sum<PE, L>(x, live, first, lpg);
 #pragma unroll 1
     for (uint32_t m = cand; m; m &= m - 1) {
         const int i = __builtin_ctz(m), id = first + lpg * i;
@@ -181,14 +179,14 @@ DEV void select_64(Exact x, uint64_t *kb, uint32_t live, uint32_t cand, int firs
 
 // The block's 256 / L tokens go through LDS: their logits, or the partial
 // logits of S slices added in slice order, 16 bytes per load.  Then L lanes
-// share a token.  The groups of experts are dealt to lanes, `lpg` lanes to a
+// share a token, up to PE experts each.  The groups of experts are dealt to lanes, `lpg` lanes to a
 // group, each lane taking every lpg-th expert of its group, so that a group's
 // best values meet in log2 lpg exchanges.  Each lane sorts its entries best
 // first in groups of KP (k rounded up to a power of two); the lanes' lists are
 // merged in log2 L rounds, after which every lane of the token has its best KP
 // and the best entry that was left out.  Then lane j finishes the j-th best
 // expert: its place in ascending id and its weight.
-template <int L, int KP>
+template <int PE, int L, int KP>
 __global__ __launch_bounds__(256) void score_select_kernel(
         const float *__restrict__ part, int S, int epad, const float *__restrict__ bias,
         const float *__restrict__ balance, float *__restrict__ logits, int *__restrict__ topk_idx,
@@ -393,7 +391,7 @@ __global__ __launch_bounds__(256) void score_select_kernel(
             const float gerr = 4.f * err + 4.f * top * 0x1p-24f;
             if (next > -INFINITY && !(worst - next > gerr)) {
                 const int sure = gs > next + gerr ? 1 : gs < worst - gerr ? -1 : 0;
-                kept = groups_64<L>(ex, live, grp, first, lpg, sure, a) && grp < a.groups;
+                kept = groups_64<PE, L>(ex, live, grp, first, lpg, sure, a) && grp < a.groups;
             }
         }
 #pragma unroll
@@ -432,7 +430,7 @@ __global__ __launch_bounds__(256) void score_select_kernel(
         int from = 0;
 #pragma unroll
         for (int j = 0; j < KP; ++j) from += j < k && (float)(bk[j] >> 8) > to_q ? 1 : 0;
-        select_64<L, KP>(ex, keys + threadIdx.x, live, cand, first, lpg, from, k, bk);
+        select_64<PE, L, KP>(ex, keys + threadIdx.x, live, cand, first, lpg, from, k, bk);
     }
 
     // ---------------- ids and weights of the chosen ----------------
@@ -631,14 +629,15 @@ int pow2(int x) {
     return p;
 }
 
-template <int L>
+template <int PE, int L>
 hipError_t select_lanes(const float *part, int S, int epad, const float *bias, const float *balance,
                         float *logits, int *idx, float *w, int T, int E, int k, int lpg,
                         const ScoreArgs &a, hipStream_t st) {
     const long per = 256 / L;
     const dim3 grid((unsigned)((T + per - 1) / per)), block(256);
 #define SELECT(KP) \
-    score_select_kernel<L, KP><<<grid, block, 0, st>>>(part, S, epad, bias, balance, logits, idx, w, T, E, k, lpg, a)
+    score_select_kernel<PE, L, KP><<<grid, block, 0, st>>>(part, S, epad, bias, balance, logits, idx, w, T, E, k, \
+                                                           lpg, a)
     switch (pow2(k)) {
         case 1: SELECT(1); break;
         case 2: SELECT(2); break;
@@ -657,19 +656,28 @@ hipError_t launch_score_select(const float *part, int S, int epad, const float *
                                const float *balance, float *logits, int *topk_idx, float *topk_w, int T,
                                int E, int k, const ScoreArgs &a, hipStream_t st) {
     if (T <= 0) return hipSuccess;
-    // lanes per group: as many as hold its experts, PE each
-    const int n = E / a.groups, lpg = pow2((n + PE - 1) / PE), L = pow2(a.groups) * lpg;
-#define LANES(N)                                                                                        \
-    case N:                                                                                             \
-        return select_lanes<N>(part, S, epad, bias, balance, logits, topk_idx, topk_w, T, E, k, lpg, a, st)
-    switch (L) {
-        LANES(1);
-        LANES(2);
-        LANES(4);
-        LANES(8);
-        LANES(16);
-        LANES(32);
-        LANES(64);
+    // Lanes per group: as many as hold its experts, 8 each, or 16 where 8 would take
+    // twice the 32 lanes (us with 8 / 16 for the whole router: 256 experts in 8
+    // groups, 1 token 12.9 / 13.8; 64 experts, 512 tokens 11.6 / 13.3; 128, 8000 tokens
+    // 26 / 28; 64 lanes of 8, 255 experts in 5 groups, 8000 tokens 43 / 40).
+    const int n = E / a.groups, g = pow2(a.groups), wide = pow2((n + 15) / 16), narrow = pow2((n + 7) / 8);
+    const int pe = g * narrow > 32 && g * wide <= 32 ? 16 : 8, lpg = pe == 16 ? wide : narrow;
+#define LANES(PE, N)                                                                                       \
+    case N:                                                                                                \
+        return select_lanes<PE, N>(part, S, epad, bias, balance, logits, topk_idx, topk_w, T, E, k, lpg, a, \
+                                   st)
+    if (pe == 16) switch (g * lpg) {
+        LANES(16, 32);
+        default: return hipErrorInvalidValue;
+    }
+    switch (g * lpg) {
+        LANES(8, 1);
+        LANES(8, 2);
+        LANES(8, 4);
+        LANES(8, 8);
+        LANES(8, 16);
+        LANES(8, 32);
+        LANES(8, 64);
         default: return hipErrorInvalidValue;
     }
 #undef LANES
