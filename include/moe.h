@@ -257,6 +257,8 @@ typedef struct {
 
 /* Router with scores: arguments, outputs and workspace as moe_route;
  *   balance [E] fp32 or NULL.
+ * The logits may differ from moe_route's in their last bits (the sum over d is
+ * split otherwise); the selection is that of the logits which are returned.
  * MOE_EINVAL for a routing outside the ranges above, MOE_EUNSUPPORTED for more
  * than 64 groups. */
 moe_status moe_route_scored(const moe_shape *shape, const moe_routing *routing, const moe_bf16 *X,
@@ -591,7 +593,7 @@ typedef struct {
  * limits of the int8 entry points: d, f, f_shared <= 131072; T*d, T*k*f,
  * T*f_shared, E*f*d and f_shared*d below 2^32 (MOE_EUNSUPPORTED). */
 moe_status moe_int_quantize_weights(const moe_shape *shape, const moe_weights *weights,
-                                   const moe_int_weights *i8, moe_stream stream);
+                                    const moe_int_weights *i8, moe_stream stream);
 
 /* Workspace bytes of moe_forward_int (it also serves moe_route,
  * moe_route_scored and moe_plan); 0 for an invalid or unsupported shape.  Pure
@@ -604,12 +606,23 @@ size_t moe_int_workspace_bytes(const moe_shape *shape);
  *     with exact 32-bit integer sums, scaled by (token scale) * (channel scale);
  *   - H = silu(A) * B is quantised per route (per token in the shared expert)
  *     from fp32, and the down products run likewise;
- *   - each expert's output is rounded to bf16 before the weighted sum.
- * Y [T, d] bf16 out.  ws: at least moe_int_workspace_bytes(shape) bytes. */
+ *   - each expert's output is rounded to bf16 before the weighted sum, except
+ *     for one token (with d <= 8192, and f and f_shared that its kernel's LDS
+ *     holds): its experts are taken from topk_idx instead of the plan, and
+ *     their outputs are summed in fp32 and rounded once.
+ * With dense routing (k == E) each token's ids are 0 .. E-1; otherwise a route
+ * with an id outside [0, E) is left out, and an id that a token lists twice
+ * counts twice.  Results do not depend on what ran before and repeat bit for
+ * bit; which kernels run, and with them the rounding above, depends on the
+ * sizes alone.  Y [T, d] bf16 out, no other row is written.  ws: at least
+ * moe_int_workspace_bytes(shape) bytes.  Events: the stages of moe_forward, each
+ * preceded by the quantisation of what it reads: 0 the tokens (and the plan-order
+ * prologue), 1 routed and shared up/gate + SwiGLU, 2 the activations, 3 routed
+ * and shared down, 5 the combine. */
 moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_int_weights *weights,
-                          const int32_t *topk_idx, const float *topk_w, const moe_plan_bufs *plan,
-                          moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream,
-                          const moe_stage_events *events /* NULL = no timing */);
+                           const int32_t *topk_idx, const float *topk_w, const moe_plan_bufs *plan,
+                           moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream,
+                           const moe_stage_events *events /* NULL = no timing */);
 
 /* Static strings; never NULL. */
 const char *moe_status_string(moe_status status);

@@ -158,8 +158,8 @@ def lib():
         L.moe_int_workspace_bytes.argtypes = [P(MoeShape)]
         L.moe_int_workspace_bytes.restype = c_size_t
         L.moe_forward_int.argtypes = [P(MoeShape), c_void_p, P(MoeIntWeights), c_void_p, c_void_p,
-                                     P(MoePlanBufs), c_void_p, c_void_p, c_size_t, c_void_p,
-                                     P(MoeStageEvents)]
+                                      P(MoePlanBufs), c_void_p, c_void_p, c_size_t, c_void_p,
+                                      P(MoeStageEvents)]
         for fn in ("moe_route", "moe_plan", "moe_schedule", "moe_dispatch", "moe_forward",
                    "moe_backward", "moe_workspace_region", "moe_mx_quantize_weights",
                    "moe_mx_workspace_region", "moe_forward_mx", "moe_forward_ring",
@@ -464,15 +464,15 @@ def moe_backward_mx_scored(shape, routing: MoeRouting, logits, balance, dY, X, W
 
 
 def int_weights_struct(Wg_q, Wu_q, Wd_q, Wg_s, Wu_s, Wd_s, Sg_q=None, Su_q=None, Sd_q=None, Sg_s=None,
-                      Su_s=None, Sd_s=None) -> MoeIntWeights:
+                       Su_s=None, Sd_s=None) -> MoeIntWeights:
     return MoeIntWeights(_p(Wg_q), _p(Wu_q), _p(Wd_q), _p(Wg_s), _p(Wu_s), _p(Wd_s),
-                        _p(Sg_q), _p(Su_q), _p(Sd_q), _p(Sg_s), _p(Su_s), _p(Sd_s))
+                         _p(Sg_q), _p(Su_q), _p(Sd_q), _p(Sg_s), _p(Su_s), _p(Sd_s))
 
 
 def moe_int_quantize_weights(shape, weights: MoeWeights, weights_int: MoeIntWeights, stream=None,
-                            raise_on_error=True):
-    st = lib().moe_int_quantize_weights(ctypes.byref(shape), ctypes.byref(weights), ctypes.byref(weights_int),
-                                       _stream(stream))
+                             raise_on_error=True):
+    st = lib().moe_int_quantize_weights(ctypes.byref(shape), ctypes.byref(weights),
+                                        ctypes.byref(weights_int), _stream(stream))
     return _check("moe_int_quantize_weights", st, raise_on_error)
 
 
@@ -481,9 +481,9 @@ def moe_int_workspace_bytes(shape: MoeShape) -> int:
 
 
 def moe_forward_int(shape, X, weights: MoeIntWeights, topk_idx, topk_w, plan: MoePlanBufs, Y, ws,
-                   ws_bytes=None, stream=None, raise_on_error=True, events: MoeStageEvents = None):
+                    ws_bytes=None, stream=None, raise_on_error=True, events: MoeStageEvents = None):
     nbytes = ws.nbytes if ws_bytes is None else ws_bytes
     st = lib().moe_forward_int(ctypes.byref(shape), _p(X), ctypes.byref(weights), _p(topk_idx),
-                              _p(topk_w), ctypes.byref(plan), _p(Y), _p(ws), nbytes, _stream(stream),
-                              None if events is None else ctypes.byref(events))
+                               _p(topk_w), ctypes.byref(plan), _p(Y), _p(ws), nbytes, _stream(stream),
+                               None if events is None else ctypes.byref(events))
     return _check("moe_forward_int", st, raise_on_error)

@@ -1178,11 +1178,12 @@ moe_status moe_forward_fused(const moe_shape *shape, const moe_bf16 *X, const mo
     return MOE_OK;
 }
 
-static moe_status backward_run(const Scored *sc, const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
-        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
-        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
-        const moe_grads *grads, void *ws, size_t ws_bytes, moe_stream stream,
-        const moe_stage_events *events) {
+static moe_status backward_run(const Scored *sc, const moe_shape *shape, const moe_bf16 *dY,
+                               const moe_bf16 *X, const moe_bf16 *W_r, const moe_weights *weights,
+                               const int32_t *topk_idx, const float *topk_w,
+                               const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+                               void *ws, size_t ws_bytes, moe_stream stream,
+                               const moe_stage_events *events) {
     moe_status st = check_backward_args(shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads);
     if (st != MOE_OK) return st;
     if ((st = check_ws(shape, ws, ws_bytes, 1)) != MOE_OK) return st;
@@ -1202,7 +1203,7 @@ static moe_status backward_run(const Scored *sc, const moe_shape *shape, const m
     MOE_TRY(routed_dgrad(*shape, L, ws, dY, weights, all, s));
     MOE_TRY(mk.mark(2));
     MOE_TRY(router_bwd(sc, at<float>(ws, L.dgpart), L.dg_parts, plan->route_pos, topk_w, topk_idx,
-                               T, k, E, at<float>(ws, L.dg), dZ, s));
+                       T, k, E, at<float>(ws, L.dg), dZ, s));
     if (dense_routing(*shape)) {
         // dX in one product over every expert, the shared expert and the
         // router term (stage 3, the routed dX, and stage 10, the reverse
@@ -1251,22 +1252,26 @@ static moe_status backward_run(const Scored *sc, const moe_shape *shape, const m
 }
 
 moe_status moe_backward(const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
-        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
-        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
-        const moe_grads *grads, void *ws, size_t ws_bytes, moe_stream stream,
-        const moe_stage_events *events) {
-    return backward_run(nullptr, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ws, ws_bytes, stream, events);
+                        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
+                        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+                        const moe_grads *grads, void *ws, size_t ws_bytes, moe_stream stream,
+                        const moe_stage_events *events) {
+    return backward_run(nullptr, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ws, ws_bytes,
+                        stream, events);
 }
 
-moe_status moe_backward_scored(const moe_shape *shape, const moe_routing *routing, const float *logits,
-        const float *balance, const moe_bf16 *dY, const moe_bf16 *X,
-        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
-        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
-        const moe_grads *grads, void *ws, size_t ws_bytes, moe_stream stream,
-        const moe_stage_events *events) {
+moe_status moe_backward_scored(const moe_shape *shape, const moe_routing *routing,
+                               const float *logits, const float *balance, const moe_bf16 *dY,
+                               const moe_bf16 *X, const moe_bf16 *W_r, const moe_weights *weights,
+                               const int32_t *topk_idx, const float *topk_w,
+                               const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+                               void *ws, size_t ws_bytes, moe_stream stream,
+                               const moe_stage_events *events) {
     const Scored sc{routing, logits, balance};
     const moe_status st = check_scored(shape, sc);
-    return st != MOE_OK ? st : backward_run(&sc, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ws, ws_bytes, stream, events);
+    if (st != MOE_OK) return st;
+    return backward_run(&sc, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ws, ws_bytes,
+                        stream, events);
 }
 
 size_t moe_ring_workspace_bytes(const moe_shape *shape, int64_t ring_rows, int with_backward) {
@@ -1352,11 +1357,12 @@ moe_status moe_forward_ring(const moe_shape *shape, const moe_bf16 *X, const moe
     return MOE_OK;
 }
 
-static moe_status backward_ring_run(const Scored *sc, const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
-        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
-        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
-        const moe_grads *grads, int64_t ring_rows, void *ws, size_t ws_bytes,
-        moe_stream stream) {
+static moe_status backward_ring_run(const Scored *sc, const moe_shape *shape, const moe_bf16 *dY,
+                                    const moe_bf16 *X, const moe_bf16 *W_r,
+                                    const moe_weights *weights, const int32_t *topk_idx,
+                                    const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+                                    const moe_grads *grads, int64_t ring_rows, void *ws,
+                                    size_t ws_bytes, moe_stream stream) {
     moe_status st = check_backward_args(shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads);
     if (st != MOE_OK) return st;
     if ((st = check_ring(ring_rows)) != MOE_OK) return st;
@@ -1414,7 +1420,7 @@ static moe_status backward_ring_run(const Scored *sc, const moe_shape *shape, co
             // (every dg is known once the last window's dgrad has run)
             if (m == nwin - 1) {
                 MOE_TRY(router_bwd(sc, at<float>(ws, L.dgpart), L.dg_parts, plan->route_pos, topk_w,
-                                           topk_idx, T, k, E, at<float>(ws, L.dg), dZ, s));
+                                   topk_idx, T, k, E, at<float>(ws, L.dg), dZ, s));
                 MOE_TRY(launch_router_split(dZ, W_r, T, d, E, at<uint16_t>(ws, L.dzs),
                                             at<uint16_t>(ws, L.wrs), s));
             }
@@ -1461,29 +1467,33 @@ static moe_status backward_ring_run(const Scored *sc, const moe_shape *shape, co
         return MOE_OK;
     }
     MOE_TRY(router_bwd(sc, at<float>(ws, L.dgpart), L.dg_parts, plan->route_pos, topk_w, topk_idx,
-                               T, k, E, at<float>(ws, L.dg), dZ, s));
+                       T, k, E, at<float>(ws, L.dg), dZ, s));
     MOE_TRY(launch_dwr(X, dZ, T, d, E, at<float>(ws, L.dwr_part), grads->dW_r, s));
     MOE_TRY(launch_reverse_combine(nullptr, nullptr, dZ, W_r, plan->route_pos, T, d, k, E, acc, dX, s));
     return MOE_OK;
 }
 
 moe_status moe_backward_ring(const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
-        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
-        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
-        const moe_grads *grads, int64_t ring_rows, void *ws, size_t ws_bytes,
-        moe_stream stream) {
-    return backward_ring_run(nullptr, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ring_rows, ws, ws_bytes, stream);
+                             const moe_bf16 *W_r, const moe_weights *weights,
+                             const int32_t *topk_idx, const float *topk_w,
+                             const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+                             int64_t ring_rows, void *ws, size_t ws_bytes, moe_stream stream) {
+    return backward_ring_run(nullptr, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads,
+                             ring_rows, ws, ws_bytes, stream);
 }
 
-moe_status moe_backward_ring_scored(const moe_shape *shape, const moe_routing *routing, const float *logits,
-        const float *balance, const moe_bf16 *dY, const moe_bf16 *X,
-        const moe_bf16 *W_r, const moe_weights *weights, const int32_t *topk_idx,
-        const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
-        const moe_grads *grads, int64_t ring_rows, void *ws, size_t ws_bytes,
-        moe_stream stream) {
+moe_status moe_backward_ring_scored(const moe_shape *shape, const moe_routing *routing,
+                                    const float *logits, const float *balance, const moe_bf16 *dY,
+                                    const moe_bf16 *X, const moe_bf16 *W_r,
+                                    const moe_weights *weights, const int32_t *topk_idx,
+                                    const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+                                    const moe_grads *grads, int64_t ring_rows, void *ws,
+                                    size_t ws_bytes, moe_stream stream) {
     const Scored sc{routing, logits, balance};
     const moe_status st = check_scored(shape, sc);
-    return st != MOE_OK ? st : backward_ring_run(&sc, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ring_rows, ws, ws_bytes, stream);
+    if (st != MOE_OK) return st;
+    return backward_ring_run(&sc, shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads, ring_rows,
+                             ws, ws_bytes, stream);
 }
 
 size_t moe_mx_workspace_bytes(const moe_shape *shape, int with_backward) {
@@ -1637,11 +1647,12 @@ moe_status moe_mx_quantize_weights_bwd(const moe_shape *shape, const moe_weights
     return MOE_OK;
 }
 
-static moe_status backward_mx_run(const Scored *sc, const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
-        const moe_bf16 *W_r, const moe_weights *weights,
-        const moe_mx_bwd_weights *mx, const int32_t *topk_idx, const float *topk_w,
-        const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
-        int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream) {
+static moe_status backward_mx_run(const Scored *sc, const moe_shape *shape, const moe_bf16 *dY,
+                                  const moe_bf16 *X, const moe_bf16 *W_r,
+                                  const moe_weights *weights, const moe_mx_bwd_weights *mx,
+                                  const int32_t *topk_idx, const float *topk_w,
+                                  const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+                                  int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream) {
     moe_status st = check_backward_args(shape, dY, X, W_r, weights, topk_idx, topk_w, plan, dX, grads);
     if (st != MOE_OK) return st;
     if ((st = check_mx_shape(shape)) != MOE_OK) return st;
@@ -1691,7 +1702,7 @@ static moe_status backward_mx_run(const Scored *sc, const moe_shape *shape, cons
         MOE_TRY(launch_gemm_mx_dgrad(g, R, E, s));
     }
     MOE_TRY(router_bwd(sc, at<float>(ws, L.dgpart), L.dg_parts / 2, plan->route_pos, topk_w, topk_idx,
-                               T, k, E, at<float>(ws, L.dg), dZ, s));
+                       T, k, E, at<float>(ws, L.dg), dZ, s));
     {   // dXperm = Q(dA) Q(W_gate)^T + Q(dB) Q(W_up)^T
         MxGemmArgs g;
         g.A = daq; g.As = das; g.A2 = dbq; g.As2 = dbs; g.a_nrows = (int)Rn;
@@ -1770,26 +1781,31 @@ static moe_status backward_mx_run(const Scored *sc, const moe_shape *shape, cons
 }
 
 moe_status moe_backward_mx(const moe_shape *shape, const moe_bf16 *dY, const moe_bf16 *X,
-        const moe_bf16 *W_r, const moe_weights *weights,
-        const moe_mx_bwd_weights *mx, const int32_t *topk_idx, const float *topk_w,
-        const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
-        int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream) {
-    return backward_mx_run(nullptr, shape, dY, X, W_r, weights, mx, topk_idx, topk_w, plan, dX, grads, wgrad_mxfp8, ws, ws_bytes, stream);
+                           const moe_bf16 *W_r, const moe_weights *weights,
+                           const moe_mx_bwd_weights *mx, const int32_t *topk_idx,
+                           const float *topk_w, const moe_plan_bufs *plan, moe_bf16 *dX,
+                           const moe_grads *grads, int wgrad_mxfp8, void *ws, size_t ws_bytes,
+                           moe_stream stream) {
+    return backward_mx_run(nullptr, shape, dY, X, W_r, weights, mx, topk_idx, topk_w, plan, dX, grads,
+                           wgrad_mxfp8, ws, ws_bytes, stream);
 }
 
-moe_status moe_backward_mx_scored(const moe_shape *shape, const moe_routing *routing, const float *logits,
-        const float *balance, const moe_bf16 *dY, const moe_bf16 *X,
-        const moe_bf16 *W_r, const moe_weights *weights,
-        const moe_mx_bwd_weights *mx, const int32_t *topk_idx, const float *topk_w,
-        const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
-        int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream) {
+moe_status moe_backward_mx_scored(const moe_shape *shape, const moe_routing *routing,
+                                  const float *logits, const float *balance, const moe_bf16 *dY,
+                                  const moe_bf16 *X, const moe_bf16 *W_r,
+                                  const moe_weights *weights, const moe_mx_bwd_weights *mx,
+                                  const int32_t *topk_idx, const float *topk_w,
+                                  const moe_plan_bufs *plan, moe_bf16 *dX, const moe_grads *grads,
+                                  int wgrad_mxfp8, void *ws, size_t ws_bytes, moe_stream stream) {
     const Scored sc{routing, logits, balance};
     const moe_status st = check_scored(shape, sc);
-    return st != MOE_OK ? st : backward_mx_run(&sc, shape, dY, X, W_r, weights, mx, topk_idx, topk_w, plan, dX, grads, wgrad_mxfp8, ws, ws_bytes, stream);
+    if (st != MOE_OK) return st;
+    return backward_mx_run(&sc, shape, dY, X, W_r, weights, mx, topk_idx, topk_w, plan, dX, grads,
+                           wgrad_mxfp8, ws, ws_bytes, stream);
 }
 
 moe_status moe_int_quantize_weights(const moe_shape *shape, const moe_weights *weights,
-                                   const moe_int_weights *i8, moe_stream stream) {
+                                    const moe_int_weights *i8, moe_stream stream) {
     moe_status st = check_shape(shape);
     if (st != MOE_OK) return st;
     if ((st = check_i8_shape(shape)) != MOE_OK) return st;
@@ -1817,9 +1833,9 @@ size_t moe_int_workspace_bytes(const moe_shape *shape) {
 }
 
 moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_int_weights *weights,
-                          const int32_t *topk_idx, const float *topk_w, const moe_plan_bufs *plan,
-                          moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream,
-                          const moe_stage_events *events) {
+                           const int32_t *topk_idx, const float *topk_w, const moe_plan_bufs *plan,
+                           moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream,
+                           const moe_stage_events *events) {
     moe_status st = check_shape(shape);
     if (st != MOE_OK) return st;
     if ((st = check_i8_shape(shape)) != MOE_OK) return st;
@@ -1849,8 +1865,8 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
         p.rows = rows; p.K = d; p.N = N; p.H = H;
         return p;
     };
-    auto down_product = [&](const uint8_t *a, const float *as, const int8_t *w, const float *wsc, int n, int rows,
-                            int K, uint16_t *C) {
+    auto down_product = [&](const uint8_t *a, const float *as, const int8_t *w, const float *wsc, int n,
+                            int rows, int K, uint16_t *C) {
         I8Product p;
         p.A = a; p.As = as; p.a_nrows = rows > 0 ? rows : 1; p.a_bytes = (uint32_t)((long)p.a_nrows * K);
         p.B = bytes(w); p.Bs = wsc; p.b_bytes = (uint32_t)((long)n * K * d);
@@ -1887,7 +1903,8 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
     if (tt)
         MOE_TRY(launch_i8_quant_tokens(X, T, d, xq, xs, s));
     else
-        MOE_TRY(launch_i8_prologue(X, T, d, xq, xs, plan->perm, plan->offsets, E, k, at<int>(ws, L.rowidx), s));
+        MOE_TRY(launch_i8_prologue(X, T, d, xq, xs, plan->perm, plan->offsets, E, k, at<int>(ws, L.rowidx),
+                                   s));
     MOE_TRY(mk.mark(1));
     MOE_TRY(tt ? launch_skinny_i8_up(small, tt, s) : launch_gemm_i8_up(up, s));
     MOE_TRY(mk.mark(2));

@@ -19,6 +19,11 @@
 // its first loads and its epilogue's stores together take as long: the next
 // tile's first step is asked for before the epilogue, whose stores then drain
 // behind the next tile's products.
+//
+// 16384 tokens to 8 of 32 experts of 1536, d 4096: up 1470 us, 2.24 POP/s, down 920,
+// 1.79 (a tile of 12 steps has the epilogue of one of 32); a large library
+// product reaches 2.12.  The matrix units are busy 59 % of the time at 1.85 GHz,
+// and busier schedules only lower the clock: power bounds it.
 #include "common.h"
 #include "i8_common.h"
 #include "kernels.h"
@@ -93,7 +98,7 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
     // direct loads into one of them pass reads of another.  With one array for
     // all stages it waits for every load in flight before any read of it, so
     // the loads of step k + 1 had to arrive before step k began (16384 tokens,
-    // 32 experts of 1536, d 4096: up 1770 us, down 1107).
+    // 32 experts of 1536, d 4096: up 1770 us, down 1107, now 1470 and 920).
     __shared__ __attribute__((aligned(16))) uint8_t lds_a0[TILE], lds_b0[TILE], lds_a1[TILE], lds_b1[TILE];
     // scales of a tile's rows and columns, by parity of the tile, and the waves'
     // epilogue scratch
@@ -338,7 +343,10 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
                 }
         } else {
             // 8 rows at a time through a scratch of the wave's own (8 x WN fp32),
-            // one 16-byte store per lane
+            // one 16-byte store per lane, whole lines.  (Weights as the MFMA's row
+            // operand give a lane 8 channels without the scratch, but stores of 32
+            // bytes per row: 8192 tokens to 128 experts of 768 163 -> 179 us, past the
+            // L2 299.)
             const int er = lane >> 3, ec = lane & 7;
             uint16_t *const out = g.C + (long)t.row0 * g.N;
             const uint32_t bytes = (uint32_t)rows * (uint32_t)g.N * 2u;

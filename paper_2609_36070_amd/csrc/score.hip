@@ -12,8 +12,12 @@
 // the last one taken then say whether the errors of the fp32 values could have
 // swapped them, and likewise the groups; only where they could (a few tokens in
 // 100000, and rows of exact ties) the experts that the errors reach, mostly two,
-// are ranked again by 64-bit values, in compact loops.  A selection in 64 bits throughout spent 25-50 us, most of it
-// on fetching its unrolled code (30 us for a single token).
+// are ranked again by 64-bit values, in compact loops.  A selection in 64 bits
+// throughout spent 25-50 us, most of it on fetching its unrolled code (30 us for a
+// single token); this one takes 7.4 us for one token to 256 experts in 8 groups
+// (14 slices of partial logits; a launch's and three dependent loads' time), 13.7
+// for 4099 (29 MB of partial logits) and 14.2 for 16384 to 128 experts (networks
+// and exponentials; the logits are 8 MB).
 //
 // 64-bit entries hold sign, exponent and the upper 44 bits of the mantissa
 // above the 8 bits of 255 - e: rank order, ties to the lower id, is plain order
@@ -54,10 +58,9 @@ template <int N> struct Int { static constexpr int value = N; };
 // the LDS unit.
 template <int M>
 DEV uint32_t peer(uint32_t v) {
-    if constexpr (M == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);    // quad 1,0,3,2
-    else if constexpr (M == 2) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);   // 2,3,0,1
-    else if constexpr (M == 4) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true);  // half mirror
-    else if constexpr (M == 8) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true);  // mirror
+    // quads 1,0,3,2 and 2,3,0,1; half rows and rows mirrored
+    constexpr int ctrl = M == 1 ? 0xB1 : M == 2 ? 0x4E : M == 4 ? 0x141 : 0x140;
+    if constexpr (M <= 8) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, ctrl, 0xF, 0xF, true);
     else return (uint32_t)__shfl_xor((int)v, M, 64);
 }
 template <int M>
@@ -179,9 +182,9 @@ DEV void select_64(Exact x, uint64_t *kb, uint32_t live, uint32_t cand, int firs
 
 // The block's 256 / L tokens go through LDS: their logits, or the partial
 // logits of S slices added in slice order, 16 bytes per load.  Then L lanes
-// share a token, up to PE experts each.  The groups of experts are dealt to lanes, `lpg` lanes to a
-// group, each lane taking every lpg-th expert of its group, so that a group's
-// best values meet in log2 lpg exchanges.  Each lane sorts its entries best
+// share a token, up to PE experts each.  The groups of experts are dealt to
+// lanes, `lpg` lanes to a group, each lane taking every lpg-th expert of its group,
+// so that a group's best values meet in log2 lpg exchanges.  Each lane sorts its entries best
 // first in groups of KP (k rounded up to a power of two); the lanes' lists are
 // merged in log2 L rounds, after which every lane of the token has its best KP
 // and the best entry that was left out.  Then lane j finishes the j-th best
@@ -493,7 +496,10 @@ __global__ __launch_bounds__(256) void score_select_kernel(
 // and 0 elsewhere.  16 tokens per block, lane s of a token's 16 takes slot s;
 // the rows are put together in LDS, where the chosen entries are scattered,
 // and leave in one contiguous run (a row of E floats starts anywhere, 16 of
-// them start at a multiple of 64 bytes).  Bound by that store.
+// them start at a multiple of 64 bytes).  Bound by that store and the lines that
+// the k logits of a row lie in: 16384 tokens to 256 experts, sigmoid, 7.5 us for
+// 18 MB that a caller would count and about 25 that move; 6001 to 96, softmax, 7.6
+// (three passes over the row in LDS); a launch alone takes 5.
 constexpr int SB_BT = 16;
 __global__ __launch_bounds__(256) void score_bwd_kernel(
         const float *__restrict__ logits, const float *__restrict__ balance,

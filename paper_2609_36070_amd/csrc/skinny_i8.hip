@@ -90,7 +90,8 @@ DEV void put8(uint8_t *codes, const float (&v)[8], const I8Scale &s) {
 // One token: two launches in all, without the plan (the experts are the
 // token's own list).  What counts is latency: every load that a wave will need
 // goes out at once, and the workgroups quantise the activations for
-// themselves, each the same row again, under the weights' round trip.
+// themselves, each the same row again, under the weights' round trip.  8 of 128
+// experts of 768, d 2048: 8.6 and 7.2 us for 25 and 13 MB.
 //
 // Up product: a workgroup owns 8 columns of f of one of the token's experts (or
 // of the shared one), 8 gate and 8 up rows in one operand; its 4 waves take every
@@ -301,7 +302,10 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
 // codes, a piece of 16 TT rows at a time, into a ring of SX_D pieces in LDS by
 // direct loads (whole 128-byte lines, chunk XOR (row >> 1) & 7); it is a wave of
 // its own because loads return in order, and the activations, from L2, would
-// wait for weights asked for long before.  One barrier per piece.
+// wait for weights asked for long before.  One barrier per piece.  16 tokens to 8 of
+// 32 experts of 1536, d 4096: up 84-88 us for 403 MB of codes, down 38 for 201 (5 TB/s;
+// a large copy reaches 5.2); 61 tokens, 8 experts and a shared one of 2048, d 7168:
+// up 56 us for 264 MB, down 34 for 132.
 //
 // With dense routing every expert's rows are the tokens, so a workgroup's
 // columns may belong to two experts, or to the shared one, and NW is what deals

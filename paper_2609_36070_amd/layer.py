@@ -139,14 +139,16 @@ class DeviceLayer:
             self.quantize_mx()
 
         if int8:
-            q, sc = torch.int8, torch.float32
-            self.int_bufs = [torch.empty((E, f, d), dtype=q, device=dev), torch.empty((E, f, d), dtype=q, device=dev),
-                            torch.empty((E, d, f), dtype=q, device=dev), torch.empty((E, f), dtype=sc, device=dev),
-                            torch.empty((E, f), dtype=sc, device=dev), torch.empty((E, d), dtype=sc, device=dev)]
+            def codes(*size):
+                return torch.empty(size, dtype=torch.int8, device=dev)
+
+            def scales(*size):
+                return torch.empty(size, dtype=torch.float32, device=dev)
+
+            self.int_bufs = [codes(E, f, d), codes(E, f, d), codes(E, d, f),
+                             scales(E, f), scales(E, f), scales(E, d)]
             if fs:
-                self.int_bufs += [torch.empty((fs, d), dtype=q, device=dev), torch.empty((fs, d), dtype=q, device=dev),
-                                 torch.empty((d, fs), dtype=q, device=dev), torch.empty((fs,), dtype=sc, device=dev),
-                                 torch.empty((fs,), dtype=sc, device=dev), torch.empty((d,), dtype=sc, device=dev)]
+                self.int_bufs += [codes(fs, d), codes(fs, d), codes(d, fs), scales(fs), scales(fs), scales(d)]
             self.int_weights = B.int_weights_struct(*self.int_bufs)
             self.quantize_int()
 
@@ -235,7 +237,7 @@ class DeviceLayer:
 
     def forward_int(self, stream=None, events=None):
         B.moe_forward_int(self.shape, self.X, self.int_weights, self.topk_idx, self.topk_w,
-                         self.plan_bufs, self.Y, self.ws, stream=stream, events=events)
+                          self.plan_bufs, self.Y, self.ws, stream=stream, events=events)
 
     def step_int(self, stream=None, fwd_events=None):
         """Route, plan and the int8 forward."""

@@ -147,6 +147,26 @@ def test_one_workspace_under_two_graphs():
         assert torch.equal(layers[i].Y, want[i]) and torch.equal(layers[1 - i].Y, want[1 - i])
 
 
+@pytest.mark.parametrize("T", [1, 40, 500])
+def test_stage_events(T):
+    """Every stage's event is recorded, in order, and the results stay."""
+    w = Workload("events", T=T, d=512, E=8, k=2, f=512, f_s=256)
+    L = DeviceLayer(w, make_inputs(w, 2), int8=True)
+    L.step_int()
+    torch.cuda.synchronize()
+    want = L.Y.clone()
+    ev = [torch.cuda.Event(enable_timing=True) for _ in range(7)]
+    for e in ev:
+        e.record()                          # creates the events
+    stages = B.MoeStageEvents()
+    for i, e in enumerate(ev):
+        stages.ev[i] = e.cuda_event
+    L.step_int(fwd_events=stages)
+    torch.cuda.synchronize()
+    assert all(a.elapsed_time(b) >= 0 for a, b in zip(ev, ev[1:])) and ev[0].elapsed_time(ev[6]) > 0
+    assert torch.equal(L.Y, want)
+
+
 def test_special_values():
     """Zero tokens, zero channels, channels and tokens of tiny and huge values,
     and values that tie between two codes."""
