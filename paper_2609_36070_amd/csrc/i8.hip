@@ -186,19 +186,18 @@ __global__ __launch_bounds__(256) void i8_quant_weights_kernel(const uint16_t *_
 }
 
 // f(NC, W) for rows of K elements, which stay in registers up to 8192: a block per
-// row, or a wave if a block's threads would have no more than one chunk each and
+// row, or a wave if a quarter of a block's threads would have nothing to do and
 // there are rows for every CU (whole forward, us by waves / by blocks: 65536 rows of
 // 768 555 / 591; 32768 of 256 85 / 105; 131072 of 1536 2850 / 2867; 8000 of 1536 260.4 /
-// 260.2; 488 of 2048 108.6 / 107.2; 128 of 1536 139 / 137).  They move 5.2 TB/s from
-// 131072 rows of 1536 (188 us), and few rows take a launch's time (5 us).
+// 260.2; 36891 of 2048, all threads busy, 1772 / 1769; 128 of 1536 139 / 137).  They move
+// 5.2 TB/s from 131072 rows of 1536 (186 us), and few rows take a launch's time (5 us).
 constexpr long QUANT_WAVE_ROWS = 2048;
 template <typename F>
 hipError_t with_chunks(long rows, int K, F f) {
-    if (rows >= QUANT_WAVE_ROWS && K <= 2048) {
+    if (rows >= QUANT_WAVE_ROWS && K <= 1536) {
         if (K <= 512) f(Const<1>{}, Const<1>{});
         else if (K <= 1024) f(Const<2>{}, Const<1>{});
-        else if (K <= 1536) f(Const<3>{}, Const<1>{});
-        else f(Const<4>{}, Const<1>{});
+        else f(Const<3>{}, Const<1>{});
     }
     else if (K <= 2048) f(Const<1>{}, Const<4>{});
     else if (K <= 4096) f(Const<2>{}, Const<4>{});
