@@ -105,7 +105,7 @@ def score_backward(Z, balance, idx, dw, score, renormalise, scale):
     live = in_play(Z, balance)
     T, E = live.shape
     u = unscaled_weights(Z, balance, idx, score, renormalise)
-    s = scores(Z, live, score)
+    s, z = scores(Z, live, score), _clamped(Z, live)
     dZ = np.zeros((T, E))
     for t in range(T):
         on = live[t, idx[t]]
@@ -114,7 +114,7 @@ def score_backward(Z, balance, idx, dw, score, renormalise, scale):
         d = scale * u[t] * (g - dot if renormalise else g)
         if score == "sigmoid":
             with np.errstate(over="ignore"):
-                d = d / (1.0 + np.exp(_clamped(Z, live)[t, idx[t]]))
+                d = d / (1.0 + np.exp(z[t, idx[t]]))
         elif not renormalise:
             dZ[t] = -s[t] * scale * dot
         for i, e in enumerate(idx[t]):

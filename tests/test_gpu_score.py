@@ -67,6 +67,12 @@ CASES = [
     Case(2049, 7168, 128, 8, groups=64, top_groups=9, group_score="pair"), Case(1025, 7168, 256, 2, "softmax"),
     Case(5000, 256, 100, 11, groups=50, top_groups=20), Case(4500, 256, 250, 13, groups=2, top_groups=1),
     Case(3, 16384, 64, 1, groups=64, top_groups=64),
+    # tiles of 128 tokens on W_r as it lies: one to many chunks of d, one slice and
+    # several, experts short of the tile
+    Case(4200, 256, 96, 6, "softmax", renormalise=False), Case(1300, 7168, 256, 8, groups=8, top_groups=4),
+    Case(5000, 512, 160, 8, groups=5, top_groups=3, group_score="pair"), Case(9001, 1280, 128, 4, bias=0.5),
+    Case(4097, 1792, 200, 8, "softmax", bias=0.5), Case(32700, 256, 72, 2, "softmax", bias=0.5),
+    Case(32768, 512, 248, 3, bias=0.5, balance=0.0),
 ]
 IDS = ["-".join(str(v) for v in dataclasses.astuple(c)) for c in CASES]
 
@@ -241,9 +247,10 @@ def test_no_tokens():
     r.check_guards()
 
 
-def test_repeats_streams_and_graph():
+@pytest.mark.parametrize("T,d", [(700, 7168), (4500, 1024)])
+def test_repeats_streams_and_graph(T, d):
     """The same bits again, on another stream, and from a replayed graph."""
-    c = Case(700, 7168, 256, 8, groups=8, top_groups=4, group_score="pair", scale=2.5)
+    c = Case(T, d, 256, 8, groups=8, top_groups=4, group_score="pair", scale=2.5)
     X, W_r, bias, balance = inputs(c, 3)
     r = Run(c, X, W_r, bias, balance)
     dw = torch.randn(c.T, c.k, device=DEV)
