@@ -14,8 +14,8 @@
 // 100000, and rows of exact ties) the experts that the errors reach, mostly two,
 // are ranked again by 64-bit values, in compact loops.  A selection in 64 bits
 // throughout spent 25-50 us, most of it on fetching its unrolled code (30 us for a
-// single token); this one takes 7.4 us for one token to 256 experts in 8 groups
-// (14 slices of partial logits; a launch's and three dependent loads' time), 13.7
+// single token); this one takes 6.5 us for one token to 256 experts in 8 groups
+// (28 slices of partial logits; a launch's and a round trip's time), 13.6
 // for 4099 (29 MB of partial logits) and 14.2 for 16384 to 128 experts (networks
 // and exponentials; the logits are 8 MB).
 //
@@ -198,7 +198,8 @@ __global__ __launch_bounds__(256) void score_select_kernel(
     __shared__ __attribute__((aligned(16))) float zs[256 * PE];   // TB rows of E <= L PE
     __shared__ uint64_t keys[256 * PE];      // room for select_64
     __shared__ float sbal[256];
-    if ((int)threadIdx.x < E) sbal[threadIdx.x] = balance ? balance[threadIdx.x] : 0.f;
+    // loads return in order: what is needed last is asked for first and used last
+    const float my_bal = balance && (int)threadIdx.x < E ? balance[threadIdx.x] : 0.f;
     const long t0 = (long)blockIdx.x * TB;
     const int nt = (int)(T - t0 < TB ? T - t0 : TB);
     float *zrow = logits + t0 * E;           // 16-byte aligned: TB is a multiple of 4
@@ -214,25 +215,28 @@ __global__ __launch_bounds__(256) void score_select_kernel(
         // pieces of 4 logits, two at a time; NB slices of each in flight
         const int ch = epad / 4, pieces = nt * ch;
         const long pitch = (long)T * epad;
-        auto add = [&](auto nb, int i0) {
-            constexpr int NB = decltype(nb)::value;
-            const float *p[2];
-            f32x4_t v[2];
+        auto add = [&](auto nb, auto nh, int i0) {
+            constexpr int NB = decltype(nb)::value, NH = decltype(nh)::value;
+            const float *p[NH];
+            f32x4_t v[NH], bz[NH];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < NH; ++h) {
                 const int i = min(i0 + 256 * h, pieces - 1);
                 p[h] = part + (t0 + i / ch) * epad + 4 * (i % ch);
                 v[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                if (bias)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) bz[h][q] = bias[min(4 * (i % ch) + q, E - 1)];
             }
             for (int s = 0; s < S; s += NB) {
-                f32x4_t u[2][NB];
+                f32x4_t u[NH][NB];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < NH; ++h)
 #pragma unroll
                     for (int j = 0; j < NB; ++j)
                         u[h][j] = *reinterpret_cast<const f32x4_t *>(p[h] + min(s + j, S - 1) * pitch);
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < NH; ++h)
 #pragma unroll
                     for (int j = 0; j < NB; ++j)
                         if (s + j < S)
@@ -240,20 +244,27 @@ __global__ __launch_bounds__(256) void score_select_kernel(
                             for (int q = 0; q < 4; ++q) v[h][q] = v[h][q] + u[h][j][q];
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < NH; ++h) {
                 const int i = i0 + 256 * h, c = 4 * (i % ch);
                 if (i >= pieces) break;
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    if (c + q < E) zs[i / ch * E + c + q] = bias ? v[h][q] + bias[c + q] : v[h][q];
+                    if (c + q < E) zs[i / ch * E + c + q] = bias ? v[h][q] + bz[h][q] : v[h][q];
             }
         };
-        for (int i = threadIdx.x; i < pieces; i += 512) {
-            if (S <= 2) add(Int<2>{}, i);
-            else if (S <= 8) add(Int<8>{}, i);
-            else add(Int<14>{}, i);
+        // few tokens: all slices in one round trip (1 token to 256 experts, 28
+        // slices: the router 13.0 -> 11.9 us)
+        if (pieces <= 256 && S > 14 && S <= 28) {
+            if ((int)threadIdx.x < pieces) add(Int<28>{}, Int<1>{}, threadIdx.x);
+        } else {
+            for (int i = threadIdx.x; i < pieces; i += 512) {
+                if (S <= 2) add(Int<2>{}, Int<2>{}, i);
+                else if (S <= 8) add(Int<8>{}, Int<2>{}, i);
+                else add(Int<14>{}, Int<2>{}, i);
+            }
         }
     }
+    if ((int)threadIdx.x < E) sbal[threadIdx.x] = my_bal;
     __syncthreads();
     if (S > 0) {
         for (int i = 4 * threadIdx.x; i < nt * E; i += 1024) {

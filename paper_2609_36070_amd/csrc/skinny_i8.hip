@@ -91,7 +91,8 @@ DEV void put8(uint8_t *codes, const float (&v)[8], const I8Scale &s) {
 // token's own list).  What counts is latency: every load that a wave will need
 // goes out at once, and the workgroups quantise the activations for
 // themselves, each the same row again, under the weights' round trip.  8 of 128
-// experts of 768, d 2048: 8.6 and 7.2 us for 25 and 13 MB.
+// experts of 768, d 2048, 25 and 13 MB of codes: 14.2 us together, 15.8 with the
+// scales asked for where they are used and the activations behind the expert's id.
 //
 // Up product: a workgroup owns 8 columns of f of one of the token's experts (or
 // of the shared one), 8 gate and 8 up rows in one operand; its 4 waves take every
@@ -113,11 +114,10 @@ __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
     const I8Product &g = sh ? a.shared : a.routed;
     const int slot = sh ? 0 : b / (g.N / 8);
     const int n0 = 8 * (sh ? b + ns : b % (g.N / 8));
-    const int e = sh ? 0 : __builtin_amdgcn_readfirstlane(a.topk_idx[slot]);
-    if (e < 0 || e >= a.E) return;   // routes outside the experts are left out
     const int K = g.K, pieces = K / SI_PIECE;
 
-    // loads return in order: the token first, then the weights
+    // loads return in order: the token first, then the weights, then their scales
+    int e = sh ? 0 : a.topk_idx[slot];
     float v[TK_HELD][8];
 #pragma unroll
     for (int i = 0; i < TK_HELD; ++i) {
@@ -127,6 +127,8 @@ __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
         if (c < K / 8) load8(a.X + 8 * c, v[i]);
     }
     __builtin_amdgcn_sched_barrier(0);
+    e = __builtin_amdgcn_readfirstlane(e);
+    if (e < 0 || e >= a.E) return;   // routes outside the experts are left out
     const uint8_t *wp = (r < 8 ? g.B : g.B2) + ((long)e * g.N + n0 + (r & 7)) * K + 16 * g4;
     u32x4_t w[TK_D][2];
     auto load = [&](int s, int u) {
@@ -136,6 +138,8 @@ __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
 #pragma unroll
     for (int s = 0; s < TK_D; ++s)
         if (wave + TK_NW * s < pieces) load(s, wave + TK_NW * s);
+    const long channel = (long)e * g.N + n0 + (tid & 7);
+    const float gate_s = g.Bs[channel], up_s = g.Bs2[channel];
     __builtin_amdgcn_sched_barrier(0);
 
     uint32_t m = 0;
@@ -183,9 +187,8 @@ __global__ __launch_bounds__(64 * TK_NW) void token_up_kernel(I8SkinnyArgs a) {
             gate += red[q][tid];
             up += red[q][8 + tid];
         }
-        const long c = (long)e * g.N + n0 + tid;
         g.H[(long)slot * g.N + n0 + tid] =
-            silu_f(xs.s * ((float)gate * g.Bs[c])) * (xs.s * ((float)up * g.Bs2[c]));
+            silu_f(xs.s * ((float)gate * gate_s)) * (xs.s * ((float)up * up_s));
     }
 }
 
@@ -208,12 +211,9 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
     for (int s0 = wave; s0 < routes; s0 += nw) {
         const bool sh = s0 < nsh;
         const I8Product &g = sh ? a.shared : a.routed;
-        const int slot = s0 - nsh, e = sh ? 0 : __builtin_amdgcn_readfirstlane(a.topk_idx[slot]);
-        if (e < 0 || e >= a.E) {
-            if (lane < 16) y[s0][lane] = 0.f;
-            continue;
-        }
-        const int K = g.K, pieces = K / SI_PIECE;
+        const int slot = s0 - nsh, K = g.K, pieces = K / SI_PIECE;
+        int e = sh ? 0 : a.topk_idx[slot];
+        const float wt = sh ? 1.0f : topk_w[slot];
         const float *h = g.Hin + (sh ? 0 : (long)slot * K);
         // the row's largest value: the first 2048 values stay in registers
         float v[4][8];
@@ -226,6 +226,11 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
             if (c < K / 8) load8(h + 8 * c, v[i]);
         }
         __builtin_amdgcn_sched_barrier(0);
+        e = __builtin_amdgcn_readfirstlane(e);
+        if (e < 0 || e >= a.E) {
+            if (lane < 16) y[s0][lane] = 0.f;
+            continue;
+        }
         const uint8_t *wp = g.B + ((long)e * g.N + n0 + (r & (COLS - 1))) * K + 16 * g4;
         u32x4_t w[TK_DD][2];
         auto load = [&](int s, int u) {
@@ -235,6 +240,7 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
 #pragma unroll
         for (int s = 0; s < TK_DD; ++s)
             if (s < pieces) load(s, s);
+        const f32x4_t sc = *reinterpret_cast<const f32x4_t *>(g.Bs + (long)e * g.N + n0 + (4 * g4 & (COLS - 1)));
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = umax(m, max8(v[i]));
@@ -274,12 +280,8 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
             }
         }
         if (r == 0 && 4 * g4 < COLS) {
-            const float wt = sh ? 1.0f : topk_w[slot];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = 4 * g4 + q;
-                y[s0][c] = wt * (hs.s * ((float)acc[q] * g.Bs[(long)e * g.N + n0 + c]));
-            }
+            for (int q = 0; q < 4; ++q) y[s0][4 * g4 + q] = wt * (hs.s * ((float)acc[q] * sc[q]));
         }
     }
     __syncthreads();
