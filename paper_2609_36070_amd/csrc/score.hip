@@ -508,9 +508,10 @@ __global__ __launch_bounds__(256) void score_select_kernel(
 // the rows are put together in LDS, where the chosen entries are scattered,
 // and leave in one contiguous run (a row of E floats starts anywhere, 16 of
 // them start at a multiple of 64 bytes).  Bound by that store and the lines that
-// the k logits of a row lie in: 16384 tokens to 256 experts, sigmoid, 7.5 us for
-// 18 MB that a caller would count and about 25 that move; 6001 to 96, softmax, 7.6
-// (three passes over the row in LDS); a launch alone takes 5.
+// the k logits of a row lie in: 16384 tokens to 256 experts, sigmoid, 7.3 us for
+// 18 MB that a caller would count and about 25 that move; 6001 to 96, softmax, 6.8
+// (8.4 with the balance read where it is compared and three passes over the row in
+// LDS); a launch and its two round trips take 5.
 constexpr int SB_BT = 16;
 __global__ __launch_bounds__(256) void score_bwd_kernel(
         const float *__restrict__ logits, const float *__restrict__ balance,
@@ -518,9 +519,14 @@ __global__ __launch_bounds__(256) void score_bwd_kernel(
         int nparts, const int *__restrict__ route_pos, float *__restrict__ dg_out,
         float *__restrict__ dZ, int T, int E, int k, ScoreArgs a) {
     __shared__ __attribute__((aligned(16))) float row[SB_BT * 256];
+    __shared__ float sbal[256];
     const int t0 = blockIdx.x * SB_BT, tl = threadIdx.x >> 4, s = threadIdx.x & 15;
     const int t = t0 + tl;
-    const bool dense = !a.sigmoid && !a.renorm;
+    const bool dense = !a.sigmoid && !a.renorm, slot = t < T && s < k;
+    const float my_bal = balance && (int)threadIdx.x < E ? balance[threadIdx.x] : 0.f;
+    const long j = (long)t * k + s;
+    int e = slot ? topk_idx[j] : -1;
+    float g = slot && dw ? dw[j] : 0.f;      // dL/dw of the slot
     const int total = min(SB_BT, T - t0) * E;
     const float *src = logits + (long)t0 * E;
     float *out = dZ + (long)t0 * E;
@@ -537,32 +543,24 @@ __global__ __launch_bounds__(256) void score_bwd_kernel(
         *reinterpret_cast<f32x4_t *>(row + 4 * i) = v;
     }
 
-    const bool slot = t < T && s < k;
-    int e = -1;
-    float g = 0.f;                           // dL/dw of the slot
-    if (slot) {
-        const long j = (long)t * k + s;
-        e = topk_idx[j];
-        if (dw) {
-            g = dw[j];
-        } else {
-            const int p = route_pos[j];
-            if (p >= 0 && p < T * k) {
-                for (int q0 = 0; q0 < nparts; q0 += 8) {
-                    float v[8];
+    if (slot && !dw) {
+        const int p = route_pos[j];
+        if (p >= 0 && p < T * k) {
+            for (int q0 = 0; q0 < nparts; q0 += 8) {
+                float v[8];
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        v[q] = q0 + q < nparts ? dgpart[(long)p * nparts + q0 + q] : 0.f;
+                for (int q = 0; q < 8; ++q)
+                    v[q] = q0 + q < nparts ? dgpart[(long)p * nparts + q0 + q] : 0.f;
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (q0 + q < nparts) g = g + v[q];
-                }
-                dg_out[p] = g;
+                for (int q = 0; q < 8; ++q)
+                    if (q0 + q < nparts) g = g + v[q];
             }
+            dg_out[p] = g;
         }
     }
+    if ((int)threadIdx.x < E) sbal[threadIdx.x] = my_bal;
     __syncthreads();
-    auto live = [&](float z, int id) { return z >= MASKED && !(balance && !(balance[id] >= MASKED)); };
+    auto live = [&](float z, int id) { return z >= MASKED && sbal[id] >= MASKED; };
     float z = 0.f;
     bool on = slot && e >= 0 && e < E;
     if (on) {
@@ -582,6 +580,7 @@ __global__ __launch_bounds__(256) void score_bwd_kernel(
         return x;
     };
     float u = 0.f, zmax = -INFINITY, zsum = 1.f;
+    float x[16];                             // softmax over the row: the lane's logits, their exponentials
     if (a.renorm) {
         const float m = max16(on ? (a.sigmoid ? fminf(z, 0.f) : z) : -INFINITY);
         if (on) u = a.sigmoid ? expf(fminf(z, 0.f) - m) / (1.0f + expf(-fabsf(z))) : expf(z - m);
@@ -590,15 +589,22 @@ __global__ __launch_bounds__(256) void score_bwd_kernel(
     } else if (a.sigmoid) {
         if (on) u = sigmoid32(z);
     } else {
-        for (int i = s; i < E; i += 16) {
-            const float x = row[tl * E + i];
-            if (live(x, i)) zmax = fmaxf(zmax, fminf(x, FLT_MAX));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int id = s + 16 * i;
+            x[i] = -INFINITY;
+            if (id < E) {
+                const float v = row[tl * E + id];
+                if (live(v, id)) x[i] = fminf(v, FLT_MAX);
+            }
+            zmax = fmaxf(zmax, x[i]);
         }
         zmax = max16(zmax);
         zsum = 0.f;
-        for (int i = s; i < E; i += 16) {
-            const float x = row[tl * E + i];
-            if (live(x, i)) zsum = zsum + expf(fminf(x, FLT_MAX) - zmax);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (16 * i < E) x[i] = x[i] > -INFINITY ? expf(x[i] - zmax) : 0.f;
+            if (16 * i < E) zsum = zsum + x[i];
         }
         zsum = sum16(zsum);
         if (on) u = expf(z - zmax) / zsum;
@@ -609,11 +615,9 @@ __global__ __launch_bounds__(256) void score_bwd_kernel(
     d = a.renorm ? d * (g - dot) : d * g;
     if (a.sigmoid) d = d / (1.0f + expf(z)); // 1 - s
     if (dense) {
-        for (int i = s; i < E; i += 16) {
-            const float x = row[tl * E + i];
-            const float p = live(x, i) ? expf(fminf(x, FLT_MAX) - zmax) / zsum : 0.f;
-            row[tl * E + i] = -p * (a.scale * dot);
-        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)         // (a row with nothing in play has the sum 0)
+            if (s + 16 * i < E) row[tl * E + s + 16 * i] = -(x[i] > 0.f ? x[i] / zsum : 0.f) * (a.scale * dot);
     }
     __syncthreads();
     // an id listed twice gets the sum, from its first slot
