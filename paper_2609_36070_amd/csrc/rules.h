@@ -216,24 +216,32 @@ inline bool route_direct(long T, long d, long E, long k) {
 
 // Logits for a selection by scores (score.hip), few tokens: the one-launch
 // router's blocks on slices of the d axis, so that about all CUs read W_r; the
-// selection adds the slices.  0: the other routers.  A block reads its slice
-// of W_r for 16 tokens, so the two cross by T d E (us with the selection, here /
-// the others): 256 experts, d 7168, 1 token 13.7 / 26.4, 512 25.4 / 33, 1024 30.6 / 32.8,
-// 2048 45 / 37; 128, d 7168, 2048 23.5 / 24.4, 3000 32 / 26.6; d 2048, 4096 18.4 / 23.9; 64,
-// d 7168, 1024 17 / 44, 4096 30 / 46; 32, d 4096, 1 token 8.5 / 16, 4096 17 / 22.5; at most
-// one slice is left past that: 32, d 4096, 8192 24 / 30, 16384 51 / 43.
-constexpr long ROUTE_SLICE_MAX = 4096, ROUTE_SLICE_BLOCKS = 256, ROUTE_SLICE_READS = 1L << 31;
+// selection adds the slices.  0: the other routers.
+//
+// A block reads its slice of W_r for 16 tokens, so the two cross by T d E (us with
+// the selection, here / the others).  256 experts, d 7168: 1 token 11.5 / 22.4, 512
+// 21.5 / 27, 1024 27.5 / 27.5, 1500 38 / 29; d 4096: 1024 20.7 / 21.1, 1500 26 / 22.5; d 2048:
+// 2048 20.7 / 20.5, 3000 26 / 23.  128, d 7168: 1024 16.5 / 18.2, 1500 20.7 / 18.6; d 2048:
+// 4096 16.4 / 19, 6000 23.6 / 20.  Up to 64 experts the others are slower: 64, d 7168:
+// 1024 14.5 / 42, 4096 27 / 44, 6000 50 / 73, 8192 59 / 53; 32, d 4096: 1 token 8 / 15, 4096
+// 15 / 20, 8192 22 / 28, 16384 49 / 41; 16, d 2048: 4096 14.3 / 16, 8192 19.4 / 18.5.
+constexpr long ROUTE_SLICE_MAX = 8192, ROUTE_SLICE_BLOCKS = 256;
 
+inline bool route_sliced(long T, long d, long E) {
+    const long ep = route_padded(E), cols = ep / 16 < 8 ? ep / 16 : 8;
+    if (T <= 0 || E % cols) return false;
+    if (ep >= 128) return T <= 1024 || (T <= 4096 && T * d * ep <= 1L << 30);
+    return T <= ROUTE_SLICE_MAX && T <= 256 * ep && T * d * ep <= 3L << 30;
+}
 inline long route_slice_steps(long d, long E) {      // slices of one step of 32 rows per wave
     const long nw = route_padded(E) <= 64 ? 16 : 8;
     const long s = d / 32 / nw;
     return s > 1 ? s : 1;
 }
 inline long route_slices(long T, long d, long E) {
-    const long ep = route_padded(E), cols = ep / 16 < 8 ? ep / 16 : 8;
-    if (T <= 0 || T > ROUTE_SLICE_MAX || T * d * ep > ROUTE_SLICE_READS || E % cols) return 0;
+    if (!route_sliced(T, d, E)) return 0;
     const long fill = ROUTE_SLICE_BLOCKS / ((T + 15) / 16), most = route_slice_steps(d, E);
-    return fill < most ? fill : most;
+    return std::max(std::min(fill, most), 1L);
 }
 // Rows of partial logits of any batch of up to T tokens.
 inline long route_slice_rows(long T, long d, long E) {

@@ -66,7 +66,8 @@ CASES = [
     Case(4096, 7168, 64, 4, "softmax", groups=16, top_groups=3, group_score="pair"),
     Case(2049, 7168, 128, 8, groups=64, top_groups=9, group_score="pair"), Case(1025, 7168, 256, 2, "softmax"),
     Case(5000, 256, 100, 11, groups=50, top_groups=20), Case(4500, 256, 250, 13, groups=2, top_groups=1),
-    Case(3, 16384, 64, 1, groups=64, top_groups=64),
+    Case(3, 16384, 64, 1, groups=64, top_groups=64), Case(8190, 512, 64, 6, groups=8, top_groups=4),
+    Case(8300, 256, 48, 4, "softmax"), Case(1100, 4096, 256, 8, groups=8, top_groups=4),
     # tiles of 128 tokens on W_r as it lies: one to many chunks of d, one slice and
     # several, experts short of the tile
     Case(4200, 256, 96, 6, "softmax", renormalise=False), Case(1300, 7168, 256, 8, groups=8, top_groups=4),

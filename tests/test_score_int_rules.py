@@ -54,20 +54,21 @@ def test_one_token():
 
 
 @pytest.mark.parametrize("T,d,E,here,others", [
-    (1, 7168, 256, 13.7, 26.4), (512, 7168, 256, 25.4, 33), (1024, 7168, 256, 30.6, 32.8), (2048, 7168, 256, 45, 37),
-    (2048, 7168, 128, 23.5, 24.4), (3000, 7168, 128, 32, 26.6), (4096, 2048, 128, 18.4, 23.9),
-    (16384, 2048, 128, 39, 32), (4096, 7168, 64, 30, 46), (8192, 7168, 64, 61, 55), (4096, 4096, 32, 17, 22.5),
-    (16384, 4096, 32, 51, 43), (16384, 2048, 16, 29, 24),
+    (1, 7168, 256, 11.5, 22.4), (512, 7168, 256, 21.5, 27), (1500, 7168, 256, 38, 29), (1024, 4096, 256, 20.7, 21.1),
+    (1500, 4096, 256, 26, 22.5), (3000, 2048, 256, 26, 23), (1024, 7168, 128, 16.5, 18.2), (1500, 7168, 128, 20.7, 18.6),
+    (4096, 2048, 128, 16.4, 19), (6000, 2048, 128, 23.6, 20), (1024, 7168, 64, 14.5, 42), (6000, 7168, 64, 50, 73),
+    (8192, 7168, 64, 59, 53), (1, 4096, 32, 8, 15), (8192, 4096, 32, 22, 28), (16384, 4096, 32, 49, 41),
+    (4096, 2048, 16, 14.3, 16), (8192, 2048, 16, 19.4, 18.5),
 ])
 def test_router_slices(T, d, E, here, others):
     assert bool(rule("slices", T, d, E)) == (here < others)
 
 
-@pytest.mark.parametrize("d,E", [(256, 1), (256, 16), (1024, 96), (7168, 256), (2048, 33), (16384, 64), (7168, 200)])
+@pytest.mark.parametrize("d,E", [(256, 1), (256, 16), (1024, 96), (7168, 256), (2048, 33), (16384, 64), (7168, 200), (256, 64), (512, 32)])
 def test_partial_logits_fit_their_rows(d, E):
     """The partial sums of every batch up to T tokens fit what T tokens reserve."""
     rows = 0
-    for T in [*range(0, 200), *range(200, 5000, 13), 4096, 4097, 100000]:
+    for T in [*range(0, 200), *range(200, 5000, 13), 4096, 4097, 8192, 8193, 16384, 100000]:
         S = rule("slices", T, d, E)
         assert 0 <= S <= rule("slice_steps", d, E)
         assert rule("slice_rows", T, d, E) >= rows
