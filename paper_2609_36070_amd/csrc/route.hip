@@ -679,11 +679,13 @@ DEV uint32_t rd_word(const u32x4_t &v, int i) { return v[i]; }
 
 constexpr int rd_waves(int EPAD) { return EPAD <= 64 ? 16 : 8; }
 
-template <int EPAD>
+// SLICED: the blocks of a tile share its d axis, S slices, and leave their sums
+// in `part` (S is 1 otherwise).
+template <int EPAD, bool SLICED>
 __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
         const uint16_t *__restrict__ X, const uint16_t *__restrict__ Wr, const float *__restrict__ bias,
         float *__restrict__ logits, int *__restrict__ topk_idx, float *__restrict__ topk_w,
-        float *__restrict__ part, int T, int d, int E, int k, int S) {
+        float *__restrict__ part, int T, int d, int E, int k, int slices) {
     constexpr int NW = rd_waves(EPAD), BT = 16;
     constexpr int CPL = EPAD / 16, VW = CPL < 8 ? CPL : 8, NV = CPL / VW;
     constexpr int U = EPAD <= 32 ? 8 : EPAD <= 128 ? 4 : 2;   // steps in flight per wave
@@ -692,8 +694,8 @@ __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
     __shared__ float zs[BT][EPAD + 1];
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
     const int g = l >> 4, r = l & 15;
+    const int S = SLICED ? slices : 1;
     const int t0 = blockIdx.x / S * BT;
-    // this block's slice of the d axis (S > 1: its sums go to `part`)
     const int ks = blockIdx.x % S, s_first = d / 32 * ks / S, nsteps = d / 32 * (ks + 1) / S;
 
     // columns past the experts re-read the last ones; their logits are not used
@@ -751,7 +753,7 @@ __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
         float z = red[0][tt][ecol] + red[1][tt][ecol];
 #pragma unroll
         for (int v = 2; v < NW; ++v) z = z + red[v][tt][ecol];
-        if (S > 1) {
+        if constexpr (SLICED) {
             if (t0 + tt < T) part[((long)ks * T + t0 + tt) * EPAD + ecol] = z;
         } else if (ecol < E) {
             if (bias) z = z + bz;
@@ -759,7 +761,7 @@ __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
             zs[tt][ecol] = z;
         }
     }
-    if (S > 1) return;
+    if constexpr (SLICED) return;
     __syncthreads();
     if (topk_idx)
         select_block<EPAD>(&zs[0][0], EPAD + 1, BT, NW, t0, T, E, k, topk_idx, topk_w);
@@ -815,8 +817,12 @@ hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bia
         const int S = slices > 1 ? slices : 1;
         const dim3 grid((unsigned)((T + 15) / 16 * S)), block(64 * rd_waves(EPAD));
 #define ROUTE_DIRECT(EP)                                                                                   \
-    route_direct_kernel<EP><<<grid, block, 0, st>>>(X, W_r, bias, logits, topk_idx, topk_w, part, T, d, E, \
-                                                    k, S)
+    if (S > 1)                                                                                             \
+        route_direct_kernel<EP, true><<<grid, block, 0, st>>>(X, W_r, bias, logits, topk_idx, topk_w, part, \
+                                                              T, d, E, k, S);                              \
+    else                                                                                                   \
+        route_direct_kernel<EP, false><<<grid, block, 0, st>>>(X, W_r, bias, logits, topk_idx, topk_w, part, \
+                                                               T, d, E, k, 1)
         switch (EPAD) {
             case 16: ROUTE_DIRECT(16); break;
             case 32: ROUTE_DIRECT(32); break;
