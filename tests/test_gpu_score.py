@@ -319,3 +319,29 @@ def test_layer_step(w, routing, kw):
     dX = g["dX"] + (dZ - g["dZ"]) @ inp["W_r"].astype(np.float64).T
     assert_close("dX", to_np(L.dX), dX, rel)
     assert_close("dW_down", to_np(L.dW_down), g["dW_down"], rel)
+
+
+def test_captured_training_step():
+    """Route, plan, forward and backward of a layer routed by scores from a
+    replayed graph, with eager steps of another layer on the same workspace
+    between the replays: every output repeats bit for bit."""
+    w = Workload("captured", T=200, d=256, E=16, k=4, f=256, f_s=256, backward=True)
+    routing = B.routing("sigmoid", 4, 2, "pair", True, 2.5)
+    balance = (np.random.default_rng(6).standard_normal(w.E) * 0.1).astype(np.float32)
+    L, other = (DeviceLayer(w, dict(make_inputs(w, s), balance=balance), routing=routing) for s in (3, 4))
+    other.ws = L.ws
+    outs = [L.logits, L.topk_idx, L.topk_w, L.Y, L.dX, L.dW_r, L.dW_gate, L.dW_up, L.dW_down, L.dWg_s, L.dWu_s,
+            L.dWd_s]
+    L.step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        L.step()
+    for _ in range(3):
+        for t in outs:
+            t.zero_()
+        other.step()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
