@@ -89,8 +89,8 @@ inline int skinny_kslices(long T, long k, long E, long d, long f, long fs, long 
 
 // Int8, one token (skinny_i8.hip): rows whose codes fit the workgroups' LDS.
 // Two launches in place of five (us here / the streaming kernels): 128 experts,
-// top 8, d 2048, f 768 15.8 / 26; 64, top 4, d 4096, f 256 12.0 / 27.6; 32, top 8, and a
-// shared one, d 7168, f 2048 80 / 98; 16, top 2, d 1024, f 512 10 / 20.6.
+// top 8, d 2048, f 768 14.1 / 26; 64, top 4, d 4096, f 256 11.3 / 27.6; 32, top 8, and a
+// shared one, d 7168, f 2048 79 / 98; 16, top 2, d 1024, f 512 9.4 / 20.6.
 constexpr long TOKEN_I8_K = 8192, TOKEN_I8_LDS = 56 * 1024;
 inline bool token_i8(long T, long d, long k, long f, long fs) {
     const long routes = k + (fs > 0), waves = routes < 16 ? routes : 16;
