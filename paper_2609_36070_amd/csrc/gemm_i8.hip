@@ -286,6 +286,9 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
         };
         // (the counter ends at 63: with more behind them, the first stores too)
         wait_vmcnt<LPS + STORES<MODE> < 63 ? LPS + STORES<MODE> : 63>();
+        // the scale, which other waves read: one that is not busy waits for no LDS
+        // access of its own before then
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         barrier_no_fence();
         if (nk == 2) {
             ask_next();
