@@ -19,9 +19,8 @@
 // for 4099 (29 MB of partial logits) and 14.2 for 16384 to 128 experts (networks
 // and exponentials; the logits are 8 MB).
 //
-// 64-bit entries hold sign, exponent and the upper 44 bits of the mantissa
-// above the 8 bits of 255 - e: rank order, ties to the lower id, is plain order
-// of the entries (2^-44 is far below the rounding of any logit).
+// The 64-bit side compares all 64 bits and then the ids: saturated sigmoids, and
+// small scores beside a balance, differ in their last bits alone.
 //
 // Out-of-play experts (logit or balance below MASKED or NaN) have score 0 and
 // rank after every other expert of the kept groups, lower ids first.  Logits
@@ -39,12 +38,11 @@ constexpr float MASKED = -1e38f;
 DEV double shfl_xor_d(double v, int m) {
     return __longlong_as_double((long long)shfl_xor_u64((uint64_t)__double_as_longlong(v), m));
 }
-// Unsigned key with the order of the double, its 8 lowest bits free.
+// Unsigned key with the order of the double, above 0 and below ~0.
 DEV uint64_t rank_key(double v) {
     const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);   // -0 and 0 are one
-    return ((b >> 63) ? ~b : (b | (1ull << 63))) & ~0xffull;
+    return (b >> 63) ? ~b : (b | (1ull << 63));
 }
-constexpr uint64_t MASKED_KEY = 0x100;   // below every rank_key, above the padding 0
 constexpr uint32_t MASKED_Q = 1, FIRST_Q = 3;   // 24-bit places: masked; in play, from
 
 DEV float sigmoid32(float z) { return 1.0f / (1.0f + expf(-z)); }
@@ -129,34 +127,35 @@ DEV bool groups_64(Exact x, uint32_t live, int grp, int first, int lpg, int sure
         b1 = fmax(b1, o1);
     }
     double gs = a.pair && b2 > -INFINITY ? b1 + b2 : b1;
-    uint64_t gk = sure > 0 ? ~0xffull : sure < 0 ? 0ull : rank_key(gs);
-    gk = grp < a.groups ? gk | (uint64_t)(255 - grp) : 0ull;
+    const uint64_t gk = sure > 0 ? ~0ull : sure < 0 ? 0ull : rank_key(gs);
     int better = 0;
 #pragma unroll 1
     for (int o = 0; o < a.groups; ++o) {
         const int lo = __shfl((int)(uint32_t)gk, o * lpg, L);
         const int hi = __shfl((int)(uint32_t)(gk >> 32), o * lpg, L);
-        better += (((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo) > gk ? 1 : 0;
+        const uint64_t og = ((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo;
+        better += og > gk || (og == gk && o < grp) ? 1 : 0;
     }
     return better < a.top_groups;
 }
 
 // Places `from` .. k - 1 of the token's chosen experts: the best, by their
-// 64-bit values, of the candidates (bits of `cand` for this lane's experts).
-// kb: room for this lane's entries, at stride 256.
+// 64-bit values, ties to the lower id, of the candidates (bits of `cand` for this
+// lane's experts, in ascending id; at least k - from of them in the token's lanes).
+// kb: room for this lane's keys, at stride 256.
 template <int PE, int L, int KP>
 DEV void select_64(Exact x, uint64_t *kb, uint32_t live, uint32_t cand, int first, int lpg, int from,
                    int k, uint32_t (&bk)[KP]) {
     exact_sum<PE, L>(x, live, first, lpg);
 #pragma unroll 1
     for (uint32_t m = cand; m; m &= m - 1) {
-        const int i = __builtin_ctz(m), id = first + lpg * i;
-        kb[256 * i] = rank_key(x.value(id)) | (uint64_t)(255 - id);
+        const int i = __builtin_ctz(m);
+        kb[256 * i] = rank_key(x.value(first + lpg * i));
     }
 #pragma unroll 1
     for (int r = from; r < k; ++r) {
         uint64_t best = 0;
-        int at = 0;
+        int at = -1;
 #pragma unroll 1
         for (uint32_t m = cand; m; m &= m - 1) {
             const int i = __builtin_ctz(m);
@@ -166,14 +165,18 @@ DEV void select_64(Exact x, uint64_t *kb, uint32_t live, uint32_t cand, int firs
                 at = i;
             }
         }
-        const uint64_t mine = best;
+        const int mine = at < 0 ? 256 : first + lpg * at;
+        int id = mine;
 #pragma unroll 1
         for (int m = 1; m < L; m <<= 1) {
             const uint64_t o = shfl_xor_u64(best, m);
-            best = o > best ? o : best;
+            const int oid = __shfl_xor(id, m, 64);
+            const bool ahead = o > best || (o == best && oid < id);
+            best = ahead ? o : best;
+            id = ahead ? oid : id;
         }
-        if (mine == best) cand &= ~(1u << at);   // ids differ, so one lane's
-        const uint32_t e = (FIRST_Q << 8) | (uint32_t)(best & 0xff);
+        if (mine == id) cand &= ~(1u << (at & 31));   // ids differ, so one lane's
+        const uint32_t e = (FIRST_Q << 8) | (uint32_t)(255 - id);
 #pragma unroll
         for (int j = 0; j < KP; ++j)
             if (j == r) bk[j] = e;
