@@ -341,14 +341,23 @@ __global__ __launch_bounds__(256) void score_select_kernel(
         lo = fminf(lo, peer_f<m.value>(lo));
         smax = fmaxf(smax, peer_f<m.value>(smax));
     });
-    // Bound of a value's error.  Sigmoid: the exponential's argument rounds to
-    // 1.5 2^-24 of itself, and |z| s (1 - s) < 0.23; an ulp each for exponential
-    // (times s (1 - s) <= 1/4), sum and reciprocal.  Softmax: |x| exp(-|x|) < 0.4
-    // times the same, an ulp each for exponential, sum, reciprocal and product,
-    // relative to the row's largest score.  Then the addition of the balance.
-    // The 24-bit places below add two units each.
+    // Bound of a value's error, in units of 2^-24 (half an ulp) of the row's largest
+    // score S; the hardware's exponential and reciprocal are an ulp off at most.
+    // Sigmoid: the exponential's argument, its constant and rounding, is off by 1.23 |z|
+    // of itself, so the score s by 1.23 |z| (1 - s) s; 2 (1 - s) s by the exponential, s
+    // by the sum, 2 s by the reciprocal.  |z| s is at most 0.28, which is 1.28 S, or,
+    // where all scores are small, S times the |z| of the largest, -ln S at most: 5 +
+    // 1.23 max(1.28, -ln S).
+    // Softmax, x = z - max: 2.23 |x| exp(-|x|) <= 0.82 by the argument, 2 by the
+    // exponential, 1 by the product.  The sum and its reciprocal scale all scores of
+    // the row alike and move a difference of two by 33 S at most: 2.23 times the
+    // mean of |x| under the scores (3.4 for 256 experts), 2 by the exponentials, 20
+    // by the additions, 3 by the reciprocal.  Half of it goes to either side: 20.5.
+    // Then the addition of the balance, and what underflows.  The 24-bit places below
+    // add two units each.
     const float top = fmaxf(fabsf(hi), fabsf(lo));
-    const float err = by_score ? smax * (a.sigmoid ? 0x1.8p-22f : 0x1p-21f) + top * 0x1p-24f : 0.f;
+    const float lost = a.sigmoid ? 8.f - 1.1f * __builtin_amdgcn_logf(fmaxf(smax, 0x1p-126f)) : 21.f;
+    const float err = by_score ? (lost * smax + top) * 0x1p-24f + 0x1p-124f : 0.f;
     const float range = hi - lo;
     const bool fits = range > 1e-30f && range < 1e30f;
     const float unit = fits ? 16777200.0f / range : 0.f;

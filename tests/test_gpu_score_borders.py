@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import score_oracle as S
-from tests.parity import to_np
+from tests.parity import say, to_np
 from tests.test_gpu_score import Case, Run
 
 pytestmark = pytest.mark.gpu
@@ -44,3 +44,42 @@ def test_scores_apart_by_their_last_bits(score, low, high, groups, top_groups, b
     Z, idx = routed(c, *one_hot_rows(T, 256, rows), None, np.full(E, balance, np.float32))
     assert np.array_equal(Z, rows[np.arange(T) % 12])
     assert np.array_equal(idx, S.select(Z, np.full(E, balance, np.float32), c.k, **c.sel))
+
+
+def select_rows(Z, balance, c):
+    """oracle.score_oracle.select for many rows without masks or exact ties."""
+    V = S.ranking_values(Z, balance, c.score, c.groups, c.group_score)
+    T, E = V.shape
+    if c.groups > 1:
+        best = np.sort(V.reshape(T, c.groups, -1), axis=2)
+        gs = best[:, :, -1] + (best[:, :, -2] if c.group_score == "pair" else 0.0)
+        keep = np.argsort(-gs, axis=1, kind="stable")[:, :c.top_groups]
+        kept = np.zeros((T, c.groups), bool)
+        np.put_along_axis(kept, keep, True, axis=1)
+        V = np.where(np.repeat(kept, E // c.groups, axis=1), V, -np.inf)
+    return np.sort(np.argsort(-V, axis=1, kind="stable")[:, :c.k], axis=1)
+
+
+NEAR = [(score, z, width, bal) for score, z, width in
+        (("sigmoid", -8.0, 1e-3), ("sigmoid", -20.0, 1e-3), ("sigmoid", -40.0, 1e-3), ("sigmoid", -60.0, 1e-3),
+         ("sigmoid", -87.0, 1e-3), ("sigmoid", -95.0, 1.0), ("sigmoid", 2.0, 1e-4), ("softmax", 0.0, 1e-4),
+         ("softmax", 0.0, 4.0))
+        for bal in (False, True)]
+
+
+@pytest.mark.parametrize("score,z,width,bal", NEAR)
+def test_close_rows_are_those_of_the_definition(score, z, width, bal):
+    """100000 rows of 64 experts whose logits lie close together around z, in
+    groups ranked by sums of two, without a balance and with one as small as the
+    differences between the scores."""
+    say(f"[gpu] {score} {z} {width} {bal}")
+    T, d, E = 100_000, 256, 64
+    c = Case(T, d, E, 8, score, 8, 4, "pair")
+    rng = np.random.default_rng(7)
+    X = torch.from_numpy(rng.standard_normal((T, d), dtype=np.float32)).bfloat16().float().numpy()
+    W_r = torch.from_numpy(rng.standard_normal((d, E), dtype=np.float32) * np.float32(width / 16)).bfloat16()
+    size = 1.0 / (1.0 + np.exp(-z)) if score == "sigmoid" else 1.0 / E
+    balance = (rng.standard_normal(E) * size * min(width, 0.1)).astype(np.float32) if bal else None
+    Z, idx = routed(c, X, W_r.float().numpy(), np.full(E, z, np.float32), balance)
+    wrong = (idx != select_rows(Z, balance, c)).any(1)
+    assert wrong.sum() == 0
