@@ -278,7 +278,7 @@ __global__ __launch_bounds__(64 * NW) void route_kernel(const uint16_t *__restri
 // tile and route_reduce_kernel adds the S partials in slice order, adds the
 // bias, writes the logits and runs the selection; with S = 1 the block does
 // that itself.
-constexpr int RT = 128;            // tokens per block
+constexpr int RT = ROUTE_TILE;     // tokens per block
 #define LDS_AS __attribute__((address_space(3)))
 
 DEV void r_load_lds16(const uint16_t *src, uint16_t *lds_dst) {
@@ -771,39 +771,25 @@ __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
 
 int route_epad(int E) { return (int)route_padded(E); }
 
-// Padded expert counts from which the split router runs.
-constexpr int ROUTE_SPLIT_MIN = 128;
-
 // Slices of the d axis the split router uses for T tokens (1: no partials);
 // 0 when the shape takes the one-pass router.
 int route_split_slices(long T, int d, int E) {
-    if (route_epad(E) < ROUTE_SPLIT_MIN) return 0;
+    if (route_epad(E) < ROUTE_TILE_MIN) return 0;
     const long ntiles = (T + RT - 1) / RT;
     int S = 1;
     while (S < 8 && ntiles * S < 256 && (d / 64) % (2 * S) == 0) S *= 2;
     return S;
 }
 
-// The same for the logits alone, whose slices are added by the selection that
-// follows: any divisor up to 8, the one whose rounds of the 256 CUs end first.
-static int route_logits_slices(long T, int d, int E) {
-    if (route_epad(E) < ROUTE_SPLIT_MIN) return 0;
-    const long ntiles = (T + RT - 1) / RT;
-    int best = 1;
-    for (int S = 2; S <= 8; ++S)
-        if ((d / 64) % S == 0 && (ntiles * S + 255) / 256 * best < (ntiles * best + 255) / 256 * S) best = S;
-    return best;
-}
-
 int route_partials(long T, int d, int E) {
     const int S = (int)route_slices(T, d, E);
-    const int n = S > 0 ? S : route_logits_slices(T, d, E);
+    const int n = S > 0 ? S : (int)route_tile_slices(T, d, E);
     return n > 1 ? n : 0;
 }
 
 size_t route_part_bytes(long T, int d, int E) {
     const int S = route_split_slices(T, d, E);
-    const size_t logits = std::max(route_logits_slices(T, d, E) > 1 ? (size_t)8 * (size_t)T : 0,
+    const size_t logits = std::max(route_tile_slices(T, d, E) > 1 ? (size_t)8 * (size_t)T : 0,
                                    (size_t)route_slice_rows(T, d, E));
     return std::max(S > 1 ? (size_t)S * (size_t)T : 0, logits) * (size_t)route_epad(E) * 4;
 }
@@ -834,7 +820,7 @@ hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bia
 #undef ROUTE_DIRECT
         return hipGetLastError();
     }
-    const int S = topk_idx ? route_split_slices(T, d, E) : route_logits_slices(T, d, E);
+    const int S = topk_idx ? route_split_slices(T, d, E) : (int)route_tile_slices(T, d, E);
     if (!topk_idx && S > 0 && E % 8 == 0) {
         if (T == 0) return hipSuccess;
         const dim3 grid((unsigned)(((T + RT - 1) / RT) * S)), block(512);

@@ -249,6 +249,34 @@ inline long route_slice_rows(long T, long d, long E) {
     return std::min(t * route_slice_steps(d, E), 16 * ROUTE_SLICE_BLOCKS);
 }
 
+// Larger batches of more than 64 experts: tiles of 128 tokens, their d axis in
+// slices that divide its chunks of 64.  More slices fill the 256 CUs, or end the last
+// round earlier, and cost a write and a read of their partial logits, which take
+// the time of a chunk per 27 tiles; a tile's first loads and its epilogue take three
+// chunks'.  Up to three rounds of tiles: past them a round is a small part, and the
+// partial logits would be the larger part of a workspace.
+//
+// Router by 1 / 2 / 4 / 8 slices (us): 256 experts, d 512: 9000 tokens 31.5 / 29.7 / 37 /
+// 43, 65536 92 / 114 / 157 / 276; d 1024: 8192 37 / 28 / 31 / 40; d 2048: 16384 54 / 45 / 54
+// / 73; d 7168: 4200 109 / 64 / 45 / 51 (7: 38), 16384 121 / 89 / 99 / 119, 33000 263 / 225 /
+// 221 / 264, 65536 323 / 363 / 402 / 492.  128 experts: d 256: 4200 16.8 / 15.7 / 17.5, 24000
+// 23.8 / 29.8 / 35; d 2048: 16384 32 / 28 / 36 / 47, 20000 34 / 39 / 43 / 53; d 7168: 40000 181 /
+// 164 / 171 / 201.  Over 480 shapes of 96 to 256 experts, d 256 to 7168 and 1100 to 65536
+// tokens at most 14 % off the best count, 1 % on average (by rounds alone 180 and 23 %).
+constexpr long ROUTE_TILE = 128, ROUTE_TILE_SLOTS = 768, ROUTE_TILE_MIN = 128;
+
+inline long route_tile_slices(long T, long d, long E) {    // 0: no tiles for so few experts
+    if (route_padded(E) < ROUTE_TILE_MIN) return 0;
+    const long n = (T + ROUTE_TILE - 1) / ROUTE_TILE, chunks = d / 64;
+    auto cost = [&](long s) {
+        return (n * s + 255) / 256 * (3.0 + (double)(chunks / s)) + (s > 1 ? 0.037 * (double)(n * s) : 0.0);
+    };
+    long best = 1;
+    for (long s = 2; s <= 8 && n * s <= ROUTE_TILE_SLOTS; ++s)
+        if (chunks % s == 0 && cost(s) < cost(best)) best = s;
+    return best;
+}
+
 // The third LDS stage of B in a row product of `rows` rows over `groups` experts
 // (DEEP in gemm.hip) pays while an expert's weights serve few m-tiles and costs
 // a little where they serve many (its loads then hit in L2 either way, and more
