@@ -162,8 +162,8 @@ hipError_t launch_dense_sum(const float *part, const float *part_s, const int *o
                             int R, int d, uint16_t *Y, hipStream_t st);
 
 int route_epad(int E);
-// Scratch of the split router (many experts): fp32 partial logits of its d
-// slices; 0 for shapes on the one-pass router.
+// Scratch of the routers: fp32 partial logits of slices of d, for any batch of up
+// to T tokens.
 size_t route_part_bytes(long T, int d, int E);
 // Slices of the d axis whose partial logits launch_route leaves in `part` when
 // it is not to select (topk_idx null); 0: it writes the logits.

@@ -771,16 +771,6 @@ __global__ __launch_bounds__(64 * rd_waves(EPAD)) void route_direct_kernel(
 
 int route_epad(int E) { return (int)route_padded(E); }
 
-// Slices of the d axis the split router uses for T tokens (1: no partials);
-// 0 when the shape takes the one-pass router.
-int route_split_slices(long T, int d, int E) {
-    if (route_epad(E) < ROUTE_TILE_MIN) return 0;
-    const long ntiles = (T + RT - 1) / RT;
-    int S = 1;
-    while (S < 8 && ntiles * S < 256 && (d / 64) % (2 * S) == 0) S *= 2;
-    return S;
-}
-
 int route_partials(long T, int d, int E) {
     const int S = (int)route_slices(T, d, E);
     const int n = S > 0 ? S : (int)route_tile_slices(T, d, E);
@@ -788,10 +778,7 @@ int route_partials(long T, int d, int E) {
 }
 
 size_t route_part_bytes(long T, int d, int E) {
-    const int S = route_split_slices(T, d, E);
-    const size_t logits = std::max(route_tile_slices(T, d, E) > 1 ? (size_t)8 * (size_t)T : 0,
-                                   (size_t)route_slice_rows(T, d, E));
-    return std::max(S > 1 ? (size_t)S * (size_t)T : 0, logits) * (size_t)route_epad(E) * 4;
+    return (size_t)route_part_rows(T, d, E) * (size_t)route_epad(E) * 4;
 }
 
 hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bias, float *logits,
@@ -820,7 +807,7 @@ hipError_t launch_route(const uint16_t *X, const uint16_t *W_r, const float *bia
 #undef ROUTE_DIRECT
         return hipGetLastError();
     }
-    const int S = topk_idx ? route_split_slices(T, d, E) : (int)route_tile_slices(T, d, E);
+    const int S = (int)(topk_idx ? route_split_slices(T, d, E) : route_tile_slices(T, d, E));
     if (!topk_idx && S > 0 && E % 8 == 0) {
         if (T == 0) return hipSuccess;
         const dim3 grid((unsigned)(((T + RT - 1) / RT) * S)), block(512);

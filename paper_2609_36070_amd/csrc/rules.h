@@ -265,16 +265,53 @@ inline long route_slice_rows(long T, long d, long E) {
 // tokens at most 14 % off the best count, 1 % on average (by rounds alone 180 and 23 %).
 constexpr long ROUTE_TILE = 128, ROUTE_TILE_SLOTS = 768, ROUTE_TILE_MIN = 128;
 
-inline long route_tile_slices(long T, long d, long E) {    // 0: no tiles for so few experts
-    if (route_padded(E) < ROUTE_TILE_MIN) return 0;
-    const long n = (T + ROUTE_TILE - 1) / ROUTE_TILE, chunks = d / 64;
-    auto cost = [&](long s) {
-        return (n * s + 255) / 256 * (3.0 + (double)(chunks / s)) + (s > 1 ? 0.037 * (double)(n * s) : 0.0);
-    };
-    long best = 1;
-    for (long s = 2; s <= 8 && n * s <= ROUTE_TILE_SLOTS; ++s)
-        if (chunks % s == 0 && cost(s) < cost(best)) best = s;
-    return best;
+// The slices for n tiles of d.
+struct RouteTiles {
+    double round[9];         // a round's time in chunks, by slices; 0: they do not divide
+    explicit RouteTiles(long d) {
+        const long chunks = d / 64;
+        for (long s = 1; s <= 8; ++s) round[s] = chunks % s ? 0.0 : 3.0 + (double)(chunks / s);
+    }
+    long slices(long n) const {
+        long best = 1;
+        double least = (double)((n + 255) / 256) * round[1];
+        for (long s = 2; s <= 8 && n * s <= ROUTE_TILE_SLOTS; ++s) {
+            if (round[s] == 0.0) continue;
+            const double c = (double)((n * s + 255) / 256) * round[s] + 0.037 * (double)(n * s);
+            if (c < least) {
+                least = c;
+                best = s;
+            }
+        }
+        return best;
+    }
+    // moe_route's, which selects in a launch of its own for partial logits alone:
+    // doubled until the tiles fill the CUs
+    long split_slices(long n) const {
+        long s = 1;
+        while (s < 8 && n * s < 256 && round[2 * s] != 0.0) s *= 2;
+        return s;
+    }
+};
+inline long route_tiles(long T) { return (T + ROUTE_TILE - 1) / ROUTE_TILE; }
+// 0: no tiles for so few experts
+inline long route_tile_slices(long T, long d, long E) {
+    return route_padded(E) < ROUTE_TILE_MIN ? 0 : RouteTiles(d).slices(route_tiles(T));
+}
+inline long route_split_slices(long T, long d, long E) {
+    return route_padded(E) < ROUTE_TILE_MIN ? 0 : RouteTiles(d).split_slices(route_tiles(T));
+}
+// Rows of partial logits of any batch of up to T tokens, for either router.
+inline long route_part_rows(long T, long d, long E) {
+    long rows = route_slice_rows(T, d, E);
+    if (route_padded(E) < ROUTE_TILE_MIN) return rows;
+    const RouteTiles r(d);
+    // no slices past SLOTS / 2 tiles, and no more than 8 of fewer
+    for (long n = std::min(route_tiles(T), ROUTE_TILE_SLOTS / 2); n > 0 && 8 * ROUTE_TILE * n > rows; --n) {
+        const long s = std::max(r.slices(n), r.split_slices(n));
+        if (s > 1) rows = std::max(rows, s * std::min(ROUTE_TILE * n, T));
+    }
+    return rows;
 }
 
 // The third LDS stage of B in a row product of `rows` rows over `groups` experts
