@@ -215,11 +215,11 @@ __global__ __launch_bounds__(256) void score_select_kernel(
             }
         }
     } else {
-        // pieces of 4 logits, two at a time; NB slices of each in flight
+        // pieces of 4 logits, NH at a time; up to NG groups of GS slices of each in flight
         const int ch = epad / 4, pieces = nt * ch;
         const long pitch = (long)T * epad;
-        auto add = [&](auto nb, auto nh, int i0) {
-            constexpr int NB = decltype(nb)::value, NH = decltype(nh)::value;
+        auto add = [&](auto gs, auto ng, auto nh, int i0) {
+            constexpr int GS = decltype(gs)::value, NG = decltype(ng)::value, NH = decltype(nh)::value;
             const float *p[NH];
             f32x4_t v[NH], bz[NH];
 #pragma unroll
@@ -231,20 +231,30 @@ __global__ __launch_bounds__(256) void score_select_kernel(
 #pragma unroll
                     for (int q = 0; q < 4; ++q) bz[h][q] = bias[min(4 * (i % ch) + q, E - 1)];
             }
-            for (int s = 0; s < S; s += NB) {
-                f32x4_t u[NH][NB];
+            for (int s0 = 0; s0 < S; s0 += GS * NG) {
+                f32x4_t u[NG][NH][GS];
 #pragma unroll
-                for (int h = 0; h < NH; ++h)
+                for (int g = 0; g < NG; ++g) {
+                    const int s = s0 + GS * g;
+                    if (s >= S) break;
 #pragma unroll
-                    for (int j = 0; j < NB; ++j)
-                        u[h][j] = *reinterpret_cast<const f32x4_t *>(p[h] + min(s + j, S - 1) * pitch);
+                    for (int h = 0; h < NH; ++h)
 #pragma unroll
-                for (int h = 0; h < NH; ++h)
+                        for (int j = 0; j < GS; ++j)
+                            u[g][h][j] = *reinterpret_cast<const f32x4_t *>(p[h] + min(s + j, S - 1) * pitch);
+                }
 #pragma unroll
-                    for (int j = 0; j < NB; ++j)
-                        if (s + j < S)
+                for (int g = 0; g < NG; ++g) {
+                    const int s = s0 + GS * g;
+                    if (s >= S) break;
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) v[h][q] = v[h][q] + u[h][j][q];
+                    for (int h = 0; h < NH; ++h)
+#pragma unroll
+                        for (int j = 0; j < GS; ++j)
+                            if (s + j < S)
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) v[h][q] = v[h][q] + u[g][h][j][q];
+                }
             }
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
@@ -255,15 +265,16 @@ __global__ __launch_bounds__(256) void score_select_kernel(
                     if (c + q < E) zs[i / ch * E + c + q] = bias ? v[h][q] + bz[h][q] : v[h][q];
             }
         };
-        // few tokens: all slices in one round trip (1 token to 256 experts, 28
-        // slices: the router 13.0 -> 11.9 us)
-        if (pieces <= 256 && S > 14 && S <= 28) {
-            if ((int)threadIdx.x < pieces) add(Int<28>{}, Int<1>{}, threadIdx.x);
+        // 32 loads in flight per thread, whatever S, and at most three past the last
+        // slice (router of 256 experts, us by slices: one token, 8 9.7, 16 10.0, 28 10.5,
+        // 32 10.7, 64 12.2; 16 tokens, two pieces per thread, 8 12.0, 16 12.8, 28 14.3, 32
+        // 14.8, 64 18.4)
+        if (pieces <= 256) {
+            if ((int)threadIdx.x < pieces) add(Int<4>{}, Int<8>{}, Int<1>{}, threadIdx.x);
         } else {
             for (int i = threadIdx.x; i < pieces; i += 512) {
-                if (S <= 2) add(Int<2>{}, Int<2>{}, i);
-                else if (S <= 8) add(Int<8>{}, Int<2>{}, i);
-                else add(Int<14>{}, Int<2>{}, i);
+                if (S <= 2) add(Int<2>{}, Int<1>{}, Int<2>{}, i);
+                else add(Int<4>{}, Int<4>{}, Int<2>{}, i);
             }
         }
     }
