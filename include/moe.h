@@ -606,10 +606,11 @@ size_t moe_int_workspace_bytes(const moe_shape *shape);
  *     with exact 32-bit integer sums, scaled by (token scale) * (channel scale);
  *   - H = silu(A) * B is quantised per route (per token in the shared expert)
  *     from fp32, and the down products run likewise;
- *   - each expert's output is rounded to bf16 before the weighted sum, except
- *     for one token (with d <= 8192, and f and f_shared that its kernel's LDS
- *     holds): its experts are taken from topk_idx instead of the plan, and
- *     their outputs are summed in fp32 and rounded once.
+ *   - the experts' outputs are summed in fp32 and rounded once in small batches
+ *     (few rows per expert, whose weights are streamed), and rounded to bf16
+ *     before the weighted sum, as in moe_forward, in large ones;
+ *   - one token (with d <= 8192, and f and f_shared that its kernel's LDS holds)
+ *     takes its experts from topk_idx instead of the plan.
  * With dense routing (k == E) each token's ids are 0 .. E-1; otherwise a route
  * with an id outside [0, E) is left out, and an id that a token lists twice
  * counts twice.  Results do not depend on what ran before and repeat bit for

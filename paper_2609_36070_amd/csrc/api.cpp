@@ -372,11 +372,14 @@ I8Layout i8_layout(const moe_shape &s) {
     L.h = take(R * f * 4);
     L.hq = take(R * f);
     L.hs = take(R * 4);
-    L.Yexp = take(R * d * 2);
+    // outputs of the experts: fp32 in the batches that stream their weights
+    const size_t Ts = std::min((long)T, skinny_i8_max_tokens((long)s.E, (long)s.k));
+    const size_t y = d * std::max(2 * T, 4 * Ts);
+    L.Yexp = take(y * s.k);
     L.hsh = take(T * fs * 4);
     L.hshq = take(T * fs);
     L.hshs = take(fs ? T * 4 : 0);
-    L.Ysh = take(fs ? T * d * 2 : 0);
+    L.Ysh = take(fs ? y : 0);
     L.total = o;
     return L;
 }
@@ -1866,20 +1869,20 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
         return p;
     };
     auto down_product = [&](const uint8_t *a, const float *as, const int8_t *w, const float *wsc, int n,
-                            int rows, int K, uint16_t *C) {
+                            int rows, int K, size_t out) {
         I8Product p;
         p.A = a; p.As = as; p.a_nrows = rows > 0 ? rows : 1; p.a_bytes = (uint32_t)((long)p.a_nrows * K);
         p.B = bytes(w); p.Bs = wsc; p.b_bytes = (uint32_t)((long)n * K * d);
-        p.rows = rows; p.K = K; p.N = d; p.C = C;
+        p.rows = rows; p.K = K; p.N = d; p.C = at<uint16_t>(ws, out); p.Cf = at<float>(ws, out);
         return p;
     };
     const moe_int_weights &w = *weights;
     I8GemmArgs down = up;
     up.routed = up_product(w.Wg_q, w.Wg_s, w.Wu_q, w.Wu_s, E, R, f, at<float>(ws, Q.h));
-    down.routed = down_product(hq, hs, w.Wd_q, w.Wd_s, E, R, f, at<uint16_t>(ws, Q.Yexp));
+    down.routed = down_product(hq, hs, w.Wd_q, w.Wd_s, E, R, f, Q.Yexp);
     if (fs > 0) {
         up.shared = up_product(w.Sg_q, w.Sg_s, w.Su_q, w.Su_s, 1, T, fs, at<float>(ws, Q.hsh));
-        down.shared = down_product(hshq, hshs, w.Sd_q, w.Sd_s, 1, T, fs, at<uint16_t>(ws, Q.Ysh));
+        down.shared = down_product(hshq, hshs, w.Sd_q, w.Sd_s, 1, T, fs, Q.Ysh);
     }
 
     I8SkinnyArgs small;
@@ -1914,8 +1917,12 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
     MOE_TRY(tt ? launch_skinny_i8_down(small, tt, s) : launch_gemm_i8_down(down, s));
     MOE_TRY(mk.mark(4));
     MOE_TRY(mk.mark(5));
-    MOE_TRY(launch_combine(at<uint16_t>(ws, Q.Yexp), fs > 0 ? at<uint16_t>(ws, Q.Ysh) : nullptr, topk_w,
-                           plan->route_pos, T, d, k, Y, s));
+    if (tt)
+        MOE_TRY(launch_combine_f32(at<float>(ws, Q.Yexp), fs > 0 ? at<float>(ws, Q.Ysh) : nullptr, topk_w,
+                                   plan->route_pos, T, d, k, Y, s));
+    else
+        MOE_TRY(launch_combine(at<uint16_t>(ws, Q.Yexp), fs > 0 ? at<uint16_t>(ws, Q.Ysh) : nullptr, topk_w,
+                               plan->route_pos, T, d, k, Y, s));
     MOE_TRY(mk.mark(6));
     return MOE_OK;
 }

@@ -280,7 +280,8 @@ struct I8Product {
     uint32_t a_bytes = 0, b_bytes = 0; // operand extents (< 4 GiB)
     float *H = nullptr;                // up product: silu(gate) * up, fp32 [rows][N]
     const float *Hin = nullptr;        // down product of one token, which quantises it: [rows][K]
-    uint16_t *C = nullptr;             // down product: bf16 [rows][N]
+    uint16_t *C = nullptr;             // down product of tiles: bf16 [rows][N]
+    float *Cf = nullptr;               // down product of small batches: fp32 [rows][N], in its place
 };
 struct I8GemmArgs {
     I8Product routed, shared;          // shared.N = 0: no shared expert
@@ -326,6 +327,8 @@ hipError_t launch_prep(const int *perm, const int *offsets, int E, const float *
 constexpr int ZERO_PAGE_ELEMS = 512;  // bf16 elements of the zero page (1 KB)
 hipError_t launch_combine(const uint16_t *Yexp, const uint16_t *Ysh, const float *topk_w,
                           const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st);
+hipError_t launch_combine_f32(const float *Yexp, const float *Ysh, const float *topk_w,
+                              const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st);
 hipError_t launch_softmax_bwd(const float *dgpart, int nparts, const int *route_pos,
                               const float *topk_w, const int *topk_idx, int T, int k, int E,
                               float *dg_out, float *dZ, hipStream_t st);

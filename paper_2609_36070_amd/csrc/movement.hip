@@ -59,14 +59,30 @@ __global__ __launch_bounds__(256) void prep_kernel(const int *__restrict__ perm,
     wperm[p] = wv;
 }
 
+// 16 bytes of a row: 8 bf16 values or 4 fp32 ones
+DEV void unpack16(const u32x4_t &v, float (&x)[8]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        x[2 * q] = bf_lo(v[q]);
+        x[2 * q + 1] = bf_hi(v[q]);
+    }
+}
+DEV void unpack16(const u32x4_t &v, float (&x)[4]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = __uint_as_float(v[q]);
+}
+
 // Y[t] = Ysh[t] + sum_slot w[t,slot] * Yexp[route_pos[t*k+slot]]  (fp32, one rounding)
-__global__ __launch_bounds__(256) void combine_kernel(const uint16_t *__restrict__ Yexp,
-                                                      const uint16_t *__restrict__ Ysh,
+// S: uint16_t (bf16 rows) or float.
+template <typename S>
+__global__ __launch_bounds__(256) void combine_kernel(const S *__restrict__ Yexp,
+                                                      const S *__restrict__ Ysh,
                                                       const float *__restrict__ topk_w,
                                                       const int *__restrict__ route_pos, int T,
                                                       int d, int k, int R,
                                                       uint16_t *__restrict__ Y) {
-    const int nc = d / 8;
+    constexpr int V = 16 / sizeof(S);
+    const int nc = d / V;
     for (int t = blockIdx.x; t < T; t += gridDim.x) {
         int pos[16];
         float wt[16];
@@ -86,34 +102,29 @@ __global__ __launch_bounds__(256) void combine_kernel(const uint16_t *__restrict
             u32x4_t rows[16];
 #pragma unroll
             for (int s = 0; s < 16; ++s)
-                if (s < k) rows[s] = ld_u32x4(Yexp + (long)max(pos[s], 0) * d + 8 * c);
-            float acc[8];
+                if (s < k) rows[s] = ld_u32x4(Yexp + (long)max(pos[s], 0) * d + V * c);
+            float acc[V];
             if (Ysh) {
-                const u32x4_t v = ld_u32x4(Ysh + (long)t * d + 8 * c);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    acc[2 * q] = bf_lo(v[q]);
-                    acc[2 * q + 1] = bf_hi(v[q]);
-                }
+                unpack16(ld_u32x4(Ysh + (long)t * d + V * c), acc);
             } else {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) acc[q] = 0.f;
+                for (int q = 0; q < V; ++q) acc[q] = 0.f;
             }
 #pragma unroll
             for (int s = 0; s < 16; ++s) {
                 if (s < k && pos[s] >= 0) {
-                    const u32x4_t v = rows[s];
+                    float x[V];
+                    unpack16(rows[s], x);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        acc[2 * q] = acc[2 * q] + wt[s] * bf_lo(v[q]);
-                        acc[2 * q + 1] = acc[2 * q + 1] + wt[s] * bf_hi(v[q]);
-                    }
+                    for (int q = 0; q < V; ++q) acc[q] = acc[q] + wt[s] * x[q];
                 }
             }
-            u32x4_t o;
+            uint32_t o[V / 2];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = pack_bf2(acc[2 * q], acc[2 * q + 1]);
-            st_u32x4(Y + (long)t * d + 8 * c, o);
+            for (int q = 0; q < V / 2; ++q) o[q] = pack_bf2(acc[2 * q], acc[2 * q + 1]);
+            uint16_t *const y = Y + (long)t * d + V * c;
+            if constexpr (V == 8) st_u32x4(y, u32x4_t{o[0], o[1], o[2], o[3]});
+            else *reinterpret_cast<u32x2_t *>(y) = u32x2_t{o[0], o[1]};
         }
     }
 }
@@ -679,14 +690,24 @@ hipError_t launch_prep(const int *perm, const int *offsets, int E, const float *
     return hipGetLastError();
 }
 
+template <typename S>
+static hipError_t combine_rows(const S *Yexp, const S *Ysh, const float *topk_w, const int *route_pos,
+                               int T, int d, int k, uint16_t *Y, hipStream_t st) {
+    if (T == 0) return hipSuccess;
+    // few tokens: a block per 256 pieces of a row (61 tokens, 9 rows of 7168 bf16 each: 1 us less)
+    constexpr int BC = 256 * (16 / (int)sizeof(S));
+    const unsigned cols = T <= 256 ? (unsigned)((d + BC - 1) / BC) : 1;
+    combine_kernel<S><<<dim3(rows_grid(T), cols), dim3(256), 0, st>>>(Yexp, Ysh, topk_w, route_pos, T, d, k,
+                                                                 T * k, Y);
+    return hipGetLastError();
+}
 hipError_t launch_combine(const uint16_t *Yexp, const uint16_t *Ysh, const float *topk_w,
                           const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st) {
-    if (T == 0) return hipSuccess;
-    // few tokens: a block per 2048 columns of one (61 tokens, 9 rows of 7168 each: 1 us less)
-    const unsigned cols = T <= 256 ? (unsigned)((d + 2047) / 2048) : 1;
-    combine_kernel<<<dim3(rows_grid(T), cols), dim3(256), 0, st>>>(Yexp, Ysh, topk_w, route_pos, T, d, k,
-                                                              T * k, Y);
-    return hipGetLastError();
+    return combine_rows(Yexp, Ysh, topk_w, route_pos, T, d, k, Y, st);
+}
+hipError_t launch_combine_f32(const float *Yexp, const float *Ysh, const float *topk_w,
+                              const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st) {
+    return combine_rows(Yexp, Ysh, topk_w, route_pos, T, d, k, Y, st);
 }
 
 hipError_t launch_softmax_bwd(const float *dgpart, int nparts, const int *route_pos,

@@ -113,6 +113,9 @@ inline int skinny_i8_tiles(long T, long k, long E, long f, long fs) {
     return T > 0 && T * k <= rows * E && T * fs <= rows * E * f ? 4 : 0;
 }
 
+// Tokens past which skinny_i8_tiles is 0 for every f and fs.
+inline long skinny_i8_max_tokens(long E, long k) { return std::max((k == E ? 192L : 96L) * E / k, 16L); }
+
 // Waves of a streaming workgroup, 8 columns of f (up product) or 16 of d each.
 // Four, unless
 // - dense routing: the columns of all experts are dealt in any parts, and a CU's
