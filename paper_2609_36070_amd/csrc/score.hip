@@ -218,18 +218,22 @@ __global__ __launch_bounds__(256) void score_select_kernel(
         // pieces of 4 logits, NH at a time; up to NG groups of GS slices of each in flight
         const int ch = epad / 4, pieces = nt * ch;
         const long pitch = (long)T * epad;
+        // 256 is a multiple of ch: a thread's pieces are of the same columns
+        const int c = 4 * (threadIdx.x % ch);
+        float bz[4] = {0.f, 0.f, 0.f, 0.f};
+        if (bias)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) bz[q] = bias[min(c + q, E - 1)];
         auto add = [&](auto gs, auto ng, auto nh, int i0) {
             constexpr int GS = decltype(gs)::value, NG = decltype(ng)::value, NH = decltype(nh)::value;
-            const float *p[NH];
-            f32x4_t v[NH], bz[NH];
+            // a piece's place after its slice's first, which is the same for every lane
+            uint32_t at[NH];
+            f32x4_t v[NH];
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
                 const int i = min(i0 + 256 * h, pieces - 1);
-                p[h] = part + (t0 + i / ch) * epad + 4 * (i % ch);
+                at[h] = 4 * (uint32_t)i;
                 v[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-                if (bias)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) bz[h][q] = bias[min(4 * (i % ch) + q, E - 1)];
             }
             for (int s0 = 0; s0 < S; s0 += GS * NG) {
                 f32x4_t u[NG][NH][GS];
@@ -241,7 +245,8 @@ __global__ __launch_bounds__(256) void score_select_kernel(
                     for (int h = 0; h < NH; ++h)
 #pragma unroll
                         for (int j = 0; j < GS; ++j)
-                            u[g][h][j] = *reinterpret_cast<const f32x4_t *>(p[h] + min(s + j, S - 1) * pitch);
+                            u[g][h][j] = *reinterpret_cast<const f32x4_t *>(
+                                part + t0 * epad + min(s + j, S - 1) * pitch + at[h]);
                 }
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
@@ -258,23 +263,24 @@ __global__ __launch_bounds__(256) void score_select_kernel(
             }
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
-                const int i = i0 + 256 * h, c = 4 * (i % ch);
+                const int i = i0 + 256 * h;
                 if (i >= pieces) break;
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    if (c + q < E) zs[i / ch * E + c + q] = bias ? v[h][q] + bz[h][q] : v[h][q];
+                    if (c + q < E) zs[i / ch * E + c + q] = bias ? v[h][q] + bz[q] : v[h][q];
             }
         };
-        // 32 loads in flight per thread, whatever S, and at most three past the last
-        // slice (router of 256 experts, us by slices: one token, 8 9.7, 16 10.0, 28 10.5,
-        // 32 10.7, 64 12.2; 16 tokens, two pieces per thread, 8 12.0, 16 12.8, 28 14.3, 32
-        // 14.8, 64 18.4)
+        // 28 or 16 loads in flight per thread, whatever S, and at most three past the last
+        // slice (router of 256 experts, us by slices: one token, 8 10.0, 16 10.3, 28 10.7,
+        // 32 11.0, 64 12.6; 16 tokens, two pieces per thread, 8 12.0, 16 13.0, 28 14.5, 32
+        // 14.9, 64 18.8).  32 of them took more than 128 registers, which leaves a SIMD
+        // two waves: 4099 tokens 37.4 -> 39.6, 16384 to 128 experts 27.7 -> 31.3.
         if (pieces <= 256) {
-            if ((int)threadIdx.x < pieces) add(Int<4>{}, Int<8>{}, Int<1>{}, threadIdx.x);
+            if ((int)threadIdx.x < pieces) add(Int<4>{}, Int<7>{}, Int<1>{}, threadIdx.x);
         } else {
             for (int i = threadIdx.x; i < pieces; i += 512) {
                 if (S <= 2) add(Int<2>{}, Int<1>{}, Int<2>{}, i);
-                else add(Int<4>{}, Int<4>{}, Int<2>{}, i);
+                else add(Int<4>{}, Int<2>{}, Int<2>{}, i);
             }
         }
     }
