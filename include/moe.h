@@ -606,9 +606,12 @@ size_t moe_int_workspace_bytes(const moe_shape *shape);
  *     with exact 32-bit integer sums, scaled by (token scale) * (channel scale);
  *   - H = silu(A) * B is quantised per route (per token in the shared expert)
  *     from fp32, and the down products run likewise;
- *   - the experts' outputs are summed in fp32 and rounded once in small batches
- *     (few rows per expert, whose weights are streamed), and rounded to bf16
- *     before the weighted sum, as in moe_forward, in large ones;
+ *   - the experts' outputs are summed in fp32; before that they are rounded to
+ *     fp16 in large batches (small ones stream the weights of few rows per
+ *     expert), their row's scale apart and the rest scaled by a power of two per
+ *     expert that keeps it in range: half a step is 2^-11 of an output, and for
+ *     outputs near 0 at most 2^-8 of one unit of the integer sum in the expert's
+ *     channel of the largest scale;
  *   - one token (with d <= 8192, and f and f_shared that its kernel's LDS holds)
  *     takes its experts from topk_idx instead of the plan.
  * With dense routing (k == E) each token's ids are 0 .. E-1; otherwise a route

@@ -359,7 +359,7 @@ moe_status check_i8_weights(const moe_shape *s, const moe_int_weights *w) {
 
 // Workspace of the int8 forward: the prefix of every layout, then its own.
 struct I8Layout {
-    size_t xq, xs, h, hq, hs, Yexp, hsh, hshq, hshs, Ysh, total;
+    size_t xq, xs, h, hq, hs, Yexp, hsh, hshq, hshs, Ysh, unit, total;
 };
 
 I8Layout i8_layout(const moe_shape &s) {
@@ -380,6 +380,7 @@ I8Layout i8_layout(const moe_shape &s) {
     L.hshq = take(T * fs);
     L.hshs = take(fs ? T * 4 : 0);
     L.Ysh = take(fs ? y : 0);
+    L.unit = take(2 * ((size_t)s.E + 1) * 4);
     L.total = o;
     return L;
 }
@@ -1859,6 +1860,7 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
 
     I8GemmArgs up;
     up.offsets = plan->offsets; up.rowidx = at<int>(ws, L.rowidx); up.E = E;
+    up.unit = at<float>(ws, Q.unit);
     auto up_product = [&](const int8_t *g, const float *gs, const int8_t *u, const float *us, int n, int rows,
                           int N, float *H) {
         I8Product p;
@@ -1903,15 +1905,18 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
         return MOE_OK;
     }
     const int tt = skinny_i8_tiles(T, k, E, f, fs);
+    I8Factors factors;                       // tile products: hs holds the routes' weights by slot
+    if (!tt) factors = I8Factors{plan->perm, plan->offsets, topk_idx, topk_w, up.unit, hs, E};
     if (tt)
         MOE_TRY(launch_i8_quant_tokens(X, T, d, xq, xs, s));
     else
-        MOE_TRY(launch_i8_prologue(X, T, d, xq, xs, plan->perm, plan->offsets, E, k, at<int>(ws, L.rowidx),
-                                   s));
+        MOE_TRY(launch_i8_prologue(X, T, d, xq, xs, plan->perm, plan->offsets, k, at<int>(ws, L.rowidx),
+                                   I8Units{w.Wd_s, w.Sd_s, f, fs, E, at<float>(ws, Q.unit)}, s));
     MOE_TRY(mk.mark(1));
     MOE_TRY(tt ? launch_skinny_i8_up(small, tt, s) : launch_gemm_i8_up(up, s));
     MOE_TRY(mk.mark(2));
-    MOE_TRY(launch_i8_quant_h(up.routed.H, R, f, hq, hs, up.shared.H, fs > 0 ? T : 0, fs, hshq, hshs, s));
+    MOE_TRY(launch_i8_quant_h(up.routed.H, R, f, hq, hs, up.shared.H, fs > 0 ? T : 0, fs, hshq, hshs,
+                              factors, s));
     MOE_TRY(mk.mark(3));
     small.routed = down.routed; small.shared = down.shared;
     MOE_TRY(tt ? launch_skinny_i8_down(small, tt, s) : launch_gemm_i8_down(down, s));
@@ -1921,8 +1926,8 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
         MOE_TRY(launch_combine_f32(at<float>(ws, Q.Yexp), fs > 0 ? at<float>(ws, Q.Ysh) : nullptr, topk_w,
                                    plan->route_pos, T, d, k, Y, s));
     else
-        MOE_TRY(launch_combine(at<uint16_t>(ws, Q.Yexp), fs > 0 ? at<uint16_t>(ws, Q.Ysh) : nullptr, topk_w,
-                               plan->route_pos, T, d, k, Y, s));
+        MOE_TRY(launch_combine_f16(at<uint16_t>(ws, Q.Yexp), fs > 0 ? at<uint16_t>(ws, Q.Ysh) : nullptr, hs,
+                                   hshs, plan->route_pos, T, d, k, Y, s));
     MOE_TRY(mk.mark(6));
     return MOE_OK;
 }

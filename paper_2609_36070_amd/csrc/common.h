@@ -44,6 +44,9 @@ DEV float sigmoid_f(float a) {
 DEV float silu_f(float a) { return a * sigmoid_f(a); }
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+template <typename T> inline constexpr bool is_half = false;
+template <> inline constexpr bool is_half<_Float16> = true;
 
 DEV int wave_lane() { return threadIdx.x & 63; }
 

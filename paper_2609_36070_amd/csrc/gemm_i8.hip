@@ -4,7 +4,14 @@
 //
 //   I8_UP    g = sx sg[n] (Xq[tok(p)] . Wg_q[e][n]), u likewise;
 //            H = silu(g) u in fp32, for the row quantiser
-//   I8_DOWN  Yexp = sh sd[n] (Hq[p] . Wd_q[e][n]) -> bf16
+//   I8_DOWN  Yexp = sd[n] (Hq[p] . Wd_q[e][n]) / u[e] -> fp16
+//
+// The route's weight in the sum over a token's experts holds the rest, the row's
+// scale times u[e], a power of two that fits the expert's largest possible value to
+// fp16: half a step is 2^-11 of a value, an eighth of bf16's, and for the smallest
+// values at most 2^-8 of one unit of the integer sum in the expert's largest channel
+// (K 768: 2^-15).  (bf16, as in moe_forward, was off by 1.4 times as much as one
+// rounding of Y.)
 //
 // Every operand is a matrix of K-contiguous byte rows with one fp32 scale per
 // row.  The dot products are exact in 32-bit integers (K <= 131072: 127^2 K
@@ -189,11 +196,16 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
     // thread tid's scale of a tile: row tid, or column tid - BM
     static_assert(NTHREADS == BM + BN && BM % 64 == 0, "a scale per thread, rows and columns in waves of their own");
     // (gate and up channels alternate by 32 lanes: a wave of columns reads both arrays)
-    auto scale_at = [&](const I8Tile &t, const Loads &l) {
+    // (down product: its columns' alone, with the expert's unit)
+    struct Scale {
+        float s, unit;
+    };
+    auto scale_of = [&](const I8Tile &t, const Loads &l) {
         const I8Product &g = t.sh ? args.shared : args.routed;
         const int c = (tid - BM) & (BN - 1);
-        return tid < BM ? g.As + l.scale
+        const float *at = MODE == I8_UP && tid < BM ? g.As + l.scale
                         : ((MODE == I8_UP) && (c & 32) ? g.Bs2 : g.Bs) + ((long)t.e * g.N + b_col(t, c));
+        return Scale{*at, MODE == I8_UP ? 1.f : args.unit[2 * (t.sh ? args.E : t.e)]};
     };
 
     I8Tile t, nt;
@@ -203,7 +215,7 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
     ask_loads(t, ld);
     set_loads(t, ld);
     nld = ld;
-    float scale = *scale_at(t, ld);
+    Scale scale = scale_of(t, ld);
     issue_b(t, 0, lds_b0);
     issue_a(t, ld, 0, lds_a0);
     issue_a(t, ld, 1, lds_a1);               // K is a multiple of 256: steps come in pairs
@@ -213,7 +225,7 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
     const int lrow = lane & 31, lhalf = lane >> 5;
     float *const scr = epi + 2 * (BM + BN) + wave * 8 * SP;
     for (int parity = 0;; parity ^= 1) {
-        epi[parity * (BM + BN) + tid] = scale;
+        epi[parity * (BM + BN) + tid] = scale.s * scale.unit;
         i32x16_t acc[TM][TN];
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -265,7 +277,7 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
         auto set_next = [&] {
             if (more) {
                 set_loads(nt, nld);
-                scale = *scale_at(nt, nld);
+                scale = scale_of(nt, nld);
             }
         };
         // the second step of a pair, and the loads of the step after it
@@ -350,7 +362,7 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
                     }
                 }
         } else {
-            // To bf16: these outputs are the largest arrays of a large batch, and fp32
+            // 16 bits: these outputs are the largest arrays of a large batch, and fp32
             // for them took 1000 tokens to 32 experts from 246 to 262 us, 8192 to 128 535 ->
             // 652, 4099 dense 1703 -> 1895, 16384 2808 -> 3247.  (Small batches hold fp32:
             // skinny_i8.hip.)
@@ -372,11 +384,8 @@ __global__ __launch_bounds__(NTHREADS, 1) void gemm_i8_kernel(I8GemmArgs args) {
                         for (int q = 0; q < 4; ++q)
                             scr[(4 * lhalf + q) * SP + 32 * j + lrow] = (float)acc[i][j][4 * qg + q] * sb[j];
                     const int rl = wm * WM + 32 * i + 8 * qg + er;
-                    const float sr = sc[rl];
-                    f32x8 v = ld_f32x8(scr + er * SP + 8 * ec);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = sr * v[k];
-                    store_b128(pack_bf8(v), out, bytes, (uint32_t)(rl * g.N + n0 + wn * WN + 8 * ec) * 2u);
+                    const f16x8_t v = __builtin_convertvector(ld_f32x8(scr + er * SP + 8 * ec), f16x8_t);
+                    store_b128(__builtin_bit_cast(u32x4_t, v), out, bytes, (uint32_t)(rl * g.N + n0 + wn * WN + 8 * ec) * 2u);
                 }
         }
         // every wave is done with the last step's stage by now

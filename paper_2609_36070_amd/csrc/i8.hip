@@ -48,16 +48,48 @@ struct QuantRows {
     int K;
 };
 
+// Where the scale of a row goes that the quantiser of H wrote for the tile
+// products: into the weight of its route, whose numbers are asked for ahead of and
+// behind the row's values.
+struct RouteFactor {
+    const I8Factors &f;
+    long row;
+    int j = -1, planned = 0;
+    int e = 0;
+    float w = 0.f;
+    DEV void ask() {                         // one thread of the row
+        j = f.perm[row];                     // (past the plan: whatever is there)
+        planned = f.offsets[f.E];
+    }
+    DEV void ask_weight(long rows) {
+        if (row >= planned || j < 0 || j >= rows) j = -1;
+        if (j < 0) return;
+        w = f.topk_w[j];
+        e = f.topk_idx[j];
+    }
+    DEV void put(float s) const {
+        if (j >= 0) f.w[j] = w * (s * f.unit[2 * min(max(e, 0), f.E - 1) + 1]);
+    }
+};
+struct RowScale {                            // the scale as it is, times a factor
+    float *at;
+    const float *unit;
+    DEV void ask() {}
+    DEV void ask_weight(long) {}
+    DEV void put(float s) const { *at = unit ? s * *unit : s; }
+};
+
 // Row `row` by W waves, 8 elements per thread and step.  Rows of up to 512 W NC
 // elements are held in registers between the two passes (NC = 0: read again).
-template <typename S, int NC, int W>
-DEV void quant_row(const QuantRows<S> &m, long row, uint32_t *red) {
+template <typename S, int NC, int W, typename P>
+DEV void quant_row(const QuantRows<S> &m, long row, uint32_t *red, P out) {
     constexpr int TH = 64 * W;
     const S *x = m.X + row * m.K;
     uint8_t *o = m.q + row * m.K;
     const int n8 = m.K / 8, tid = threadIdx.x % TH;
     float v[NC > 0 ? NC : 1][8];
     uint32_t amax = 0;
+    if (tid == 0) out.ask();
     auto put = [&](const float (&y)[8], const I8Scale &s, int c) {
         *reinterpret_cast<u32x2_t *>(o + 8 * c) =
             u32x2_t{pack_i8(s.code(y[0]), s.code(y[1]), s.code(y[2]), s.code(y[3])),
@@ -72,55 +104,92 @@ DEV void quant_row(const QuantRows<S> &m, long row, uint32_t *red) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
         }
+        if (tid == 0) out.ask_weight(m.rows);
 #pragma unroll
         for (int i = 0; i < NC; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) amax = umax(amax, abs_bits(v[i][j]));
         const I8Scale s(row_max<W>(amax, red));
-        if (tid == 0) m.sc[row] = s.s;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = tid + TH * i;
             if (c < n8) put(v[i], s, c);
         }
+        if (tid == 0) out.put(s.s);
     } else {
         for (int c = tid; c < n8; c += TH) {
             load8(x + 8 * c, v[0]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) amax = umax(amax, abs_bits(v[0][j]));
         }
+        if (tid == 0) out.ask_weight(m.rows);
         const I8Scale s(row_max<W>(amax, red));
-        if (tid == 0) m.sc[row] = s.s;
         for (int c = tid; c < n8; c += TH) {
             load8(x + 8 * c, v[0]);
             put(v[0], s, c);
         }
+        if (tid == 0) out.put(s.s);
     }
 }
 
-// Rows of one matrix, then of another, 4 / W per block.
-template <typename S, int NC, int W>
-__global__ __launch_bounds__(256) void i8_quant_rows_kernel(QuantRows<S> m0, QuantRows<S> m1) {
+// Rows of one matrix, then of another, 4 / W per block.  ROUTES: the scales go
+// into factors of the outputs.
+template <typename S, int NC, int W, bool ROUTES>
+__global__ __launch_bounds__(256) void i8_quant_rows_kernel(QuantRows<S> m0, QuantRows<S> m1, I8Factors f) {
     __shared__ uint32_t red[4];
     constexpr int RB = 4 / W;
     const long n0 = (m0.rows + RB - 1) / RB, b = blockIdx.x;
     const bool first = b < n0;
     const long row = RB * (first ? b : b - n0) + threadIdx.x / (64 * W);
-    if (row < (first ? m0.rows : m1.rows)) quant_row<S, NC, W>(first ? m0 : m1, row, red);
+    if (row >= (first ? m0.rows : m1.rows)) return;
+    if constexpr (ROUTES) {
+        if (first) quant_row<S, NC, W>(m0, row, red, RouteFactor{f, row});
+        else quant_row<S, NC, W>(m1, row, red, RowScale{m1.sc + row, f.unit + 2 * f.E + 1});
+    } else {
+        const QuantRows<S> &m = first ? m0 : m1;
+        quant_row<S, NC, W>(m, row, red, RowScale{m.sc + row, nullptr});
+    }
 }
 
-// The tile products' prologue in one launch: the tokens' rows, and the token of
-// every position of the plan (0 where the plan has none), 256 per block.
+// Power of two u for an expert's down products: y / u, y = sd[n] (Hq . Wd_q) with K
+// codes of at most 127 on either side, lies below 2^15 for the largest channel scale.
+DEV float down_unit(uint32_t most, int K) {
+    const int dot = 32 - __builtin_clz(127u * 127u * (uint32_t)K - 1u);   // |Hq . Wd_q| <= 2^dot
+    const int x = dot + ((int)(most >> 23) - 126) - 15;
+    return ldexpf(1.0f, min(max(x, -126), 126));
+}
+
+// The tile products' prologue in one launch: the experts' units, one per block,
+// the tokens' rows, and the token of every position of the plan (0 where the plan
+// has none), 256 per block.
 template <int NC, int W>
 __global__ __launch_bounds__(256) void i8_prologue_kernel(QuantRows<uint16_t> x, const int *__restrict__ perm,
-                                                          const int *__restrict__ offsets, int E, int k, int R,
-                                                          int *__restrict__ rowidx) {
+                                                          const int *__restrict__ offsets, int k, int R,
+                                                          int *__restrict__ rowidx, I8Units un) {
     __shared__ uint32_t red[4];
     constexpr int RB = 4 / W;
-    const long n0 = (x.rows + RB - 1) / RB, b = blockIdx.x;
+    const int E = un.E, units = E + (un.fs > 0 ? 1 : 0);
+    if ((int)blockIdx.x < units) {
+        const int e = (int)blockIdx.x, N = x.K;
+        const float *s = e < E ? un.Wd_s + (long)e * N : un.Sd_s;
+        uint32_t most = 0;                   // (NaN scales aside: their channels are NaN anyway)
+        for (int c = 8 * threadIdx.x; c < N; c += 2048) {
+            float v[8];
+            load8(s + c, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = umax(most, abs_bits(v[j]) < 0x7f800000u ? abs_bits(v[j]) : 0u);
+        }
+        const float u = down_unit(row_max<4>(most, red), e < E ? un.f : un.fs);
+        if (threadIdx.x == 0) {
+            un.unit[2 * e] = 1.0f / u;
+            un.unit[2 * e + 1] = u;
+        }
+        return;
+    }
+    const long n0 = (x.rows + RB - 1) / RB, b = (long)blockIdx.x - units;
     if (b < n0) {
         const long row = RB * b + threadIdx.x / (64 * W);
-        if (row < x.rows) quant_row<uint16_t, NC, W>(x, row, red);
+        if (row < x.rows) quant_row<uint16_t, NC, W>(x, row, red, RowScale{x.sc + row, nullptr});
         return;
     }
     const int p = (int)(b - n0) * 256 + threadIdx.x;
@@ -213,28 +282,35 @@ hipError_t launch_i8_quant_tokens(const uint16_t *X, long rows, int K, uint8_t *
     if (rows <= 0) return hipSuccess;
     const QuantRows<uint16_t> m{X, q, sc, rows, K};
     return with_chunks(rows, K, [&](auto nc, auto w) {
-        i8_quant_rows_kernel<uint16_t, decltype(nc)::value, decltype(w)::value>
-            <<<dim3(row_blocks(rows, w.value)), dim3(256), 0, st>>>(m, QuantRows<uint16_t>{});
+        i8_quant_rows_kernel<uint16_t, decltype(nc)::value, decltype(w)::value, false>
+            <<<dim3(row_blocks(rows, w.value)), dim3(256), 0, st>>>(m, QuantRows<uint16_t>{}, I8Factors{});
     });
 }
 hipError_t launch_i8_prologue(const uint16_t *X, int T, int d, uint8_t *q, float *sc, const int *perm,
-                              const int *offsets, int E, int k, int *rowidx, hipStream_t st) {
+                              const int *offsets, int k, int *rowidx, const I8Units &units,
+                              hipStream_t st) {
     if (T <= 0) return hipSuccess;
     const QuantRows<uint16_t> m{X, q, sc, T, d};
     const int R = T * k;
     return with_chunks(T, d, [&](auto nc, auto w) {
-        const dim3 grid(row_blocks(T, w.value) + (unsigned)((R + 255) / 256));
+        const dim3 grid((unsigned)(units.E + (units.fs > 0)) + row_blocks(T, w.value) + (unsigned)((R + 255) / 256));
         i8_prologue_kernel<decltype(nc)::value, decltype(w)::value><<<grid, dim3(256), 0, st>>>(
-            m, perm, offsets, E, k, R, rowidx);
+            m, perm, offsets, k, R, rowidx, units);
     });
 }
 hipError_t launch_i8_quant_h(const float *H, long rows, int f, uint8_t *q, float *sc, const float *Hs,
-                             long rows_s, int fs, uint8_t *qs, float *scs, hipStream_t st) {
+                             long rows_s, int fs, uint8_t *qs, float *scs, const I8Factors &factors,
+                             hipStream_t st) {
     if (rows + rows_s <= 0) return hipSuccess;
     const QuantRows<float> m{H, q, sc, rows, f}, ms{Hs, qs, scs, rows_s, fs};
     return with_chunks(rows + rows_s, rows_s > 0 && fs > f ? fs : f, [&](auto nc, auto w) {
         const dim3 grid(row_blocks(rows, w.value) + row_blocks(rows_s, w.value));
-        i8_quant_rows_kernel<float, decltype(nc)::value, decltype(w)::value><<<grid, dim3(256), 0, st>>>(m, ms);
+        if (factors.perm)
+            i8_quant_rows_kernel<float, decltype(nc)::value, decltype(w)::value, true>
+                <<<grid, dim3(256), 0, st>>>(m, ms, factors);
+        else
+            i8_quant_rows_kernel<float, decltype(nc)::value, decltype(w)::value, false>
+                <<<grid, dim3(256), 0, st>>>(m, ms, factors);
     });
 }
 hipError_t launch_i8_quant_weights(const uint16_t *W, int E, int K, int N, uint8_t *q, float *sc,

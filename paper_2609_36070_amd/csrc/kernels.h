@@ -280,13 +280,14 @@ struct I8Product {
     uint32_t a_bytes = 0, b_bytes = 0; // operand extents (< 4 GiB)
     float *H = nullptr;                // up product: silu(gate) * up, fp32 [rows][N]
     const float *Hin = nullptr;        // down product of one token, which quantises it: [rows][K]
-    uint16_t *C = nullptr;             // down product of tiles: bf16 [rows][N]
+    uint16_t *C = nullptr;             // down product of tiles: fp16 [rows][N], without As
     float *Cf = nullptr;               // down product of small batches: fp32 [rows][N], in its place
 };
 struct I8GemmArgs {
     I8Product routed, shared;          // shared.N = 0: no shared expert
     const int *offsets = nullptr;      // [E+1] expert regions
     const int *rowidx = nullptr;       // up product: token of each plan row
+    const float *unit = nullptr;       // down product: {1 / u, u} of every expert, then the shared one
     int E = 0;
     int shared_grid = 0, routed_grid = 0;   // set by the launcher: slots of the rasters
 };
@@ -307,13 +308,30 @@ hipError_t launch_token_i8_up(const I8SkinnyArgs &a, hipStream_t st);
 hipError_t launch_token_i8_down(const I8SkinnyArgs &a, const float *topk_w, uint16_t *Y, hipStream_t st);
 hipError_t launch_gemm_i8_up(const I8GemmArgs &a, hipStream_t st);
 hipError_t launch_gemm_i8_down(const I8GemmArgs &a, hipStream_t st);
-// X to codes; the same with the token of every plan position (tile products);
-// H of the routed experts' rows and of the shared expert's (rows_s of them).
+// Tile products: powers of two that take the experts' outputs to fp16 (E experts of
+// f and a shared one of fs, channel scales [E][d] and [d]), and the routes' weights
+// that make up for them.
+struct I8Units {
+    const float *Wd_s = nullptr, *Sd_s = nullptr;
+    int f = 0, fs = 0, E = 0;
+    float *unit = nullptr;             // {1 / u, u} of every expert, then the shared one
+};
+struct I8Factors {
+    const int *perm = nullptr;         // null: none
+    const int *offsets = nullptr, *topk_idx = nullptr;
+    const float *topk_w = nullptr, *unit = nullptr;
+    float *w = nullptr;                // [T][k] topk_w x row scale x u; the shared rows' scales x u
+    int E = 0;
+};
+// X to codes; the same with the token of every plan position and the units (tile
+// products); H of the routed experts' rows and of the shared expert's (rows_s of them).
 hipError_t launch_i8_quant_tokens(const uint16_t *X, long rows, int K, uint8_t *q, float *sc, hipStream_t st);
 hipError_t launch_i8_prologue(const uint16_t *X, int T, int d, uint8_t *q, float *sc, const int *perm,
-                              const int *offsets, int E, int k, int *rowidx, hipStream_t st);
+                              const int *offsets, int k, int *rowidx, const I8Units &units,
+                              hipStream_t st);
 hipError_t launch_i8_quant_h(const float *H, long rows, int f, uint8_t *q, float *sc, const float *Hs,
-                             long rows_s, int fs, uint8_t *qs, float *scs, hipStream_t st);
+                             long rows_s, int fs, uint8_t *qs, float *scs, const I8Factors &factors,
+                             hipStream_t st);
 hipError_t launch_i8_quant_weights(const uint16_t *W, int E, int K, int N, uint8_t *q, float *sc,
                                    hipStream_t st);
 hipError_t launch_schedule(const int *A, int R, int NK, int L, int c, int *M, int *S, int *phi,
@@ -327,6 +345,9 @@ hipError_t launch_prep(const int *perm, const int *offsets, int E, const float *
 constexpr int ZERO_PAGE_ELEMS = 512;  // bf16 elements of the zero page (1 KB)
 hipError_t launch_combine(const uint16_t *Yexp, const uint16_t *Ysh, const float *topk_w,
                           const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st);
+// fp16 rows of the int8 tile products: w [T][k] and ysh_f [T] hold the rows' factors.
+hipError_t launch_combine_f16(const uint16_t *Yexp, const uint16_t *Ysh, const float *w, const float *ysh_f,
+                              const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st);
 hipError_t launch_combine_f32(const float *Yexp, const float *Ysh, const float *topk_w,
                               const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st);
 hipError_t launch_softmax_bwd(const float *dgpart, int nparts, const int *route_pos,

@@ -59,28 +59,35 @@ __global__ __launch_bounds__(256) void prep_kernel(const int *__restrict__ perm,
     wperm[p] = wv;
 }
 
-// 16 bytes of a row: 8 bf16 values or 4 fp32 ones
-DEV void unpack16(const u32x4_t &v, float (&x)[8]) {
+// 16 bytes of a row: 8 bf16 (uint16_t) or fp16 values, or 4 fp32 ones
+template <typename S>
+DEV void unpack16(const u32x4_t &v, float (&x)[16 / sizeof(S)]) {
+    if constexpr (sizeof(S) == 4) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        x[2 * q] = bf_lo(v[q]);
-        x[2 * q + 1] = bf_hi(v[q]);
+        for (int q = 0; q < 4; ++q) x[q] = __uint_as_float(v[q]);
+    } else if constexpr (is_half<S>) {
+        const f16x8_t h = __builtin_bit_cast(f16x8_t, v);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = (float)h[q];
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            x[2 * q] = bf_lo(v[q]);
+            x[2 * q + 1] = bf_hi(v[q]);
+        }
     }
-}
-DEV void unpack16(const u32x4_t &v, float (&x)[4]) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] = __uint_as_float(v[q]);
 }
 
 // Y[t] = Ysh[t] + sum_slot w[t,slot] * Yexp[route_pos[t*k+slot]]  (fp32, one rounding)
-// S: uint16_t (bf16 rows) or float.
+// S: uint16_t (bf16 rows), float, or _Float16, whose shared rows have a factor each.
 template <typename S>
 __global__ __launch_bounds__(256) void combine_kernel(const S *__restrict__ Yexp,
                                                       const S *__restrict__ Ysh,
                                                       const float *__restrict__ topk_w,
                                                       const int *__restrict__ route_pos, int T,
                                                       int d, int k, int R,
-                                                      uint16_t *__restrict__ Y) {
+                                                      uint16_t *__restrict__ Y,
+                                                      const float *__restrict__ ysh_f) {
     constexpr int V = 16 / sizeof(S);
     const int nc = d / V;
     for (int t = blockIdx.x; t < T; t += gridDim.x) {
@@ -96,6 +103,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const S *__restrict__ Yexp
                 wt[s] = topk_w[(long)t * k + s];
             }
         }
+        const float fs = is_half<S> && Ysh ? ysh_f[t] : 1.f;
         for (int c = threadIdx.x + 256 * blockIdx.y; c < nc; c += 256 * gridDim.y) {
             // every load first (slots past k or without a position read row 0
             // and are not added), so they are in flight together
@@ -105,7 +113,10 @@ __global__ __launch_bounds__(256) void combine_kernel(const S *__restrict__ Yexp
                 if (s < k) rows[s] = ld_u32x4(Yexp + (long)max(pos[s], 0) * d + V * c);
             float acc[V];
             if (Ysh) {
-                unpack16(ld_u32x4(Ysh + (long)t * d + V * c), acc);
+                unpack16<S>(ld_u32x4(Ysh + (long)t * d + V * c), acc);
+                if constexpr (is_half<S>)
+#pragma unroll
+                    for (int q = 0; q < V; ++q) acc[q] = fs * acc[q];
             } else {
 #pragma unroll
                 for (int q = 0; q < V; ++q) acc[q] = 0.f;
@@ -114,7 +125,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const S *__restrict__ Yexp
             for (int s = 0; s < 16; ++s) {
                 if (s < k && pos[s] >= 0) {
                     float x[V];
-                    unpack16(rows[s], x);
+                    unpack16<S>(rows[s], x);
 #pragma unroll
                     for (int q = 0; q < V; ++q) acc[q] = acc[q] + wt[s] * x[q];
                 }
@@ -692,18 +703,24 @@ hipError_t launch_prep(const int *perm, const int *offsets, int E, const float *
 
 template <typename S>
 static hipError_t combine_rows(const S *Yexp, const S *Ysh, const float *topk_w, const int *route_pos,
-                               int T, int d, int k, uint16_t *Y, hipStream_t st) {
+                               int T, int d, int k, uint16_t *Y, hipStream_t st,
+                               const float *ysh_f = nullptr) {
     if (T == 0) return hipSuccess;
     // few tokens: a block per 256 pieces of a row (61 tokens, 9 rows of 7168 bf16 each: 1 us less)
     constexpr int BC = 256 * (16 / (int)sizeof(S));
     const unsigned cols = T <= 256 ? (unsigned)((d + BC - 1) / BC) : 1;
     combine_kernel<S><<<dim3(rows_grid(T), cols), dim3(256), 0, st>>>(Yexp, Ysh, topk_w, route_pos, T, d, k,
-                                                                 T * k, Y);
+                                                                 T * k, Y, ysh_f);
     return hipGetLastError();
 }
 hipError_t launch_combine(const uint16_t *Yexp, const uint16_t *Ysh, const float *topk_w,
                           const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st) {
     return combine_rows(Yexp, Ysh, topk_w, route_pos, T, d, k, Y, st);
+}
+hipError_t launch_combine_f16(const uint16_t *Yexp, const uint16_t *Ysh, const float *w, const float *ysh_f,
+                              const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st) {
+    return combine_rows(reinterpret_cast<const _Float16 *>(Yexp), reinterpret_cast<const _Float16 *>(Ysh),
+                        w, route_pos, T, d, k, Y, st, ysh_f);
 }
 hipError_t launch_combine_f32(const float *Yexp, const float *Ysh, const float *topk_w,
                               const int *route_pos, int T, int d, int k, uint16_t *Y, hipStream_t st) {
