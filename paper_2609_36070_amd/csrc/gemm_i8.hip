@@ -29,8 +29,9 @@
 //
 // 16384 tokens to 8 of 32 experts of 1536, d 4096: up 1470 us, 2.24 POP/s, down 920,
 // 1.79 (a tile of 12 steps has the epilogue of one of 32); a large library
-// product reaches 2.12.  The matrix units are busy 59 % of the time at 1.85 GHz,
-// and busier schedules only lower the clock: power bounds it.
+// product reaches 2.12.  The matrix units are busy 58 and 46 % of the time, at 1.88
+// GHz (2.1 to 2.3 in launches of 0.1 to 0.2 ms); waves wait half of theirs, next to
+// none of it for LDS.
 #include "common.h"
 #include "i8_common.h"
 #include "kernels.h"

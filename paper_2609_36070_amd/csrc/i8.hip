@@ -201,7 +201,11 @@ __global__ __launch_bounds__(256) void i8_prologue_kernel(QuantRows<uint16_t> x,
 // A block per 64 channels of an expert: the channels' largest magnitudes over
 // all K rows, then the codes, 128 rows at a time through LDS so that reads
 // (along n) and writes (along k) are whole 128-byte lines.  The second pass
-// reads what the first left in the caches.
+// reads what the first left in the caches, or in HBM again where the weights in work
+// are larger: 128 experts of 768, d 2048 606 us for 1.2 GB of weights and 0.6 of
+// codes, which is 5 TB/s with both passes (348 at a large copy's 5.2 TB/s with one); 32 of
+// 1536, d 4096 661, the same bytes.  Few experts leave it to latency, a block per 64
+// channels: 8 of 2048 and a shared one, d 7168 920 us for 1.2 GB in all (229).
 constexpr int QW_PITCH = 128 + 16;
 __global__ __launch_bounds__(256) void i8_quant_weights_kernel(const uint16_t *__restrict__ W, int K,
                                                                int N, uint8_t *__restrict__ q,
@@ -260,6 +264,9 @@ __global__ __launch_bounds__(256) void i8_quant_weights_kernel(const uint16_t *_
 // 768 555 / 591; 32768 of 256 85 / 105; 131072 of 1536 2850 / 2867; 8000 of 1536 260.4 /
 // 260.2; 36891 of 2048, all threads busy, 1772 / 1769; 128 of 1536 139 / 137).  They move
 // 5.2 TB/s from 131072 rows of 1536 (186 us), and few rows take a launch's time (5 us).
+// The weights of the tile products' routes cost the rows' launch three dependent
+// loads: 8192 tokens to 8 of 128 experts of 768 45 -> 52 us, 4099 to 8 and a shared one
+// of 2048 68 -> 82, which the down product and the sum save.
 constexpr long QUANT_WAVE_ROWS = 2048;
 template <typename F>
 hipError_t with_chunks(long rows, int K, F f) {

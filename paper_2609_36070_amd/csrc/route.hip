@@ -478,7 +478,7 @@ __global__ __launch_bounds__(256) void route_reduce_kernel(const float *__restri
 // which transposes W_r falls away (4099 tokens to 256 experts, d 7168, with the
 // selection 45 -> 42 us; 16384 to 128, d 2048, 34 -> 32; 3000 to 128, d 7168, 24 ->
 // 22).  Rows of W_r must be whole 16-byte pieces.  What bounds it are the lines a
-// CU can have on their way: the first of these loads 177 MB in 25 us, 7 TB/s; tiles
+// CU can have on their way: the first of these loads 180 MB in 25 us, 7 TB/s; tiles
 // of 256 tokens would load a third less and write as much more in partial sums.
 //
 // LDS: X as in the split router; W_r's 64-byte blocks of a row XOR k & 3, so that

@@ -10,14 +10,16 @@
 // smallest and largest, 8 bits below hold 255 - e, and the entries go through
 // sorting networks of integer maxima and minima.  The first expert left out and
 // the last one taken then say whether the errors of the fp32 values could have
-// swapped them, and likewise the groups; only where they could (a few tokens in
+// swapped them, and likewise the groups; only where they could (some 15 tokens in
 // 100000, and rows of exact ties) the experts that the errors reach, mostly two,
 // are ranked again by 64-bit values, in compact loops.  A selection in 64 bits
 // throughout spent 25-50 us, most of it on fetching its unrolled code (30 us for a
-// single token); this one takes 6.5 us for one token to 256 experts in 8 groups
-// (28 slices of partial logits; a launch's and a round trip's time), 13.6
-// for 4099 (29 MB of partial logits) and 14.2 for 16384 to 128 experts (networks
-// and exponentials; the logits are 8 MB).
+// single token); this one takes 6.7 us for one token to 256 experts in 8 groups
+// (28 slices of partial logits; a launch's and a round trip's time), 13.1
+// for 4099 (29 MB of partial logits) and 13.8 for 16384 to 128 experts (networks
+// and exponentials; the partial logits are 17 MB).  Where every expert of every
+// token ties, as with a router of zeros, whole calls take 56 us for 39 (4099 tokens)
+// and 47 for 29 (16384).
 //
 // The 64-bit side compares all 64 bits and then the ids: saturated sigmoids, and
 // small scores beside a balance, differ in their last bits alone.

@@ -305,9 +305,9 @@ __global__ __launch_bounds__(1024) void token_down_kernel(I8SkinnyArgs a, const 
 // direct loads (whole 128-byte lines, chunk XOR (row >> 1) & 7); it is a wave of
 // its own because loads return in order, and the activations, from L2, would
 // wait for weights asked for long before.  One barrier per piece.  16 tokens to 8 of
-// 32 experts of 1536, d 4096: up 84-88 us for 403 MB of codes, down 38 for 201 (5 TB/s;
+// 32 experts of 1536, d 4096: up 79 us for 403 MB of codes, down 39 for 201 (5 TB/s;
 // a large copy reaches 5.2); 61 tokens, 8 experts and a shared one of 2048, d 7168:
-// up 56 us for 264 MB, down 34 for 132.
+// up 55 us for 264 MB, down 36 for 132.
 //
 // With dense routing every expert's rows are the tokens, so a workgroup's
 // columns may belong to two experts, or to the shared one, and NW is what deals
