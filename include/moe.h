@@ -596,8 +596,8 @@ moe_status moe_int_quantize_weights(const moe_shape *shape, const moe_weights *w
                                     const moe_int_weights *i8, moe_stream stream);
 
 /* Workspace bytes of moe_forward_int (it also serves moe_route,
- * moe_route_scored and moe_plan); 0 for an invalid or unsupported shape.  Pure
- * host function. */
+ * moe_route_scored and moe_plan); 0 for an invalid or unsupported shape.  It
+ * never falls as T grows.  Pure host function. */
 size_t moe_int_workspace_bytes(const moe_shape *shape);
 
 /* Forward of the layer with routed and shared experts in 8-bit integers

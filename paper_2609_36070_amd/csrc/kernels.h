@@ -320,7 +320,7 @@ struct I8Factors {
     const int *perm = nullptr;         // null: none
     const int *offsets = nullptr, *topk_idx = nullptr;
     const float *topk_w = nullptr, *unit = nullptr;
-    float *w = nullptr;                // [T][k] topk_w x row scale x u; the shared rows' scales x u
+    float *w = nullptr;                // [T][k] topk_w x row scale x u (shared rows: their scales x u)
     int E = 0;
 };
 // X to codes; the same with the token of every plan position and the units (tile
