@@ -628,6 +628,68 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
                            moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream,
                            const moe_stage_events *events /* NULL = no timing */);
 
+/* Joining a block to the residual stream.  A block (this layer, or any other) has
+ * made y from the stream x; the join puts y back and makes the next block's
+ * input h, T rows of d:
+ *     n = N_y(y)                           N none, rms or layer:
+ *     v = n / (1 - p) where kept, else 0     rms    u = y / sqrt(mean(y^2) + eps)
+ *     r = x + scale gate[c] token_gate[t] v  layer  u = (y - mean) / sqrt(var + eps)
+ *     h = N_r(r)                             N(y) = u weight + bias
+ * Statistics and sums are fp32.  r is rounded to the stream's type, and h is the
+ * norm of that rounded r, itself rounded to bf16.
+ * Dropout: 16 bits per element come from Philox4x32-10 with the key rng[0] and the
+ * counter (j, t, rng[1]) for elements 8 j .. 8 j + 7 of row t: its four words hold
+ * them in order, lower halves first.  An element is kept where its bits are at
+ * least n = floor(65536 drop + 1/2), and p = n / 65536.  The mask is not stored:
+ * the backward takes it from the same rng, a DEVICE array that a program moves on
+ * between steps (a captured graph reads what is there when it is replayed). */
+typedef enum { MOE_STREAM_BF16 = 0, MOE_STREAM_FP32 = 1 } moe_stream_type;
+typedef enum { MOE_NORM_NONE = 0, MOE_NORM_RMS = 1, MOE_NORM_LAYER = 2 } moe_norm;
+typedef struct {
+    int64_t T, d;          /* d % 8 == 0, 8 <= d <= 16384; T < 2^31 */
+    int32_t stream_type;   /* moe_stream_type of x, r, dr, dx */
+    int32_t y_norm, r_norm; /* moe_norm */
+    float y_eps, r_eps;    /* finite and > 0 where the norm is not none */
+    float scale;           /* finite */
+    float drop;            /* 0 <= drop, rounded to 16 bits below 1 */
+} moe_join;
+typedef struct {           /* fp32, caller-owned; each may be NULL */
+    const float *y_weight, *y_bias;    /* [d] (NULL: 1 and 0); none without the norm */
+    const float *gate;                 /* [d] (NULL: 1) */
+    const float *token_gate;           /* [T] (NULL: 1) */
+    const float *r_weight, *r_bias;    /* [d] */
+} moe_join_params;
+typedef struct {           /* fp32, overwritten; NULL: not wanted (the parameter must be there) */
+    float *y_weight, *y_bias, *gate, *token_gate, *r_weight, *r_bias;
+} moe_join_grads;
+
+/* Forward.  x [T, d] in the stream's type, y [T, d] bf16, rng [2] (NULL iff drop
+ * rounds to 0); out: r [T, d] in the stream's type, h [T, d] bf16, stats [T, 4] fp32.
+ * r may be x itself.
+ * y NULL: there is no block yet and h is the norm of x; r is NULL then, y's norm is
+ * none, drop is 0 and there are no gates.
+ * h NULL: only r is wanted; r's norm is none then.
+ * stats (mean and 1 / deviation of y's row, then of r's; 0 where there is no norm)
+ * is what moe_join_backward reads; NULL where none follows. */
+moe_status moe_join_forward(const moe_join *join, const void *x, const moe_bf16 *y,
+                            const moe_join_params *params, const int64_t *rng, void *r, moe_bf16 *h,
+                            float *stats, moe_stream stream);
+
+/* Workspace bytes of moe_join_backward (sums over the rows); 0 for an invalid or
+ * unsupported join.  Never falls as T grows.  Pure host function. */
+size_t moe_join_workspace_bytes(const moe_join *join);
+
+/* Gradient.  join, params, rng, y, r (x where there was no y) and stats as the forward had
+ * or left them; dr [T, d] in the stream's type and dh [T, d] bf16: gradients wrt r
+ * and h (either may be NULL: none comes from there).  Out: dx [T, d] in the
+ * stream's type, dy [T, d] bf16 (NULL iff y is), and what grads asks for.
+ * dx may be dr itself.  Sums over the rows are added in an order that depends on
+ * the sizes alone. */
+moe_status moe_join_backward(const moe_join *join, const moe_bf16 *y, const void *r, const float *stats,
+                             const moe_join_params *params, const int64_t *rng, const void *dr,
+                             const moe_bf16 *dh, void *dx, moe_bf16 *dy, const moe_join_grads *grads,
+                             void *ws, size_t ws_bytes, moe_stream stream);
+
 /* Static strings; never NULL. */
 const char *moe_status_string(moe_status status);
 const char *moe_version(void);

@@ -34,7 +34,8 @@ EXPORTS = ("moe_workspace_bytes", "moe_workspace_region", "moe_route", "moe_plan
            "moe_mx_quantize_weights_bwd", "moe_backward_mx", "moe_plan_noalloc", "moe_status_string",
            "moe_version", "moe_route_scored", "moe_score_backward", "moe_backward_scored",
            "moe_backward_ring_scored", "moe_backward_mx_scored", "moe_int_quantize_weights",
-           "moe_int_workspace_bytes", "moe_forward_int")
+           "moe_int_workspace_bytes", "moe_forward_int", "moe_join_forward",
+           "moe_join_workspace_bytes", "moe_join_backward")
 PLAN_NOALLOC_SCRATCH_BYTES = 4 << 20
 
 
@@ -67,6 +68,25 @@ GROUP_SCORES = ("max", "pair")
 class MoeRouting(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("score", "groups", "top_groups", "group_score",
                                               "renormalise")] + [("scale", ctypes.c_float)]
+
+
+STREAM_TYPES = ("bf16", "f32")
+NORMS = ("none", "rms", "layer")
+JOIN_PARAMS = ("y_weight", "y_bias", "gate", "token_gate", "r_weight", "r_bias")
+
+
+class MoeJoin(ctypes.Structure):
+    _fields_ = ([("T", c_int64), ("d", c_int64)]
+                + [(n, ctypes.c_int32) for n in ("stream_type", "y_norm", "r_norm")]
+                + [(n, ctypes.c_float) for n in ("y_eps", "r_eps", "scale", "drop")])
+
+
+class MoeJoinParams(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in JOIN_PARAMS]
+
+
+class MoeJoinGrads(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in JOIN_PARAMS]
 
 
 class MoePlanBufs(ctypes.Structure):
@@ -160,13 +180,18 @@ def lib():
         L.moe_forward_int.argtypes = [P(MoeShape), c_void_p, P(MoeIntWeights), c_void_p, c_void_p,
                                       P(MoePlanBufs), c_void_p, c_void_p, c_size_t, c_void_p,
                                       P(MoeStageEvents)]
+        L.moe_join_forward.argtypes = [P(MoeJoin), c_void_p, c_void_p, P(MoeJoinParams)] + [c_void_p] * 5
+        L.moe_join_workspace_bytes.argtypes = [P(MoeJoin)]
+        L.moe_join_workspace_bytes.restype = c_size_t
+        L.moe_join_backward.argtypes = ([P(MoeJoin)] + [c_void_p] * 3 + [P(MoeJoinParams)] + [c_void_p] * 5
+                                        + [P(MoeJoinGrads), c_void_p, c_size_t, c_void_p])
         for fn in ("moe_route", "moe_plan", "moe_schedule", "moe_dispatch", "moe_forward",
                    "moe_backward", "moe_workspace_region", "moe_mx_quantize_weights",
                    "moe_mx_workspace_region", "moe_forward_mx", "moe_forward_ring",
                    "moe_backward_ring", "moe_forward_fused", "moe_mx_quantize_weights_bwd",
                    "moe_backward_mx", "moe_route_scored", "moe_score_backward", "moe_backward_scored",
                    "moe_backward_ring_scored", "moe_backward_mx_scored", "moe_int_quantize_weights",
-                   "moe_forward_int"):
+                   "moe_forward_int", "moe_join_forward", "moe_join_backward"):
             getattr(L, fn).restype = c_int
         L.moe_status_string.argtypes = [c_int]
         L.moe_status_string.restype = ctypes.c_char_p
@@ -487,3 +512,41 @@ def moe_forward_int(shape, X, weights: MoeIntWeights, topk_idx, topk_w, plan: Mo
                                _p(topk_w), ctypes.byref(plan), _p(Y), _p(ws), nbytes, _stream(stream),
                                None if events is None else ctypes.byref(events))
     return _check("moe_forward_int", st, raise_on_error)
+
+
+def join(T, d, stream="bf16", y_norm="none", r_norm="rms", y_eps=1e-6, r_eps=1e-6, scale=1.0,
+         drop=0.0) -> MoeJoin:
+    """How a block's output joins the residual stream of T rows of d ("bf16" or "f32"): the norms
+    ("none", "rms", "layer") of the output and of the sum, its scale, the share that dropout takes."""
+    return MoeJoin(T, d, STREAM_TYPES.index(stream), NORMS.index(y_norm), NORMS.index(r_norm), y_eps, r_eps,
+                   scale, drop)
+
+
+def join_params(y_weight=None, y_bias=None, gate=None, token_gate=None, r_weight=None,
+                r_bias=None) -> MoeJoinParams:
+    return MoeJoinParams(_p(y_weight), _p(y_bias), _p(gate), _p(token_gate), _p(r_weight), _p(r_bias))
+
+
+def join_grads(y_weight=None, y_bias=None, gate=None, token_gate=None, r_weight=None,
+               r_bias=None) -> MoeJoinGrads:
+    return MoeJoinGrads(_p(y_weight), _p(y_bias), _p(gate), _p(token_gate), _p(r_weight), _p(r_bias))
+
+
+def moe_join_forward(join: MoeJoin, x, y, params: MoeJoinParams, rng, r, h, stats=None, stream=None,
+                     raise_on_error=True):
+    st = lib().moe_join_forward(ctypes.byref(join), _p(x), _p(y), ctypes.byref(params), _p(rng), _p(r), _p(h),
+                                _p(stats), _stream(stream))
+    return _check("moe_join_forward", st, raise_on_error)
+
+
+def moe_join_workspace_bytes(join: MoeJoin) -> int:
+    return int(lib().moe_join_workspace_bytes(ctypes.byref(join)))
+
+
+def moe_join_backward(join: MoeJoin, y, r, stats, params: MoeJoinParams, rng, dr, dh, dx, dy,
+                      grads: MoeJoinGrads, ws, ws_bytes=None, stream=None, raise_on_error=True):
+    nbytes = ws.nbytes if ws_bytes is None else ws_bytes
+    st = lib().moe_join_backward(ctypes.byref(join), _p(y), _p(r), _p(stats), ctypes.byref(params), _p(rng),
+                                 _p(dr), _p(dh), _p(dx), _p(dy), ctypes.byref(grads), _p(ws), nbytes,
+                                 _stream(stream))
+    return _check("moe_join_backward", st, raise_on_error)

@@ -8,6 +8,7 @@
 #include <cstdint>
 #include <cstring>
 #include <mutex>
+#include <utility>
 
 #include "../../include/moe.h"
 #include "kernels.h"
@@ -329,6 +330,54 @@ hipError_t router_bwd(const Scored *sc, const float *dgpart, int nparts, const i
     if (!sc) return launch_softmax_bwd(dgpart, nparts, route_pos, topk_w, topk_idx, T, k, E, dg, dZ, s);
     return launch_score_bwd(sc->logits, sc->balance, topk_idx, nullptr, dgpart, nparts, route_pos, dg, dZ,
                             T, E, k, score_args(*sc->routing), s);
+}
+
+// Joining a block to the residual stream.
+uint32_t join_dropped(const moe_join &j) { return (uint32_t)std::floor((double)j.drop * 65536.0 + 0.5); }
+
+moe_status check_join(const moe_join *j) {
+    if (!j || j->T < 0 || j->d <= 0) return MOE_EINVAL;
+    if (j->stream_type != MOE_STREAM_BF16 && j->stream_type != MOE_STREAM_FP32) return MOE_EINVAL;
+    for (const auto &n : {std::make_pair(j->y_norm, j->y_eps), std::make_pair(j->r_norm, j->r_eps)}) {
+        if (n.first < MOE_NORM_NONE || n.first > MOE_NORM_LAYER) return MOE_EINVAL;
+        if (n.first != MOE_NORM_NONE && !(std::isfinite(n.second) && n.second > 0.f)) return MOE_EINVAL;
+    }
+    if (!std::isfinite(j->scale)) return MOE_EINVAL;
+    if (!(j->drop >= 0.f && j->drop < 1.f) || join_dropped(*j) > 65535) return MOE_EINVAL;
+    if (j->d % 8 || j->d > JOIN_MAX_D || j->T >= (int64_t(1) << 31)) return MOE_EUNSUPPORTED;
+    return MOE_OK;
+}
+
+// The parameters belong to norms and gates that are there.
+moe_status check_join_params(const moe_join &j, const moe_join_params *p, bool block, const int64_t *rng) {
+    if (!p) return MOE_EINVAL;
+    for (const float *q : {p->y_weight, p->y_bias, p->gate, p->token_gate, p->r_weight, p->r_bias})
+        if (!opt_ok(q)) return MOE_EINVAL;
+    if (j.y_norm == MOE_NORM_NONE && (p->y_weight || p->y_bias)) return MOE_EINVAL;
+    if (j.r_norm == MOE_NORM_NONE && (p->r_weight || p->r_bias)) return MOE_EINVAL;
+    if (!opt_ok(rng) || (rng != nullptr) != (join_dropped(j) > 0)) return MOE_EINVAL;
+    if (!block && (j.y_norm != MOE_NORM_NONE || p->gate || p->token_gate || rng)) return MOE_EINVAL;
+    return MOE_OK;
+}
+
+JoinArgs join_args(const moe_join &j, const moe_join_params &p, const moe_bf16 *y, const int64_t *rng) {
+    JoinArgs g;
+    g.T = j.T; g.d = (int)j.d;
+    g.f32 = j.stream_type == MOE_STREAM_FP32;
+    g.y_norm = j.y_norm; g.r_norm = j.r_norm;
+    g.y_eps = j.y_eps; g.r_eps = j.r_eps;
+    g.scale = j.scale;
+    g.out = join_dropped(j);
+    g.keep = (float)(65536.0 / (65536.0 - g.out));
+    g.rng = rng;
+    g.y_weight = p.y_weight; g.y_bias = p.y_bias; g.gate = p.gate; g.token_gate = p.token_gate;
+    g.r_weight = p.r_weight; g.r_bias = p.r_bias;
+    g.y = y;
+    return g;
+}
+
+size_t join_bytes(const moe_join &j) {
+    return std::max<size_t>((size_t)join_blocks(j.T, (int)j.d) * 5 * (size_t)j.d * 4, 16);
 }
 
 // Int8 experts: every operand is addressed with 32-bit offsets, and a dot
@@ -1929,6 +1978,58 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
         MOE_TRY(launch_combine_f16(at<uint16_t>(ws, Q.Yexp), fs > 0 ? at<uint16_t>(ws, Q.Ysh) : nullptr, hs,
                                    hshs, plan->route_pos, T, d, k, Y, s));
     MOE_TRY(mk.mark(6));
+    return MOE_OK;
+}
+
+moe_status moe_join_forward(const moe_join *join, const void *x, const moe_bf16 *y,
+                            const moe_join_params *params, const int64_t *rng, void *r, moe_bf16 *h,
+                            float *stats, moe_stream stream) {
+    moe_status st = check_join(join);
+    if (st != MOE_OK) return st;
+    if ((st = check_join_params(*join, params, y != nullptr, rng)) != MOE_OK) return st;
+    if (!ptr_ok(x) || !opt_ok(y) || !opt_ok(r) || !opt_ok(h) || !opt_ok(stats)) return MOE_EINVAL;
+    if ((y != nullptr) != (r != nullptr) || (!r && !h)) return MOE_EINVAL;
+    if (!h && join->r_norm != MOE_NORM_NONE) return MOE_EINVAL;
+    JoinArgs g = join_args(*join, *params, y, rng);
+    g.x = x; g.r = r; g.h = h; g.stats = stats;
+    MOE_TRY(launch_join_forward(g, static_cast<hipStream_t>(stream)));
+    return MOE_OK;
+}
+
+size_t moe_join_workspace_bytes(const moe_join *join) {
+    return check_join(join) == MOE_OK ? join_bytes(*join) : 0;
+}
+
+moe_status moe_join_backward(const moe_join *join, const moe_bf16 *y, const void *r, const float *stats,
+                             const moe_join_params *params, const int64_t *rng, const void *dr,
+                             const moe_bf16 *dh, void *dx, moe_bf16 *dy, const moe_join_grads *grads,
+                             void *ws, size_t ws_bytes, moe_stream stream) {
+    moe_status st = check_join(join);
+    if (st != MOE_OK) return st;
+    if ((st = check_join_params(*join, params, y != nullptr, rng)) != MOE_OK) return st;
+    if (!opt_ok(y) || !ptr_ok(r) || !ptr_ok(stats) || !opt_ok(dr) || !opt_ok(dh) || !ptr_ok(dx) ||
+        !opt_ok(dy) || !grads)
+        return MOE_EINVAL;
+    if ((y != nullptr) != (dy != nullptr) || (!dr && !dh)) return MOE_EINVAL;
+    const moe_join_params &p = *params;
+    const struct { float *grad; const float *param; } all[6] = {
+        {grads->r_weight, p.r_weight}, {grads->r_bias, p.r_bias}, {grads->gate, p.gate},
+        {grads->y_weight, p.y_weight}, {grads->y_bias, p.y_bias}, {grads->token_gate, p.token_gate}};
+    for (const auto &a : all)
+        if (!opt_ok(a.grad) || (a.grad && !a.param)) return MOE_EINVAL;
+    if (!ptr_ok(ws)) return MOE_EINVAL;
+    if (ws_bytes < join_bytes(*join)) return MOE_ENOSPACE;
+    JoinArgs g = join_args(*join, p, y, rng);
+    g.r_in = r; g.dr = dr; g.dh = dh; g.stats_in = stats;
+    g.dx = dx; g.dy = dy;
+    g.dtoken_gate = grads->token_gate;
+    for (int i = 0; i < 5; ++i)
+        if (all[i].grad) {
+            g.sums |= 1 << i;
+            g.out_sums[g.nsums++] = all[i].grad;
+        }
+    g.part = static_cast<float *>(ws);
+    MOE_TRY(launch_join_backward(g, static_cast<hipStream_t>(stream)));
     return MOE_OK;
 }
 

@@ -337,6 +337,40 @@ hipError_t launch_i8_quant_weights(const uint16_t *W, int E, int K, int N, uint8
 hipError_t launch_schedule(const int *A, int R, int NK, int L, int c, int *M, int *S, int *phi,
                            long phi_rows, int *counts, int *flags, int *err, hipStream_t st);
 
+// Joining a block to the residual stream, and its gradient (join.hip).
+enum JoinNorm { JOIN_NONE = 0, JOIN_RMS = 1, JOIN_LAYER = 2 };   // as moe_norm
+struct JoinArgs {
+    long T = 0, row0 = 0;              // row0: set by the launcher
+    int d = 0, f32 = 0, y_norm = 0, r_norm = 0;
+    float y_eps = 0.f, r_eps = 0.f, scale = 1.f;
+    uint32_t out = 0;                  // an element is kept where its 16 bits are at least this,
+    float keep = 1.f;                  //   and multiplied with this
+    const int64_t *rng = nullptr;      // {seed, offset}, null: everything is kept
+    const float *y_weight = nullptr, *y_bias = nullptr, *gate = nullptr, *token_gate = nullptr;
+    const float *r_weight = nullptr, *r_bias = nullptr;
+    const uint16_t *y = nullptr;
+    // forward
+    const void *x = nullptr;
+    void *r = nullptr;
+    uint16_t *h = nullptr;
+    float *stats = nullptr;            // [T][4] mean and 1 / deviation of y's row, of r's
+    // backward
+    const void *r_in = nullptr, *dr = nullptr;
+    const uint16_t *dh = nullptr;
+    const float *stats_in = nullptr;
+    void *dx = nullptr;
+    uint16_t *dy = nullptr;
+    float *dtoken_gate = nullptr;
+    // sums over the rows that are asked for: bits 0 .. 4 of weight and bias of r's
+    // norm, gate, weight and bias of y's norm; nsums of them, in that order
+    int sums = 0, nsums = 0;
+    float *out_sums[5] = {};
+    float *part = nullptr;             // [join_blocks][nsums][d]
+};
+int join_blocks(long T, int d);        // workgroups of a backward
+hipError_t launch_join_forward(const JoinArgs &g, hipStream_t st);
+hipError_t launch_join_backward(JoinArgs g, hipStream_t st);
+
 int dwr_nchunks(long T);
 hipError_t launch_gather(const uint16_t *X, const int *perm, const int *offsets, int E, int k, int T,
                          int d, uint16_t *Xperm, hipStream_t st);

@@ -351,3 +351,11 @@ inline bool mx_keep_l2(long R, long E, long K, long N) {
     const long bytes = 8 * R * N;
     return K <= 1024 && R >= 1024 * E && bytes >= (64L << 20) && bytes <= (208L << 20);
 }
+
+// Joining a block to the residual stream (join.hip): rows up to which a row gets
+// as many threads as have something to load.
+constexpr long JOIN_FEW_ROWS = 256;
+// Workgroups of the backward at most; each leaves a row of sums.
+constexpr long JOIN_BLOCKS = 256;
+// Row lengths: what a workgroup's registers hold.
+constexpr long JOIN_MAX_D = 16384;
