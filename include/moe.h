@@ -628,6 +628,21 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
                            moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream,
                            const moe_stage_events *events /* NULL = no timing */);
 
+/* The whole layer for a few tokens (inference): what moe_route_scored, moe_plan and
+ * moe_forward do, in two launches.  Arguments and outputs are those of
+ * moe_route_scored and moe_forward; T <= 16 (MOE_EUNSUPPORTED beyond), the other
+ * limits are the layer's.  Results are those of the definition: the gated activation
+ * is kept to 16 significant bits, sums are fp32, and Y is rounded once.  An expert
+ * reaches the tokens that chose it alone, also where its values are infinite or NaN.
+ *   ws: at least moe_few_workspace_bytes(shape) bytes, holding anything; calls that
+ *   can overlap need one each.  Its first int32 is not 0 after a call whose waits between
+ *   workgroups gave up (the outputs are then invalid). */
+size_t moe_few_workspace_bytes(const moe_shape *shape);   /* 0: invalid or unsupported; never falls with T */
+moe_status moe_forward_few(const moe_shape *shape, const moe_routing *routing, const moe_bf16 *X,
+                           const moe_bf16 *W_r, const float *bias, const float *balance,
+                           const moe_weights *weights, float *logits, int32_t *topk_idx, float *topk_w,
+                           moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream);
+
 /* Joining a block to the residual stream.  A block (this layer, or any other) has
  * made y from the stream x; the join puts y back and makes the next block's
  * input h, T rows of d:

@@ -35,7 +35,7 @@ EXPORTS = ("moe_workspace_bytes", "moe_workspace_region", "moe_route", "moe_plan
            "moe_version", "moe_route_scored", "moe_score_backward", "moe_backward_scored",
            "moe_backward_ring_scored", "moe_backward_mx_scored", "moe_int_quantize_weights",
            "moe_int_workspace_bytes", "moe_forward_int", "moe_join_forward",
-           "moe_join_workspace_bytes", "moe_join_backward")
+           "moe_join_workspace_bytes", "moe_join_backward", "moe_few_workspace_bytes", "moe_forward_few")
 PLAN_NOALLOC_SCRATCH_BYTES = 4 << 20
 
 
@@ -180,6 +180,10 @@ def lib():
         L.moe_forward_int.argtypes = [P(MoeShape), c_void_p, P(MoeIntWeights), c_void_p, c_void_p,
                                       P(MoePlanBufs), c_void_p, c_void_p, c_size_t, c_void_p,
                                       P(MoeStageEvents)]
+        L.moe_few_workspace_bytes.argtypes = [P(MoeShape)]
+        L.moe_few_workspace_bytes.restype = c_size_t
+        L.moe_forward_few.argtypes = ([P(MoeShape), P(MoeRouting)] + [c_void_p] * 4 + [P(MoeWeights)]
+                                      + [c_void_p] * 5 + [c_size_t, c_void_p])
         L.moe_join_forward.argtypes = [P(MoeJoin), c_void_p, c_void_p, P(MoeJoinParams)] + [c_void_p] * 5
         L.moe_join_workspace_bytes.argtypes = [P(MoeJoin)]
         L.moe_join_workspace_bytes.restype = c_size_t
@@ -191,7 +195,7 @@ def lib():
                    "moe_backward_ring", "moe_forward_fused", "moe_mx_quantize_weights_bwd",
                    "moe_backward_mx", "moe_route_scored", "moe_score_backward", "moe_backward_scored",
                    "moe_backward_ring_scored", "moe_backward_mx_scored", "moe_int_quantize_weights",
-                   "moe_forward_int", "moe_join_forward", "moe_join_backward"):
+                   "moe_forward_int", "moe_forward_few", "moe_join_forward", "moe_join_backward"):
             getattr(L, fn).restype = c_int
         L.moe_status_string.argtypes = [c_int]
         L.moe_status_string.restype = ctypes.c_char_p
@@ -512,6 +516,19 @@ def moe_forward_int(shape, X, weights: MoeIntWeights, topk_idx, topk_w, plan: Mo
                                _p(topk_w), ctypes.byref(plan), _p(Y), _p(ws), nbytes, _stream(stream),
                                None if events is None else ctypes.byref(events))
     return _check("moe_forward_int", st, raise_on_error)
+
+
+def moe_few_workspace_bytes(shape: MoeShape) -> int:
+    return int(lib().moe_few_workspace_bytes(ctypes.byref(shape)))
+
+
+def moe_forward_few(shape, routing: MoeRouting, X, W_r, bias, balance, weights: MoeWeights, logits, topk_idx,
+                    topk_w, Y, ws, ws_bytes=None, stream=None, raise_on_error=True):
+    nbytes = ws.nbytes if ws_bytes is None else ws_bytes
+    st = lib().moe_forward_few(ctypes.byref(shape), ctypes.byref(routing), _p(X), _p(W_r), _p(bias),
+                               _p(balance), ctypes.byref(weights), _p(logits), _p(topk_idx), _p(topk_w), _p(Y),
+                               _p(ws), nbytes, _stream(stream))
+    return _check("moe_forward_few", st, raise_on_error)
 
 
 def join(T, d, stream="bf16", y_norm="none", r_norm="rms", y_eps=1e-6, r_eps=1e-6, scale=1.0,

@@ -29,7 +29,7 @@ FLAGS = [
     f"-I{os.path.join(ROOT, 'include')}",
 ] + os.environ.get("MOE_HIPCC_EXTRA", "").split()
 SOURCES = ["route.hip", "score.hip", "plan.hip", "schedule.hip", "movement.hip", "gemm.hip", "skinny.hip",
-           "mx.hip", "gemm_mx.hip", "i8.hip", "gemm_i8.hip", "skinny_i8.hip", "join.hip",
+           "mx.hip", "gemm_mx.hip", "i8.hip", "gemm_i8.hip", "skinny_i8.hip", "few.hip", "join.hip",
            "api.cpp"]
 
 

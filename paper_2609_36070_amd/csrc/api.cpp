@@ -11,6 +11,7 @@
 #include <utility>
 
 #include "../../include/moe.h"
+#include "few.h"
 #include "kernels.h"
 #include "rules.h"
 
@@ -331,6 +332,15 @@ hipError_t router_bwd(const Scored *sc, const float *dgpart, int nparts, const i
     return launch_score_bwd(sc->logits, sc->balance, topk_idx, nullptr, dgpart, nparts, route_pos, dg, dZ,
                             T, E, k, score_args(*sc->routing), s);
 }
+
+// The whole layer for a few tokens.
+moe_status check_few_shape(const moe_shape *s) {
+    const moe_status st = check_shape(s);
+    if (st != MOE_OK) return st;
+    return s->T <= FEW_MAX_T ? MOE_OK : MOE_EUNSUPPORTED;
+}
+
+FewLayout few_sizes(const moe_shape &s) { return few_layout(s.T, s.d, s.E, s.k, s.f, s.f_shared); }
 
 // Joining a block to the residual stream.
 uint32_t join_dropped(const moe_join &j) { return (uint32_t)std::floor((double)j.drop * 65536.0 + 0.5); }
@@ -1978,6 +1988,41 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
         MOE_TRY(launch_combine_f16(at<uint16_t>(ws, Q.Yexp), fs > 0 ? at<uint16_t>(ws, Q.Ysh) : nullptr, hs,
                                    hshs, plan->route_pos, T, d, k, Y, s));
     MOE_TRY(mk.mark(6));
+    return MOE_OK;
+}
+
+size_t moe_few_workspace_bytes(const moe_shape *shape) {
+    return check_few_shape(shape) == MOE_OK ? (size_t)few_sizes(*shape).total : 0;
+}
+
+moe_status moe_forward_few(const moe_shape *shape, const moe_routing *routing, const moe_bf16 *X,
+                           const moe_bf16 *W_r, const float *bias, const float *balance,
+                           const moe_weights *weights, float *logits, int32_t *topk_idx, float *topk_w,
+                           moe_bf16 *Y, void *ws, size_t ws_bytes, moe_stream stream) {
+    moe_status st = check_few_shape(shape);
+    if (st != MOE_OK) return st;
+    if ((st = check_routing(shape, routing)) != MOE_OK) return st;
+    if (!ptr_ok(X) || !ptr_ok(W_r) || !opt_ok(bias) || !opt_ok(balance) || !ptr_ok(logits) ||
+        !ptr_ok(topk_idx) || !ptr_ok(topk_w) || !ptr_ok(Y))
+        return MOE_EINVAL;
+    if ((st = check_weights(shape, weights)) != MOE_OK) return st;
+    if (!ptr_ok(ws)) return MOE_EINVAL;
+    const FewLayout L = few_sizes(*shape);
+    if (ws_bytes < (size_t)L.total) return MOE_ENOSPACE;
+    FewArgs g;
+    g.T = (int)shape->T; g.d = (int)shape->d; g.E = (int)shape->E; g.k = (int)shape->k;
+    g.f = (int)shape->f; g.fs = (int)shape->f_shared;
+    g.S = g.T > 0 ? few_router_slices(g.T, g.d, g.E) : 0;
+    g.score = score_args(*routing);
+    g.X = X; g.W_r = W_r; g.bias = bias; g.balance = balance;
+    g.Wg = weights->W_gate; g.Wu = weights->W_up; g.Wd = weights->W_down;
+    g.Wg_s = weights->Wg_s; g.Wu_s = weights->Wu_s; g.Wd_s = weights->Wd_s;
+    g.logits = logits; g.topk_idx = topk_idx; g.topk_w = topk_w; g.Y = Y;
+    g.counters = at<int>(ws, L.counters);
+    g.ncounters = L.ncounters; g.up_counters = L.up_counters;
+    g.part = at<float>(ws, L.part); g.up_part = at<float>(ws, L.up_part);
+    g.y_part = at<float>(ws, L.y_part); g.H = at<uint16_t>(ws, L.h);
+    MOE_TRY(launch_few(g, static_cast<hipStream_t>(stream)));
     return MOE_OK;
 }
 

@@ -337,6 +337,23 @@ hipError_t launch_i8_quant_weights(const uint16_t *W, int E, int K, int N, uint8
 hipError_t launch_schedule(const int *A, int R, int NK, int L, int c, int *M, int *S, int *phi,
                            long phi_rows, int *counts, int *flags, int *err, hipStream_t st);
 
+// The whole layer for a few tokens (few.hip).
+struct FewArgs {
+    int T = 0, d = 0, E = 0, k = 0, f = 0, fs = 0, S = 0;   // S: slices of the router's partial logits
+    ScoreArgs score;
+    const uint16_t *X = nullptr, *W_r = nullptr;
+    const float *bias = nullptr, *balance = nullptr;
+    const uint16_t *Wg = nullptr, *Wu = nullptr, *Wd = nullptr, *Wg_s = nullptr, *Wu_s = nullptr, *Wd_s = nullptr;
+    float *logits = nullptr, *topk_w = nullptr;
+    int *topk_idx = nullptr;
+    uint16_t *Y = nullptr;
+    int *counters = nullptr;           // see few.h
+    int ncounters = 0, up_counters = 0;
+    float *part = nullptr, *up_part = nullptr, *y_part = nullptr;
+    uint16_t *H = nullptr;
+};
+hipError_t launch_few(const FewArgs &g, hipStream_t st);
+
 // Joining a block to the residual stream, and its gradient (join.hip).
 enum JoinNorm { JOIN_NONE = 0, JOIN_RMS = 1, JOIN_LAYER = 2 };   // as moe_norm
 struct JoinArgs {
