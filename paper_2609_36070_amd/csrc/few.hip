@@ -31,290 +31,326 @@ namespace {
 constexpr float MASKED = -1e38f;
 
 // ---------------------------------------------------------------- router
-// Partial logits of a slice of the d axis: part [S][T][E].  W_r's rows go to RT
-// threads, V experts each; 1024 / RT rows at a time.  Clears the counters, too.
+// Partial logits of a slice of the d axis and 64 experts: part [S][T][E] (slices
+// at a pitch of g.pitch).  A row's experts go to 64 / V threads, V each; the weights
+// of up to 8 rows per thread are asked for before the tokens that meet them.
+// Clears the counters, too.
 template <int V, int TT>
-__global__ __launch_bounds__(1024) void few_router_kernel(FewArgs g, int RT) {
-    constexpr int CHUNK = 128, TC = TT < 4 ? TT : 4;
-    __shared__ float xs[TT][CHUNK];
-    __shared__ float red[TC][16][64 * V];
+__global__ __launch_bounds__(1024) void few_router_kernel(FewArgs g) {
+    constexpr int RT = 64 / V, RG = 1024 / RT, CHUNK = 512, NB = CHUNK / RG < 8 ? CHUNK / RG : 8;
+    constexpr int STEP = NB * RG;            // rows of a pass
+    __shared__ __attribute__((aligned(16))) float xs[STEP][TT];
+    __shared__ float red[16][TT][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (blockIdx.x == 0)
+    if (blockIdx.x == 0 && blockIdx.y == 0)
         for (int i = tid; i < g.ncounters; i += 1024) g.counters[i] = 0;
-    const int units = g.d / CHUNK, S = gridDim.x;
-    const int u0 = (int)((long)units * blockIdx.x / S), u1 = (int)((long)units * (blockIdx.x + 1) / S);
-    const int c = tid % RT, RG = 1024 / RT, rg = tid / RT, e0 = c * V;
+    const int units = g.d / 64, S = gridDim.x;
+    const int k0 = 64 * (int)((long)units * blockIdx.x / S), k1 = 64 * (int)((long)units * (blockIdx.x + 1) / S);
+    const int rg = tid / RT, e0 = 64 * blockIdx.y + tid % RT * V;
+    const uint16_t *Wr = g.W_r + (e0 < g.E ? e0 : 0);
     float acc[TT][V];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[t][v] = 0.f;
-    for (int u = u0; u < u1; ++u) {
-        const long k0 = (long)u * CHUNK;
-        for (int i = tid; i < TT * CHUNK; i += 1024) {
-            const int t = i / CHUNK;
-            xs[t][i % CHUNK] = t < g.T ? bf2f(g.X[(long)t * g.d + k0 + i % CHUNK]) : 0.f;
+    for (int base = k0; base < k1; base += STEP) {
+        uint16_t w[NB][V];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int r = base + rg + j * RG;
+            const uint16_t *p = Wr + (long)(r < k1 ? r : k0) * g.E;
+            if constexpr (V == 4) {
+                const u32x2_t q = ld_u32x2(p);
+                w[j][0] = (uint16_t)q[0]; w[j][1] = (uint16_t)(q[0] >> 16);
+                w[j][2] = (uint16_t)q[1]; w[j][3] = (uint16_t)(q[1] >> 16);
+            } else {
+                w[j][0] = *p;
+            }
+        }
+        if (base > k0) __syncthreads();
+        for (int i = tid; i < TT * STEP; i += 1024) {
+            const int t = i / STEP, r = i % STEP;
+            xs[r][t] = t < g.T && base + r < k1 ? bf2f(g.X[(long)t * g.d + base + r]) : 0.f;
         }
         __syncthreads();
-        if (e0 < g.E)
-            for (int r0 = rg; r0 < CHUNK; r0 += 8 * RG) {
-                uint16_t w[8][V];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int r = r0 + j * RG;
-                    const uint16_t *p = g.W_r + (k0 + (r < CHUNK ? r : r0)) * g.E + e0;
-                    if constexpr (V == 4) {
-                        const u32x2_t q = ld_u32x2(p);
-                        w[j][0] = (uint16_t)q[0]; w[j][1] = (uint16_t)(q[0] >> 16);
-                        w[j][2] = (uint16_t)q[1]; w[j][3] = (uint16_t)(q[1] >> 16);
-                    } else {
-                        w[j][0] = *p;
-                    }
-                }
+        for (int j = 0; j < NB; ++j) {
+            float x[TT];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int r = r0 + j * RG;
-                    if (r >= CHUNK) break;
+            for (int t = 0; t < TT; ++t) x[t] = xs[rg + j * RG][t];   // 0 past the slice
+            if (base + rg + j * RG < k1)
 #pragma unroll
-                    for (int t = 0; t < TT; ++t)
+                for (int t = 0; t < TT; ++t)
 #pragma unroll
-                        for (int v = 0; v < V; ++v) acc[t][v] = acc[t][v] + xs[t][r] * bf2f(w[j][v]);
-                }
-            }
-        __syncthreads();
+                    for (int v = 0; v < V; ++v) acc[t][v] = acc[t][v] + x[t] * bf2f(w[j][v]);
+        }
     }
     // rows of one wave, then the waves in order
+#pragma unroll
     for (int m = RT; m < 64; m <<= 1)
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[t][v] = acc[t][v] + shfl_xor_f(acc[t][v], m);
-    const int span = RT < 64 ? 1 : RT / 64;          // waves side by side in a row
+    if (lane < RT)
 #pragma unroll
-    for (int t0 = 0; t0 < TT; t0 += TC) {
-        if (t0 >= g.T) break;
+        for (int t = 0; t < TT; ++t)
 #pragma unroll
-        for (int t = 0; t < TC; ++t)
+            for (int v = 0; v < V; ++v) red[wave][t][lane * V + v] = acc[t][v];
+    __syncthreads();
+    const int t = tid / 64, e = 64 * blockIdx.y + lane;
+    if (t < g.T && t < TT && e < g.E) {
+        float s = red[0][t][lane];
 #pragma unroll
-            for (int v = 0; v < V; ++v) red[t][wave][lane * V + v] = acc[t0 + t][v];
-        __syncthreads();
-        for (int i = tid; i < TC * g.E; i += 1024) {
-            const int t = i / g.E, e = i % g.E;
-            if (t0 + t >= g.T) break;
-            const int cc = e / V, w0 = cc / 64, at = (cc % 64) * V + e % V;
-            float s = red[t][w0][at];
-            for (int w = w0 + span; w < 16; w += span) s = s + red[t][w][at];
-            g.part[((long)blockIdx.x * g.T + t0 + t) * g.E + e] = s;
-        }
-        __syncthreads();
+        for (int w = 1; w < 16; ++w) s = s + red[w][t][lane];
+        g.part[(long)blockIdx.x * g.pitch + t * g.E + e] = s;
     }
 }
 
 // ---------------------------------------------------------------- selection
-// The same for every lane: largest of the wave's values.
-DEV uint32_t wave_max(uint32_t v) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)v, m, 64);
-        v = o > v ? o : v;
-    }
+// Within rows of 16 lanes, the same for each of them: DPP moves within quads, then
+// mirrored half rows and rows.
+template <typename F>
+DEV float row16(float v, F f) {
+#define STEP(CTRL)                                                                              \
+    v = f(v, __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xF, 0xF, true)))
+    STEP(0xB1);
+    STEP(0x4E);
+    STEP(0x141);
+    STEP(0x140);
+#undef STEP
     return v;
 }
-DEV double wave_sum_d(double v) {
-#pragma unroll 1
-    for (int m = 1; m < 64; m <<= 1) {
-        const uint64_t b = (uint64_t)__double_as_longlong(v);
-        const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)b, m, 64);
-        const uint32_t hi = (uint32_t)__shfl_xor((int)(uint32_t)(b >> 32), m, 64);
-        v += __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
-    }
-    return v;
-}
-DEV double shfl_d(double v, int src) {
+DEV double shfl_xor_d(double v, int m) {
     const uint64_t b = (uint64_t)__double_as_longlong(v);
-    const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)b, src, 64);
-    const uint32_t hi = (uint32_t)__shfl((int)(uint32_t)(b >> 32), src, 64);
+    const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)b, m, 64);
+    const uint32_t hi = (uint32_t)__shfl_xor((int)(uint32_t)(b >> 32), m, 64);
     return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
-// Unsigned key with the order of the double, above 1.
+// Unsigned key with the order of the double, above 1, and back.
 DEV uint64_t rank_key(double v) {
     const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);   // -0 and 0 are one
     return (b >> 63) ? ~b : (b | (1ull << 63));
 }
+DEV double key_value(uint64_t k) {
+    return k <= 1 ? -INFINITY : __longlong_as_double((long long)((k >> 63) ? k & ~(1ull << 63) : ~k));
+}
+// a / b for 0 <= a < 2^24, rb = 1 / b rounded
+DEV int div24(int a, int b, float rb) {
+    int q = (int)((float)a * rb);
+    const int r = a - q * b;
+    q += r >= b ? 1 : 0;
+    q -= r < 0 ? 1 : 0;
+    return q;
+}
 
-// One token's experts, by one wave, ranked by 64-bit values as moe_route_scored
-// defines them; compact loops, since a call fetches this code from memory once.
-// z: its logits (LDS); val: room for E doubles; ids and w: its k places.
-DEV void select_token(const FewArgs &g, const float *z, double *val, int *ids, float *w, int lane) {
+constexpr int NW = 4, NT = 64 * NW, PITCH = 128 + 4;
+
+struct Select {                      // scratch of the start
+    __attribute__((aligned(16))) float z[FEW_MAX_T * 256];         // [T][E]
+    __attribute__((aligned(16))) uint32_t hi[FEW_MAX_T * 256];     // [T][E rounded up to 4]
+    double gs[FEW_MAX_T][64], sum[FEW_MAX_T];
+    float zmax[FEW_MAX_T], bal[256], w[FEW_MAX_T][16];
+    uint32_t kept[FEW_MAX_T][2], bits[FEW_MAX_T][8], mask[256];
+    int ids[FEW_MAX_T][16], slot_of[256], n[FEW_MAX_T], cnt[NW];
+};
+
+// The tokens' experts, as moe_route_scored defines them, by a whole workgroup:
+// from the logits in s.z and the balance in s.bal to s.ids and s.w (ascending ids),
+// and the tokens of each expert in s.mask.  Experts are ranked by 64-bit keys: an
+// expert is chosen if fewer than k of its token have a larger upper half, and
+// where that leaves more than k, those are ranked again by whole keys and ids.
+// lo: room for the lower halves.
+DEV void select_experts(const FewArgs &g, Select &s, uint32_t *lo, int tid) {
     const ScoreArgs &a = g.score;
-    const int E = g.E, n = E / a.groups, k = g.k;
-    const bool by_score = g.balance || (a.groups > 1 && a.pair);
+    const int T = g.T, E = g.E, EP = (E + 3) & ~3, k = g.k, G = a.groups, n = E / G;
+    const int lane = tid & 63, wave = tid >> 6;
+    const float rE = 1.0f / (float)E, rG = 1.0f / (float)G, rn = 1.0f / (float)n;
+    const bool by_score = g.balance || (G > 1 && a.pair);
     const bool row_sum = !a.sigmoid && (by_score || !a.renorm);
-    auto live = [&](int e) { return z[e] >= MASKED && (!g.balance || g.balance[e] >= MASKED); };
-    float zmax = -INFINITY;
-    double sum = 0.0;
-    if (row_sum) {
-        for (int e = lane; e < E; e += 64) zmax = fmaxf(zmax, live(e) ? fminf(z[e], FLT_MAX) : -INFINITY);
+    auto live = [&](int t, int e) { return s.z[t * E + e] >= MASKED && s.bal[e] >= MASKED; };
+    if (row_sum) {                   // a wave to a token
+#pragma unroll 1
+        for (int t = wave; t < T; t += NW) {
+            float m = -INFINITY;
+            for (int e = lane; e < E; e += 64) m = fmaxf(m, live(t, e) ? fminf(s.z[t * E + e], FLT_MAX) : -INFINITY);
 #pragma unroll
-        for (int m = 1; m < 64; m <<= 1) zmax = fmaxf(zmax, shfl_xor_f(zmax, m));
-    }
+            for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, shfl_xor_f(m, x));
+            double sum = 0.0;
 #pragma unroll 1
-    for (int e = lane; e < E; e += 64) {
-        double v = (double)fminf(z[e], FLT_MAX);
-        if (by_score || row_sum) {
-            const double x = exp(a.sigmoid ? -v : v - (double)zmax);
-            if (live(e)) sum += x;
-            if (by_score) v = a.sigmoid ? 1.0 / (1.0 + x) : x;
+            for (int e = lane; e < E; e += 64)
+                if (live(t, e)) sum += exp((double)fminf(s.z[t * E + e], FLT_MAX) - (double)m);
+#pragma unroll 1
+            for (int x = 1; x < 64; x <<= 1) sum += shfl_xor_d(sum, x);
+            if (lane == 0) {
+                s.zmax[t] = m;
+                s.sum[t] = sum;
+            }
         }
-        val[e] = v;
+        __syncthreads();
     }
-    if (row_sum) sum = wave_sum_d(sum);
 #pragma unroll 1
-    for (int e = lane; e < E; e += 64) {
-        double v = val[e];
+    for (int i = tid; i < T * E; i += NT) {
+        const int t = div24(i, E, rE), e = i - t * E;
+        double v = (double)fminf(s.z[i], FLT_MAX);
         if (by_score) {
-            if (!a.sigmoid) v = v / sum;
-            if (g.balance) v += (double)g.balance[e];
+            const double x = exp(a.sigmoid ? -v : v - (double)s.zmax[t]);
+            v = (a.sigmoid ? 1.0 / (1.0 + x) : x / s.sum[t]) + (double)s.bal[e];
         }
-        val[e] = live(e) ? v : -INFINITY;
+        const uint64_t key = live(t, e) ? rank_key(v) : 1;
+        s.hi[t * EP + e] = (uint32_t)(key >> 32);
+        lo[t * EP + e] = (uint32_t)key;
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    // groups: lpg lanes each
-    uint64_t kept = ~0ull;
-    int lpg = 64;
-    if (a.groups > 1) {
-        while (lpg * a.groups > 64) lpg >>= 1;
-        const int grp = lane / lpg;
-        double b1 = -INFINITY, b2 = -INFINITY;
-        if (grp < a.groups)
+    if (tid < T) {
+        for (int e = E; e < EP; ++e) s.hi[tid * EP + e] = 0;
+        s.n[tid] = 0;
+        s.kept[tid][0] = s.kept[tid][1] = 0;
+    }
+    if (tid < T * 8) s.bits[tid / 8][tid % 8] = 0;
+    __syncthreads();
+    auto key = [&](int t, int e) { return (uint64_t)s.hi[t * EP + e] << 32 | lo[t * EP + e]; };
+    if (G > 1) {
+        // 8 lanes to a group: its two best
 #pragma unroll 1
-            for (int i = lane % lpg; i < n; i += lpg) {
-                const double v = val[grp * n + i];
+        for (int i = tid; i < (T * G * 8 + 63) / 64 * 64; i += NT) {
+            const int j = i / 8 < T * G ? i / 8 : 0, t = div24(j, G, rG), o = j - t * G;
+            double b1 = -INFINITY, b2 = -INFINITY;
+#pragma unroll 1
+            for (int e = i % 8; e < n; e += 8) {
+                const double v = key_value(key(t, o * n + e));
                 b2 = fmax(b2, fmin(b1, v));
                 b1 = fmax(b1, v);
             }
 #pragma unroll 1
-        for (int m = 1; m < lpg; m <<= 1) {
-            const double o1 = shfl_d(b1, lane ^ m), o2 = shfl_d(b2, lane ^ m);
-            b2 = fmax(fmin(b1, o1), fmax(b2, o2));
-            b1 = fmax(b1, o1);
-        }
-        const double gs = a.pair && b2 > -INFINITY ? b1 + b2 : b1;
-        int better = 0;
-#pragma unroll 1
-        for (int o = 0; o < a.groups; ++o) {
-            const double og = shfl_d(gs, o * lpg);
-            better += og > gs || (og == gs && o < grp) ? 1 : 0;
-        }
-        kept = __ballot(better < a.top_groups);
-    }
-    // the lane's experts: `per` consecutive ones, so that lower lanes hold lower ids
-    const int per = (E + 63) / 64;
-    uint64_t key[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int e = lane * per + i;
-        key[i] = 0;
-        if (i < per && e < E && (a.groups == 1 || ((kept >> (e / n * lpg)) & 1)))
-            key[i] = val[e] > -INFINITY ? rank_key(val[e]) : 1;
-    }
-    uint32_t chosen = 0;
-#pragma unroll 1
-    for (int r = 0; r < k; ++r) {
-        uint64_t best = key[0];
-        int at = 0;
-#pragma unroll
-        for (int i = 1; i < 4; ++i)
-            if (key[i] > best) {
-                best = key[i];
-                at = i;
+            for (int m = 1; m < 8; m <<= 1) {
+                const double o1 = shfl_xor_d(b1, m), o2 = shfl_xor_d(b2, m);
+                b2 = fmax(fmin(b1, o1), fmax(b2, o2));
+                b1 = fmax(b1, o1);
             }
-        const uint32_t hi = (uint32_t)(best >> 32), lo = (uint32_t)best;
-        uint32_t m = wave_max(hi);
-        unsigned long long c = __ballot(hi == m);
-        if (c & (c - 1)) {
-            const uint32_t l = wave_max(hi == m ? lo : 0u);
-            c = __ballot(hi == m && lo == l);
+            if (i % 8 == 0 && i / 8 < T * G) s.gs[t][o] = a.pair && b2 > -INFINITY ? b1 + b2 : b1;
         }
-        if (lane == __builtin_ctzll(c)) {
-            chosen |= 1u << at;
+        __syncthreads();
+#pragma unroll 1
+        for (int i = tid; i < T * G; i += NT) {
+            const int t = div24(i, G, rG), o = i - t * G;
+            const double mine = s.gs[t][o];
+            int better = 0;
+#pragma unroll 4
+            for (int q = 0; q < G; ++q) {
+                const double v = s.gs[t][q];
+                better += v > mine || (v == mine && q < o) ? 1 : 0;
+            }
+            if (better < a.top_groups) atomicOr(&s.kept[t][o >> 5], 1u << (o & 31));
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int i = tid; i < T * E; i += NT) {
+            const int t = div24(i, E, rE), e = i - t * E, o = div24(e, n, rn);
+            if (!((s.kept[t][o >> 5] >> (o & 31)) & 1)) s.hi[t * EP + e] = lo[t * EP + e] = 0;
+        }
+        __syncthreads();
+    }
+#pragma unroll 1
+    for (int i = tid; i < T * E; i += NT) {
+        const int t = div24(i, E, rE), e = i - t * E;
+        const uint32_t mine = s.hi[t * EP + e];
+        const u32x4_t *row = reinterpret_cast<const u32x4_t *>(s.hi + t * EP);
+        int above = 0;
+#pragma unroll 4
+        for (int o = 0; o < EP / 4; ++o) {
+            const u32x4_t v = row[o];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i == at) key[i] = 0;
+            for (int q = 0; q < 4; ++q) above += v[q] > mine ? 1 : 0;
+        }
+        if (above < k) {
+            atomicAdd(&s.n[t], 1);
+            atomicOr(&s.bits[t][e >> 5], 1u << (e & 31));
         }
     }
-    // places in ascending id
-    int before = 0;
-    const unsigned long long below = (1ull << lane) - 1;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) before += __popcll(__ballot((chosen >> i) & 1) & below);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if ((chosen >> i) & 1) ids[before++] = lane * per + i;
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    // weights: lane j takes place j; renormalised ones are ratios of scores, taken
-    // to the largest of them, so that scores that underflow together keep theirs
-    const int id = lane < k ? ids[lane] : 0;
-    const bool on = lane < k && live(id);
-    const float zc = on ? fminf(z[id], FLT_MAX) : 0.f;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < T * E; i += NT) {          // more than k: ties of the upper halves
+        const int t = div24(i, E, rE), e = i - t * E;
+        if (s.n[t] == k || !((s.bits[t][e >> 5] >> (e & 31)) & 1)) continue;
+        const uint64_t mine = key(t, e);
+        int above = 0;
+#pragma unroll 1
+        for (int o = 0; o < E; ++o) {
+            const uint64_t v = key(t, o);
+            above += v > mine || (v == mine && o < e) ? 1 : 0;
+        }
+        if (above >= k) atomicAnd(&s.bits[t][e >> 5], ~(1u << (e & 31)));
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < T * E; i += NT) {          // places in ascending id
+        const int t = div24(i, E, rE), e = i - t * E;
+        const uint32_t b = s.bits[t][e >> 5];
+        if (!((b >> (e & 31)) & 1)) continue;
+        int at = __popc(b & ((1u << (e & 31)) - 1));
+        for (int q = 0; q < (e >> 5); ++q) at += __popc(s.bits[t][q]);
+        s.ids[t][at] = e;
+        atomicOr(&s.mask[e], 1u << t);
+    }
+    __syncthreads();
+    // weights, 16 lanes to a token: renormalised ones are ratios of scores, taken to
+    // the largest of them, so that scores that underflow together keep theirs
+    const int t = tid / 16, j = tid % 16;
+    const bool route = t < T && j < k;
+    const int id = route ? s.ids[t][j] : 0;
+    const bool on = route && live(t, id);
+    const float zc = on ? fminf(s.z[t * E + id], FLT_MAX) : 0.f;
     float u = 0.f, total = 1.f;
     if (a.renorm) {
-        float m = on ? (a.sigmoid ? fminf(zc, 0.f) : zc) : -INFINITY;
-#pragma unroll
-        for (int x = 1; x < 16; x <<= 1) m = fmaxf(m, shfl_xor_f(m, x));
-        const float x = expf((a.sigmoid ? fminf(zc, 0.f) : zc) - m);
+        const float c = a.sigmoid ? fminf(zc, 0.f) : zc;
+        const float m = row16(on ? c : -INFINITY, [](float x, float y) { return fmaxf(x, y); });
+        const float x = expf(c - m);
         if (on) u = a.sigmoid ? x / (1.0f + expf(-fabsf(zc))) : x;
-        total = u;
-#pragma unroll
-        for (int x = 1; x < 16; x <<= 1) total = total + shfl_xor_f(total, x);
+        total = row16(u, [](float x, float y) { return x + y; });
     } else if (on) {
-        const float x = expf(a.sigmoid ? -zc : zc - zmax);
-        u = a.sigmoid ? 1.0f / (1.0f + x) : x / (float)sum;
+        const float x = expf(a.sigmoid ? -zc : zc - s.zmax[t]);
+        u = a.sigmoid ? 1.0f / (1.0f + x) : x / (float)s.sum[t];
     }
-    if (lane < k) w[lane] = u > 0.f ? a.scale * (u / total) : 0.f;
+    if (route) s.w[t][j] = u > 0.f ? a.scale * (u / total) : 0.f;
 }
 
 // ---------------------------------------------------------------- the layer
-// Waits between workgroups.  A producer's waves have stored, wait for that
-// (vmcnt), meet at a barrier, and one thread adds to a counter with release; a
-// consumer's thread polls, and its workgroup acquires behind a barrier.  Waits end
-// after 0.2 s in any case (wall clock of 100 MHz), with the error word set.
+// Waits between workgroups.  What one workgroup writes for others goes through
+// its XCD's L2 to memory (agent-scope stores); its waves wait for that, meet at a
+// barrier, and one thread adds to a counter.  A consumer's thread polls the counter
+// and its workgroup passes a barrier; what it then loads was never read before in
+// this launch, so no cache holds an older copy.  A release and an acquire
+// instead write back and invalidate whole caches: 2 to 5 us for each tile.  Waits
+// end after 0.2 s in any case (wall clock of 100 MHz), with the error word set.
 constexpr unsigned long long WAIT_TICKS = 20000000ull;
 DEV void poll(const int *ctr, int need, int *err) {
     const unsigned long long t0 = wall_clock64();
     while (__hip_atomic_load(ctr, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < need) {
-        if (__hip_atomic_load(err, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) return;
         if (wall_clock64() - t0 > WAIT_TICKS) {
             __hip_atomic_store(err, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             return;
         }
-        __builtin_amdgcn_s_sleep(1);
+        __builtin_amdgcn_s_sleep(4);
     }
 }
-DEV void acquire() { __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent"); }
+DEV void st_agent(void *p, f32x4_t v) {
+    const u32x4_t u = __builtin_bit_cast(u32x4_t, v);
+    uint64_t *q = reinterpret_cast<uint64_t *>(p);
+    __hip_atomic_store(q, (uint64_t)u[1] << 32 | u[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(q + 1, (uint64_t)u[3] << 32 | u[2], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+DEV void st_agent(void *p, uint32_t lo, uint32_t hi) {
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), (uint64_t)hi << 32 | lo, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+// This wave's stores have arrived, but for the LATER loads that followed them.
+template <int LATER>
 DEV void stores_done() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
 }
-DEV int add_release(int *ctr) {
-    return __hip_atomic_fetch_add(ctr, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-}
+DEV int add(int *ctr) { return __hip_atomic_fetch_add(ctr, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-constexpr int NW = 4, PITCH = 128 + 4;
-
-struct Select {                      // scratch of the start
-    float z[FEW_MAX_T * 256];
-    double val[NW][256];
-    int ids[FEW_MAX_T][16];
-    float w[FEW_MAX_T][16];
-    uint32_t mask[256];
-    int slot_of[256];
-    int cnt[NW];
-};
-
-__global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
+__global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
     __shared__ __attribute__((aligned(16))) union {
         float red[NW][16][PITCH];
         Select sel;
@@ -326,50 +362,65 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g4 = lane >> 4;
     const int T = g.T, d = g.d, f = g.f, fs = g.fs;
-    int *err = g.counters, *queue = g.counters + 1, *h_done = g.counters + 4;
-    int *up_done = h_done + 257, *down_done = up_done + g.up_counters;
+    int *err = g.counters, *queue = err + FEW_LINE, *h_done = queue + FEW_LINE;     // h_done: a line each
+    int *up_done = h_done + 257 * FEW_LINE, *down_done = up_done + g.up_counters;
 
-    if (tid == 0) s_next = __hip_atomic_fetch_add(queue, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    int next = 0;
+    if (tid == 0) next = add(queue);
     // ---------------- routing: every workgroup for itself ----------------
     {
         Select &s = sh.sel;
-        for (int i = tid; i < T * g.E; i += 64 * NW) {
-            float v = 0.f;
-#pragma unroll 4
-            for (int q = 0; q < g.S; ++q) v = v + g.part[(long)q * T * g.E + i];
-            if (g.bias) v = v + g.bias[i % g.E];
-            s.z[i] = v;
+        const float my_bias = g.bias && tid < g.E ? g.bias[tid] : 0.f;
+        const float my_bal = g.balance && tid < g.E ? g.balance[tid] : 0.f;
+        // slices added in order, all of them under way at once
+        for (int i = 4 * tid; i < T * g.E; i += 4 * NT) {
+            f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f}, u[FEW_ROUTER_SLICES];
+#pragma unroll
+            for (int q = 0; q < FEW_ROUTER_SLICES; ++q)
+                u[q] = *reinterpret_cast<const f32x4_t *>(g.part + (long)(q < g.S ? q : 0) * g.pitch + i);
+#pragma unroll
+            for (int q = 0; q < FEW_ROUTER_SLICES; ++q)
+                if (q < g.S)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) v[p] = v[p] + u[q][p];
+            *reinterpret_cast<f32x4_t *>(s.z + i) = v;
         }
+        s.bal[tid] = my_bal;
         s.mask[tid] = 0;
         __syncthreads();
-#pragma unroll 1
-        for (int t = wave; t < T; t += NW)
-            select_token(g, s.z + t * g.E, s.val[wave], s.ids[t], s.w[t], lane);
-        __syncthreads();
-        const int t = tid / 16, j = tid % 16;
-        const bool route = t < T && j < g.k;
-        if (route) atomicOr(&s.mask[s.ids[t][j]], 1u << t);
-        __syncthreads();
-        const unsigned long long b = __ballot(s.mask[tid] != 0);
+        if (g.bias) {
+            if (tid < g.E)
+                for (int t = 0; t < T; ++t) s.z[t * g.E + tid] = s.z[t * g.E + tid] + my_bias;
+            __syncthreads();
+        }
+        select_experts(g, s, reinterpret_cast<uint32_t *>(s_w), tid);
+        // slots: the experts that some token chose
+        const uint32_t m = s.mask[tid];
+        const unsigned long long b = __ballot(m != 0);
         if (lane == 0) s.cnt[wave] = __popcll(b);
         __syncthreads();
         int at = __popcll(b & ((1ull << lane) - 1));
         for (int w = 0; w < wave; ++w) at += s.cnt[w];
-        if (s.mask[tid]) {
+        if (m) {
             s_list[at] = tid;
-            s_mask[at] = (int)s.mask[tid];
+            s_mask[at] = (int)m;
             s.slot_of[tid] = at;
         }
+        if (tid == 0) {
+            s_last = s.cnt[0] + s.cnt[1] + s.cnt[2] + s.cnt[3];
+            s_next = next;
+        }
         __syncthreads();
-        if (route) s_w[s.slot_of[s.ids[t][j]]][t] = s.w[t][j];
-        if (blockIdx.x == 0) {
-            if (route) {
+        const int t = tid / 16, j = tid % 16;
+        if (t < T && j < g.k) {
+            s_w[s.slot_of[s.ids[t][j]]][t] = s.w[t][j];
+            if (blockIdx.x == 0) {
                 g.topk_idx[t * g.k + j] = s.ids[t][j];
                 g.topk_w[t * g.k + j] = s.w[t][j];
             }
-            for (int i = tid; i < T * g.E; i += 64 * NW) g.logits[i] = s.z[i];
         }
-        if (tid == 0) s_last = s.cnt[0] + s.cnt[1] + s.cnt[2] + s.cnt[3];
+        if (blockIdx.x == 0)
+            for (int i = tid; i < T * g.E; i += NT) g.logits[i] = s.z[i];
         __syncthreads();
     }
     const int slots = __builtin_amdgcn_readfirstlane(s_last);
@@ -378,6 +429,10 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
     const int ks = few_slices(up_tiles, d / FEW_UNIT);
     const int cols = d / FEW_DOWN_COLS, ds = few_slices(cols, units);
     const int up_items = up_tiles * ks, items = up_items + cols * ds;
+    // units of a slice; the first ones have one more
+    const int up_q = d / FEW_UNIT / ks, up_r = d / FEW_UNIT % ks, down_q = units / ds, down_r = units % ds;
+    const float r_ks = 1.0f / (float)ks, r_up = 1.0f / (float)up_e, r_cols = 1.0f / (float)cols,
+                r_fu = 1.0f / (float)fu;
 
     // ---------------- items ----------------
     struct Item {
@@ -389,30 +444,29 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
         Item it;
         it.up = q < up_items;
         if (it.up) {
-            it.tile = q / ks;
+            it.tile = div24(q, ks, r_ks);
             it.s = q - it.tile * ks;
-            const int n = d / FEW_UNIT;
-            it.u0 = (int)((long)n * it.s / ks);
-            it.u1 = (int)((long)n * (it.s + 1) / ks);
+            it.u0 = it.s * up_q + min(it.s, up_r);
+            it.u1 = it.u0 + up_q + (it.s < up_r ? 1 : 0);
             if (it.tile < up_sh) {
                 it.slot = -1;
                 it.n0 = it.tile * FEW_UP_COLS;
             } else {
-                it.slot = (it.tile - up_sh) / up_e;
+                it.slot = div24(it.tile - up_sh, up_e, r_up);
                 it.n0 = (it.tile - up_sh - it.slot * up_e) * FEW_UP_COLS;
             }
         } else {
-            it.s = (q - up_items) / cols;
+            it.s = div24(q - up_items, cols, r_cols);
             it.tile = q - up_items - it.s * cols;
             it.n0 = it.tile * FEW_DOWN_COLS;
-            it.u0 = (int)((long)units * it.s / ds);
-            it.u1 = (int)((long)units * (it.s + 1) / ds);
+            it.u0 = it.s * down_q + min(it.s, down_r);
+            it.u1 = it.u0 + down_q + (it.s < down_r ? 1 : 0);
             it.slot = 0;
         }
         return it;
     };
     // slot of a unit of the down product's K, -1 for the shared expert's
-    auto slot_of = [&](int u) { return u < su ? -1 : (u - su) / fu; };
+    auto slot_of = [&](int u) { return u < su ? -1 : div24(u - su, fu, r_fu); };
     const int kw = 32 * wave + 8 * g4;          // the lane's first row of a step
     auto down_ptr = [&](int u, int n0) {
         const int s = slot_of(u);
@@ -470,8 +524,7 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
         else load(w0, down_ptr(it.u0, it.n0), d);
     }
     while (q < items) {
-        int next = 0;
-        if (tid == 0) next = __hip_atomic_fetch_add(queue, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (tid == 0) next = add(queue);
         clear(acc);
         f32x4_t total[8];
         if (it.up) {
@@ -502,11 +555,10 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
             const int sa = slot_of(it.u0), sb = slot_of(it.u1 - 1);
             if (tid <= sb - sa) {
                 const int s = sa + tid;
-                poll(h_done + 1 + s, s < 0 ? up_sh : up_e, err);
+                poll(h_done + FEW_LINE * (1 + s), s < 0 ? up_sh : up_e, err);
             }
-            if (tid == 0 && sb - sa == 256) poll(h_done + 1 + sb, up_e, err);
+            if (tid == 0 && sb - sa == 256) poll(h_done + FEW_LINE * (1 + sb), up_e, err);
             __syncthreads();
-            acquire();
             const uint16_t *hp = H + ((long)it.u0 * T + tok) * FEW_UNIT + kw;
             u32x4_t h0 = ld_u32x4(hp), l0 = ld_u32x4(hp + plane), h1, l1;
             int s = sa;
@@ -559,10 +611,8 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
         const Item cur = it;
         q = __builtin_amdgcn_readfirstlane(s_next);
         it = decode(q);
-        if (q < items) {
-            if (it.up) load(w0, up_ptr(it), it.slot < 0 ? fs : f);
-            else load(w0, down_ptr(it.u0, it.n0), d);
-        }
+        const uint16_t *np = q >= items ? g.X : it.up ? up_ptr(it) : down_ptr(it.u0, it.n0);
+        const long nld = q >= items ? 0 : it.up ? (it.slot < 0 ? fs : f) : d;
         // a thread finishes 4 columns of tokens et and et + 8
         const int en = 4 * (tid & 31);
         f32x4_t v[2];
@@ -577,29 +627,31 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
                 for (int p = 0; p < 4; ++p) v[eh][p] = v[eh][p] + u[p];
             }
         }
-        // Slices of K: each leaves its sums, the last one to come adds all of them in order.
+        // Slices of K: each leaves its sums, [tile][slice][T][128], and the last one
+        // to come adds all of them in order.  The next item's first loads follow the
+        // stores.
         const int slices = cur.up ? ks : ds;
         bool finish = true;
         if (slices > 1) {
-            // [tile][slice][T][128]
             float *base = (cur.up ? g.up_part : g.y_part) + (long)cur.tile * slices * T * 128;
 #pragma unroll
             for (int eh = 0; eh < 2; ++eh) {
                 const int et = (tid >> 5) + 8 * eh;
-                if (et < T) *reinterpret_cast<f32x4_t *>(base + ((long)cur.s * T + et) * 128 + en) = v[eh];
+                if (et < T) st_agent(base + ((long)cur.s * T + et) * 128 + en, v[eh]);
             }
-            stores_done();
-            if (tid == 0) s_last = add_release((cur.up ? up_done : down_done) + cur.tile) == slices - 1;
+            load(w0, np, nld);
+            stores_done<8>();
+            __syncthreads();
+            if (tid == 0) s_last = add((cur.up ? up_done : down_done) + cur.tile) == slices - 1;
             __syncthreads();
             finish = s_last != 0;
             if (finish) {
-                acquire();
 #pragma unroll
                 for (int eh = 0; eh < 2; ++eh) {
                     const int et = (tid >> 5) + 8 * eh;
                     v[eh] = f32x4_t{0.f, 0.f, 0.f, 0.f};
                     if (et < T)
-#pragma unroll 4
+#pragma unroll 8
                         for (int i = 0; i < slices; ++i) {
                             const f32x4_t u = *reinterpret_cast<const f32x4_t *>(base + ((long)i * T + et) * 128 + en);
 #pragma unroll
@@ -625,13 +677,20 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
                 }
                 if (et < T && en < FEW_UP_COLS) {
                     uint16_t *p = g.H + ((long)unit * T + et) * FEW_UNIT + cur.n0 % FEW_UNIT + en;
-                    *reinterpret_cast<u32x2_t *>(p) = u32x2_t{pack_bf2(h[0], h[1]), pack_bf2(h[2], h[3])};
-                    *reinterpret_cast<u32x2_t *>(p + plane) = u32x2_t{pack_bf2(l[0], l[1]), pack_bf2(l[2], l[3])};
+                    st_agent(p, pack_bf2(h[0], h[1]), pack_bf2(h[2], h[3]));
+                    st_agent(p + plane, pack_bf2(l[0], l[1]), pack_bf2(l[2], l[3]));
                 }
             }
-            stores_done();
-            if (tid == 0) add_release(h_done + 1 + cur.slot);
+            if (slices > 1) {
+                stores_done<0>();
+            } else {
+                load(w0, np, nld);
+                stores_done<8>();
+            }
+            __syncthreads();
+            if (tid == 0) add(h_done + FEW_LINE * (1 + cur.slot));
         } else if (finish) {
+            if (slices == 1) load(w0, np, nld);
 #pragma unroll
             for (int eh = 0; eh < 2; ++eh) {
                 const int et = (tid >> 5) + 8 * eh;
@@ -648,11 +707,9 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(FewArgs g) {
 
 hipError_t launch_few(const FewArgs &g, hipStream_t st) {
     if (g.T <= 0) return hipSuccess;
-    int RT = 1;
-    const int V = g.E % 4 ? 1 : 4;
-    while (RT * V < g.E) RT *= 2;
-#define FEW_ROUTER(V, TT) few_router_kernel<V, TT><<<dim3(g.S), dim3(1024), 0, st>>>(g, RT)
-    if (V == 4) {
+#define FEW_ROUTER(V, TT)                                                                             \
+    few_router_kernel<V, TT><<<dim3((unsigned)g.S, (unsigned)((g.E + 63) / 64)), dim3(1024), 0, st>>>(g)
+    if (g.E % 4 == 0) {
         if (g.T == 1) FEW_ROUTER(4, 1);
         else if (g.T <= 4) FEW_ROUTER(4, 4);
         else FEW_ROUTER(4, 16);
@@ -664,6 +721,6 @@ hipError_t launch_few(const FewArgs &g, hipStream_t st) {
 #undef FEW_ROUTER
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    few_kernel<<<dim3(FEW_WGS), dim3(64 * NW), 0, st>>>(g);
+    few_kernel<<<dim3(FEW_WGS), dim3(NT), 0, st>>>(g);
     return hipGetLastError();
 }

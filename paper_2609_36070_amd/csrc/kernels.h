@@ -348,7 +348,7 @@ struct FewArgs {
     int *topk_idx = nullptr;
     uint16_t *Y = nullptr;
     int *counters = nullptr;           // see few.h
-    int ncounters = 0, up_counters = 0;
+    int ncounters = 0, up_counters = 0, pitch = 0;   // pitch: floats between slices of part
     float *part = nullptr, *up_part = nullptr, *y_part = nullptr;
     uint16_t *H = nullptr;
 };
