@@ -31,79 +31,72 @@ namespace {
 constexpr float MASKED = -1e38f;
 
 // ---------------------------------------------------------------- router
-// Partial logits of a slice of the d axis and 64 experts: part [S][T][E] (slices
-// at a pitch of g.pitch).  A row's experts go to 64 / V threads, V each; the weights
-// of up to 8 rows per thread are asked for before the tokens that meet them.
-// Clears the counters, too.
-template <int V, int TT>
-__global__ __launch_bounds__(1024) void few_router_kernel(FewArgs g) {
-    constexpr int RT = 64 / V, RG = 1024 / RT, CHUNK = 512, NB = CHUNK / RG < 8 ? CHUNK / RG : 8;
-    constexpr int STEP = NB * RG;            // rows of a pass
-    __shared__ __attribute__((aligned(16))) float xs[STEP][TT];
-    __shared__ float red[16][TT][64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (blockIdx.x == 0 && blockIdx.y == 0)
-        for (int i = tid; i < g.ncounters; i += 1024) g.counters[i] = 0;
-    const int units = g.d / 64, S = gridDim.x;
-    const int k0 = 64 * (int)((long)units * blockIdx.x / S), k1 = 64 * (int)((long)units * (blockIdx.x + 1) / S);
-    const int rg = tid / RT, e0 = 64 * blockIdx.y + tid % RT * V;
-    const uint16_t *Wr = g.W_r + (e0 < g.E ? e0 : 0);
-    float acc[TT][V];
+// Partial logits of a slice of the d axis and 16 V experts: part [S][T][E] (slices at a
+// pitch of g.pitch).  As the layer's tiles below: a wave's step is 32 rows, a lane
+// loads V experts of 8 rows as they lie, the tokens are the column operand; the
+// 8 waves' sums meet in LDS in order.  Clears the counters, too.
+constexpr int RW = 8;
+template <int V>
+__global__ __launch_bounds__(64 * RW) void few_router_kernel(FewArgs g) {
+    constexpr int NB = 4, COLS = 16 * V;     // steps under way, experts
+    __shared__ float red[RW][FEW_MAX_T][COLS + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g4 = lane >> 4;
+    const int steps = g.d / 32, S = gridDim.x, eb = COLS * blockIdx.y;
+    const int s0 = (int)((long)steps * blockIdx.x / S), s1 = (int)((long)steps * (blockIdx.x + 1) / S);
+    const uint16_t *Wr = g.W_r + (eb + V * r < g.E ? eb + V * r : 0);
+    const uint16_t *X = g.X + (long)(r < g.T ? r : g.T - 1) * g.d + 8 * g4;
+    f32x4_t acc[V];
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
+    for (int i = 0; i < V; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int b = s0 + wave; b < s1; b += NB * RW) {
+        u32x4_t x[NB];
+        uint32_t w[NB][8][(V + 1) / 2];
 #pragma unroll
-        for (int v = 0; v < V; ++v) acc[t][v] = 0.f;
-    for (int base = k0; base < k1; base += STEP) {
-        uint16_t w[NB][V];
+        for (int n = 0; n < NB; ++n) {
+            const int st = min(b + n * RW, s1 - 1);
+            x[n] = ld_u32x4(X + 32l * st);
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const int r = base + rg + j * RG;
-            const uint16_t *p = Wr + (long)(r < k1 ? r : k0) * g.E;
-            if constexpr (V == 4) {
-                const u32x2_t q = ld_u32x2(p);
-                w[j][0] = (uint16_t)q[0]; w[j][1] = (uint16_t)(q[0] >> 16);
-                w[j][2] = (uint16_t)q[1]; w[j][3] = (uint16_t)(q[1] >> 16);
-            } else {
-                w[j][0] = *p;
+            for (int j = 0; j < 8; ++j) {
+                const uint16_t *p = Wr + (32l * st + 8 * g4 + j) * g.E;
+                if constexpr (V == 4) {
+                    const u32x2_t q = ld_u32x2(p);
+                    w[n][j][0] = q[0];
+                    w[n][j][1] = q[1];
+                } else {
+                    w[n][j][0] = *p;
+                }
             }
         }
-        if (base > k0) __syncthreads();
-        for (int i = tid; i < TT * STEP; i += 1024) {
-            const int t = i / STEP, r = i % STEP;
-            xs[r][t] = t < g.T && base + r < k1 ? bf2f(g.X[(long)t * g.d + base + r]) : 0.f;
-        }
-        __syncthreads();
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            float x[TT];
+        for (int n = 0; n < NB; ++n) {
+            if (b + n * RW >= s1) break;
 #pragma unroll
-            for (int t = 0; t < TT; ++t) x[t] = xs[rg + j * RG][t];   // 0 past the slice
-            if (base + rg + j * RG < k1)
+            for (int i = 0; i < V; ++i) {
+                u32x4_t a;
 #pragma unroll
-                for (int t = 0; t < TT; ++t)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) acc[t][v] = acc[t][v] + x[t] * bf2f(w[j][v]);
+                for (int q = 0; q < 4; ++q)
+                    a[q] = __builtin_amdgcn_perm(w[n][2 * q + 1][i >> 1], w[n][2 * q][i >> 1],
+                                                 (i & 1) ? 0x07060302u : 0x05040100u);
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
+                                                                 __builtin_bit_cast(bf16x8_t, x[n]), acc[i], 0, 0, 0);
+            }
         }
     }
-    // rows of one wave, then the waves in order
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = tid; i < g.ncounters; i += 64 * RW) g.counters[i] = 0;
+    // accumulators: lane (g4, r), register p of product i: expert V (4 g4 + p) + i, token r
 #pragma unroll
-    for (int m = RT; m < 64; m <<= 1)
+    for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-#pragma unroll
-            for (int v = 0; v < V; ++v) acc[t][v] = acc[t][v] + shfl_xor_f(acc[t][v], m);
-    if (lane < RT)
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-#pragma unroll
-            for (int v = 0; v < V; ++v) red[wave][t][lane * V + v] = acc[t][v];
+        for (int p = 0; p < 4; ++p) red[wave][r][V * (4 * g4 + p) + i] = acc[i][p];
     __syncthreads();
-    const int t = tid / 64, e = 64 * blockIdx.y + lane;
-    if (t < g.T && t < TT && e < g.E) {
-        float s = red[0][t][lane];
+    for (int i = tid; i < g.T * COLS; i += 64 * RW) {
+        const int t = i / COLS, c = i % COLS;
+        if (eb + c >= g.E) continue;
+        float s = red[0][t][c];
 #pragma unroll
-        for (int w = 1; w < 16; ++w) s = s + red[w][t][lane];
-        g.part[(long)blockIdx.x * g.pitch + t * g.E + e] = s;
+        for (int w = 1; w < RW; ++w) s = s + red[w][t][c];
+        g.part[(long)blockIdx.x * g.pitch + t * g.E + eb + c] = s;
     }
 }
 
@@ -146,160 +139,180 @@ DEV int div24(int a, int b, float rb) {
 
 constexpr int NW = 4, NT = 64 * NW, PITCH = 128 + 4;
 
+// The largest of the wave's values, the same for every lane: DPP moves within rows and to
+// the next rows, then the last lane's.
+DEV uint32_t wave_max(uint32_t v) {
+    auto step = [&](int o) { v = (uint32_t)o > v ? (uint32_t)o : v; };
+    step(__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));
+    step(__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));
+    step(__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true));
+    step(__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true));
+    step(__builtin_amdgcn_update_dpp((int)v, (int)v, 0x142, 0xA, 0xF, false));   // lane 15 to the next row
+    step(__builtin_amdgcn_update_dpp((int)v, (int)v, 0x143, 0xC, 0xF, false));   // lane 31 to the upper half
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+// LDS written by a wave and read by its other lanes
+DEV void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 struct Select {                      // scratch of the start
     __attribute__((aligned(16))) float z[FEW_MAX_T * 256];         // [T][E]
-    __attribute__((aligned(16))) uint32_t hi[FEW_MAX_T * 256];     // [T][E rounded up to 4]
-    double gs[FEW_MAX_T][64], sum[FEW_MAX_T];
-    float zmax[FEW_MAX_T], bal[256], w[FEW_MAX_T][16];
-    uint32_t kept[FEW_MAX_T][2], bits[FEW_MAX_T][8], mask[256];
-    int ids[FEW_MAX_T][16], slot_of[256], n[FEW_MAX_T], cnt[NW];
+    float bal[256], w[FEW_MAX_T][16], zmax[FEW_MAX_T], sum[FEW_MAX_T];
+    uint32_t mask[256];
+    int ids[FEW_MAX_T][16], slot_of[256], cnt[NW];
+    __attribute__((aligned(16))) struct {
+        uint64_t key[256];           // then the candidates
+        uint32_t top[64];
+        double gs[64];
+    } wave[NW];
 };
 
-// The tokens' experts, as moe_route_scored defines them, by a whole workgroup:
-// from the logits in s.z and the balance in s.bal to s.ids and s.w (ascending ids),
-// and the tokens of each expert in s.mask.  Experts are ranked by 64-bit keys: an
-// expert is chosen if fewer than k of its token have a larger upper half, and
-// where that leaves more than k, those are ranked again by whole keys and ids.
-// lo: room for the lower halves.
-DEV void select_experts(const FewArgs &g, Select &s, uint32_t *lo, int tid) {
+// One token's experts, as moe_route_scored defines them, by one wave: from its logits z
+// to k ascending ids, each also in s.mask.  Lane l holds experts l, 64 + l, ...  Experts
+// are ranked by 64-bit keys; only those can be chosen whose key's upper half is not
+// below the k-th largest of the lanes' best ones, mostly few more than k, and where
+// these are more than k they are ranked by whole keys and ids.  Loops stay compact:
+// every call fetches this code from memory.
+DEV void select_experts(const FewArgs &g, Select &s, int t, int wave, int lane) {
     const ScoreArgs &a = g.score;
-    const int T = g.T, E = g.E, EP = (E + 3) & ~3, k = g.k, G = a.groups, n = E / G;
-    const int lane = tid & 63, wave = tid >> 6;
-    const float rE = 1.0f / (float)E, rG = 1.0f / (float)G, rn = 1.0f / (float)n;
+    const int E = g.E, k = g.k, G = a.groups, n = E / G;
+    const float *z = s.z + t * E;
+    auto &m = s.wave[wave];
     const bool by_score = g.balance || (G > 1 && a.pair);
-    const bool row_sum = !a.sigmoid && (by_score || !a.renorm);
-    auto live = [&](int t, int e) { return s.z[t * E + e] >= MASKED && s.bal[e] >= MASKED; };
-    if (row_sum) {                   // a wave to a token
-#pragma unroll 1
-        for (int t = wave; t < T; t += NW) {
-            float m = -INFINITY;
-            for (int e = lane; e < E; e += 64) m = fmaxf(m, live(t, e) ? fminf(s.z[t * E + e], FLT_MAX) : -INFINITY);
+    auto live = [&](int e) { return z[e] >= MASKED && s.bal[e] >= MASKED; };
+    float zmax = -INFINITY;
+    double sum = 0.0;
+    if (!a.sigmoid && (by_score || !a.renorm)) {     // the softmax's sum
+        for (int e = lane; e < E; e += 64) zmax = fmaxf(zmax, live(e) ? fminf(z[e], FLT_MAX) : -INFINITY);
 #pragma unroll
-            for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, shfl_xor_f(m, x));
-            double sum = 0.0;
+        for (int x = 1; x < 64; x <<= 1) zmax = fmaxf(zmax, shfl_xor_f(zmax, x));
 #pragma unroll 1
-            for (int e = lane; e < E; e += 64)
-                if (live(t, e)) sum += exp((double)fminf(s.z[t * E + e], FLT_MAX) - (double)m);
+        for (int e = lane; e < E; e += 64)
+            if (live(e)) sum += exp((double)fminf(z[e], FLT_MAX) - (double)zmax);
 #pragma unroll 1
-            for (int x = 1; x < 64; x <<= 1) sum += shfl_xor_d(sum, x);
-            if (lane == 0) {
-                s.zmax[t] = m;
-                s.sum[t] = sum;
-            }
+        for (int x = 1; x < 64; x <<= 1) sum += shfl_xor_d(sum, x);
+        if (lane == 0) {
+            s.zmax[t] = zmax;
+            s.sum[t] = (float)sum;
         }
-        __syncthreads();
     }
 #pragma unroll 1
-    for (int i = tid; i < T * E; i += NT) {
-        const int t = div24(i, E, rE), e = i - t * E;
-        double v = (double)fminf(s.z[i], FLT_MAX);
+    for (int e = lane; e < E; e += 64) {
+        double v = (double)fminf(z[e], FLT_MAX);
         if (by_score) {
-            const double x = exp(a.sigmoid ? -v : v - (double)s.zmax[t]);
-            v = (a.sigmoid ? 1.0 / (1.0 + x) : x / s.sum[t]) + (double)s.bal[e];
+            const double x = exp(a.sigmoid ? -v : v - (double)zmax);
+            v = (a.sigmoid ? 1.0 / (1.0 + x) : x / sum) + (double)s.bal[e];
         }
-        const uint64_t key = live(t, e) ? rank_key(v) : 1;
-        s.hi[t * EP + e] = (uint32_t)(key >> 32);
-        lo[t * EP + e] = (uint32_t)key;
+        m.key[e] = live(e) ? rank_key(v) : 1;        // a key of 0 is no expert
     }
-    if (tid < T) {
-        for (int e = E; e < EP; ++e) s.hi[tid * EP + e] = 0;
-        s.n[tid] = 0;
-        s.kept[tid][0] = s.kept[tid][1] = 0;
-    }
-    if (tid < T * 8) s.bits[tid / 8][tid % 8] = 0;
-    __syncthreads();
-    auto key = [&](int t, int e) { return (uint64_t)s.hi[t * EP + e] << 32 | lo[t * EP + e]; };
+    wave_sync();
+    uint64_t kept = ~0ull;                           // by group
     if (G > 1) {
-        // 8 lanes to a group: its two best
+        int lpg = 32;                                // lanes to a group
+        while (lpg * G > 64) lpg >>= 1;
+        const int o = lane / lpg;
+        double b1 = -INFINITY, b2 = -INFINITY;
+        if (o < G)
 #pragma unroll 1
-        for (int i = tid; i < (T * G * 8 + 63) / 64 * 64; i += NT) {
-            const int j = i / 8 < T * G ? i / 8 : 0, t = div24(j, G, rG), o = j - t * G;
-            double b1 = -INFINITY, b2 = -INFINITY;
-#pragma unroll 1
-            for (int e = i % 8; e < n; e += 8) {
-                const double v = key_value(key(t, o * n + e));
+            for (int e = lane % lpg; e < n; e += lpg) {
+                const double v = key_value(m.key[o * n + e]);
                 b2 = fmax(b2, fmin(b1, v));
                 b1 = fmax(b1, v);
             }
 #pragma unroll 1
-            for (int m = 1; m < 8; m <<= 1) {
-                const double o1 = shfl_xor_d(b1, m), o2 = shfl_xor_d(b2, m);
-                b2 = fmax(fmin(b1, o1), fmax(b2, o2));
-                b1 = fmax(b1, o1);
-            }
-            if (i % 8 == 0 && i / 8 < T * G) s.gs[t][o] = a.pair && b2 > -INFINITY ? b1 + b2 : b1;
+        for (int x = 1; x < lpg; x <<= 1) {
+            const double o1 = shfl_xor_d(b1, x), o2 = shfl_xor_d(b2, x);
+            b2 = fmax(fmin(b1, o1), fmax(b2, o2));
+            b1 = fmax(b1, o1);
         }
-        __syncthreads();
-#pragma unroll 1
-        for (int i = tid; i < T * G; i += NT) {
-            const int t = div24(i, G, rG), o = i - t * G;
-            const double mine = s.gs[t][o];
-            int better = 0;
+        if (o < G && lane % lpg == 0) m.gs[o] = a.pair && b2 > -INFINITY ? b1 + b2 : b1;
+        wave_sync();
+        const double mine = m.gs[lane < G ? lane : 0];
+        int better = 0;
 #pragma unroll 4
-            for (int q = 0; q < G; ++q) {
-                const double v = s.gs[t][q];
-                better += v > mine || (v == mine && q < o) ? 1 : 0;
-            }
-            if (better < a.top_groups) atomicOr(&s.kept[t][o >> 5], 1u << (o & 31));
+        for (int q = 0; q < G; ++q) {
+            const double v = m.gs[q];
+            better += v > mine || (v == mine && q < lane) ? 1 : 0;
         }
-        __syncthreads();
-#pragma unroll 1
-        for (int i = tid; i < T * E; i += NT) {
-            const int t = div24(i, E, rE), e = i - t * E, o = div24(e, n, rn);
-            if (!((s.kept[t][o >> 5] >> (o & 31)) & 1)) s.hi[t * EP + e] = lo[t * EP + e] = 0;
-        }
-        __syncthreads();
+        kept = __ballot(lane < G && better < a.top_groups);
     }
-#pragma unroll 1
-    for (int i = tid; i < T * E; i += NT) {
-        const int t = div24(i, E, rE), e = i - t * E;
-        const uint32_t mine = s.hi[t * EP + e];
-        const u32x4_t *row = reinterpret_cast<const u32x4_t *>(s.hi + t * EP);
-        int above = 0;
-#pragma unroll 4
-        for (int o = 0; o < EP / 4; ++o) {
-            const u32x4_t v = row[o];
+    const float rn = 1.0f / (float)n;
+    uint64_t key[4];
+    uint32_t top = 0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) above += v[q] > mine ? 1 : 0;
-        }
-        if (above < k) {
-            atomicAdd(&s.n[t], 1);
-            atomicOr(&s.bits[t][e >> 5], 1u << (e & 31));
-        }
+    for (int q = 0; q < 4; ++q) {
+        const int e = lane + 64 * q;
+        key[q] = 0;
+        if (e < E && ((kept >> (G > 1 ? div24(e, n, rn) : 0)) & 1)) key[q] = m.key[e];
+        top = max(top, (uint32_t)(key[q] >> 32));
     }
-    __syncthreads();
-#pragma unroll 1
-    for (int i = tid; i < T * E; i += NT) {          // more than k: ties of the upper halves
-        const int t = div24(i, E, rE), e = i - t * E;
-        if (s.n[t] == k || !((s.bits[t][e >> 5] >> (e & 31)) & 1)) continue;
-        const uint64_t mine = key(t, e);
-        int above = 0;
-#pragma unroll 1
-        for (int o = 0; o < E; ++o) {
-            const uint64_t v = key(t, o);
-            above += v > mine || (v == mine && o < e) ? 1 : 0;
+    m.top[lane] = top;
+    wave_sync();
+    int above = 0;
+    {
+        u32x4_t v[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) v[q] = *reinterpret_cast<const u32x4_t *>(&m.top[4 * q]);
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+#pragma unroll
+            for (int p = 0; p < 4; ++p) above += v[q][p] > top ? 1 : 0;
+    }
+    const uint32_t least = ~wave_max(above < k ? ~top : 0u);
+    unsigned long long cand[4];
+    int count = 0;
+    const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        cand[q] = __ballot(key[q] != 0 && (uint32_t)(key[q] >> 32) >= least);
+        count += __popcll(cand[q]);
+    }
+    if (count > k) {
+        // the candidates in ascending id: of equal keys, the one before is better
+        int at[4], first = 0;
+        wave_sync();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            at[q] = first + __popcll(cand[q] & below);
+            if ((cand[q] >> lane) & 1) m.key[at[q]] = key[q];
+            first += __popcll(cand[q]);
         }
-        if (above >= k) atomicAnd(&s.bits[t][e >> 5], ~(1u << (e & 31)));
+        wave_sync();
+        int better[4] = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int o = 0; o < count; ++o) {
+            const uint64_t v = m.key[o];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) better[q] += v > key[q] || (v == key[q] && o < at[q]) ? 1 : 0;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) cand[q] &= __ballot(better[q] < k);
     }
-    __syncthreads();
-#pragma unroll 1
-    for (int i = tid; i < T * E; i += NT) {          // places in ascending id
-        const int t = div24(i, E, rE), e = i - t * E;
-        const uint32_t b = s.bits[t][e >> 5];
-        if (!((b >> (e & 31)) & 1)) continue;
-        int at = __popc(b & ((1u << (e & 31)) - 1));
-        for (int q = 0; q < (e >> 5); ++q) at += __popc(s.bits[t][q]);
-        s.ids[t][at] = e;
-        atomicOr(&s.mask[e], 1u << t);
+    int first = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if ((cand[q] >> lane) & 1) {
+            s.ids[t][first + __popcll(cand[q] & below)] = lane + 64 * q;
+            atomicOr(&s.mask[lane + 64 * q], 1u << t);
+        }
+        first += __popcll(cand[q]);
     }
-    __syncthreads();
-    // weights, 16 lanes to a token: renormalised ones are ratios of scores, taken to
-    // the largest of them, so that scores that underflow together keep theirs
+    wave_sync();                                     // m is free again
+}
+
+// The weights of the tokens' experts, 16 lanes to a token: renormalised ones are ratios
+// of scores, taken to the largest of them, so that scores that underflow together
+// keep theirs.
+DEV void weigh_experts(const FewArgs &g, Select &s, int tid) {
+    const ScoreArgs &a = g.score;
     const int t = tid / 16, j = tid % 16;
-    const bool route = t < T && j < k;
+    const bool route = t < g.T && j < g.k;
     const int id = route ? s.ids[t][j] : 0;
-    const bool on = route && live(t, id);
-    const float zc = on ? fminf(s.z[t * E + id], FLT_MAX) : 0.f;
+    const float z = route ? s.z[t * g.E + id] : 0.f;
+    const bool on = route && z >= MASKED && s.bal[id] >= MASKED;
+    const float zc = on ? fminf(z, FLT_MAX) : 0.f;
     float u = 0.f, total = 1.f;
     if (a.renorm) {
         const float c = a.sigmoid ? fminf(zc, 0.f) : zc;
@@ -309,7 +322,7 @@ DEV void select_experts(const FewArgs &g, Select &s, uint32_t *lo, int tid) {
         total = row16(u, [](float x, float y) { return x + y; });
     } else if (on) {
         const float x = expf(a.sigmoid ? -zc : zc - s.zmax[t]);
-        u = a.sigmoid ? 1.0f / (1.0f + x) : x / (float)s.sum[t];
+        u = a.sigmoid ? 1.0f / (1.0f + x) : x / s.sum[t];
     }
     if (route) s.w[t][j] = u > 0.f ? a.scale * (u / total) : 0.f;
 }
@@ -366,7 +379,6 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
     int *up_done = h_done + 257 * FEW_LINE, *down_done = up_done + g.up_counters;
 
     int next = 0;
-    if (tid == 0) next = add(queue);
     // ---------------- routing: every workgroup for itself ----------------
     {
         Select &s = sh.sel;
@@ -385,6 +397,7 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
                     for (int p = 0; p < 4; ++p) v[p] = v[p] + u[q][p];
             *reinterpret_cast<f32x4_t *>(s.z + i) = v;
         }
+        if (tid == 0) next = add(queue);     // after the loads: they return in order
         s.bal[tid] = my_bal;
         s.mask[tid] = 0;
         __syncthreads();
@@ -393,7 +406,10 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
                 for (int t = 0; t < T; ++t) s.z[t * g.E + tid] = s.z[t * g.E + tid] + my_bias;
             __syncthreads();
         }
-        select_experts(g, s, reinterpret_cast<uint32_t *>(s_w), tid);
+#pragma unroll 1
+        for (int t = wave; t < T; t += NW) select_experts(g, s, t, wave, lane);
+        __syncthreads();
+        weigh_experts(g, s, tid);
         // slots: the experts that some token chose
         const uint32_t m = s.mask[tid];
         const unsigned long long b = __ballot(m != 0);
@@ -707,18 +723,10 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
 
 hipError_t launch_few(const FewArgs &g, hipStream_t st) {
     if (g.T <= 0) return hipSuccess;
-#define FEW_ROUTER(V, TT)                                                                             \
-    few_router_kernel<V, TT><<<dim3((unsigned)g.S, (unsigned)((g.E + 63) / 64)), dim3(1024), 0, st>>>(g)
-    if (g.E % 4 == 0) {
-        if (g.T == 1) FEW_ROUTER(4, 1);
-        else if (g.T <= 4) FEW_ROUTER(4, 4);
-        else FEW_ROUTER(4, 16);
-    } else {
-        if (g.T == 1) FEW_ROUTER(1, 1);
-        else if (g.T <= 4) FEW_ROUTER(1, 4);
-        else FEW_ROUTER(1, 16);
-    }
-#undef FEW_ROUTER
+    if (g.E % 4 == 0)
+        few_router_kernel<4><<<dim3((unsigned)g.S, (unsigned)((g.E + 63) / 64)), dim3(64 * RW), 0, st>>>(g);
+    else
+        few_router_kernel<1><<<dim3((unsigned)g.S, (unsigned)((g.E + 15) / 16)), dim3(64 * RW), 0, st>>>(g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     few_kernel<<<dim3(FEW_WGS), dim3(NT), 0, st>>>(g);
