@@ -375,9 +375,13 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g4 = lane >> 4;
     const int T = g.T, d = g.d, f = g.f, fs = g.fs;
-    int *err = g.counters, *queue = err + FEW_LINE, *h_done = queue + FEW_LINE;     // h_done: a line each
+    int *err = g.counters, *queue = err + FEW_LINE, *h_done = queue + (1 + FEW_QUEUES) * FEW_LINE;
     int *up_done = h_done + 257 * FEW_LINE, *down_done = up_done + g.up_counters;
 
+    // A workgroup's first item comes from one of FEW_QUEUES counters (item FEW_QUEUES i +
+    // q for the i-th that asks counter q: adds to one counter take 12 ns each, 6 us for
+    // all workgroups), the others in order from `queue`.
+    int *firsts = queue + FEW_LINE;
     int next = 0;
     // ---------------- routing: every workgroup for itself ----------------
     {
@@ -397,7 +401,7 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
                     for (int p = 0; p < 4; ++p) v[p] = v[p] + u[q][p];
             *reinterpret_cast<f32x4_t *>(s.z + i) = v;
         }
-        if (tid == 0) next = add(queue);     // after the loads: they return in order
+        if (tid == 0) next = add(firsts + blockIdx.x % FEW_QUEUES * FEW_LINE);   // after the loads: they return in order
         s.bal[tid] = my_bal;
         s.mask[tid] = 0;
         __syncthreads();
@@ -424,7 +428,7 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
         }
         if (tid == 0) {
             s_last = s.cnt[0] + s.cnt[1] + s.cnt[2] + s.cnt[3];
-            s_next = next;
+            s_next = FEW_QUEUES * next + blockIdx.x % FEW_QUEUES;
         }
         __syncthreads();
         const int t = tid / 16, j = tid % 16;
@@ -442,8 +446,8 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
     const int slots = __builtin_amdgcn_readfirstlane(s_last);
     const int fu = f / FEW_UNIT, su = fs / FEW_UNIT, units = su + slots * fu;
     const int up_sh = fs / FEW_UP_COLS, up_e = f / FEW_UP_COLS, up_tiles = up_sh + slots * up_e;
-    const int ks = few_slices(up_tiles, d / FEW_UNIT);
-    const int cols = d / FEW_DOWN_COLS, ds = few_slices(cols, units);
+    const int ks = few_slices(up_tiles, d / FEW_UNIT, FEW_UP_ITEMS, 2);
+    const int cols = d / FEW_DOWN_COLS, ds = few_slices(cols, units, FEW_DOWN_ITEMS, 3);
     const int up_items = up_tiles * ks, items = up_items + cols * ds;
     // units of a slice; the first ones have one more
     const int up_q = d / FEW_UNIT / ks, up_r = d / FEW_UNIT % ks, down_q = units / ds, down_r = units % ds;
@@ -535,17 +539,61 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
 
     int q = __builtin_amdgcn_readfirstlane(s_next);
     Item it = decode(q);
-    if (q < items) {
-        if (it.up) load(w0, up_ptr(it), it.slot < 0 ? fs : f);
-        else load(w0, down_ptr(it.u0, it.n0), d);
+    const uint16_t *np = it.up ? up_ptr(it) : g.X;
+    long nld = it.up ? (it.slot < 0 ? fs : f) : 0;
+    if (q < items && !it.up) {
+        np = down_ptr(it.u0, it.n0);
+        nld = d;
     }
+    load(w0, np, nld);
+    // Before its first wait a workgroup looks whether all first items of the up product
+    // are taken; one that is not belongs to a workgroup which has not started, and it
+    // does that item itself, its own one (`held`) after it.
+    const int first_ups = min((int)gridDim.x, up_items);
+    bool waits = false;
+    int held = -1;
     while (q < items) {
-        if (tid == 0) next = add(queue);
+        if (!it.up && !waits) {
+            if (wave == 0) {
+                int i = -1;
+                for (;;) {
+                    const int c = __hip_atomic_load(firsts + lane % FEW_QUEUES * FEW_LINE, __ATOMIC_RELAXED,
+                                                    __HIP_MEMORY_SCOPE_AGENT);
+                    const unsigned long long left =
+                        __ballot(lane < FEW_QUEUES && FEW_QUEUES * c + lane < first_ups);
+                    if (!left) break;
+                    const int from = __builtin_ctzll(left);
+                    int n = 0;
+                    if (lane == 0) n = add(firsts + from * FEW_LINE);
+                    n = FEW_QUEUES * __builtin_amdgcn_readfirstlane(n) + from;
+                    if (n < first_ups) {
+                        i = n;
+                        break;
+                    }
+                }
+                if (lane == 0) s_next = i;
+            }
+            __syncthreads();
+            const int i = __builtin_amdgcn_readfirstlane(s_next);
+            __syncthreads();
+            waits = i < 0;
+            if (i >= 0) {
+                held = q;
+                q = i;
+                it = decode(q);
+                np = up_ptr(it);
+                nld = it.slot < 0 ? fs : f;
+                load(w0, np, nld);
+            }
+        }
+        // the next item is asked for early, but by an item that waits not before it has
+        // what it waited for: others would have nothing
+        if (tid == 0 && held < 0 && it.up) next = add(queue) + gridDim.x;
         clear(acc);
         f32x4_t total[8];
         if (it.up) {
             const long ld = it.slot < 0 ? fs : f;
-            const uint16_t *wp = up_ptr(it);
+            const uint16_t *wp = np;
             const uint16_t *xp = g.X + (long)tok * d + (long)it.u0 * FEW_UNIT + kw;
             u32x4_t x0 = ld_u32x4(xp), x1;
 #pragma unroll 1
@@ -575,10 +623,11 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
             }
             if (tid == 0 && sb - sa == 256) poll(h_done + FEW_LINE * (1 + sb), up_e, err);
             __syncthreads();
+            if (tid == 0) next = add(queue) + gridDim.x;
             const uint16_t *hp = H + ((long)it.u0 * T + tok) * FEW_UNIT + kw;
             u32x4_t h0 = ld_u32x4(hp), l0 = ld_u32x4(hp + plane), h1, l1;
             int s = sa;
-            const uint16_t *wp = down_ptr(it.u0, it.n0);
+            const uint16_t *wp = np;
 #pragma unroll 1
             for (int u = it.u0; u < it.u1; ++u) {
                 h1 = ld_u32x4(hp + 128);
@@ -622,13 +671,18 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
             for (int h = 0; h < 2; ++h)
                 *reinterpret_cast<f32x4_t *>(&sh.red[wave][r][8 * (4 * g4 + p) + 4 * h]) =
                     f32x4_t{acc[4 * h][p], acc[4 * h + 1][p], acc[4 * h + 2][p], acc[4 * h + 3][p]};
-        if (tid == 0) s_next = next;
+        if (tid == 0) s_next = held < 0 ? next : held;
+        held = -1;
         __syncthreads();
         const Item cur = it;
         q = __builtin_amdgcn_readfirstlane(s_next);
         it = decode(q);
-        const uint16_t *np = q >= items ? g.X : it.up ? up_ptr(it) : down_ptr(it.u0, it.n0);
-        const long nld = q >= items ? 0 : it.up ? (it.slot < 0 ? fs : f) : d;
+        np = g.X;                            // none left: anything, once
+        nld = 0;
+        if (q < items) {
+            np = it.up ? up_ptr(it) : down_ptr(it.u0, it.n0);
+            nld = it.up ? (it.slot < 0 ? fs : f) : d;
+        }
         // a thread finishes 4 columns of tokens et and et + 8
         const int en = 4 * (tid & 31);
         f32x4_t v[2];
@@ -643,45 +697,19 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
                 for (int p = 0; p < 4; ++p) v[eh][p] = v[eh][p] + u[p];
             }
         }
-        // Slices of K: each leaves its sums, [tile][slice][T][128], and the last one
-        // to come adds all of them in order.  The next item's first loads follow the
-        // stores.
-        const int slices = cur.up ? ks : ds;
-        bool finish = true;
-        if (slices > 1) {
-            float *base = (cur.up ? g.up_part : g.y_part) + (long)cur.tile * slices * T * 128;
+        // the sums of the whole K: H of an up tile, Y of a down tile
+        auto finish = [&]() {
 #pragma unroll
             for (int eh = 0; eh < 2; ++eh) {
                 const int et = (tid >> 5) + 8 * eh;
-                if (et < T) st_agent(base + ((long)cur.s * T + et) * 128 + en, v[eh]);
-            }
-            load(w0, np, nld);
-            stores_done<8>();
-            __syncthreads();
-            if (tid == 0) s_last = add((cur.up ? up_done : down_done) + cur.tile) == slices - 1;
-            __syncthreads();
-            finish = s_last != 0;
-            if (finish) {
-#pragma unroll
-                for (int eh = 0; eh < 2; ++eh) {
-                    const int et = (tid >> 5) + 8 * eh;
-                    v[eh] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                if (!cur.up) {
                     if (et < T)
-#pragma unroll 8
-                        for (int i = 0; i < slices; ++i) {
-                            const f32x4_t u = *reinterpret_cast<const f32x4_t *>(base + ((long)i * T + et) * 128 + en);
-#pragma unroll
-                            for (int p = 0; p < 4; ++p) v[eh][p] = v[eh][p] + u[p];
-                        }
+                        *reinterpret_cast<u32x2_t *>(g.Y + (long)et * d + cur.n0 + en) =
+                            u32x2_t{pack_bf2(v[eh][0], v[eh][1]), pack_bf2(v[eh][2], v[eh][3])};
+                    continue;
                 }
-            }
-        }
-        if (finish && cur.up) {
-            // the first half of a token's threads hold the gate, the second the up columns
-            const int unit = (cur.slot < 0 ? 0 : su + cur.slot * fu) + cur.n0 / FEW_UNIT;
-#pragma unroll
-            for (int eh = 0; eh < 2; ++eh) {
-                const int et = (tid >> 5) + 8 * eh;
+                // the first half of a token's threads hold the gate, the second the up columns
+                const int unit = (cur.slot < 0 ? 0 : su + cur.slot * fu) + cur.n0 / FEW_UNIT;
                 float h[4], l[4];
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
@@ -697,25 +725,52 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
                     st_agent(p + plane, pack_bf2(l[0], l[1]), pack_bf2(l[2], l[3]));
                 }
             }
-            if (slices > 1) {
-                stores_done<0>();
-            } else {
-                load(w0, np, nld);
-                stores_done<8>();
-            }
-            __syncthreads();
-            if (tid == 0) add(h_done + FEW_LINE * (1 + cur.slot));
-        } else if (finish) {
-            if (slices == 1) load(w0, np, nld);
+        };
+        // Slices of K: each leaves its sums, [tile][slice][T][128], and the last one
+        // to come adds all of them in order.
+        const int slices = cur.up ? ks : ds;
+        float *base = (cur.up ? g.up_part : g.y_part) + (long)cur.tile * slices * T * 128;
+        if (slices > 1) {
 #pragma unroll
             for (int eh = 0; eh < 2; ++eh) {
                 const int et = (tid >> 5) + 8 * eh;
+                if (et < T) st_agent(base + ((long)cur.s * T + et) * 128 + en, v[eh]);
+            }
+        } else {
+            finish();
+        }
+        // the next item's first loads follow the stores
+        asm volatile("" ::: "memory");
+        load(w0, np, nld);
+        stores_done<8>();
+        __syncthreads();
+        int *h_ctr = h_done + FEW_LINE * (1 + cur.slot);
+        if (slices == 1) {
+            if (tid == 0 && cur.up) add(h_ctr);
+            continue;
+        }
+        if (tid == 0) s_last = add((cur.up ? up_done : down_done) + cur.tile) == slices - 1;
+        __syncthreads();
+        if (s_last) {
+#pragma unroll
+            for (int eh = 0; eh < 2; ++eh) {
+                const int et = (tid >> 5) + 8 * eh;
+                v[eh] = f32x4_t{0.f, 0.f, 0.f, 0.f};
                 if (et < T)
-                    *reinterpret_cast<u32x2_t *>(g.Y + (long)et * d + cur.n0 + en) =
-                        u32x2_t{pack_bf2(v[eh][0], v[eh][1]), pack_bf2(v[eh][2], v[eh][3])};
+#pragma unroll 8
+                    for (int i = 0; i < slices; ++i) {
+                        const f32x4_t u = *reinterpret_cast<const f32x4_t *>(base + ((long)i * T + et) * 128 + en);
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) v[eh][p] = v[eh][p] + u[p];
+                    }
+            }
+            finish();
+            if (cur.up) {
+                stores_done<0>();
+                __syncthreads();
+                if (tid == 0) add(h_ctr);
             }
         }
-        __syncthreads();                     // red and s_last are free again
     }
 }
 
