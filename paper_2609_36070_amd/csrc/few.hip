@@ -334,8 +334,8 @@ DEV void weigh_experts(const FewArgs &g, Select &s, int tid) {
 // and its workgroup passes a barrier; what it then loads was never read before in
 // this launch, so no cache holds an older copy.  A release and an acquire
 // instead write back and invalidate whole caches: 2 to 5 us for each tile.  Waits
-// end after 0.2 s in any case (wall clock of 100 MHz), with the error word set.
-constexpr unsigned long long WAIT_TICKS = 20000000ull;
+// end after 2 s in any case (wall clock of 100 MHz), with the error word set.
+constexpr unsigned long long WAIT_TICKS = 200000000ull;
 DEV void poll(const int *ctr, int need, int *err) {
     const unsigned long long t0 = wall_clock64();
     while (__hip_atomic_load(ctr, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < need) {

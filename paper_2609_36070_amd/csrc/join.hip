@@ -44,8 +44,15 @@ DEV Words philox(uint64_t seed, uint64_t offset, uint32_t chunk, uint32_t row) {
     }
     return Words{{c0, c1, c2, c3}};
 }
-DEV bool kept(const Words &w, int i, uint32_t out) {
-    return (i & 1 ? w.w[i >> 1] >> 16 : w.w[i >> 1] & 0xffffu) >= out;
+// n where kept, else 0; out: what an element's 16 bits must reach
+DEV f32x8 drop8(const f32x8 &n, const Words &w, uint32_t out) {
+    f32x8 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = (uint16_t)w.w[i] >= (uint16_t)out ? n[2 * i] : 0.f;
+        v[2 * i + 1] = w.w[i] >= out << 16 ? n[2 * i + 1] : 0.f;
+    }
+    return v;
 }
 
 // ---------------------------------------------------------------- rows
@@ -92,38 +99,67 @@ DEV f32x8 put(void *p, long i, const f32x8 &v) {
 }
 
 // ---------------------------------------------------------------- sums over a row
-DEV float wave_sum(float v) {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) v = v + shfl_xor_f(v, m);
+template <int CTRL>
+DEV float add_peer(float v) {
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+template <int CTRL, int ROWS>
+DEV float add_before(float v) {
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xF, false));
+}
+// Over N = 1, 2, 4, 8 or 16 neighbouring lanes, the same in each: quads, then
+// mirrored half rows and rows.
+template <int N>
+DEV float lanes_sum(float v) {
+    if constexpr (N > 1) v = add_peer<0xB1>(v);
+    if constexpr (N > 2) v = add_peer<0x4E>(v);
+    if constexpr (N > 4) v = add_peer<0x141>(v);
+    if constexpr (N > 8) v = add_peer<0x140>(v);
     return v;
 }
+// Over the wave, in its last lane.
+DEV float wave_sum_last(float v) {
+    v = lanes_sum<16>(v);
+    v = add_before<0x142, 0xA>(v);           // lane 15 of the row before
+    return add_before<0x143, 0xC>(v);        // lane 31
+}
 // N sums over the G threads of a row, the same in each of them.  Rows of more
-// than a wave meet in `red` (a slot per wave, N used of 4), which must not be
-// written again before every thread has passed another barrier: callers
-// alternate between slots.
-template <int G, int NT, int N>
+// than a wave meet in `red` (a slot per wave), which must not be written again
+// before every thread has passed another barrier: callers alternate.
+template <int G, int N>
 DEV void row_sums(float (&v)[N], float (*red)[4]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
-    if constexpr (G > 64) {
-        const int wave = threadIdx.x >> 6, w0 = wave / (G / 64) * (G / 64);
-        if ((threadIdx.x & 63) == 0)
+    for (int i = 0; i < N; ++i) v[i] = wave_sum_last(v[i]);
+    if constexpr (G == 64) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[i]), 63));
+    } else {
+        constexpr int W = G / 64;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        if (lane == 63)
 #pragma unroll
             for (int i = 0; i < N; ++i) red[wave][i] = v[i];
         __syncthreads();
+        const float *from = red[wave / W * W + lane % W];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float s = red[w0][i];
-#pragma unroll
-            for (int w = 1; w < G / 64; ++w) s = s + red[w0 + w][i];
-            v[i] = s;
-        }
+        for (int i = 0; i < N; ++i) v[i] = lanes_sum<W>(from[i]);
     }
+}
+DEV float sum8(const f32x8 &v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
+DEV f32x8 zero8() { return f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
+
+// The pointer, for loads that are to stay where they are: weights that the compiler
+// moves out of the loop over the rows take registers that the sums need.
+DEV const float *again(const float *p) {
+    asm volatile("" : "+s"(p));
+    return p;
 }
 
 DEV float dev_inv(float var, float eps) { return 1.0f / sqrtf(var + eps); }
 
 // ---------------------------------------------------------------- forward
+// Values past the row's end are loaded as zeros.
 template <bool F32, int G, int CH>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArgs g) {
     constexpr int NT = G < 256 ? 256 : G, NW = NT / 64;
@@ -142,87 +178,79 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
     for (int c = 0; c < CH; ++c) {
         col[c] = 8 * (lane + G * c);
         ok[c] = col[c] < g.d;
-        if (!ok[c]) col[c] = 0;
-        xr[c].load(g.x, t * g.d + col[c]);
-        if (g.y) yr[c].load(g.y, t * g.d + col[c]);
+        if (ok[c]) {
+            xr[c].load(g.x, t * g.d + col[c]);
+        } else {
+            col[c] = 0;
+            xr[c].clear();
+        }
     }
-    f32x8 r[CH];
+    if (g.y)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            yr[c].clear();
+            if (ok[c]) yr[c].load(g.y, t * g.d + col[c]);
+        }
     float ym = 0.f, ys = 0.f, rm = 0.f, rs = 0.f;
-    // mean and deviation of the rows in v, two sums one after the other
+    // mean and 1 / deviation of the row in v
     auto stats = [&](const f32x8 (&v)[CH], int kind, float eps, float &m, float &s, int at) {
         float sum[1] = {0.f};
-        m = 0.f;
         if (kind == JOIN_LAYER) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[0] = sum[0] + (ok[c] ? v[c][i] : 0.f);
-            row_sums<G, NT>(sum, red[at]);
+            for (int c = 0; c < CH; ++c) sum[0] = sum[0] + sum8(v[c]);
+            row_sums<G>(sum, red[at]);
             m = sum[0] * inv_d;
-        }
-        sum[0] = 0.f;
+            sum[0] = 0.f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float u = v[c][i] - m;
-                sum[0] = sum[0] + (ok[c] ? u * u : 0.f);
+            for (int c = 0; c < CH; ++c) {
+                const f32x8 u = v[c] - m;
+                const float q = sum8(u * u);
+                sum[0] = sum[0] + (ok[c] ? q : 0.f);
             }
-        row_sums<G, NT>(sum, red[at + 1]);
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) sum[0] = sum[0] + sum8(v[c] * v[c]);
+        }
+        row_sums<G>(sum, red[at + 1]);
         s = dev_inv(sum[0] * inv_d, eps);
     };
-    auto normed = [&](const f32x8 &v, float m, float s, const float *w, const float *b, int at) {
-        f32x8 n;
-        f32x8 wv, bv;
-        if (w) wv = ld_f32x8(w + at);
-        if (b) bv = ld_f32x8(b + at);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            n[i] = (v[i] - m) * s;
-            if (w) n[i] = n[i] * wv[i];
-            if (b) n[i] = n[i] + bv[i];
-        }
+    auto normed = [&](const f32x8 &v, int kind, float m, float s, const float *w, const float *b, int at) {
+        f32x8 n = kind == JOIN_LAYER ? (v - m) * s : v * s;
+        if (w) n = n * ld_f32x8(w + at);
+        if (b) n = n + ld_f32x8(b + at);
         return n;
     };
+    f32x8 r[CH];
     if (g.y) {
-        f32x8 v[CH];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) v[c] = yr[c].get();
+        for (int c = 0; c < CH; ++c) r[c] = yr[c].get();
         if (g.y_norm) {
-            stats(v, g.y_norm, g.y_eps, ym, ys, 0);
+            stats(r, g.y_norm, g.y_eps, ym, ys, 0);
 #pragma unroll
-            for (int c = 0; c < CH; ++c) v[c] = normed(v[c], ym, ys, g.y_weight, g.y_bias, col[c]);
+            for (int c = 0; c < CH; ++c) r[c] = normed(r[c], g.y_norm, ym, ys, g.y_weight, g.y_bias, col[c]);
         }
         uint64_t seed = 0, offset = 0;
         if (g.rng) {
             seed = (uint64_t)g.rng[0];
             offset = (uint64_t)g.rng[1];
         }
-        const float tg = g.token_gate ? g.token_gate[t] : 1.f;
+        const float a = g.scale * g.keep * (g.token_gate ? g.token_gate[t] : 1.f);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            f32x8 a;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] = g.scale;
-            if (g.gate) {
-                const f32x8 w = ld_f32x8(g.gate + col[c]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) a[i] = a[i] * w[i];
-            }
-            if (g.rng) {
-                const Words w = philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[c][i] = kept(w, i, g.out) ? v[c][i] * g.keep : 0.f;
-            }
-            const f32x8 x = xr[c].get();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r[c][i] = x[i] + a[i] * tg * v[c][i];
+            f32x8 v = r[c];
+            if (g.gate) v = v * ld_f32x8(g.gate + col[c]);
+            v = v * a;
+            if (g.rng) v = drop8(v, philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t), g.out);
+            r[c] = xr[c].get() + v;
             if constexpr (!F32) {
                 Raw<false> q;
                 q.a = pack_bf8(r[c]);
                 r[c] = q.get();
+                if (on && ok[c]) st_u32x4((uint16_t *)g.r + (t * g.d + col[c]), q.a);
+            } else {
+                if (on && ok[c]) st_f32x8((float *)g.r + (t * g.d + col[c]), r[c]);
             }
-            if (on && ok[c]) put<F32>(g.r, t * g.d + col[c], r[c]);
+            if (!ok[c]) r[c] = zero8();      // what a bias has left there
         }
     } else {
 #pragma unroll
@@ -232,37 +260,38 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
     if (g.h)
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const f32x8 n = g.r_norm ? normed(r[c], rm, rs, g.r_weight, g.r_bias, col[c]) : r[c];
-            if (on && ok[c]) st_u32x4(g.h + t * g.d + col[c], pack_bf8(n));
+            if (g.r_norm) r[c] = normed(r[c], g.r_norm, rm, rs, g.r_weight, g.r_bias, col[c]);
+            if (on && ok[c]) st_u32x4(g.h + (t * g.d + col[c]), pack_bf8(r[c]));
         }
     if (g.stats && on && lane == 0)
         *reinterpret_cast<f32x4_t *>(g.stats + 4 * t) = f32x4_t{ym, ys, rm, rs};
 }
 
 // ---------------------------------------------------------------- backward
-// A workgroup takes rows in steps of the whole grid and keeps its sums over them
-// in registers; each row is loaded one step ahead.
-template <bool F32, int G, int CH>
-__global__ __launch_bounds__(512) void join_backward_kernel(JoinArgs g) {
-    constexpr int NT = 512, NG = NT / G;
+// A workgroup takes rows in steps of the whole grid, G threads to a row, and keeps its
+// sums over them in registers; each row is loaded one step ahead.  What lies past
+// a row's end, and rows past the last, are zeros.  SUMS: the sums it has room for;
+// LAYER: the norms may be layer norms.  (All five sums and both means take 40 more
+// registers than a thread of 1024 has.)
+template <bool F32, int SUMS, bool LAYER, int NT, int G, int CH>
+__global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
+    constexpr int NG = NT / G;
     __shared__ float red[4][NT / 64][4];
+    extern __shared__ __attribute__((aligned(16))) float cols[];     // [d] if NG > 1
     const int lane = threadIdx.x % G, group = threadIdx.x / G;
     const float inv_d = 1.0f / (float)g.d;
     bool ok[CH];
     int col[CH];
+    f32x8 sum[5][CH];        // weight and bias of r's norm, gate, weight and bias of y's
+    const int sums = g.sums & SUMS;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         col[c] = 8 * (lane + G * c);
         ok[c] = col[c] < g.d;
         if (!ok[c]) col[c] = 0;
+#pragma unroll
+        for (int a = 0; a < 5; ++a) sum[a][c] = zero8();
     }
-    f32x8 sum[5][CH];        // weight and bias of r's norm, gate, weight and bias of y's
-#pragma unroll
-    for (int a = 0; a < 5; ++a)
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[a][c][i] = 0.f;
     uint64_t seed = 0, offset = 0;
     if (g.rng) {
         seed = (uint64_t)g.rng[0];
@@ -270,134 +299,131 @@ __global__ __launch_bounds__(512) void join_backward_kernel(JoinArgs g) {
     }
     Raw<F32> rr[CH], dr[CH];
     Raw<false> yr[CH], hr[CH];
-    f32x4_t st4;
-    const long step = (long)gridDim.x * NG;
+    f32x4_t st = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const long step = (long)gridDim.x * NG, rounds = (g.T + step - 1) / step;
     long row = (long)blockIdx.x * NG + group;
-    const long rounds = (g.T + step - 1) / step;
-    auto load = [&](long at) {
-        const long t = at < g.T ? at : g.T - 1;
-        st4 = *reinterpret_cast<const f32x4_t *>(g.stats_in + 4 * t);
+    auto load_r = [&](long t) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
+            const bool in = t < g.T && ok[c];
             const long i = t * g.d + col[c];
-            if (g.dh) hr[c].load(g.dh, i);
-            if (g.dh && g.r_norm) rr[c].load(g.r_in, i);
-            if (g.dr) dr[c].load(g.dr, i);
-            if (g.y) yr[c].load(g.y, i);
+            rr[c].clear();
+            hr[c].clear();
+            dr[c].clear();
+            if (in && g.dh && g.r_norm) rr[c].load(g.r_in, i);
+            if (in && g.dh) hr[c].load(g.dh, i);
+            if (in && g.dr) dr[c].load(g.dr, i);
         }
     };
-    load(row);
+    auto load_y = [&](long t) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            yr[c].clear();
+            if (g.y && t < g.T && ok[c]) yr[c].load(g.y, t * g.d + col[c]);
+        }
+        st = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (t < g.T) st = *reinterpret_cast<const f32x4_t *>(g.stats_in + 4 * t);
+    };
+    load_r(row);
+    load_y(row);
     for (long k = 0; k < rounds; ++k, row += step) {
         const bool on = row < g.T;
         const long t = on ? row : g.T - 1;
-        const float ym = st4[0], ys = st4[1], rm = st4[2], rs = st4[3];
-        f32x8 D[CH], y[CH];
+        const float ym = st[0], ys = st[1], rm = st[2], rs = st[3];
         // ---- D = dr + N_r^T dh
-        {
+        f32x8 D[CH];
+        if (g.dh && g.r_norm) {
             f32x8 u[CH];
-            float s[2] = {0.f, 0.f};
+            float s[LAYER ? 2 : 1] = {};
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const bool in = on && ok[c];
-                if (g.y) y[c] = yr[c].get();
-                if (g.dr) D[c] = dr[c].get();
-                else
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) D[c][i] = 0.f;
-                if (!g.dh) continue;
-                f32x8 dh = hr[c].get();
-                if (g.r_norm) u[c] = rr[c].get();
-                f32x8 w;
-                if (g.r_weight) w = ld_f32x8(g.r_weight + col[c]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (!g.r_norm) {
-                        D[c][i] = D[c][i] + dh[i];
-                        continue;
-                    }
-                    u[c][i] = (u[c][i] - rm) * rs;
-                    sum[0][c][i] = sum[0][c][i] + (in ? dh[i] * u[c][i] : 0.f);
-                    sum[1][c][i] = sum[1][c][i] + (in ? dh[i] : 0.f);
-                    const float gw = g.r_weight ? dh[i] * w[i] : dh[i];
-                    s[0] = s[0] + (in ? gw * u[c][i] : 0.f);
-                    s[1] = s[1] + (in ? gw : 0.f);
-                }
+                f32x8 gw = hr[c].get();
+                u[c] = LAYER ? (rr[c].get() - rm) * rs : rr[c].get() * rs;
+                if (SUMS & 1 && sums & 1) sum[0][c] = sum[0][c] + gw * u[c];
+                if (SUMS & 2 && sums & 2) sum[1][c] = sum[1][c] + gw;
+                if (g.r_weight) gw = gw * ld_f32x8(again(g.r_weight) + col[c]);
+                s[0] = s[0] + sum8(gw * u[c]);
+                if constexpr (LAYER) s[1] = s[1] + sum8(gw);
+                D[c] = gw;
             }
-            if (g.dh && g.r_norm) {
-                row_sums<G, NT>(s, red[2 * (k & 1)]);
-                const float a = s[0] * inv_d, b = g.r_norm == JOIN_LAYER ? s[1] * inv_d : 0.f;
+            row_sums<G>(s, red[2 * (k & 1)]);
+            const float a = s[0] * inv_d;
+            float b = 0.f;
+            if constexpr (LAYER) b = g.r_norm == JOIN_LAYER ? s[1] * inv_d : 0.f;
 #pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    const f32x8 dh = hr[c].get();
-                    f32x8 w;
-                    if (g.r_weight) w = ld_f32x8(g.r_weight + col[c]);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float gw = g.r_weight ? dh[i] * w[i] : dh[i];
-                        D[c][i] = D[c][i] + rs * (gw - u[c][i] * a - b);
-                    }
-                }
+            for (int c = 0; c < CH; ++c) {
+                D[c] = D[c] - u[c] * a;
+                if constexpr (LAYER) D[c] = D[c] - b;
+                D[c] = dr[c].get() + rs * D[c];
             }
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) D[c] = dr[c].get() + hr[c].get();
         }
-        load(row + step);
+        load_r(row + step);
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
-            if (on && ok[c]) put<F32>(g.dx, t * g.d + col[c], D[c]);
-        if (!g.y) continue;
+        for (int c = 0; c < CH; ++c) {
+            if (!ok[c]) D[c] = zero8();
+            else if (on) put<F32>(g.dx, t * g.d + col[c], D[c]);
+        }
+        if (!g.y) {
+            load_y(row + step);
+            continue;
+        }
         // ---- through the gates, the dropout and y's norm
-        const float tg = g.token_gate ? g.token_gate[t] : 1.f;
-        float s[3] = {0.f, 0.f, 0.f};
+        f32x8 y[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) y[c] = yr[c].get();
+        load_y(row + step);
+        const float tg = g.token_gate ? g.token_gate[t] : 1.f, f = g.scale * g.keep;
+        float s[LAYER ? 3 : 2] = {};                     // the last one: of the token's gate
+        constexpr int TG = LAYER ? 2 : 1;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const bool in = on && ok[c];
-            f32x8 gt, w, b;
-            if (g.gate) gt = ld_f32x8(g.gate + col[c]);
-            if (g.y_weight) w = ld_f32x8(g.y_weight + col[c]);
-            if (g.y_bias) b = ld_f32x8(g.y_bias + col[c]);
-            Words bits{};
-            if (g.rng) bits = philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float u = g.y_norm ? (y[c][i] - ym) * ys : y[c][i];
-                float n = u;
-                if (g.y_weight) n = n * w[i];
-                if (g.y_bias) n = n + b[i];
-                const bool keep = !g.rng || kept(bits, i, g.out);
-                const float mul = keep ? g.keep : 0.f;
-                const float v = keep ? n * g.keep : 0.f;
-                const float vd = g.scale * v * D[c][i];
-                sum[2][c][i] = sum[2][c][i] + (in ? vd * tg : 0.f);
-                s[2] = s[2] + (in ? (g.gate ? vd * gt[i] : vd) : 0.f);
-                float a = g.scale;
-                if (g.gate) a = a * gt[i];
-                const float dn = keep ? a * tg * D[c][i] * mul : 0.f;
-                sum[3][c][i] = sum[3][c][i] + (in ? dn * u : 0.f);
-                sum[4][c][i] = sum[4][c][i] + (in ? dn : 0.f);
-                const float gw = g.y_weight ? dn * w[i] : dn;
-                s[0] = s[0] + (in ? gw * u : 0.f);
-                s[1] = s[1] + (in ? gw : 0.f);
-                D[c][i] = gw;
-                y[c][i] = u;
+            if (g.y_norm) y[c] = LAYER ? (y[c] - ym) * ys : y[c] * ys;
+            f32x8 n = y[c], w, e = D[c] * f;             // e: of the kept elements, without gates
+            if (g.rng) e = drop8(e, philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t), g.out);
+            if (g.y_weight) {
+                w = ld_f32x8(again(g.y_weight) + col[c]);
+                n = n * w;
             }
+            if (g.y_bias) n = n + ld_f32x8(again(g.y_bias) + col[c]);
+            n = n * e;
+            if (SUMS & 4 && sums & 4) sum[2][c] = sum[2][c] + n * tg;
+            if (g.gate) {
+                const f32x8 gt = ld_f32x8(again(g.gate) + col[c]);
+                e = e * gt;
+                if (g.dtoken_gate) n = n * gt;
+            }
+            if (g.dtoken_gate) s[TG] = s[TG] + sum8(n);
+            e = e * tg;
+            if (SUMS & 8 && sums & 8) sum[3][c] = sum[3][c] + e * y[c];
+            if (SUMS & 16 && sums & 16) sum[4][c] = sum[4][c] + e;
+            if (g.y_weight) e = e * w;
+            s[0] = s[0] + sum8(e * y[c]);
+            if constexpr (LAYER) s[1] = s[1] + sum8(e);
+            D[c] = e;
         }
-        if (g.y_norm || g.token_gate) row_sums<G, NT>(s, red[2 * (k & 1) + 1]);
-        if (g.dtoken_gate && on && lane == 0) g.dtoken_gate[t] = s[2];
-        const float a = s[0] * inv_d, b = g.y_norm == JOIN_LAYER ? s[1] * inv_d : 0.f;
+        if (g.y_norm || g.dtoken_gate) row_sums<G>(s, red[2 * (k & 1) + 1]);
+        if (g.dtoken_gate && on && lane == 0) g.dtoken_gate[t] = s[TG];
+        const float a = s[0] * inv_d;
+        float b = 0.f;
+        if constexpr (LAYER) b = g.y_norm == JOIN_LAYER ? s[1] * inv_d : 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            f32x8 dy = D[c];
-            if (g.y_norm)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) dy[i] = ys * (dy[i] - y[c][i] * a - b);
-            if (on && ok[c]) st_u32x4(g.dy + t * g.d + col[c], pack_bf8(dy));
+            if (g.y_norm) {
+                D[c] = D[c] - y[c] * a;
+                if constexpr (LAYER) D[c] = D[c] - b;
+                D[c] = ys * D[c];
+            }
+            if (on && ok[c]) st_u32x4(g.dy + (t * g.d + col[c]), pack_bf8(D[c]));
         }
     }
     // ---- the workgroup's sums over its rows: groups in order, then to `part`
-    extern __shared__ __attribute__((aligned(16))) float cols[];     // [d]
     int n = 0;
 #pragma unroll
     for (int a = 0; a < 5; ++a) {
-        if (!(g.sums >> a & 1)) continue;
+        if (!(SUMS >> a & 1) || !(sums >> a & 1)) continue;
         for (int q = 0; q < NG; ++q) {
             if (NG > 1) __syncthreads();
             if (group == q)
@@ -405,11 +431,7 @@ __global__ __launch_bounds__(512) void join_backward_kernel(JoinArgs g) {
                 for (int c = 0; c < CH; ++c)
                     if (ok[c]) {
                         f32x8 v = sum[a][c];
-                        if (q > 0) {
-                            const f32x8 u = ld_f32x8(cols + col[c]);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) v[i] = u[i] + v[i];
-                        }
+                        if (q > 0) v = ld_f32x8(cols + col[c]) + v;
                         if (q < NG - 1) st_f32x8(cols + col[c], v);
                         else st_f32x8(g.part + ((long)blockIdx.x * g.nsums + n) * g.d + col[c], v);
                     }
@@ -472,27 +494,36 @@ hipError_t forward(JoinArgs g, hipStream_t st) {
 #undef JOIN_FWD
 }
 
-template <bool F32>
+template <bool F32, int SUMS, bool LAYER>
 hipError_t backward(const JoinArgs &g, int blocks, hipStream_t st) {
-#define JOIN_BWD(G, CH)                                                                              \
+#define JOIN_BWD(NT, G, CH)                                                                          \
     do {                                                                                             \
-        const size_t lds = G < 512 && g.nsums ? (size_t)g.d * 4 : 0;                                 \
-        join_backward_kernel<F32, G, CH><<<dim3((unsigned)blocks), dim3(512), lds, st>>>(g);         \
+        const size_t lds = G < NT && g.nsums ? (size_t)g.d * 4 : 0;                                  \
+        join_backward_kernel<F32, SUMS, LAYER, NT, G, CH>                                            \
+            <<<dim3((unsigned)blocks), dim3(NT), lds, st>>>(g);                                      \
         return hipGetLastError();                                                                    \
     } while (0)
-    if (g.d <= 512) JOIN_BWD(64, 1);
-    if (g.d <= 1024) JOIN_BWD(64, 2);
-    if (g.d <= 2048) JOIN_BWD(128, 2);
-    if (g.d <= 4096) JOIN_BWD(256, 2);
-    if (g.d <= 8192) JOIN_BWD(512, 2);
-    JOIN_BWD(512, 4);
+    const bool wide = join_threads(g.T, g.d) == 1024;
+    if (g.d <= 512) { if (wide) JOIN_BWD(1024, 64, 1); JOIN_BWD(256, 64, 1); }
+    if (g.d <= 1024) { if (wide) JOIN_BWD(1024, 128, 1); JOIN_BWD(256, 128, 1); }
+    if (g.d <= 2048) { if (wide) JOIN_BWD(1024, 256, 1); JOIN_BWD(256, 256, 1); }
+    if (g.d <= 4096) { if (wide) JOIN_BWD(1024, 512, 1); JOIN_BWD(512, 512, 1); }
+    if (g.d <= 8192) JOIN_BWD(1024, 1024, 1);
+    JOIN_BWD(1024, 1024, 2);
 #undef JOIN_BWD
+}
+template <bool F32>
+hipError_t backward(const JoinArgs &g, int blocks, hipStream_t st) {
+    const bool layer = g.r_norm == JOIN_LAYER || g.y_norm == JOIN_LAYER;
+    if (!layer && !(g.sums & ~13)) return backward<F32, 13, false>(g, blocks, st);
+    if (!(g.sums & ~7)) return backward<F32, 7, true>(g, blocks, st);
+    return backward<F32, 31, true>(g, blocks, st);
 }
 
 }  // namespace
 
 int join_blocks(long T, int d) {
-    const long rows = d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1;    // of a workgroup at a time
+    const long rows = join_threads(T, d) / join_row_threads(d);      // of a workgroup at a time
     const long n = (T + rows - 1) / rows;
     return (int)(n < JOIN_BLOCKS ? n : JOIN_BLOCKS);
 }
