@@ -19,6 +19,8 @@
 // The mask of the dropout is computed again where it is needed (Philox4x32-10:
 // Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011;
 // 8 elements per block of the generator).
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 #include "rules.h"
@@ -60,7 +62,7 @@ DEV f32x8 drop8(const f32x8 &n, const Words &w, uint32_t out) {
 template <bool F32> struct Raw;
 template <> struct Raw<false> {
     u32x4_t a;
-    DEV void load(const void *p, long i) { a = ld_u32x4((const uint16_t *)p + i); }
+    DEV void load(const void *p, int i) { a = ld_u32x4((const uint16_t *)p + i); }
     DEV void clear() { a = u32x4_t{0u, 0u, 0u, 0u}; }
     DEV f32x8 get() const {
         return f32x8{bf_lo(a[0]), bf_hi(a[0]), bf_lo(a[1]), bf_hi(a[1]),
@@ -69,7 +71,7 @@ template <> struct Raw<false> {
 };
 template <> struct Raw<true> {
     u32x4_t a, b;
-    DEV void load(const void *p, long i) {
+    DEV void load(const void *p, int i) {
         a = ld_u32x4((const float *)p + i);
         b = ld_u32x4((const float *)p + i + 4);
     }
@@ -84,18 +86,10 @@ template <> struct Raw<true> {
         return v;
     }
 };
-// stores v and returns what a reader of the stream finds there
 template <bool F32>
-DEV f32x8 put(void *p, long i, const f32x8 &v) {
-    if constexpr (F32) {
-        st_f32x8((float *)p + i, v);
-        return v;
-    } else {
-        Raw<false> r;
-        r.a = pack_bf8(v);
-        st_u32x4((uint16_t *)p + i, r.a);
-        return r.get();
-    }
+DEV void put(void *p, int i, const f32x8 &v) {
+    if constexpr (F32) st_f32x8((float *)p + i, v);
+    else st_u32x4((uint16_t *)p + i, pack_bf8(v));
 }
 
 // ---------------------------------------------------------------- sums over a row
@@ -147,6 +141,15 @@ DEV void row_sums(float (&v)[N], float (*red)[4]) {
     }
 }
 DEV float sum8(const f32x8 &v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
+DEV float dot8(const f32x8 &a, const f32x8 &b) {
+    float x = a[0] * b[0], y = a[1] * b[1];
+#pragma unroll
+    for (int i = 2; i < 8; i += 2) {
+        x = fmaf(a[i], b[i], x);
+        y = fmaf(a[i + 1], b[i + 1], y);
+    }
+    return x + y;
+}
 DEV f32x8 zero8() { return f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
 
 // The pointer, for loads that are to stay where they are: weights that the compiler
@@ -165,11 +168,14 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
     constexpr int NT = G < 256 ? 256 : G, NW = NT / 64;
     __shared__ float red[4][NW][4];
     const int lane = threadIdx.x % G;
-    const long row = g.row0 + (long)blockIdx.x * (NT / G) + threadIdx.x / G;
+    // a row's threads are whole waves: its addresses are scalar
+    const long row = g.row0 + (long)blockIdx.x * (NT / G) + __builtin_amdgcn_readfirstlane(threadIdx.x / G);
     if (G <= 64 && row >= g.T) return;       // a wave to a row: no barriers
     const bool on = row < g.T;
     const long t = on ? row : g.T - 1;
     const float inv_d = 1.0f / (float)g.d;
+    const size_t ts = (size_t)(t * g.d) * (F32 ? 4 : 2);         // bytes to the row in the stream
+    const char *xp = (const char *)g.x + ts;
     bool ok[CH];
     int col[CH];
     Raw<F32> xr[CH];
@@ -179,7 +185,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
         col[c] = 8 * (lane + G * c);
         ok[c] = col[c] < g.d;
         if (ok[c]) {
-            xr[c].load(g.x, t * g.d + col[c]);
+            xr[c].load(xp, col[c]);
         } else {
             col[c] = 0;
             xr[c].clear();
@@ -189,7 +195,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             yr[c].clear();
-            if (ok[c]) yr[c].load(g.y, t * g.d + col[c]);
+            if (ok[c]) yr[c].load(g.y + t * g.d, col[c]);
         }
     float ym = 0.f, ys = 0.f, rm = 0.f, rs = 0.f;
     // mean and 1 / deviation of the row in v
@@ -204,12 +210,12 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const f32x8 u = v[c] - m;
-                const float q = sum8(u * u);
+                const float q = dot8(u, u);
                 sum[0] = sum[0] + (ok[c] ? q : 0.f);
             }
         } else {
 #pragma unroll
-            for (int c = 0; c < CH; ++c) sum[0] = sum[0] + sum8(v[c] * v[c]);
+            for (int c = 0; c < CH; ++c) sum[0] = sum[0] + dot8(v[c], v[c]);
         }
         row_sums<G>(sum, red[at + 1]);
         s = dev_inv(sum[0] * inv_d, eps);
@@ -246,9 +252,9 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
                 Raw<false> q;
                 q.a = pack_bf8(r[c]);
                 r[c] = q.get();
-                if (on && ok[c]) st_u32x4((uint16_t *)g.r + (t * g.d + col[c]), q.a);
+                if (on && ok[c]) st_u32x4((uint16_t *)((char *)g.r + ts) + col[c], q.a);
             } else {
-                if (on && ok[c]) st_f32x8((float *)g.r + (t * g.d + col[c]), r[c]);
+                if (on && ok[c]) st_f32x8((float *)((char *)g.r + ts) + col[c], r[c]);
             }
             if (!ok[c]) r[c] = zero8();      // what a bias has left there
         }
@@ -261,7 +267,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (g.r_norm) r[c] = normed(r[c], g.r_norm, rm, rs, g.r_weight, g.r_bias, col[c]);
-            if (on && ok[c]) st_u32x4(g.h + (t * g.d + col[c]), pack_bf8(r[c]));
+            if (on && ok[c]) st_u32x4(g.h + t * g.d + col[c], pack_bf8(r[c]));
         }
     if (g.stats && on && lane == 0)
         *reinterpret_cast<f32x4_t *>(g.stats + 4 * t) = f32x4_t{ym, ys, rm, rs};
@@ -277,8 +283,10 @@ template <bool F32, int SUMS, bool LAYER, int NT, int G, int CH>
 __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
     constexpr int NG = NT / G;
     __shared__ float red[4][NT / 64][4];
-    extern __shared__ __attribute__((aligned(16))) float cols[];     // [d] if NG > 1
-    const int lane = threadIdx.x % G, group = threadIdx.x / G;
+    // weights, where they fit; in the end [d] sums if NG > 1
+    extern __shared__ __attribute__((aligned(16))) float cols[];
+    constexpr bool LDS_W = CH <= 2;
+    const int lane = threadIdx.x % G, group = __builtin_amdgcn_readfirstlane(threadIdx.x / G);
     const float inv_d = 1.0f / (float)g.d;
     bool ok[CH];
     int col[CH];
@@ -292,6 +300,29 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
 #pragma unroll
         for (int a = 0; a < 5; ++a) sum[a][c] = zero8();
     }
+    // Weights come from LDS: a load from memory would return after the next row's,
+    // which are asked for before it.  Two planes of 4 columns of 8 each.
+    const float *weights[4] = {g.r_weight, g.y_weight, g.y_bias, g.gate};
+    int at[4], n_w = 0;
+#pragma unroll
+    for (int a = 0; a < 4; ++a) at[a] = weights[a] ? n_w++ * g.d : 0;
+    if constexpr (LDS_W) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+            if (weights[a])
+                for (int j = threadIdx.x; j < g.d / 4; j += NT)
+                    *reinterpret_cast<f32x4_t *>(cols + at[a] + (j & 1) * (g.d / 2) + 4 * (j >> 1)) =
+                        *reinterpret_cast<const f32x4_t *>(weights[a] + 4 * j);
+        __syncthreads();
+    }
+    auto weight = [&](int a, int c) {
+        if constexpr (!LDS_W) return ld_f32x8(again(weights[a]) + col[c]);
+        const float *p = cols + at[a] + col[c] / 2;
+        const f32x4_t lo = *reinterpret_cast<const f32x4_t *>(p);
+        const f32x4_t hi = *reinterpret_cast<const f32x4_t *>(p + g.d / 2);
+        return f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    enum { RW, YW, YB, GATE };
     uint64_t seed = 0, offset = 0;
     if (g.rng) {
         seed = (uint64_t)g.rng[0];
@@ -302,29 +333,45 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
     f32x4_t st = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const long step = (long)gridDim.x * NG, rounds = (g.T + step - 1) / step;
     long row = (long)blockIdx.x * NG + group;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {           // lanes past the row's end keep the zeros
+        rr[c].clear();
+        dr[c].clear();
+        yr[c].clear();
+        hr[c].clear();
+    }
+    constexpr int SZ = F32 ? 4 : 2;
     auto load_r = [&](long t) {
+        const size_t i = (size_t)(t * g.d);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const bool in = t < g.T && ok[c];
-            const long i = t * g.d + col[c];
-            rr[c].clear();
-            hr[c].clear();
-            dr[c].clear();
-            if (in && g.dh && g.r_norm) rr[c].load(g.r_in, i);
-            if (in && g.dh) hr[c].load(g.dh, i);
-            if (in && g.dr) dr[c].load(g.dr, i);
+            if (t >= g.T) {
+                rr[c].clear();
+                hr[c].clear();
+            } else if (ok[c]) {
+                if (g.dh && g.r_norm) rr[c].load((const char *)g.r_in + i * SZ, col[c]);
+                if (g.dh) hr[c].load(g.dh + i, col[c]);
+            }
+        }
+    };
+    auto load_dr = [&](long t) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (t >= g.T) dr[c].clear();
+            else if (g.dr && ok[c]) dr[c].load((const char *)g.dr + (size_t)(t * g.d) * SZ, col[c]);
         }
     };
     auto load_y = [&](long t) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            yr[c].clear();
-            if (g.y && t < g.T && ok[c]) yr[c].load(g.y, t * g.d + col[c]);
-        }
         st = f32x4_t{0.f, 0.f, 0.f, 0.f};
         if (t < g.T) st = *reinterpret_cast<const f32x4_t *>(g.stats_in + 4 * t);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (t >= g.T) yr[c].clear();
+            else if (g.y && ok[c]) yr[c].load(g.y + t * g.d, col[c]);
+        }
     };
     load_r(row);
+    load_dr(row);
     load_y(row);
     for (long k = 0; k < rounds; ++k, row += step) {
         const bool on = row < g.T;
@@ -341,11 +388,12 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
                 u[c] = LAYER ? (rr[c].get() - rm) * rs : rr[c].get() * rs;
                 if (SUMS & 1 && sums & 1) sum[0][c] = sum[0][c] + gw * u[c];
                 if (SUMS & 2 && sums & 2) sum[1][c] = sum[1][c] + gw;
-                if (g.r_weight) gw = gw * ld_f32x8(again(g.r_weight) + col[c]);
-                s[0] = s[0] + sum8(gw * u[c]);
+                if (g.r_weight) gw = gw * weight(RW, c);
+                s[0] = s[0] + dot8(gw, u[c]);
                 if constexpr (LAYER) s[1] = s[1] + sum8(gw);
                 D[c] = gw;
             }
+            load_r(row + step);
             row_sums<G>(s, red[2 * (k & 1)]);
             const float a = s[0] * inv_d;
             float b = 0.f;
@@ -359,12 +407,13 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
         } else {
 #pragma unroll
             for (int c = 0; c < CH; ++c) D[c] = dr[c].get() + hr[c].get();
+            load_r(row + step);
         }
-        load_r(row + step);
+        load_dr(row + step);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (!ok[c]) D[c] = zero8();
-            else if (on) put<F32>(g.dx, t * g.d + col[c], D[c]);
+            else if (on) put<F32>((char *)g.dx + (size_t)(t * g.d) * SZ, col[c], D[c]);
         }
         if (!g.y) {
             load_y(row + step);
@@ -375,7 +424,9 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) y[c] = yr[c].get();
         load_y(row + step);
-        const float tg = g.token_gate ? g.token_gate[t] : 1.f, f = g.scale * g.keep;
+        const float tg = g.token_gate ? g.token_gate[t] : 1.f;
+        // the token's gate comes last where its own gradient is wanted
+        const float f = g.dtoken_gate ? g.scale * g.keep : g.scale * g.keep * tg;
         float s[LAYER ? 3 : 2] = {};                     // the last one: of the token's gate
         constexpr int TG = LAYER ? 2 : 1;
 #pragma unroll
@@ -384,23 +435,22 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
             f32x8 n = y[c], w, e = D[c] * f;             // e: of the kept elements, without gates
             if (g.rng) e = drop8(e, philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t), g.out);
             if (g.y_weight) {
-                w = ld_f32x8(again(g.y_weight) + col[c]);
+                w = weight(YW, c);
                 n = n * w;
             }
-            if (g.y_bias) n = n + ld_f32x8(again(g.y_bias) + col[c]);
-            n = n * e;
-            if (SUMS & 4 && sums & 4) sum[2][c] = sum[2][c] + n * tg;
-            if (g.gate) {
-                const f32x8 gt = ld_f32x8(again(g.gate) + col[c]);
-                e = e * gt;
-                if (g.dtoken_gate) n = n * gt;
+            if (g.y_bias) n = n + weight(YB, c);
+            if (g.dtoken_gate) {
+                f32x8 ge = e;
+                if (g.gate) ge = ge * weight(GATE, c);
+                s[TG] = s[TG] + dot8(n, ge);
+                e = e * tg;
             }
-            if (g.dtoken_gate) s[TG] = s[TG] + sum8(n);
-            e = e * tg;
+            if (SUMS & 4 && sums & 4) sum[2][c] = sum[2][c] + n * e;
+            if (g.gate) e = e * weight(GATE, c);
             if (SUMS & 8 && sums & 8) sum[3][c] = sum[3][c] + e * y[c];
             if (SUMS & 16 && sums & 16) sum[4][c] = sum[4][c] + e;
             if (g.y_weight) e = e * w;
-            s[0] = s[0] + sum8(e * y[c]);
+            s[0] = s[0] + dot8(e, y[c]);
             if constexpr (LAYER) s[1] = s[1] + sum8(e);
             D[c] = e;
         }
@@ -416,7 +466,7 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
                 if constexpr (LAYER) D[c] = D[c] - b;
                 D[c] = ys * D[c];
             }
-            if (on && ok[c]) st_u32x4(g.dy + (t * g.d + col[c]), pack_bf8(D[c]));
+            if (on && ok[c]) st_u32x4(g.dy + t * g.d + col[c], pack_bf8(D[c]));
         }
     }
     // ---- the workgroup's sums over its rows: groups in order, then to `part`
@@ -425,7 +475,7 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
     for (int a = 0; a < 5; ++a) {
         if (!(SUMS >> a & 1) || !(sums >> a & 1)) continue;
         for (int q = 0; q < NG; ++q) {
-            if (NG > 1) __syncthreads();
+            if (NG > 1) __syncthreads();     // and the last row's weights have been read
             if (group == q)
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
@@ -498,18 +548,19 @@ template <bool F32, int SUMS, bool LAYER>
 hipError_t backward(const JoinArgs &g, int blocks, hipStream_t st) {
 #define JOIN_BWD(NT, G, CH)                                                                          \
     do {                                                                                             \
-        const size_t lds = G < NT && g.nsums ? (size_t)g.d * 4 : 0;                                  \
+        const size_t lds = (size_t)(CH <= 2 ? std::max(n_w, 1) : 1) * g.d * 4;                       \
         join_backward_kernel<F32, SUMS, LAYER, NT, G, CH>                                            \
             <<<dim3((unsigned)blocks), dim3(NT), lds, st>>>(g);                                      \
         return hipGetLastError();                                                                    \
     } while (0)
-    const bool wide = join_threads(g.T, g.d) == 1024;
-    if (g.d <= 512) { if (wide) JOIN_BWD(1024, 64, 1); JOIN_BWD(256, 64, 1); }
-    if (g.d <= 1024) { if (wide) JOIN_BWD(1024, 128, 1); JOIN_BWD(256, 128, 1); }
-    if (g.d <= 2048) { if (wide) JOIN_BWD(1024, 256, 1); JOIN_BWD(256, 256, 1); }
-    if (g.d <= 4096) { if (wide) JOIN_BWD(1024, 512, 1); JOIN_BWD(512, 512, 1); }
-    if (g.d <= 8192) JOIN_BWD(1024, 1024, 1);
-    JOIN_BWD(1024, 1024, 2);
+    const int n_w = !!g.r_weight + !!g.y_weight + !!g.y_bias + !!g.gate;
+    const bool wide = join_threads(g.T, g.d) == 512;
+    if (g.d <= 512) { if (wide) JOIN_BWD(512, 64, 1); JOIN_BWD(256, 64, 1); }
+    if (g.d <= 1024) { if (wide) JOIN_BWD(512, 128, 1); JOIN_BWD(256, 128, 1); }
+    if (g.d <= 2048) { if (wide) JOIN_BWD(512, 256, 1); JOIN_BWD(256, 256, 1); }
+    if (g.d <= 4096) JOIN_BWD(512, 512, 1);
+    if (g.d <= 8192) JOIN_BWD(512, 512, 2);
+    JOIN_BWD(512, 512, 4);
 #undef JOIN_BWD
 }
 template <bool F32>

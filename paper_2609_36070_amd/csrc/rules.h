@@ -361,8 +361,8 @@ constexpr long JOIN_BLOCKS = 256;
 constexpr long JOIN_MAX_D = 16384;
 // Threads of a row in the backward, 8 values each (16 past 8192), and of a workgroup:
 // several rows at a time where there are enough of them.
-inline int join_row_threads(long d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024; }
+inline int join_row_threads(long d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : 512; }
 inline int join_threads(long T, long d) {
     const int g = join_row_threads(d);
-    return T >= 2 * JOIN_BLOCKS * (1024 / g) ? 1024 : g < 256 ? 256 : g;
+    return g >= 512 ? g : T >= 2 * JOIN_BLOCKS * (512 / g) ? 512 : 256;
 }
