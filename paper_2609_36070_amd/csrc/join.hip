@@ -122,6 +122,14 @@ DEV float wave_sum_last(float v) {
 // before every thread has passed another barrier: callers alternate.
 template <int G, int N>
 DEV void row_sums(float (&v)[N], float (*red)[4]) {
+    if constexpr (G < 64) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = lanes_sum<(G < 16 ? G : 16)>(v[i]);
+            if constexpr (G == 32) v[i] = v[i] + shfl_xor_f(v[i], 16);
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave_sum_last(v[i]);
     if constexpr (G == 64) {
@@ -129,7 +137,7 @@ DEV void row_sums(float (&v)[N], float (*red)[4]) {
         for (int i = 0; i < N; ++i)
             v[i] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[i]), 63));
     } else {
-        constexpr int W = G / 64;
+        constexpr int W = G < 64 ? 1 : G / 64;
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         if (lane == 63)
 #pragma unroll
@@ -141,6 +149,11 @@ DEV void row_sums(float (&v)[N], float (*red)[4]) {
     }
 }
 DEV float sum8(const f32x8 &v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
+// Which of its workgroup's rows a thread has: of whole waves, so that addresses are scalar
+template <int G>
+DEV int row_of_thread() {
+    return G >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : (int)threadIdx.x / G;
+}
 DEV float dot8(const f32x8 &a, const f32x8 &b) {
     float x = a[0] * b[0], y = a[1] * b[1];
 #pragma unroll
@@ -168,9 +181,8 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
     constexpr int NT = G < 256 ? 256 : G, NW = NT / 64;
     __shared__ float red[4][NW][4];
     const int lane = threadIdx.x % G;
-    // a row's threads are whole waves: its addresses are scalar
-    const long row = g.row0 + (long)blockIdx.x * (NT / G) + __builtin_amdgcn_readfirstlane(threadIdx.x / G);
-    if (G <= 64 && row >= g.T) return;       // a wave to a row: no barriers
+    const long row = g.row0 + (long)blockIdx.x * (NT / G) + row_of_thread<G>();
+    if (G <= 64 && row >= g.T) return;       // no barriers then
     const bool on = row < g.T;
     const long t = on ? row : g.T - 1;
     const float inv_d = 1.0f / (float)g.d;
@@ -286,7 +298,7 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
     // weights, where they fit; in the end [d] sums if NG > 1
     extern __shared__ __attribute__((aligned(16))) float cols[];
     constexpr bool LDS_W = CH <= 2;
-    const int lane = threadIdx.x % G, group = __builtin_amdgcn_readfirstlane(threadIdx.x / G);
+    const int lane = threadIdx.x % G, group = row_of_thread<G>();
     const float inv_d = 1.0f / (float)g.d;
     bool ok[CH];
     int col[CH];
@@ -469,20 +481,28 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
             if (on && ok[c]) st_u32x4(g.dy + t * g.d + col[c], pack_bf8(D[c]));
         }
     }
-    // ---- the workgroup's sums over its rows: groups in order, then to `part`
+    // ---- the workgroup's sums over its rows: the rows of a wave, then the others' in
+    // order, to `part`
+    constexpr int STEP = G < 64 ? 64 : G, TURNS = NT / STEP;
     int n = 0;
 #pragma unroll
     for (int a = 0; a < 5; ++a) {
         if (!(SUMS >> a & 1) || !(sums >> a & 1)) continue;
-        for (int q = 0; q < NG; ++q) {
-            if (NG > 1) __syncthreads();     // and the last row's weights have been read
-            if (group == q)
+#pragma unroll
+        for (int m = G; m < 64; m <<= 1)
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[a][c][i] = sum[a][c][i] + shfl_xor_f(sum[a][c][i], m);
+        for (int q = 0; q < TURNS; ++q) {
+            if (TURNS > 1) __syncthreads();  // and the last row's weights have been read
+            if ((int)threadIdx.x / STEP == q && (int)threadIdx.x % STEP < G)
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
                     if (ok[c]) {
                         f32x8 v = sum[a][c];
                         if (q > 0) v = ld_f32x8(cols + col[c]) + v;
-                        if (q < NG - 1) st_f32x8(cols + col[c], v);
+                        if (q < TURNS - 1) st_f32x8(cols + col[c], v);
                         else st_f32x8(g.part + ((long)blockIdx.x * g.nsums + n) * g.d + col[c], v);
                     }
         }
@@ -527,6 +547,9 @@ hipError_t forward(JoinArgs g, hipStream_t st) {
         }                                                                                            \
         return hipGetLastError();                                                                    \
     } while (0)
+    if (g.d <= 64) JOIN_FWD(8, 1);
+    if (g.d <= 128) JOIN_FWD(16, 1);
+    if (g.d <= 256) JOIN_FWD(32, 1);
     if (g.T <= JOIN_FEW_ROWS) {
         if (g.d <= 512) JOIN_FWD(64, 1);
         if (g.d <= 1024) JOIN_FWD(128, 1);
@@ -554,10 +577,12 @@ hipError_t backward(const JoinArgs &g, int blocks, hipStream_t st) {
         return hipGetLastError();                                                                    \
     } while (0)
     const int n_w = !!g.r_weight + !!g.y_weight + !!g.y_bias + !!g.gate;
-    const bool wide = join_threads(g.T, g.d) == 512;
-    if (g.d <= 512) { if (wide) JOIN_BWD(512, 64, 1); JOIN_BWD(256, 64, 1); }
-    if (g.d <= 1024) { if (wide) JOIN_BWD(512, 128, 1); JOIN_BWD(256, 128, 1); }
-    if (g.d <= 2048) { if (wide) JOIN_BWD(512, 256, 1); JOIN_BWD(256, 256, 1); }
+    if (g.d <= 64) JOIN_BWD(256, 8, 1);
+    if (g.d <= 128) JOIN_BWD(256, 16, 1);
+    if (g.d <= 256) JOIN_BWD(256, 32, 1);
+    if (g.d <= 512) JOIN_BWD(256, 64, 1);
+    if (g.d <= 1024) JOIN_BWD(256, 128, 1);
+    if (g.d <= 2048) JOIN_BWD(256, 256, 1);
     if (g.d <= 4096) JOIN_BWD(512, 512, 1);
     if (g.d <= 8192) JOIN_BWD(512, 512, 2);
     JOIN_BWD(512, 512, 4);
@@ -573,11 +598,7 @@ hipError_t backward(const JoinArgs &g, int blocks, hipStream_t st) {
 
 }  // namespace
 
-int join_blocks(long T, int d) {
-    const long rows = join_threads(T, d) / join_row_threads(d);      // of a workgroup at a time
-    const long n = (T + rows - 1) / rows;
-    return (int)(n < JOIN_BLOCKS ? n : JOIN_BLOCKS);
-}
+int join_blocks(long T, int d) { return (int)join_workgroups(T, d); }
 
 hipError_t launch_join_forward(const JoinArgs &g, hipStream_t st) {
     if (g.T <= 0) return hipSuccess;

@@ -355,14 +355,19 @@ inline bool mx_keep_l2(long R, long E, long K, long N) {
 // Joining a block to the residual stream (join.hip): rows up to which a row gets
 // as many threads as have something to load.
 constexpr long JOIN_FEW_ROWS = 256;
-// Workgroups of the backward at most; each leaves a row of sums.
-constexpr long JOIN_BLOCKS = 256;
 // Row lengths: what a workgroup's registers hold.
 constexpr long JOIN_MAX_D = 16384;
-// Threads of a row in the backward, 8 values each (16 past 8192), and of a workgroup:
-// several rows at a time where there are enough of them.
-inline int join_row_threads(long d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : 512; }
-inline int join_threads(long T, long d) {
-    const int g = join_row_threads(d);
-    return g >= 512 ? g : T >= 2 * JOIN_BLOCKS * (512 / g) ? 512 : 256;
+// The backward: threads of a row (8 values each up to 4096), of a workgroup, and the
+// workgroups, which leave a row of sums each: one to a CU where a row takes 512 threads,
+// else three, if each has 4 rounds of rows left (us with 256 / 768: 16384 x 2048 116 /
+// 100, 20000 x 1024 75 / 66, 40000 x 512 80 / 67, 100000 x 64 114 / 29, 4000 x 2048 32 / 34).
+inline long join_row_threads(long d) {
+    long g = 8;
+    while (g < 512 && 8 * g < d) g *= 2;
+    return g;
+}
+inline long join_threads(long d) { return join_row_threads(d) < 256 ? 256 : join_row_threads(d); }
+inline long join_workgroups(long T, long d) {
+    const long rows = join_threads(d) / join_row_threads(d), n = (T + rows - 1) / rows;
+    return n <= 256 ? n : std::min(join_threads(d) < 512 ? 768L : 256L, std::max(256L, n / 4));
 }

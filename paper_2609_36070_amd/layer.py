@@ -32,12 +32,13 @@ class DeviceLayer:
     """All tensors of one layer instance on the GPU, laid out as the C ABI expects."""
 
     def __init__(self, w: Workload, inputs: dict, device="cuda", with_backward=None, mx=False,
-                 ring_rows=None, mx_wgrad=False, routing=None, int8=False):
+                 ring_rows=None, mx_wgrad=False, routing=None, int8=False, few=False):
         """ring_rows: run forward/backward in bounded memory, with the per-route
         activations in a ring of that many rows (None: room for all T*k routes).
         mx_wgrad: the MXFP8 backward computes its weight gradients in MXFP8.
         routing: route by scores (a MoeRouting), with inputs["balance"] if given.
-        int8: the experts in 8-bit integers too (forward_int, step_int)."""
+        int8: the experts in 8-bit integers too (forward_int, step_int).
+        few: up to 16 tokens in two launches too (step_few)."""
         self.w = w
         self.mx = mx
         self.routing = routing
@@ -96,6 +97,11 @@ class DeviceLayer:
             if int_bytes == 0:
                 raise ValueError(f"shape unsupported in int8 {w}")
             nbytes = max(nbytes, int_bytes)
+        if few:
+            few_bytes = B.moe_few_workspace_bytes(self.shape)
+            if few_bytes == 0:
+                raise ValueError(f"not a shape of a few tokens {w}")
+            nbytes = max(nbytes, few_bytes)
         self.ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
         self.weights = B.weights_struct(self.W_gate, self.W_up, self.W_down,
                                         self.Wg_s, self.Wu_s, self.Wd_s)
@@ -239,6 +245,12 @@ class DeviceLayer:
         B.moe_forward_int(self.shape, self.X, self.int_weights, self.topk_idx, self.topk_w,
                           self.plan_bufs, self.Y, self.ws, stream=stream, events=events)
 
+    def step_few(self, stream=None):
+        """Route, plan and forward of up to 16 tokens in two launches."""
+        B.moe_forward_few(self.shape, B.routing() if self.routing is None else self.routing, self.X, self.W_r,
+                          self.bias, self.balance, self.weights, self.logits, self.topk_idx, self.topk_w,
+                          self.Y, self.ws, stream=stream)
+
     def step_int(self, stream=None, fwd_events=None):
         """Route, plan and the int8 forward."""
         self.route(stream)
@@ -274,3 +286,72 @@ class DeviceLayer:
 
     def error_word(self) -> int:
         return int(self.ws_tensor(B.WS_ERROR, torch.int32, (1,)).item())
+
+
+class DeviceBlock:
+    """A layer between the norms of a residual block, on the GPU:
+
+        h0 = N(x), y = layer(h0), r = x + scale gate token_gate dropout(N_y(y)), h = N_r(r)
+
+    r goes on as the stream and h into the next block.  The layer's inputs["X"] is
+    the stream x; params holds numpy arrays: in_weight and in_bias of the first
+    norm, and those of the join (binding.JOIN_PARAMS), each optional.  With up
+    to 16 tokens and no backward the layer runs as step_few."""
+
+    def __init__(self, w: Workload, inputs: dict, params: dict | None = None, stream="bf16", in_norm="rms",
+                 y_norm="none", r_norm="rms", eps=1e-6, scale=1.0, drop=0.0, seed=0, device="cuda",
+                 with_backward=None, **layer_options):
+        backward = w.backward if with_backward is None else with_backward
+        self.few = not backward and 0 < w.T <= 16
+        self.layer = L = DeviceLayer(w, inputs, device, with_backward=backward, few=self.few, **layer_options)
+        dev, T, d = L.device, w.T, w.d
+        kind = torch.float32 if stream == "f32" else torch.bfloat16
+        params = params or {}
+        up = {n: None if v is None else torch.from_numpy(np.ascontiguousarray(v, np.float32)).to(dev)
+              for n, v in params.items()}
+        self.x = _empty((T, d), kind, dev)
+        if T:
+            self.x.copy_(torch.from_numpy(np.ascontiguousarray(inputs["X"], np.float32)).to(kind))
+        self.first = B.join(T, d, stream, "none", in_norm, r_eps=eps)
+        self.first_tensors = dict(r_weight=up.get("in_weight"), r_bias=up.get("in_bias"))
+        self.join = B.join(T, d, stream, y_norm, r_norm, eps, eps, scale, drop)
+        self.tensors = {n: up.get(n) for n in B.JOIN_PARAMS}
+        self.first_params = B.join_params(**self.first_tensors)
+        self.params = B.join_params(**self.tensors)
+        # seed and offset; a program moves the offset on from step to step
+        self.rng = torch.tensor([seed, 0], dtype=torch.int64, device=dev) if drop else None
+        self.r, self.h = _empty((T, d), kind, dev), _empty((T, d), torch.bfloat16, dev)
+        self.first_stats = self.stats = None
+        if backward:
+            self.first_stats, self.stats = (_empty((T, 4), torch.float32, dev) for _ in range(2))
+            self.dr, self.dx = _empty((T, d), kind, dev), _empty((T, d), kind, dev)
+            self.dh, L.dY = (_empty((T, d), torch.bfloat16, dev) for _ in range(2))
+            self.first_grads, self.grads = ({n: torch.empty_like(v) for n, v in t.items() if v is not None}
+                                            for t in (self.first_tensors, self.tensors))
+            self.first_grads_struct = B.join_grads(**self.first_grads)
+            self.grads_struct = B.join_grads(**self.grads)
+            nbytes = max(B.moe_join_workspace_bytes(j) for j in (self.first, self.join))
+            self.ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+
+    def forward(self, stream=None):
+        L = self.layer
+        B.moe_join_forward(self.first, self.x, None, self.first_params, None, None, L.X, self.first_stats,
+                           stream=stream)
+        if self.few:
+            L.step_few(stream)
+        else:
+            L.route(stream)
+            L.plan(stream)
+            L.forward(stream=stream)
+        B.moe_join_forward(self.join, self.x, L.Y, self.params, self.rng, self.r, self.h, self.stats,
+                           stream=stream)
+
+    def backward(self, stream=None):
+        """From dr and dh to dx (the gradient of x, through the stream and the layer), the layer's gradients
+        and those of the norms and gates (grads, first_grads)."""
+        L = self.layer
+        B.moe_join_backward(self.join, L.Y, self.r, self.stats, self.params, self.rng, self.dr, self.dh,
+                            self.dx, L.dY, self.grads_struct, self.ws, stream=stream)
+        L.backward(stream)
+        B.moe_join_backward(self.first, None, self.x, self.first_stats, self.first_params, None, self.dx, L.dX,
+                            self.dx, None, self.first_grads_struct, self.ws, stream=stream)
