@@ -386,8 +386,9 @@ JoinArgs join_args(const moe_join &j, const moe_join_params &p, const moe_bf16 *
     return g;
 }
 
+size_t join_part_bytes(const moe_join &j) { return up((size_t)join_blocks(j.T, (int)j.d) * 5 * (size_t)j.d * 4 + 16); }
 size_t join_bytes(const moe_join &j) {
-    return std::max<size_t>((size_t)join_blocks(j.T, (int)j.d) * 5 * (size_t)j.d * 4, 16);
+    return join_part_bytes(j) + (j.d > JOIN_SUMS_D ? up((size_t)j.T * 8) : 0);
 }
 
 // Int8 experts: every operand is addressed with 32-bit offsets, and a dot
@@ -2075,6 +2076,7 @@ moe_status moe_join_backward(const moe_join *join, const moe_bf16 *y, const void
             g.out_sums[g.nsums++] = all[i].grad;
         }
     g.part = static_cast<float *>(ws);
+    if (join->d > JOIN_SUMS_D) g.means = at<float>(ws, join_part_bytes(*join));
     MOE_TRY(launch_join_backward(g, static_cast<hipStream_t>(stream)));
     return MOE_OK;
 }

@@ -297,7 +297,7 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
     __shared__ float red[4][NT / 64][4];
     // weights, where they fit; in the end [d] sums if NG > 1
     extern __shared__ __attribute__((aligned(16))) float cols[];
-    constexpr bool LDS_W = CH <= 2;
+    constexpr bool LDS_W = CH <= 2;          // (beyond, they would take up to 256 KB)
     const int lane = threadIdx.x % G, group = row_of_thread<G>();
     const float inv_d = 1.0f / (float)g.d;
     bool ok[CH];
@@ -410,6 +410,12 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
             const float a = s[0] * inv_d;
             float b = 0.f;
             if constexpr (LAYER) b = g.r_norm == JOIN_LAYER ? s[1] * inv_d : 0.f;
+            if constexpr (SUMS == 0) {
+                if (g.means && on && lane == 0) {
+                    g.means[2 * t] = a;
+                    g.means[2 * t + 1] = b;
+                }
+            }
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 D[c] = D[c] - u[c] * a;
@@ -422,6 +428,12 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
             load_r(row + step);
         }
         load_dr(row + step);
+        if constexpr (SUMS == 0) {
+            if (!g.dx) {                     // the means alone
+                load_y(row + step);
+                continue;
+            }
+        }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (!ok[c]) D[c] = zero8();
@@ -510,6 +522,79 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
     }
 }
 
+// Rows longer than 8192, whose sums the registers above cannot hold: the sums alone,
+// with the rows' means that the kernel above has left.  A wave takes 512 columns of every
+// fourth row of its workgroup's share.  4096 rows of 12288: 344 us in all, 629 in one
+// kernel whose sums went to memory; 604 MB and, for the sums, 403 of them again.
+template <bool F32>
+__global__ __launch_bounds__(256) void join_columns_kernel(JoinArgs g) {
+    __shared__ __attribute__((aligned(16))) float red[3][512];
+    constexpr int SZ = F32 ? 4 : 2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int col = 512 * blockIdx.y + 8 * lane;
+    const bool ok = col < g.d;
+    if (!ok) col = 0;
+    const long rows = (g.T + gridDim.x - 1) / gridDim.x, t0 = rows * blockIdx.x;
+    const long t1 = t0 + rows < g.T ? t0 + rows : g.T;
+    f32x8 sum[5], rw = zero8() + 1.f, yw = rw, gt = rw, yb = zero8();
+#pragma unroll
+    for (int a = 0; a < 5; ++a) sum[a] = zero8();
+    if (g.r_weight) rw = ld_f32x8(g.r_weight + col);
+    if (g.y_weight) yw = ld_f32x8(g.y_weight + col);
+    if (g.y_bias) yb = ld_f32x8(g.y_bias + col);
+    if (g.gate) gt = ld_f32x8(g.gate + col);
+    uint64_t seed = 0, offset = 0;
+    if (g.rng) {
+        seed = (uint64_t)g.rng[0];
+        offset = (uint64_t)g.rng[1];
+    }
+#pragma unroll 2
+    for (long t = t0 + wave; t < t1; t += 4) {
+        const size_t i = (size_t)(t * g.d);
+        const f32x4_t st = *reinterpret_cast<const f32x4_t *>(g.stats_in + 4 * t);
+        Raw<F32> rr, dr;
+        Raw<false> hr, yr;
+        rr.clear();
+        dr.clear();
+        hr.clear();
+        if (g.dh && g.r_norm) rr.load((const char *)g.r_in + i * SZ, col);
+        if (g.dh) hr.load(g.dh + i, col);
+        if (g.dr) dr.load((const char *)g.dr + i * SZ, col);
+        if (g.y) yr.load(g.y + i, col);
+        f32x8 D = hr.get();
+        if (g.dh && g.r_norm) {
+            const f32x8 u = (rr.get() - st[2]) * st[3];
+            sum[0] = sum[0] + D * u;
+            sum[1] = sum[1] + D;
+            D = st[3] * (D * rw - u * g.means[2 * t] - g.means[2 * t + 1]);
+        }
+        if (!g.y) continue;
+        D = D + dr.get();
+        f32x8 y = yr.get();
+        if (g.y_norm) y = (y - st[0]) * st[1];
+        f32x8 e = D * (g.scale * g.keep * (g.token_gate ? g.token_gate[t] : 1.f));
+        if (g.rng) e = drop8(e, philox(seed, offset, (uint32_t)col / 8, (uint32_t)t), g.out);
+        sum[2] = sum[2] + (y * yw + yb) * e;
+        e = e * gt;
+        sum[3] = sum[3] + e * y;
+        sum[4] = sum[4] + e;
+    }
+    int n = 0;
+#pragma unroll
+    for (int a = 0; a < 5; ++a) {
+        if (!(g.sums >> a & 1)) continue;
+        __syncthreads();
+        if (wave) st_f32x8(red[wave - 1] + 8 * lane, sum[a]);
+        __syncthreads();
+        if (!wave) {
+#pragma unroll
+            for (int w = 0; w < 3; ++w) sum[a] = sum[a] + ld_f32x8(red[w] + 8 * lane);
+            if (ok) st_f32x8(g.part + ((long)blockIdx.x * g.nsums + n) * g.d + col, sum[a]);
+        }
+        ++n;
+    }
+}
+
 // The workgroups' sums added up, in their order within 16 strided lists whose
 // sums are then added in order: out of array n, columns 4 at a time.
 constexpr int JS_LISTS = 16;
@@ -584,12 +669,30 @@ hipError_t backward(const JoinArgs &g, int blocks, hipStream_t st) {
     if (g.d <= 1024) JOIN_BWD(256, 128, 1);
     if (g.d <= 2048) JOIN_BWD(256, 256, 1);
     if (g.d <= 4096) JOIN_BWD(512, 512, 1);
-    if (g.d <= 8192) JOIN_BWD(512, 512, 2);
-    JOIN_BWD(512, 512, 4);
+    JOIN_BWD(512, 512, 2);
 #undef JOIN_BWD
 }
 template <bool F32>
-hipError_t backward(const JoinArgs &g, int blocks, hipStream_t st) {
+hipError_t backward(JoinArgs g, int blocks, hipStream_t st) {
+    if (g.d > JOIN_SUMS_D) {
+        auto rows = [&](const JoinArgs &q) {
+            join_backward_kernel<F32, 0, true, 512, 512, 4><<<dim3((unsigned)blocks), dim3(512), 0, st>>>(q);
+        };
+        auto columns = [&] {
+            join_columns_kernel<F32><<<dim3((unsigned)blocks, (unsigned)((g.d + 511) / 512)), dim3(256), 0, st>>>(g);
+        };
+        if (!g.nsums) g.means = nullptr;
+        const bool first = g.nsums && g.dx == g.dr;  // before the rows write over what the sums read
+        if (first) {
+            JoinArgs means = g;
+            means.dx = nullptr;
+            rows(means);
+            columns();
+        }
+        rows(g);
+        if (g.nsums && !first) columns();
+        return hipGetLastError();
+    }
     const bool layer = g.r_norm == JOIN_LAYER || g.y_norm == JOIN_LAYER;
     if (!layer && !(g.sums & ~13)) return backward<F32, 13, false>(g, blocks, st);
     if (!(g.sums & ~7)) return backward<F32, 7, true>(g, blocks, st);

@@ -383,6 +383,7 @@ struct JoinArgs {
     int sums = 0, nsums = 0;
     float *out_sums[5] = {};
     float *part = nullptr;             // [join_blocks][nsums][d]
+    float *means = nullptr;            // d > JOIN_SUMS_D: [T][2]
 };
 int join_blocks(long T, int d);        // workgroups of a backward
 hipError_t launch_join_forward(const JoinArgs &g, hipStream_t st);

@@ -355,8 +355,8 @@ inline bool mx_keep_l2(long R, long E, long K, long N) {
 // Joining a block to the residual stream (join.hip): rows up to which a row gets
 // as many threads as have something to load.
 constexpr long JOIN_FEW_ROWS = 256;
-// Row lengths: what a workgroup's registers hold.
-constexpr long JOIN_MAX_D = 16384;
+// Row lengths: what a workgroup's registers hold; with the sums over the rows beside it.
+constexpr long JOIN_MAX_D = 16384, JOIN_SUMS_D = 8192;
 // The backward: threads of a row (8 values each up to 4096), of a workgroup, and the
 // workgroups, which leave a row of sums each: one to a CU where a row takes 512 threads,
 // else three, if each has 4 rounds of rows left (us with 256 / 768: 16384 x 2048 116 /

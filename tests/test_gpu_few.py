@@ -264,10 +264,12 @@ def test_an_expert_reaches_its_tokens_alone(value):
     bad.check_guards()
 
 
-def test_repeats_streams_and_two_at_once():
-    """The same bits again, on another stream, and with another call running beside."""
-    a, b = Case(16, 2048, 64, 4, 768, 512, balance=0.1), Case(3, 4096, 16, 4, 1024)
-    runs = [(Run(c, inputs(c, 3)), Run(c, inputs(c, 3))) for c in (a, b)]
+def test_repeats_streams_and_several_at_once():
+    """The same bits again, on other streams, with three other calls running beside (more workgroups
+    than the GPU holds at once)."""
+    cases = (Case(16, 2048, 64, 4, 768, 512, balance=0.1), Case(3, 4096, 16, 4, 1024), Case(16, 1024, 32, 8, 1536),
+             Case(9, 512, 128, 8, 512, 256, "sigmoid"))
+    runs = [(Run(c, inputs(c, 3)), Run(c, inputs(c, 3))) for c in cases]
     for r, _ in runs:
         r.call()
     torch.cuda.synchronize()

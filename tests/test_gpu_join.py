@@ -50,6 +50,8 @@ CASES = [
     Case(600, 4096, y_norm="layer", r_norm="none"), Case(259, 4104, "f32", "rms", "rms", True, True, 0.3, 0.01),
     Case(520, 7168, gate=True, drop=0.1), Case(261, 8192, "f32", "layer", "layer"), Case(16, 8200, y_norm="none"),
     Case(301, 16384, "f32", "layer", "layer", True, True, 0.7, 0.1), Case(300, 12296, gate=True, drop=0.5),
+    Case(1025, 9224, "f32", "none", "layer", True, False, 0.5), Case(2, 16384, y_norm="layer", r_norm="none", drop=0.2),
+    Case(300, 8200, block=False, y_norm="none"), Case(70, 12288, "f32", "rms", "rms", weights=False),
     Case(256, 2048, r_norm="none", y_norm="none", drop=0.1), Case(5, 24, "f32", "rms", "none", weights=False),
     # the norm before the first block; norms without weights
     Case(1, 2048, block=False, y_norm="none"), Case(400, 4096, "f32", "none", "layer", block=False),
@@ -174,7 +176,11 @@ def test_against_the_definition(c):
 
 
 def test_repeats_bit_for_bit_and_on_another_stream():
-    c = Case(1111, 2048, "f32", "layer", "rms", True, True, 0.5, 0.1)
+    for c in (Case(1111, 2048, "f32", "layer", "rms", True, True, 0.5, 0.1), Case(600, 8400, token_gate=True, drop=0.1)):
+        repeat(c)
+
+
+def repeat(c):
     first = Run(c)
     first.forward()
     first.backward()
@@ -190,8 +196,9 @@ def test_repeats_bit_for_bit_and_on_another_stream():
         assert torch.equal(t, again.outputs()[n]), n
 
 
-def test_in_place_gives_the_same():
-    c = Case(300, 1000, "bf16", "rms", "layer", True, False, 1.0, 0.2)
+@pytest.mark.parametrize("c", [Case(300, 1000, "bf16", "rms", "layer", True, False, 1.0, 0.2),
+                               Case(270, 9000, "bf16", "rms", "layer", True, True, 1.0, 0.2)], ids=("1000", "9000"))
+def test_in_place_gives_the_same(c):
     a, b = Run(c), Run(c)
     a.forward()
     a.backward()
@@ -203,6 +210,8 @@ def test_in_place_gives_the_same():
     assert torch.equal(a.r[:c.T], b.x) and torch.equal(a.dx[:c.T], b.dr)
     for n in ("h", "stats", "dy"):
         assert torch.equal(getattr(a, n), getattr(b, n)), n
+    for n in a.g:
+        assert torch.equal(a.g[n], b.g[n]), n
 
 
 @pytest.mark.parametrize("which", ("dr", "dh"))
