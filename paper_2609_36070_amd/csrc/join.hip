@@ -175,19 +175,16 @@ DEV const float *again(const float *p) {
 DEV float dev_inv(float var, float eps) { return 1.0f / sqrtf(var + eps); }
 
 // ---------------------------------------------------------------- forward
-// Values past the row's end are loaded as zeros.
-template <bool F32, int G, int CH>
-__global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArgs g) {
-    constexpr int NT = G < 256 ? 256 : G, NW = NT / 64;
-    __shared__ float red[4][NW][4];
+// Values past the row's end are loaded as zeros.  ROWS: a workgroup takes rows in
+// steps of the whole grid, with the weights in LDS and each row asked for while the
+// one before is worked on; otherwise NT / G rows.
+template <bool F32, bool ROWS, int NT, int G, int CH>
+__global__ __launch_bounds__(NT) void join_forward_kernel(JoinArgs g) {
+    constexpr int NG = NT / G, SZ = F32 ? 4 : 2;
+    __shared__ float red[ROWS ? 8 : 4][NT / 64][4];
+    extern __shared__ __attribute__((aligned(16))) float w_lds[];
     const int lane = threadIdx.x % G;
-    const long row = g.row0 + (long)blockIdx.x * (NT / G) + row_of_thread<G>();
-    if (G <= 64 && row >= g.T) return;       // no barriers then
-    const bool on = row < g.T;
-    const long t = on ? row : g.T - 1;
     const float inv_d = 1.0f / (float)g.d;
-    const size_t ts = (size_t)(t * g.d) * (F32 ? 4 : 2);         // bytes to the row in the stream
-    const char *xp = (const char *)g.x + ts;
     bool ok[CH];
     int col[CH];
     Raw<F32> xr[CH];
@@ -196,93 +193,131 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void join_forward_kernel(JoinArg
     for (int c = 0; c < CH; ++c) {
         col[c] = 8 * (lane + G * c);
         ok[c] = col[c] < g.d;
-        if (ok[c]) {
-            xr[c].load(xp, col[c]);
-        } else {
-            col[c] = 0;
-            xr[c].clear();
-        }
+        if (!ok[c]) col[c] = 0;
+        xr[c].clear();
+        yr[c].clear();
     }
-    if (g.y)
+    enum { YW, YB, GATE, RW, RB };
+    const float *weights[5] = {g.y_weight, g.y_bias, g.gate, g.r_weight, g.r_bias};
+    int at[5], n_w = 0;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            yr[c].clear();
-            if (ok[c]) yr[c].load(g.y + t * g.d, col[c]);
-        }
-    float ym = 0.f, ys = 0.f, rm = 0.f, rs = 0.f;
-    // mean and 1 / deviation of the row in v
-    auto stats = [&](const f32x8 (&v)[CH], int kind, float eps, float &m, float &s, int at) {
-        float sum[1] = {0.f};
-        if (kind == JOIN_LAYER) {
+    for (int a = 0; a < 5; ++a) at[a] = weights[a] ? n_w++ * g.d : 0;
+    if constexpr (ROWS) {                    // two planes of 4 columns of 8 each
 #pragma unroll
-            for (int c = 0; c < CH; ++c) sum[0] = sum[0] + sum8(v[c]);
-            row_sums<G>(sum, red[at]);
-            m = sum[0] * inv_d;
-            sum[0] = 0.f;
+        for (int a = 0; a < 5; ++a)
+            if (weights[a])
+                for (int j = threadIdx.x; j < g.d / 4; j += NT)
+                    *reinterpret_cast<f32x4_t *>(w_lds + at[a] + (j & 1) * (g.d / 2) + 4 * (j >> 1)) =
+                        *reinterpret_cast<const f32x4_t *>(weights[a] + 4 * j);
+        __syncthreads();
+    }
+    auto weight = [&](int a, int c) {
+        if constexpr (!ROWS) return ld_f32x8(weights[a] + col[c]);
+        const float *p = w_lds + at[a] + col[c] / 2;
+        const f32x4_t lo = *reinterpret_cast<const f32x4_t *>(p);
+        const f32x4_t hi = *reinterpret_cast<const f32x4_t *>(p + g.d / 2);
+        return f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    uint64_t seed = 0, offset = 0;
+    if (g.rng) {
+        seed = (uint64_t)g.rng[0];
+        offset = (uint64_t)g.rng[1];
+    }
+    const long step = (long)gridDim.x * NG, rounds = ROWS ? (g.T + step - 1) / step : 1;
+    long row = g.row0 + (long)blockIdx.x * NG + row_of_thread<G>();
+    if (!ROWS && G <= 64 && row >= g.T) return;      // no barriers then
+    // (a row past the last is the last one again, and not stored)
+    auto load_x = [&](long t) {
+        const size_t i = (size_t)((t < g.T ? t : g.T - 1) * g.d);
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (ok[c]) xr[c].load((const char *)g.x + i * SZ, col[c]);
+    };
+    auto load_y = [&](long t) {
+        const size_t i = (size_t)((t < g.T ? t : g.T - 1) * g.d);
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (ok[c] && g.y) yr[c].load(g.y + i, col[c]);
+    };
+    load_x(row);
+    load_y(row);
+    for (long k = 0; k < rounds; ++k, row += step) {
+        const bool on = row < g.T;
+        const long t = on ? row : g.T - 1;
+        const size_t i = (size_t)(t * g.d);
+        float (*slots)[NT / 64][4] = red + (ROWS ? 4 * (k & 1) : 0);
+        float ym = 0.f, ys = 0.f, rm = 0.f, rs = 0.f;
+        // mean and 1 / deviation of the row in v
+        auto stats = [&](const f32x8 (&v)[CH], int kind, float eps, float &m, float &s, int slot) {
+            float sum[1] = {0.f};
+            if (kind == JOIN_LAYER) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c) sum[0] = sum[0] + sum8(v[c]);
+                row_sums<G>(sum, slots[slot]);
+                m = sum[0] * inv_d;
+                sum[0] = 0.f;
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const f32x8 u = v[c] - m;
+                    const float q = dot8(u, u);
+                    sum[0] = sum[0] + (ok[c] ? q : 0.f);
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < CH; ++c) sum[0] = sum[0] + dot8(v[c], v[c]);
+            }
+            row_sums<G>(sum, slots[slot + 1]);
+            s = dev_inv(sum[0] * inv_d, eps);
+        };
+        auto normed = [&](const f32x8 &v, int kind, float m, float s, int w, int b, int c) {
+            f32x8 n = kind == JOIN_LAYER ? (v - m) * s : v * s;
+            if (weights[w]) n = n * weight(w, c);
+            if (weights[b]) n = n + weight(b, c);
+            return n;
+        };
+        f32x8 r[CH];
+        if (g.y) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) r[c] = yr[c].get();
+            if constexpr (ROWS) load_y(row + step);
+            if (g.y_norm) {
+                stats(r, g.y_norm, g.y_eps, ym, ys, 0);
+#pragma unroll
+                for (int c = 0; c < CH; ++c) r[c] = normed(r[c], g.y_norm, ym, ys, YW, YB, c);
+            }
+            const float a = g.scale * g.keep * (g.token_gate ? g.token_gate[t] : 1.f);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const f32x8 u = v[c] - m;
-                const float q = dot8(u, u);
-                sum[0] = sum[0] + (ok[c] ? q : 0.f);
+                f32x8 v = r[c];
+                if (g.gate) v = v * weight(GATE, c);
+                v = v * a;
+                if (g.rng) v = drop8(v, philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t), g.out);
+                r[c] = xr[c].get() + v;
+                if constexpr (!F32) {
+                    Raw<false> q;
+                    q.a = pack_bf8(r[c]);
+                    r[c] = q.get();
+                    if (on && ok[c]) st_u32x4((uint16_t *)g.r + i + col[c], q.a);
+                } else {
+                    if (on && ok[c]) st_f32x8((float *)g.r + i + col[c], r[c]);
+                }
+                if (!ok[c]) r[c] = zero8();          // what a bias has left there
             }
         } else {
 #pragma unroll
-            for (int c = 0; c < CH; ++c) sum[0] = sum[0] + dot8(v[c], v[c]);
+            for (int c = 0; c < CH; ++c) r[c] = xr[c].get();
         }
-        row_sums<G>(sum, red[at + 1]);
-        s = dev_inv(sum[0] * inv_d, eps);
-    };
-    auto normed = [&](const f32x8 &v, int kind, float m, float s, const float *w, const float *b, int at) {
-        f32x8 n = kind == JOIN_LAYER ? (v - m) * s : v * s;
-        if (w) n = n * ld_f32x8(w + at);
-        if (b) n = n + ld_f32x8(b + at);
-        return n;
-    };
-    f32x8 r[CH];
-    if (g.y) {
+        if constexpr (ROWS) load_x(row + step);
+        if (g.r_norm) stats(r, g.r_norm, g.r_eps, rm, rs, 2);
+        if (g.h)
 #pragma unroll
-        for (int c = 0; c < CH; ++c) r[c] = yr[c].get();
-        if (g.y_norm) {
-            stats(r, g.y_norm, g.y_eps, ym, ys, 0);
-#pragma unroll
-            for (int c = 0; c < CH; ++c) r[c] = normed(r[c], g.y_norm, ym, ys, g.y_weight, g.y_bias, col[c]);
-        }
-        uint64_t seed = 0, offset = 0;
-        if (g.rng) {
-            seed = (uint64_t)g.rng[0];
-            offset = (uint64_t)g.rng[1];
-        }
-        const float a = g.scale * g.keep * (g.token_gate ? g.token_gate[t] : 1.f);
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            f32x8 v = r[c];
-            if (g.gate) v = v * ld_f32x8(g.gate + col[c]);
-            v = v * a;
-            if (g.rng) v = drop8(v, philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t), g.out);
-            r[c] = xr[c].get() + v;
-            if constexpr (!F32) {
-                Raw<false> q;
-                q.a = pack_bf8(r[c]);
-                r[c] = q.get();
-                if (on && ok[c]) st_u32x4((uint16_t *)((char *)g.r + ts) + col[c], q.a);
-            } else {
-                if (on && ok[c]) st_f32x8((float *)((char *)g.r + ts) + col[c], r[c]);
+            for (int c = 0; c < CH; ++c) {
+                if (g.r_norm) r[c] = normed(r[c], g.r_norm, rm, rs, RW, RB, c);
+                if (on && ok[c]) st_u32x4(g.h + i + col[c], pack_bf8(r[c]));
             }
-            if (!ok[c]) r[c] = zero8();      // what a bias has left there
-        }
-    } else {
-#pragma unroll
-        for (int c = 0; c < CH; ++c) r[c] = xr[c].get();
+        if (g.stats && on && lane == 0)
+            *reinterpret_cast<f32x4_t *>(g.stats + 4 * t) = f32x4_t{ym, ys, rm, rs};
     }
-    if (g.r_norm) stats(r, g.r_norm, g.r_eps, rm, rs, 2);
-    if (g.h)
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if (g.r_norm) r[c] = normed(r[c], g.r_norm, rm, rs, g.r_weight, g.r_bias, col[c]);
-            if (on && ok[c]) st_u32x4(g.h + t * g.d + col[c], pack_bf8(r[c]));
-        }
-    if (g.stats && on && lane == 0)
-        *reinterpret_cast<f32x4_t *>(g.stats + 4 * t) = f32x4_t{ym, ys, rm, rs};
 }
 
 // ---------------------------------------------------------------- backward
@@ -624,14 +659,28 @@ hipError_t forward(JoinArgs g, hipStream_t st) {
     // a launch takes fewer than 2^32 threads
 #define JOIN_FWD(G, CH)                                                                              \
     do {                                                                                             \
-        const long per = G < 256 ? 256 / G : 1, most = 1l << 21;                                     \
+        constexpr int NT = G < 256 ? 256 : G;                                                        \
+        const long per = NT / G, most = 1l << 21;                                                    \
         for (g.row0 = 0; g.row0 < g.T; g.row0 += most * per) {                                       \
             const long n = (g.T - g.row0 + per - 1) / per;                                           \
-            join_forward_kernel<F32, G, CH>                                                          \
-                <<<dim3((unsigned)(n < most ? n : most)), dim3(G < 256 ? 256 : G), 0, st>>>(g);      \
+            join_forward_kernel<F32, false, NT, G, CH>                                               \
+                <<<dim3((unsigned)(n < most ? n : most)), dim3(NT), 0, st>>>(g);                     \
         }                                                                                            \
         return hipGetLastError();                                                                    \
     } while (0)
+#define JOIN_ROWS(G, CH)                                                                             \
+    do {                                                                                             \
+        join_forward_kernel<F32, true, 1024, G, CH><<<dim3(256), dim3(1024), lds, st>>>(g);          \
+        return hipGetLastError();                                                                    \
+    } while (0)
+    const int n_w = !!g.r_weight + !!g.r_bias + !!g.y_weight + !!g.y_bias + !!g.gate;
+    const size_t lds = (size_t)n_w * g.d * 4;
+    if (join_forward_rows(g.T, g.d, n_w, g.y != nullptr)) {
+        if (g.d <= 1024) JOIN_ROWS(128, 1);
+        if (g.d <= 2048) JOIN_ROWS(256, 1);
+        if (g.d <= 4096) JOIN_ROWS(512, 1);
+        JOIN_ROWS(512, 2);
+    }
     if (g.d <= 64) JOIN_FWD(8, 1);
     if (g.d <= 128) JOIN_FWD(16, 1);
     if (g.d <= 256) JOIN_FWD(32, 1);
@@ -650,6 +699,7 @@ hipError_t forward(JoinArgs g, hipStream_t st) {
     if (g.d <= 8192) JOIN_FWD(256, 4);
     JOIN_FWD(512, 4);
 #undef JOIN_FWD
+#undef JOIN_ROWS
 }
 
 template <bool F32, int SUMS, bool LAYER>

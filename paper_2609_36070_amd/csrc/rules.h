@@ -355,6 +355,14 @@ inline bool mx_keep_l2(long R, long E, long K, long N) {
 // Joining a block to the residual stream (join.hip): rows up to which a row gets
 // as many threads as have something to load.
 constexpr long JOIN_FEW_ROWS = 256;
+// The forward: one workgroup of 1024 threads to a CU, with the weights in LDS, if it has 12
+// rounds of rows (us, a workgroup per 1 to 4 rows / this: 16384 x 7168 211 / 189, in fp32 291 /
+// 257; 8192 x 4096 66 / 61; 16384 x 2048 59 / 57; 6001 x 2048 31.7 / 32.8; 2100 x 7168 26 / 30).  A
+// norm alone has little to read again: 4099 x 4096 13.7 / 17.2.
+inline bool join_forward_rows(long T, long d, int weights, bool block) {
+    const long rows = d <= 1024 ? 8 : d <= 2048 ? 4 : 2;     // of a workgroup at a time
+    return block && d > 512 && d <= 8192 && T >= 12 * 256 * rows && weights * d * 4 <= 144 * 1024;
+}
 // Row lengths: what a workgroup's registers hold; with the sums over the rows beside it.
 constexpr long JOIN_MAX_D = 16384, JOIN_SUMS_D = 8192;
 // The backward: threads of a row (8 values each up to 4096), of a workgroup, and the

@@ -50,6 +50,9 @@ CASES = [
     Case(600, 4096, y_norm="layer", r_norm="none"), Case(259, 4104, "f32", "rms", "rms", True, True, 0.3, 0.01),
     Case(520, 7168, gate=True, drop=0.1), Case(261, 8192, "f32", "layer", "layer"), Case(16, 8200, y_norm="none"),
     Case(301, 16384, "f32", "layer", "layer", True, True, 0.7, 0.1), Case(300, 12296, gate=True, drop=0.5),
+    # workgroups that take many rows of the forward, a ragged number of them
+    Case(24577, 520, y_norm="none", drop=0.1), Case(12289, 1032, "f32", "layer", "layer", True), Case(6145, 2056, gate=True),
+    Case(6150, 4104, "f32", "none", "rms", token_gate=True, drop=0.1),
     Case(1025, 9224, "f32", "none", "layer", True, False, 0.5), Case(2, 16384, y_norm="layer", r_norm="none", drop=0.2),
     Case(300, 8200, block=False, y_norm="none"), Case(70, 12288, "f32", "rms", "rms", weights=False),
     Case(256, 2048, r_norm="none", y_norm="none", drop=0.1), Case(5, 24, "f32", "rms", "none", weights=False),
