@@ -624,26 +624,37 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
             if (tid == 0 && sb - sa == 256) poll(h_done + FEW_LINE * (1 + sb), up_e, err);
             __syncthreads();
             if (tid == 0) next = add(queue) + gridDim.x;
-            const uint16_t *hp = H + ((long)it.u0 * T + tok) * FEW_UNIT + kw;
-            u32x4_t h0 = ld_u32x4(hp), l0 = ld_u32x4(hp + plane), h1, l1;
-            int s = sa;
-            const uint16_t *wp = np;
+            // A token that did not choose an expert takes the H of one that did: its
+            // column is dropped, and the loads fetch no lines of their own.
+            auto h_at = [&](int q) {
+                const int chose = q < 0 ? 0 : s_mask[q], t = (chose >> r) & 1 ? r : __builtin_ctz(chose | 0x10000);
+                return (q < 0 ? tok : t) * FEW_UNIT + kw;
+            };
+            int s = sa, left = s < 0 ? su - it.u0 : fu - (it.u0 - su - s * fu);    // units of it
+            const uint16_t *hu = H + (long)it.u0 * T * FEW_UNIT, *wp = np;
+            int at = h_at(s);
+            u32x4_t h0 = ld_u32x4(hu + at), l0 = ld_u32x4(hu + plane + at), h1, l1;
 #pragma unroll 1
             for (int u = it.u0; u < it.u1; ++u) {
-                h1 = ld_u32x4(hp + 128);
-                l1 = ld_u32x4(hp + plane + 128);
+                h1 = ld_u32x4(hu + at + 128);
+                l1 = ld_u32x4(hu + plane + at + 128);
                 load(w1, wp + 128l * d, d);
                 __builtin_amdgcn_sched_barrier(0);
                 mul2(w0, h0, l0);
                 __builtin_amdgcn_sched_barrier(0);
-                hp += (long)T * FEW_UNIT;
                 int sn = s;
                 if (u + 1 < it.u1) {
-                    h0 = ld_u32x4(hp);
-                    l0 = ld_u32x4(hp + plane);
-                    wp = down_ptr(u + 1, it.n0);
+                    hu += (long)T * FEW_UNIT;
+                    wp += 256l * d;
+                    if (--left == 0) {
+                        sn = s + 1;
+                        left = fu;
+                        at = h_at(sn);
+                        wp = down_ptr(u + 1, it.n0);
+                    }
+                    h0 = ld_u32x4(hu + at);
+                    l0 = ld_u32x4(hu + plane + at);
                     load(w0, wp, d);
-                    sn = slot_of(u + 1);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 mul2(w1, h1, l1);
