@@ -25,6 +25,7 @@
 #include "common.h"
 #include "few.h"
 #include "kernels.h"
+#include "rules.h"
 
 namespace {
 
@@ -363,6 +364,8 @@ DEV void stores_done() {
 }
 DEV int add(int *ctr) { return __hip_atomic_fetch_add(ctr, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
+// PAST: weights are loaded past the caches (few_past_caches).
+template <bool PAST>
 __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
     __shared__ __attribute__((aligned(16))) union {
         float red[NW][16][PITCH];
@@ -504,7 +507,10 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
     u32x4_t w0[8], w1[8];
     auto load = [&](u32x4_t (&w)[8], const uint16_t *p, long ld) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = ld_u32x4(p + j * ld);
+        for (int j = 0; j < 8; ++j) {
+            const u32x4_t *q = reinterpret_cast<const u32x4_t *>(p + j * ld);
+            w[j] = PAST ? __builtin_nontemporal_load(q) : *q;
+        }
     };
     f32x4_t acc[8];
     auto operand = [&](const u32x4_t (&w)[8], int i) {
@@ -795,6 +801,7 @@ hipError_t launch_few(const FewArgs &g, hipStream_t st) {
         few_router_kernel<1><<<dim3((unsigned)g.S, (unsigned)((g.E + 15) / 16)), dim3(64 * RW), 0, st>>>(g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    few_kernel<<<dim3(FEW_WGS), dim3(NT), 0, st>>>(g);
+    if (few_past_caches(g.T, g.d, g.E, g.k, g.f, g.fs)) few_kernel<true><<<dim3(FEW_WGS), dim3(NT), 0, st>>>(g);
+    else few_kernel<false><<<dim3(FEW_WGS), dim3(NT), 0, st>>>(g);
     return hipGetLastError();
 }

@@ -352,6 +352,16 @@ inline bool mx_keep_l2(long R, long E, long K, long N) {
     return K <= 1024 && R >= 1024 * E && bytes >= (64L << 20) && bytes <= (208L << 20);
 }
 
+// The whole layer for a few tokens (few.hip): weights that are more than the 256 MB of the
+// memory's cache are loaded past it.  us through the caches / past them, the calls taking
+// turns on 4 sets of weights: 76 MB 37.5 / 37.9, 152 MB 53.3 / 51.3, 353 MB 94 / 88, 500 MB 120
+// / 114, 794 MB 177 / 167; on one set, which the cache holds up to there: 76 MB 32.8 / 36.6, 152
+// MB 45.9 / 51.2, 202 MB 52 / 60, 353 MB 88 / 88.
+inline bool few_past_caches(long T, long d, long E, long k, long f, long fs) {
+    const double reached = E * (1.0 - std::pow(1.0 - (double)k / E, (double)T));
+    return 6.0 * d * (reached * f + fs) > 256e6;
+}
+
 // Joining a block to the residual stream (join.hip): rows up to which a row gets
 // as many threads as have something to load.
 constexpr long JOIN_FEW_ROWS = 256;

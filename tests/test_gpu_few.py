@@ -66,6 +66,7 @@ CASES = [
     Case(13, 512, 51, 16, 256, 768, "softmax", 3, 2, "pair", True, 0.5, 0.0), Case(5, 4096, 12, 4, 512, 0, "sigmoid"),
     Case(16, 1280, 20, 4, 1024, 512, "softmax", 4, 2, balance=0.1), Case(9, 256, 160, 6, 512, 256, "sigmoid", 8, 3, "pair"),
     Case(16, 256, 4, 4, 256, 256), Case(6, 2304, 60, 1, 768), Case(11, 1792, 96, 6, 256, 2048, "sigmoid", renormalise=False),
+    Case(9, 2048, 16, 8, 1536),      # more weights than the caches hold
     Case(16, 1024, 2, 1, 2048, bias=1.0), Case(10, 512, 7, 7, 256, 0, "sigmoid", 7, 7, "pair"),
 ]
 IDS = ["-".join(str(v) for v in dataclasses.astuple(c)) for c in CASES]
