@@ -58,11 +58,24 @@ DEV f32x8 drop8(const f32x8 &n, const Words &w, uint32_t out) {
 }
 
 // ---------------------------------------------------------------- rows
+// PAST: past the caches, which hold none of what is that large.
+template <bool PAST>
+DEV u32x4_t ld16(const void *p) {
+    const u32x4_t *q = reinterpret_cast<const u32x4_t *>(p);
+    return PAST ? __builtin_nontemporal_load(q) : *q;
+}
+template <bool PAST>
+DEV void st16(void *p, u32x4_t v) {
+    u32x4_t *q = reinterpret_cast<u32x4_t *>(p);
+    if constexpr (PAST) __builtin_nontemporal_store(v, q);
+    else *q = v;
+}
 // 8 consecutive values as they lie in memory
 template <bool F32> struct Raw;
 template <> struct Raw<false> {
     u32x4_t a;
-    DEV void load(const void *p, int i) { a = ld_u32x4((const uint16_t *)p + i); }
+    template <bool PAST = false>
+    DEV void load(const void *p, int i) { a = ld16<PAST>((const uint16_t *)p + i); }
     DEV void clear() { a = u32x4_t{0u, 0u, 0u, 0u}; }
     DEV f32x8 get() const {
         return f32x8{bf_lo(a[0]), bf_hi(a[0]), bf_lo(a[1]), bf_hi(a[1]),
@@ -71,9 +84,10 @@ template <> struct Raw<false> {
 };
 template <> struct Raw<true> {
     u32x4_t a, b;
+    template <bool PAST = false>
     DEV void load(const void *p, int i) {
-        a = ld_u32x4((const float *)p + i);
-        b = ld_u32x4((const float *)p + i + 4);
+        a = ld16<PAST>((const float *)p + i);
+        b = ld16<PAST>((const float *)p + i + 4);
     }
     DEV void clear() { a = b = u32x4_t{0u, 0u, 0u, 0u}; }
     DEV f32x8 get() const {
@@ -86,10 +100,20 @@ template <> struct Raw<true> {
         return v;
     }
 };
-template <bool F32>
+template <bool F32, bool PAST = false>
 DEV void put(void *p, int i, const f32x8 &v) {
-    if constexpr (F32) st_f32x8((float *)p + i, v);
-    else st_u32x4((uint16_t *)p + i, pack_bf8(v));
+    if constexpr (F32) {
+        u32x4_t lo, hi;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            lo[q] = __float_as_uint(v[q]);
+            hi[q] = __float_as_uint(v[4 + q]);
+        }
+        st16<PAST>((float *)p + i, lo);
+        st16<PAST>((float *)p + i + 4, hi);
+    } else {
+        st16<PAST>((uint16_t *)p + i, pack_bf8(v));
+    }
 }
 
 // ---------------------------------------------------------------- sums over a row
@@ -177,7 +201,8 @@ DEV float dev_inv(float var, float eps) { return 1.0f / sqrtf(var + eps); }
 // ---------------------------------------------------------------- forward
 // Values past the row's end are loaded as zeros.  ROWS: a workgroup takes rows in
 // steps of the whole grid, with the weights in LDS and each row asked for while the
-// one before is worked on; otherwise NT / G rows.
+// one before is worked on, past the caches (16384 x 7168: 162 us, through them 173); otherwise
+// NT / G rows.
 template <bool F32, bool ROWS, int NT, int G, int CH>
 __global__ __launch_bounds__(NT) void join_forward_kernel(JoinArgs g) {
     constexpr int NG = NT / G, SZ = F32 ? 4 : 2;
@@ -222,13 +247,13 @@ __global__ __launch_bounds__(NT) void join_forward_kernel(JoinArgs g) {
         const size_t i = (size_t)((t < g.T ? t : g.T - 1) * g.d);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
-            if (ok[c]) xr[c].load((const char *)g.x + i * SZ, col[c]);
+            if (ok[c]) xr[c].template load<ROWS>((const char *)g.x + i * SZ, col[c]);
     };
     auto load_y = [&](long t) {
         const size_t i = (size_t)((t < g.T ? t : g.T - 1) * g.d);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
-            if (ok[c] && g.y) yr[c].load(g.y + i, col[c]);
+            if (ok[c] && g.y) yr[c].template load<ROWS>(g.y + i, col[c]);
     };
     load_x(row);
     load_y(row);
@@ -297,9 +322,9 @@ __global__ __launch_bounds__(NT) void join_forward_kernel(JoinArgs g) {
                     Raw<false> q;
                     q.a = pack_bf8(r[c]);
                     r[c] = q.get();
-                    if (on && ok[c]) st_u32x4((uint16_t *)g.r + i + col[c], q.a);
+                    if (on && ok[c]) st16<ROWS>((uint16_t *)g.r + i + col[c], q.a);
                 } else {
-                    if (on && ok[c]) st_f32x8((float *)g.r + i + col[c], r[c]);
+                    if (on && ok[c]) put<true, ROWS>((float *)g.r + i, col[c], r[c]);
                 }
                 if (!ok[c]) r[c] = zero8();          // what a bias has left there
             }
@@ -313,7 +338,7 @@ __global__ __launch_bounds__(NT) void join_forward_kernel(JoinArgs g) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 if (g.r_norm) r[c] = normed(r[c], g.r_norm, rm, rs, RW, RB, c);
-                if (on && ok[c]) st_u32x4(g.h + i + col[c], pack_bf8(r[c]));
+                if (on && ok[c]) put<false, ROWS>(g.h + i, col[c], r[c]);
             }
         if (g.stats && on && lane == 0)
             *reinterpret_cast<f32x4_t *>(g.stats + 4 * t) = f32x4_t{ym, ys, rm, rs};
