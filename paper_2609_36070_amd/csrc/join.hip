@@ -19,6 +19,19 @@
 // The mask of the dropout is computed again where it is needed (Philox4x32-10:
 // Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011;
 // 8 elements per block of the generator).
+//
+// Statistics, sums and everything between load and store are fp32.  r is rounded
+// where it is stored, and h is made from that value, which is what the backward and
+// the next block find; h and dy are bf16, as the layer's inputs and outputs.
+//
+// Bound by memory: 16384 x 7168 in bf16 162 us (0.94 GB, 5.8 TB/s), its gradient 312 (1.41
+// GB, 4.5; a copy of 2 GiB 4.9).  The gradient has 40 vector instructions for an element
+// and those of the generator, 55 % of the SIMDs' time, between two sums over the row, so
+// what counts is that a row's loads are on their way during the row before it, and that
+// nothing waits behind them: weights from memory instead of LDS return after them (367
+// us), and so do registers that were spilt (1117 us with room for all five sums).
+// Tried and slower: 1024 threads of 8 values for such a row (128 registers; 378 us), rows
+// of two workgroups on a CU, each with its own sums (390).
 #include <algorithm>
 
 #include "common.h"
@@ -655,33 +668,35 @@ __global__ __launch_bounds__(256) void join_columns_kernel(JoinArgs g) {
     }
 }
 
-// The workgroups' sums added up, in their order within 16 strided lists (16 loads
-// under way in each: 7 -> 3.5 us for 768 workgroups) whose sums are then added in order: array
-// n, columns 4 at a time.
-constexpr int JS_LISTS = 16;
+// The workgroups' sums added up, in their order within 32 strided lists whose sums are
+// then added in order: array n, columns 4 at a time, 8 of those to a workgroup (768
+// workgroups, 3 x 2048 columns: 5.6 us, with 16 lists of 64 columns 6.4).
+constexpr int JS_LISTS = 32, JS_QUADS = 8, JS_LOADS = 8;     // loads under way in a list
 __global__ __launch_bounds__(256) void join_sum_kernel(JoinArgs g, int blocks) {
-    __shared__ __attribute__((aligned(16))) float red[JS_LISTS][16][4];
-    const int c = 4 * (blockIdx.x * 16 + (threadIdx.x & 15)), list = threadIdx.x >> 4, n = blockIdx.y;
+    __shared__ __attribute__((aligned(16))) float red[JS_LISTS][JS_QUADS][4];
+    const int quad = threadIdx.x % JS_QUADS, list = threadIdx.x / JS_QUADS, n = blockIdx.y;
+    const int c = 4 * (blockIdx.x * JS_QUADS + quad);
     f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (c < g.d)
-        for (int b = list; b < blocks; b += JS_LISTS * 16) {
-            f32x4_t u[16];
+        for (int b = list; b < blocks; b += JS_LISTS * JS_LOADS) {
+            f32x4_t u[JS_LOADS];
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
+            for (int j = 0; j < JS_LOADS; ++j)
                 u[j] = *reinterpret_cast<const f32x4_t *>(
                     g.part + ((long)min(b + JS_LISTS * j, blocks - 1) * g.nsums + n) * g.d + c);
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
+            for (int j = 0; j < JS_LOADS; ++j)
                 if (b + JS_LISTS * j < blocks)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) v[q] = v[q] + u[j][q];
         }
-    *reinterpret_cast<f32x4_t *>(red[list][threadIdx.x & 15]) = v;
+    *reinterpret_cast<f32x4_t *>(red[list][quad]) = v;
     __syncthreads();
-    if (threadIdx.x < 16 && c < g.d) {
+    if (list == 0 && c < g.d) {
+#pragma unroll
         for (int l = 1; l < JS_LISTS; ++l)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = v[q] + red[l][threadIdx.x][q];
+            for (int q = 0; q < 4; ++q) v[q] = v[q] + red[l][quad][q];
         *reinterpret_cast<f32x4_t *>(g.out_sums[n] + c) = v;
     }
 }
@@ -797,6 +812,7 @@ hipError_t launch_join_backward(JoinArgs g, hipStream_t st) {
         if (e != hipSuccess) return e;
     }
     if (!g.nsums) return hipSuccess;
-    join_sum_kernel<<<dim3((unsigned)((g.d + 63) / 64), (unsigned)g.nsums), dim3(256), 0, st>>>(g, blocks);
+    join_sum_kernel<<<dim3((unsigned)((g.d + 4 * JS_QUADS - 1) / (4 * JS_QUADS)), (unsigned)g.nsums), dim3(256), 0, st>>>(
+        g, blocks);
     return hipGetLastError();
 }
