@@ -444,6 +444,8 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
         if (tid == 0) {
             s_last = s.cnt[0] + s.cnt[1] + s.cnt[2] + s.cnt[3];
             s_next = FEW_QUEUES * next + blockIdx.x % FEW_QUEUES;
+            // others have done this workgroup's first item: it goes on where they are
+            if (s_next >= (int)gridDim.x) s_next = add(queue) + gridDim.x;
         }
         __syncthreads();
         const int t = tid / 16, j = tid % 16;
@@ -581,11 +583,13 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
                         __ballot(lane < FEW_QUEUES && FEW_QUEUES * c + lane < first_ups);
                     if (!left) break;
                     const int from = __builtin_ctzll(left);
-                    int n = 0;
-                    if (lane == 0) n = add(firsts + from * FEW_LINE);
-                    n = FEW_QUEUES * __builtin_amdgcn_readfirstlane(n) + from;
-                    if (n < first_ups) {
-                        i = n;
+                    // (no add: behind the last up item are items that nobody else would do)
+                    int n = c;
+                    const bool won = lane == from && __hip_atomic_compare_exchange_strong(
+                        firsts + from * FEW_LINE, &n, c + 1, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
+                        __HIP_MEMORY_SCOPE_AGENT);
+                    if (__ballot(won)) {
+                        i = FEW_QUEUES * __builtin_amdgcn_readlane(c, from) + from;
                         break;
                     }
                 }

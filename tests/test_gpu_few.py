@@ -334,3 +334,34 @@ def test_agrees_with_the_separate_calls():
     assert (w - r.w[:T]).abs().max() < 1e-5
     # H, each expert's output and Y rounded to bf16 there, Y alone here
     assert (Y.float() - r.Y[:T].float()).abs().max() <= 4 * 2.0 ** -8 * Y.float().abs().max()
+
+
+def test_workgroups_that_start_late():
+    """Beside joins whose workgroups leave no room on a CU (143 KB of its LDS): workgroups of a call start in
+    dribs, after others have done the items that they would have begun with; none is done twice or left."""
+    T, d = 6144, 7168
+    j = B.join(T, d, y_norm="layer", r_norm="layer")
+    x, y, out, h = (torch.zeros(T, d, dtype=torch.bfloat16, device=DEV) for _ in range(4))
+    weights = {n: torch.ones(d, device=DEV) for n in B.JOIN_PARAMS if n != "token_gate"}
+    params = B.join_params(**weights)
+    # items of the up product fewer than the workgroups, about as many, and more
+    cases = (Case(2, 512, 16, 2, 512), Case(16, 1024, 32, 4, 768, 256), Case(16, 2048, 64, 4, 1536))
+    runs = [(Run(c, inputs(c, 5)), Run(c, inputs(c, 5))) for c in cases]
+    for r, _ in runs:
+        r.call()
+    torch.cuda.synchronize()
+    joins, few = torch.cuda.Stream(), torch.cuda.Stream()
+    for turn in range(10):
+        for r, other in runs:
+            other.Y[:other.c.T].fill_(777.0)
+            for s in (joins, few):
+                s.wait_stream(torch.cuda.current_stream())
+            for _ in range(3):
+                B.moe_join_forward(j, x, y, params, None, out, h, None, stream=joins)
+                other.call(few)
+            for s in (joins, few):
+                torch.cuda.current_stream().wait_stream(s)
+            torch.cuda.synchronize()
+            for a, b in zip(r.outputs(), other.outputs()):
+                assert torch.equal(a, b), (turn, r.c)
+            other.check_guards()
