@@ -635,8 +635,8 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
  * is kept to 16 significant bits, sums are fp32, and Y is rounded once.  An expert
  * reaches the tokens that chose it alone, also where its values are infinite or NaN.
  *   ws: at least moe_few_workspace_bytes(shape) bytes, holding anything; calls that
- *   can overlap need one each.  Its first int32 is not 0 after a call whose waits between
- *   workgroups gave up (the outputs are then invalid). */
+ *   can overlap need one each.  Its first int32 is 0 after a call (T = 0 leaves it), and
+ *   something else if waits between workgroups gave up (the outputs are then invalid). */
 size_t moe_few_workspace_bytes(const moe_shape *shape);   /* 0: invalid or unsupported; never falls with T */
 moe_status moe_forward_few(const moe_shape *shape, const moe_routing *routing, const moe_bf16 *X,
                            const moe_bf16 *W_r, const float *bias, const float *balance,

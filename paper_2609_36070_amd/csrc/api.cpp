@@ -2020,6 +2020,8 @@ moe_status moe_forward_few(const moe_shape *shape, const moe_routing *routing, c
     g.Wg_s = weights->Wg_s; g.Wu_s = weights->Wu_s; g.Wd_s = weights->Wd_s;
     g.logits = logits; g.topk_idx = topk_idx; g.topk_w = topk_w; g.Y = Y;
     g.pitch = (g.T * g.E + 3) / 4 * 4;
+    g.err = static_cast<int *>(ws);
+    ws = reinterpret_cast<void *>((reinterpret_cast<uintptr_t>(ws) + 4 + FEW_ALIGN - 1) / FEW_ALIGN * FEW_ALIGN);
     g.counters = at<int>(ws, L.counters);
     g.ncounters = L.ncounters; g.up_counters = L.up_counters;
     g.part = at<float>(ws, L.part); g.up_part = at<float>(ws, L.up_part);

@@ -45,26 +45,30 @@ struct FewLayout {
     long counters, part, up_part, h, y_part, total;    // byte offsets
     int ncounters, up_counters;
 };
-// counters: error word, items taken, first items taken; tiles of H per expert slot (shared first),
-// polled, so a line each; slices done per up tile, per down tile
+// counters: items taken, first items taken; tiles of H per expert slot (shared first),
+// polled, so a line each; slices done per up tile, per down tile.
+// All of it lies behind the workspace's first int32, the error word, from the next multiple
+// of FEW_ALIGN bytes on: no cache line may hold what two tiles leave, or a workgroup that
+// reads the one would go on reading the other as it was before it was there.
+constexpr int FEW_ALIGN = 256;
 FEW_FN FewLayout few_layout(long T, long d, long E, long k, long f, long fs) {
     const long slots = E < T * k ? E : T * k;
     const long up_tiles = slots * (f / FEW_UP_COLS) + fs / FEW_UP_COLS, down_tiles = d / FEW_DOWN_COLS;
     const long units = slots * (f / FEW_UNIT) + fs / FEW_UNIT;
     FewLayout L;
-    long o = 0;
+    long o = 0;                      // from the aligned address
     auto take = [&](long bytes) {
         const long at = o;
-        o += (bytes + 255) / 256 * 256;
+        o += (bytes + FEW_ALIGN - 1) / FEW_ALIGN * FEW_ALIGN;
         return at;
     };
     L.up_counters = (int)(up_tiles < FEW_UP_ITEMS ? up_tiles : FEW_UP_ITEMS);
-    L.ncounters = (int)((2 + FEW_QUEUES + 257) * FEW_LINE + L.up_counters + down_tiles);
+    L.ncounters = (int)((1 + FEW_QUEUES + 257) * FEW_LINE + L.up_counters + down_tiles);
     L.counters = take(4l * L.ncounters);
     L.part = take(4l * FEW_ROUTER_SLICES * ((T * E + 3) / 4 * 4));
     L.up_part = take(few_sliced(up_tiles, FEW_UP_ITEMS) * T * 2 * FEW_UP_COLS * 4);
     L.h = take(units * T * FEW_UNIT * 2 * 2);
     L.y_part = take(few_sliced(down_tiles, FEW_DOWN_ITEMS) * T * FEW_DOWN_COLS * 4);
-    L.total = o;
+    L.total = o + FEW_ALIGN + 4;
     return L;
 }

@@ -95,8 +95,10 @@ __global__ __launch_bounds__(64 * RW) void few_router_kernel(FewArgs g) {
             }
         }
     }
-    if (blockIdx.x == 0 && blockIdx.y == 0)
+    if (blockIdx.x == 0 && blockIdx.y == 0) {
+        if (tid == 0) *g.err = 0;
         for (int i = tid; i < g.ncounters; i += 64 * RW) g.counters[i] = 0;
+    }
     // accumulators: lane (g4, r), register p of product i: expert V (4 g4 + p) + i, token r
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -344,8 +346,8 @@ DEV void weigh_experts(const FewArgs &g, Select &s, int tid) {
 // Waits between workgroups.  What one workgroup writes for others goes through
 // its XCD's L2 to memory (agent-scope stores); its waves wait for that, meet at a
 // barrier, and one thread adds to a counter.  A consumer's thread polls the counter
-// and its workgroup passes a barrier; what it then loads was never read before in
-// this launch, so no cache holds an older copy.  A release and an acquire
+// and its workgroup passes a barrier; what it then loads, whole lines, was never read
+// before in this launch, so no cache holds an older copy.  A release and an acquire
 // instead write back and invalidate whole caches: 2 to 5 us for each tile.  Waits
 // end after 2 s in any case (wall clock of 100 MHz), with the error word set.
 constexpr unsigned long long WAIT_TICKS = 200000000ull;
@@ -390,7 +392,7 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g4 = lane >> 4;
     const int T = g.T, d = g.d, f = g.f, fs = g.fs;
-    int *err = g.counters, *queue = err + FEW_LINE, *h_done = queue + (1 + FEW_QUEUES) * FEW_LINE;
+    int *err = g.err, *queue = g.counters, *h_done = queue + (1 + FEW_QUEUES) * FEW_LINE;
     int *up_done = h_done + 257 * FEW_LINE, *down_done = up_done + g.up_counters;
 
     // A workgroup's first item comes from one of FEW_QUEUES counters (item FEW_QUEUES i +

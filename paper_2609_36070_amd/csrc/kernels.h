@@ -347,6 +347,7 @@ struct FewArgs {
     float *logits = nullptr, *topk_w = nullptr;
     int *topk_idx = nullptr;
     uint16_t *Y = nullptr;
+    int *err = nullptr;
     int *counters = nullptr;           // see few.h
     int ncounters = 0, up_counters = 0, pitch = 0;   // pitch: floats between slices of part
     float *part = nullptr, *up_part = nullptr, *y_part = nullptr;

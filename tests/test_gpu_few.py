@@ -287,6 +287,23 @@ def test_repeats_streams_and_several_at_once():
         other.check_guards()
 
 
+@pytest.mark.parametrize("offset", [16, 64, 112, 240])
+def test_workspaces_of_any_alignment(offset):
+    """A workspace from any multiple of 16 bytes: the same bits, and nothing past its end."""
+    for c in (Case(7, 1024, 32, 4, 512, 256), Case(3, 2048, 16, 4, 768)):
+        inp = inputs(c, 6)
+        r, other = Run(c, inp), Run(c, inp)
+        other.ws = torch.full((other.nbytes + 512,), 0xA5, dtype=torch.uint8, device=DEV)[offset:]
+        assert other.ws.data_ptr() % 256 == offset
+        r.call()
+        for _ in range(3):
+            other.call()
+            torch.cuda.synchronize()
+            for a, b in zip(r.outputs(), other.outputs()):
+                assert torch.equal(a, b)
+            other.check_guards()
+
+
 def test_captured_and_replayed():
     c = Case(5, 1024, 40, 5, 512, 256, "sigmoid", 4, 2, "pair", True, 2.0, 0.1)
     r, ref = Run(c, inputs(c)), Run(c, inputs(c))
