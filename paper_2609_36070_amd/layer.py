@@ -319,7 +319,7 @@ class DeviceBlock:
         self.first_params = B.join_params(**self.first_tensors)
         self.params = B.join_params(**self.tensors)
         # seed and offset; a program moves the offset on from step to step
-        self.rng = torch.tensor([seed, 0], dtype=torch.int64, device=dev) if drop >= 2.0 ** -17 else None
+        self.rng = torch.tensor([seed, 0], dtype=torch.int64, device=dev) if self.join.drop >= 2.0 ** -17 else None
         self.r, self.h = _empty((T, d), kind, dev), _empty((T, d), torch.bfloat16, dev)
         self.first_stats = self.stats = None
         if backward:
