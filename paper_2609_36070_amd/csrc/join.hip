@@ -529,13 +529,17 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (g.y_norm) y[c] = LAYER ? (y[c] - ym) * ys : y[c] * ys;
-            f32x8 n = y[c], w, e = D[c] * f;             // e: of the kept elements, without gates
-            if (g.rng) e = drop8(e, philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t), g.out);
+            f32x8 n = y[c], w, e = D[c] * f;             // of the kept elements; e without gates
             if (g.y_weight) {
                 w = weight(YW, c);
                 n = n * w;
             }
             if (g.y_bias) n = n + weight(YB, c);
+            if (g.rng) {
+                const Words bits = philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t);
+                e = drop8(e, bits, g.out);
+                n = drop8(n, bits, g.out);               // (what is infinite or NaN there is left out)
+            }
             if (g.dtoken_gate) {
                 f32x8 ge = e;
                 if (g.gate) ge = ge * weight(GATE, c);
@@ -646,8 +650,13 @@ __global__ __launch_bounds__(256) void join_columns_kernel(JoinArgs g) {
         f32x8 y = yr.get();
         if (g.y_norm) y = (y - st[0]) * st[1];
         f32x8 e = D * (g.scale * g.keep * (g.token_gate ? g.token_gate[t] : 1.f));
-        if (g.rng) e = drop8(e, philox(seed, offset, (uint32_t)col / 8, (uint32_t)t), g.out);
-        sum[2] = sum[2] + (y * yw + yb) * e;
+        f32x8 n = y * yw + yb;
+        if (g.rng) {
+            const Words bits = philox(seed, offset, (uint32_t)col / 8, (uint32_t)t);
+            e = drop8(e, bits, g.out);
+            n = drop8(n, bits, g.out);
+        }
+        sum[2] = sum[2] + n * e;
         e = e * gt;
         sum[3] = sum[3] + e * y;
         sum[4] = sum[4] + e;

@@ -288,6 +288,26 @@ def test_rows_that_are_zero_infinite_or_nan():
     assert torch.equal(run.r[:4][gone], run.x[gone]) and run.r[:4][~gone].isnan().all()
 
 
+@pytest.mark.parametrize("c", [Case(37, 64, "f32", "none", "rms", True, True, drop=0.5),
+                               Case(300, 1000, "bf16", "none", "layer", True, True, 0.7, 0.25),
+                               Case(20, 9000, "bf16", "none", "none", True, True, 1.0, 0.5)],
+                         ids=lambda c: str(c.d))
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_dropped_values_reach_no_gradient(c, value):
+    """What dropout takes out of y is nothing to the gates' gradients either, whatever it was."""
+    runs = [Run(c), Run(c)]
+    gone = torch.from_numpy(J.keep_mask(c.T, c.d, c.drop, *runs[0].key) == 0).to(DEV)
+    for run, v in zip(runs, (0.0, value)):
+        run.y[gone] = v
+        run.forward()
+        run.backward()
+    torch.cuda.synchronize()
+    zero, other = (run.outputs() for run in runs)
+    assert other["gate"].isfinite().all() and other["token_gate"].isfinite().all()
+    for n in zero:
+        assert torch.equal(zero[n], other[n]), n
+
+
 def test_no_rows():
     c = Case(0, 64, "f32", "layer", "layer", True)
     run = Run(c)
