@@ -33,6 +33,7 @@
 // Tried and slower: 1024 threads of 8 values for such a row (128 registers; 378 us), rows
 // of two workgroups on a CU, each with its own sums (390).
 #include <algorithm>
+#include <cfloat>
 
 #include "common.h"
 #include "kernels.h"
@@ -449,14 +450,20 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
     load_r(row);
     load_dr(row);
     load_y(row);
+    bool odd_weights = true;                 // infinite or NaN ones, of y's norm (true where nobody asks)
     if constexpr (LDS_W) {
+        bool odd = false;
 #pragma unroll
         for (int a = 0; a < 4; ++a)
             if (weights[a])
-                for (int j = threadIdx.x; j < g.d / 4; j += NT)
-                    *reinterpret_cast<f32x4_t *>(cols + at[a] + (j & 1) * (g.d / 2) + 4 * (j >> 1)) =
-                        *reinterpret_cast<const f32x4_t *>(weights[a] + 4 * j);
-        __syncthreads();
+                for (int j = threadIdx.x; j < g.d / 4; j += NT) {
+                    const f32x4_t v = *reinterpret_cast<const f32x4_t *>(weights[a] + 4 * j);
+                    *reinterpret_cast<f32x4_t *>(cols + at[a] + (j & 1) * (g.d / 2) + 4 * (j >> 1)) = v;
+                    if (CH > 1 && (a == YW || a == YB))
+                        for (int q = 0; q < 4; ++q) odd = odd || !(fabsf(v[q]) <= FLT_MAX);
+                }
+        if constexpr (CH > 1) odd_weights = __syncthreads_or(odd);
+        else __syncthreads();
     }
     for (long k = 0; k < rounds; ++k, row += step) {
         const bool on = row < g.T;
@@ -524,21 +531,34 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
         const float tg = g.token_gate ? g.token_gate[t] : 1.f;
         // the token's gate comes last where its own gradient is wanted
         const float f = g.dtoken_gate ? g.scale * g.keep : g.scale * g.keep * tg;
+        // What dropout has taken out is 0 for the gates too, also where it is infinite or NaN.
+        // Longer rows have no registers for the words that long (16384 x 7168: 339 us, 311 this way)
+        // and make them again if a row needs it: one with such values has no finite deviation.
+        constexpr bool WORDS = CH == 1;
+        bool odd = false;
+        if constexpr (!WORDS) odd = g.rng && __ballot(!g.y_norm || odd_weights || !(ys > 0.f && ys <= FLT_MAX));
         float s[LAYER ? 3 : 2] = {};                     // the last one: of the token's gate
         constexpr int TG = LAYER ? 2 : 1;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (g.y_norm) y[c] = LAYER ? (y[c] - ym) * ys : y[c] * ys;
-            f32x8 n = y[c], w, e = D[c] * f;             // of the kept elements; e without gates
+            f32x8 n = y[c], w, e = D[c] * f;             // e: of the kept elements, without gates
+            Words bits;
+            if (g.rng) {
+                bits = philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t);
+                e = drop8(e, bits, g.out);
+            }
             if (g.y_weight) {
                 w = weight(YW, c);
                 n = n * w;
             }
             if (g.y_bias) n = n + weight(YB, c);
-            if (g.rng) {
-                const Words bits = philox(seed, offset, (uint32_t)col[c] / 8, (uint32_t)t);
-                e = drop8(e, bits, g.out);
-                n = drop8(n, bits, g.out);               // (what is infinite or NaN there is left out)
+            if constexpr (WORDS) {
+                if (g.rng) n = drop8(n, bits, g.out);
+            } else if (odd) {
+                uint32_t j = (uint32_t)col[c] / 8;
+                asm volatile("" : "+v"(j));
+                n = drop8(n, philox(seed, offset, j, (uint32_t)t), g.out);
             }
             if (g.dtoken_gate) {
                 f32x8 ge = e;

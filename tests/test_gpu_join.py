@@ -290,6 +290,7 @@ def test_rows_that_are_zero_infinite_or_nan():
 
 @pytest.mark.parametrize("c", [Case(37, 64, "f32", "none", "rms", True, True, drop=0.5),
                                Case(300, 1000, "bf16", "none", "layer", True, True, 0.7, 0.25),
+                               Case(20, 7000, "bf16", "none", "rms", True, True, 0.7, 0.25),
                                Case(20, 9000, "bf16", "none", "none", True, True, 1.0, 0.5)],
                          ids=lambda c: str(c.d))
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
@@ -306,6 +307,31 @@ def test_dropped_values_reach_no_gradient(c, value):
     assert other["gate"].isfinite().all() and other["token_gate"].isfinite().all()
     for n in zero:
         assert torch.equal(zero[n], other[n]), n
+
+
+@pytest.mark.parametrize("d", [512, 5000])
+@pytest.mark.parametrize("where", ["y", "y_weight", "y_bias"])
+def test_dropped_values_of_a_norm(d, where):
+    """A NaN that y's norm spreads over a row, or its weights over a column, reaches the gates' sums of the
+    elements that were kept and no others."""
+    c = Case(9, d, "f32", "layer", "none", True, True, 1.0, 0.5)
+    run = Run(c)
+    gone = J.keep_mask(c.T, d, 0.5, *run.key) == 0
+    if where == "y":
+        run.y[4, 17] = float("nan")
+        bad = np.zeros((9, d), bool)
+        bad[4] = True
+    else:
+        run.p[where][17] = float("inf")
+        bad = np.zeros((9, d), bool)
+        bad[:, 17] = True
+    run.forward()
+    run.backward()
+    torch.cuda.synchronize()
+    bad &= ~gone
+    for n, axis in (("gate", 0), ("token_gate", 1)):
+        got = ~np.isfinite(to_np(run.g[n])[:bad.shape[1 - axis]])
+        assert np.array_equal(got, bad.any(axis)), n
 
 
 def test_no_rows():
