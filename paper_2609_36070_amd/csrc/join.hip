@@ -591,12 +591,13 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
         }
     }
     // ---- the workgroup's sums over its rows: the rows of a wave, then the others' in
-    // order, to `part`
+    // order, to `part`, or where they belong if it is the only one
     constexpr int STEP = G < 64 ? 64 : G, TURNS = NT / STEP;
     int n = 0;
 #pragma unroll
     for (int a = 0; a < 5; ++a) {
         if (!(SUMS >> a & 1) || !(sums >> a & 1)) continue;
+        float *to = gridDim.x == 1 ? g.out_sums[n] : g.part + ((long)blockIdx.x * g.nsums + n) * g.d;
 #pragma unroll
         for (int m = G; m < 64; m <<= 1)
 #pragma unroll
@@ -612,7 +613,7 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
                         f32x8 v = sum[a][c];
                         if (q > 0) v = ld_f32x8(cols + col[c]) + v;
                         if (q < TURNS - 1) st_f32x8(cols + col[c], v);
-                        else st_f32x8(g.part + ((long)blockIdx.x * g.nsums + n) * g.d + col[c], v);
+                        else st_f32x8(to + col[c], v);
                     }
         }
         ++n;
@@ -840,7 +841,7 @@ hipError_t launch_join_backward(JoinArgs g, hipStream_t st) {
         const hipError_t e = g.f32 ? backward<true>(g, blocks, st) : backward<false>(g, blocks, st);
         if (e != hipSuccess) return e;
     }
-    if (!g.nsums) return hipSuccess;
+    if (!g.nsums || (blocks == 1 && g.d <= JOIN_SUMS_D)) return hipSuccess;
     join_sum_kernel<<<dim3((unsigned)((g.d + 4 * JS_QUADS - 1) / (4 * JS_QUADS)), (unsigned)g.nsums), dim3(256), 0, st>>>(
         g, blocks);
     return hipGetLastError();

@@ -379,6 +379,9 @@ constexpr long JOIN_MAX_D = 16384, JOIN_SUMS_D = 8192;
 // workgroups, which leave a row of sums each: one to a CU where a row takes 512 threads,
 // else three, if each has 4 rounds of rows left (us with 256 / 768: 16384 x 2048 116 /
 // 100, 20000 x 1024 75 / 66, 40000 x 512 80 / 67, 100000 x 64 114 / 29, 4000 x 2048 32 / 34).
+// Two rounds of rows go to one workgroup up to 4096 columns: it writes the sums itself, without
+// the launch that adds them up (us, 2 workgroups / one: 64 rows of 64 10.6 / 9.0, 2 of 2048
+// 9.6 / 8.3, 2 of 4096 10.9 / 9.8, 2 of 7168 17.4 / 19.3; four rounds 9.6 / 12.2).
 inline long join_row_threads(long d) {
     long g = 8;
     while (g < 512 && 8 * g < d) g *= 2;
@@ -387,5 +390,6 @@ inline long join_row_threads(long d) {
 inline long join_threads(long d) { return join_row_threads(d) < 256 ? 256 : join_row_threads(d); }
 inline long join_workgroups(long T, long d) {
     const long rows = join_threads(d) / join_row_threads(d), n = (T + rows - 1) / rows;
+    if (n <= 2 && d <= 4096) return 1;
     return n <= 256 ? n : std::min(join_threads(d) < 512 ? 768L : 256L, std::max(256L, n / 4));
 }

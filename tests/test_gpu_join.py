@@ -179,6 +179,17 @@ def test_against_the_definition(c):
     check(run)
 
 
+@pytest.mark.parametrize("T, d", [(32, 64), (33, 64), (64, 64), (65, 64), (16, 256), (17, 256), (2, 2048), (3, 2048),
+                                  (2, 4096), (3, 4096), (1, 7168), (2, 7168)])
+def test_a_workgroup_or_more(T, d):
+    """Rows that one workgroup takes, which leaves the sums itself, and those past them."""
+    run = Run(Case(T, d, "bf16", "layer", "layer", True, True, 0.5, 0.1))
+    run.forward()
+    run.backward()
+    torch.cuda.synchronize()
+    check(run)
+
+
 def test_repeats_bit_for_bit_and_on_another_stream():
     for c in (Case(1111, 2048, "f32", "layer", "rms", True, True, 0.5, 0.1), Case(600, 8400, token_gate=True, drop=0.1)):
         repeat(c)
