@@ -386,7 +386,7 @@ JoinArgs join_args(const moe_join &j, const moe_join_params &p, const moe_bf16 *
     return g;
 }
 
-size_t join_part_bytes(const moe_join &j) { return up((size_t)join_blocks(j.T, (int)j.d) * 5 * (size_t)j.d * 4 + 16); }
+size_t join_part_bytes(const moe_join &j) { return up((size_t)join_part_rows(j.T, j.d) * 5 * (size_t)j.d * 4 + 16); }
 size_t join_bytes(const moe_join &j) {
     return join_part_bytes(j) + (j.d > JOIN_SUMS_D ? up((size_t)j.T * 8) : 0);
 }

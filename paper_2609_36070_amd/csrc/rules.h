@@ -376,20 +376,29 @@ inline bool join_forward_rows(long T, long d, int weights, bool block) {
 // Row lengths: what a workgroup's registers hold; with the sums over the rows beside it.
 constexpr long JOIN_MAX_D = 16384, JOIN_SUMS_D = 8192;
 // The backward: threads of a row (8 values each up to 4096), of a workgroup, and the
-// workgroups, which leave a row of sums each: one to a CU where a row takes 512 threads,
-// else three, if each has 4 rounds of rows left (us with 256 / 768: 16384 x 2048 116 /
-// 100, 20000 x 1024 75 / 66, 40000 x 512 80 / 67, 100000 x 64 114 / 29, 4000 x 2048 32 / 34).
+// workgroups, which leave a row of sums each.  Up to 512 of them (384 of longer rows) have rows
+// for one round and read the weights where they lie (us, 256 with several rounds / these: 600 x
+// 1000 15.3 / 13.6, 1024 x 1000 15.7 / 15.5, 512 x 2048 17.7 / 16.3, 300 x 4096 20.2 / 18.1, 512 x 4096 20.4
+// / 22.9, 300 x 7168 39 / 29; 800 x 2048 20.7 / 20.7, 800 x 7168 60 / 64).  Beyond, one to a CU where a
+// row takes 512 threads, else three, if each has 4 rounds of rows left (us with 256 / 768: 16384 x
+// 2048 116 / 100, 20000 x 1024 75 / 66, 40000 x 512 80 / 67, 100000 x 64 114 / 29, 4000 x 2048 32 / 34).
 // Two rounds of rows go to one workgroup up to 4096 columns: it writes the sums itself, without
-// the launch that adds them up (us, 2 workgroups / one: 64 rows of 64 10.6 / 9.0, 2 of 2048
-// 9.6 / 8.3, 2 of 4096 10.9 / 9.8, 2 of 7168 17.4 / 19.3; four rounds 9.6 / 12.2).
+// the launch that adds them up (us, 2 workgroups / one: 64 rows of 64 11 / 9.0, 2 of 2048
+// 10.2 / 8.7, 2 of 4096 10.2 / 10.0, 2 of 7168 12 / 19).
 inline long join_row_threads(long d) {
     long g = 8;
     while (g < 512 && 8 * g < d) g *= 2;
     return g;
 }
 inline long join_threads(long d) { return join_row_threads(d) < 256 ? 256 : join_row_threads(d); }
+inline long join_rows(long d) { return join_threads(d) / join_row_threads(d); }   // of a workgroup
 inline long join_workgroups(long T, long d) {
-    const long rows = join_threads(d) / join_row_threads(d), n = (T + rows - 1) / rows;
+    const long n = (T + join_rows(d) - 1) / join_rows(d);
     if (n <= 2 && d <= 4096) return 1;
-    return n <= 256 ? n : std::min(join_threads(d) < 512 ? 768L : 256L, std::max(256L, n / 4));
+    if (n <= (d <= 2048 ? 512 : d <= JOIN_SUMS_D ? 384 : 256)) return n;
+    return std::min(d <= 2048 ? 768L : 256L, std::max(256L, n / 4));
+}
+// At least as many, and never fewer for more rows: what the workspace is made for.
+inline long join_part_rows(long T, long d) {
+    return std::min((T + join_rows(d) - 1) / join_rows(d), d <= 2048 ? 768L : 384L);
 }

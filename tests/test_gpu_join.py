@@ -180,13 +180,18 @@ def test_against_the_definition(c):
 
 
 @pytest.mark.parametrize("T, d", [(32, 64), (33, 64), (64, 64), (65, 64), (16, 256), (17, 256), (2, 2048), (3, 2048),
-                                  (2, 4096), (3, 4096), (1, 7168), (2, 7168)])
-def test_a_workgroup_or_more(T, d):
-    """Rows that one workgroup takes, which leaves the sums itself, and those past them."""
+                                  (2, 4096), (3, 4096), (1, 7168), (2, 7168), (1023, 1000), (1027, 1000), (512, 2048),
+                                  (513, 2048), (384, 4096), (385, 4096), (384, 7168), (385, 7168), (300, 8200)])
+def test_a_workgroup_a_round_or_more(T, d):
+    """Rows that one workgroup takes, which leaves the sums itself, those for which there is one round, and
+    those past them; nothing is written past the workspace."""
     run = Run(Case(T, d, "bf16", "layer", "layer", True, True, 0.5, 0.1))
+    n = B.moe_join_workspace_bytes(run.join)
+    run.ws = torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
     run.forward()
     run.backward()
     torch.cuda.synchronize()
+    assert (run.ws[n:] == 0xA5).all()
     check(run)
 
 
