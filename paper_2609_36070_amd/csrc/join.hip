@@ -623,7 +623,7 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
 
 // Rows longer than 8192, whose sums the registers above cannot hold: the sums alone,
 // with the rows' means that the kernel above has left.  A wave takes 512 columns of every
-// fourth row of its workgroup's share.  4096 rows of 12288: 344 us in all, 629 in one
+// fourth row of its workgroup's share.  4096 rows of 12288: 350 us in all, 629 in one
 // kernel whose sums went to memory; 604 MB and, for the sums, 403 of them again.
 template <bool F32>
 __global__ __launch_bounds__(256) void join_columns_kernel(JoinArgs g) {
