@@ -301,12 +301,15 @@ class DeviceBlock:
     def __init__(self, w: Workload, inputs: dict, params: dict | None = None, stream="bf16", in_norm="rms",
                  y_norm="none", r_norm="rms", eps=1e-6, scale=1.0, drop=0.0, seed=0, device="cuda",
                  with_backward=None, **layer_options):
+        params = params or {}
+        unknown = sorted(set(params) - {"in_weight", "in_bias", *B.JOIN_PARAMS})
+        if unknown:
+            raise ValueError(f"no parameters of a block: {unknown}")
         backward = w.backward if with_backward is None else with_backward
         self.few = not backward and 0 < w.T <= 16
         self.layer = L = DeviceLayer(w, inputs, device, with_backward=backward, few=self.few, **layer_options)
         dev, T, d = L.device, w.T, w.d
         kind = torch.float32 if stream == "f32" else torch.bfloat16
-        params = params or {}
         up = {n: None if v is None else torch.from_numpy(np.ascontiguousarray(v, np.float32)).to(dev)
               for n, v in params.items()}
         self.x = _empty((T, d), kind, dev)

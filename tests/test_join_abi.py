@@ -94,3 +94,10 @@ def test_workspace_never_falls(d):
 
 def test_empty_forward_is_accepted():
     assert _forward(_join(T=0)) == B.MOE_OK
+
+
+def test_a_block_refuses_parameters_that_it_does_not_have():
+    from paper_2609_36070_amd.layer import DeviceBlock
+    from paper_2609_36070_amd.workloads import Workload
+    with pytest.raises(ValueError, match="y_wieght"):
+        DeviceBlock(Workload("few", T=6, d=256, E=8, k=2, f=256), {}, {"y_wieght": None, "gate": None}, device="cpu")
