@@ -560,6 +560,7 @@ __global__ __launch_bounds__(NT, 2) void few_kernel(FewArgs g) {
     const uint16_t *H = g.H;
 
     int q = __builtin_amdgcn_readfirstlane(s_next);
+    __syncthreads();                            // the search below and the first item's end write s_next again
     Item it = decode(q);
     const uint16_t *np = it.up ? up_ptr(it) : g.X;
     long nld = it.up ? (it.slot < 0 ? fs : f) : 0;
