@@ -451,7 +451,9 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
     load_r(row);
     load_dr(row);
     load_y(row);
-    bool odd_weights = true;                 // infinite or NaN ones, of y's norm (true where nobody asks)
+    // Weights of y's norm that can make a finite row infinite, NaN ones too (true where nobody asks):
+    // its values are within sqrt(d) < 2^7 deviations, so 2^119 leaves all of them below 2^127.
+    bool odd_weights = true;
     if constexpr (LDS_W) {
         bool odd = false;
 #pragma unroll
@@ -461,7 +463,7 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
                     const f32x4_t v = *reinterpret_cast<const f32x4_t *>(weights[a] + 4 * j);
                     *reinterpret_cast<f32x4_t *>(cols + at[a] + (j & 1) * (g.d / 2) + 4 * (j >> 1)) = v;
                     if (CH > 1 && (a == YW || a == YB))
-                        for (int q = 0; q < 4; ++q) odd = odd || !(fabsf(v[q]) <= FLT_MAX);
+                        for (int q = 0; q < 4; ++q) odd = odd || !(fabsf(v[q]) <= 0x1p119f);
                 }
         if constexpr (CH > 1) odd_weights = __syncthreads_or(odd);
         else __syncthreads();
@@ -534,7 +536,7 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
         const float f = g.dtoken_gate ? g.scale * g.keep : g.scale * g.keep * tg;
         // What dropout has taken out is 0 for the gates too, also where it is infinite or NaN.
         // Longer rows have no registers for the words that long (16384 x 7168: 339 us, 311 this way)
-        // and make them again if a row needs it: one with such values has no finite deviation.
+        // and make them again if a row needs it: one with such values has no finite deviation, or large weights.
         constexpr bool WORDS = CH == 1;
         bool odd = false;
         if constexpr (!WORDS) odd = g.rng && __ballot(!g.y_norm || odd_weights || !(ys > 0.f && ys <= FLT_MAX));
