@@ -296,7 +296,8 @@ class DeviceBlock:
     r goes on as the stream and h into the next block.  The layer's inputs["X"] is
     the stream x; params holds numpy arrays: in_weight and in_bias of the first
     norm, and those of the join (binding.JOIN_PARAMS), each optional.  With up
-    to 16 tokens and no backward the layer runs as step_few."""
+    to 16 tokens and no backward the layer runs as step_few.  layer_options are
+    DeviceLayer's; the experts run in bf16, and mx, mx_wgrad and int8 are refused."""
 
     def __init__(self, w: Workload, inputs: dict, params: dict | None = None, stream="bf16", in_norm="rms",
                  y_norm="none", r_norm="rms", eps=1e-6, scale=1.0, drop=0.0, seed=0, device="cuda",
@@ -305,6 +306,9 @@ class DeviceBlock:
         unknown = sorted(set(params) - {"in_weight", "in_bias", *B.JOIN_PARAMS})
         if unknown:
             raise ValueError(f"no parameters of a block: {unknown}")
+        other = sorted(n for n in ("mx", "mx_wgrad", "int8") if layer_options.get(n))
+        if other:
+            raise ValueError(f"a block's experts are in bf16: {other}")
         backward = w.backward if with_backward is None else with_backward
         self.few = not backward and 0 < w.T <= 16
         self.layer = L = DeviceLayer(w, inputs, device, with_backward=backward, few=self.few, **layer_options)
