@@ -296,8 +296,9 @@ class DeviceBlock:
     r goes on as the stream and h into the next block.  The layer's inputs["X"] is
     the stream x; params holds numpy arrays: in_weight and in_bias of the first
     norm, and those of the join (binding.JOIN_PARAMS), each optional.  With up
-    to 16 tokens and no backward the layer runs as step_few.  layer_options are
-    DeviceLayer's; the experts run in bf16, and mx, mx_wgrad and int8 are refused."""
+    to 16 tokens, no backward and no ring_rows the layer runs as step_few.
+    layer_options are DeviceLayer's; the experts run in bf16, and mx, mx_wgrad and
+    int8 are refused."""
 
     def __init__(self, w: Workload, inputs: dict, params: dict | None = None, stream="bf16", in_norm="rms",
                  y_norm="none", r_norm="rms", eps=1e-6, scale=1.0, drop=0.0, seed=0, device="cuda",
@@ -310,7 +311,7 @@ class DeviceBlock:
         if other:
             raise ValueError(f"a block's experts are in bf16: {other}")
         backward = w.backward if with_backward is None else with_backward
-        self.few = not backward and 0 < w.T <= 16
+        self.few = not backward and 0 < w.T <= 16 and layer_options.get("ring_rows") is None
         self.layer = L = DeviceLayer(w, inputs, device, with_backward=backward, few=self.few, **layer_options)
         dev, T, d = L.device, w.T, w.d
         kind = torch.float32 if stream == "f32" else torch.bfloat16
