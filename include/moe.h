@@ -634,6 +634,7 @@ moe_status moe_forward_int(const moe_shape *shape, const moe_bf16 *X, const moe_
  * limits are the layer's.  Results are those of the definition: the gated activation
  * is kept to 16 significant bits, sums are fp32, and Y is rounded once.  An expert
  * reaches the tokens that chose it alone, also where its values are infinite or NaN.
+ * No plan and no activations are left for a backward.
  *   ws: at least moe_few_workspace_bytes(shape) bytes, holding anything; calls that
  *   can overlap need one each.  Its first int32 is 0 after a call (T = 0 leaves it), and
  *   something else if waits between workgroups gave up (the outputs are then invalid). */

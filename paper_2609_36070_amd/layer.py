@@ -38,7 +38,8 @@ class DeviceLayer:
         mx_wgrad: the MXFP8 backward computes its weight gradients in MXFP8.
         routing: route by scores (a MoeRouting), with inputs["balance"] if given.
         int8: the experts in 8-bit integers too (forward_int, step_int).
-        few: up to 16 tokens in two launches too (step_few)."""
+        few: up to 16 tokens in two launches too (step_few); for inference, without a
+        backward."""
         self.w = w
         self.mx = mx
         self.routing = routing
@@ -98,6 +99,7 @@ class DeviceLayer:
                 raise ValueError(f"shape unsupported in int8 {w}")
             nbytes = max(nbytes, int_bytes)
         if few:
+            self._no_backward()
             few_bytes = B.moe_few_workspace_bytes(self.shape)
             if few_bytes == 0:
                 raise ValueError(f"not a shape of a few tokens {w}")
@@ -245,8 +247,14 @@ class DeviceLayer:
         B.moe_forward_int(self.shape, self.X, self.int_weights, self.topk_idx, self.topk_w,
                           self.plan_bufs, self.Y, self.ws, stream=stream, events=events)
 
+    def _no_backward(self):
+        if self.with_backward:
+            raise ValueError("the few-token path leaves nothing for a backward: the layer has to be without one")
+
     def step_few(self, stream=None):
-        """Route, plan and forward of up to 16 tokens in two launches."""
+        """Route, plan and forward of up to 16 tokens in two launches (inference: no plan and no activations
+        are left, and the workspace is written over)."""
+        self._no_backward()
         B.moe_forward_few(self.shape, B.routing() if self.routing is None else self.routing, self.X, self.W_r,
                           self.bias, self.balance, self.weights, self.logits, self.topk_idx, self.topk_w,
                           self.Y, self.ws, stream=stream)
