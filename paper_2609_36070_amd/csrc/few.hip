@@ -6,9 +6,12 @@
 // items from one queue: tiles of the up product (64 gate and 64 up columns, the
 // shared expert's first), then tiles of the down product (128 columns, over the
 // rows of all reached experts one after the other), each cut along K so that there
-// are enough of them.  A tile of the down product waits for the H of its rows.  An
-// item depends on items before it in the queue alone, which running workgroups have
-// taken, so no wait needs a workgroup that has not started.
+// are enough of them.  A tile of the down product waits for the H of its rows.  No
+// wait needs a workgroup that has not started, or one that waits itself: first items
+// come from counters of their own, out of the queue's order, so before its first wait
+// a workgroup sees every first item of the up product taken, and does those that are
+// not; the others are taken in order; and a workgroup that waits holds no item but the
+// one it waits for, since it asks for the next one afterwards.
 //
 // A tile's arithmetic: 4 waves take every fourth 32-row slice of K; a wave's step
 // is 32 rows x 128 columns, 8 loads of 16 bytes per lane straight into registers, 8

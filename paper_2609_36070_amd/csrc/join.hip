@@ -29,7 +29,11 @@
 // and those of the generator, 55 % of the SIMDs' time, between two sums over the row, so
 // what counts is that a row's loads are on their way during the row before it, and that
 // nothing waits behind them: weights from memory instead of LDS return after them (367
-// us), and so do registers that were spilt (1117 us with room for all five sums).
+// us), and so do registers that are spilt: sums that neither three of RMS norms (SUMS 13) nor
+// three of the sum's norm and the gate (7) cover take the form with room for all five, which
+// spills 38 of them at 4096 to 8192 columns, 88 with an fp32 stream.  The same size takes 690
+// (RMS, then layer norm) to 754 us (two layer norms) there, in fp32 999 to 1040; with three
+// sums in fp32, 11 spilt, 535.
 // Tried and slower: 1024 threads of 8 values for such a row (128 registers; 378 us), rows
 // of two workgroups on a CU, each with its own sums (390).
 #include <algorithm>
@@ -625,8 +629,9 @@ __global__ __launch_bounds__(NT) void join_backward_kernel(JoinArgs g) {
 
 // Rows longer than 8192, whose sums the registers above cannot hold: the sums alone,
 // with the rows' means that the kernel above has left.  A wave takes 512 columns of every
-// fourth row of its workgroup's share.  4096 rows of 12288: 350 us in all, 629 in one
-// kernel whose sums went to memory; 604 MB and, for the sums, 403 of them again.
+// fourth row of its workgroup's share.  4096 rows of 12288, three sums and dropout: 350 to 388 us in
+// all by the box, 629 in one kernel whose sums went to memory; 604 MB and, for the sums, 403
+// of them again.  Five sums 384 to 413; without dropout 283 and 307.  The row kernel spills 50 registers, 158 in fp32.
 template <bool F32>
 __global__ __launch_bounds__(256) void join_columns_kernel(JoinArgs g) {
     __shared__ __attribute__((aligned(16))) float red[3][512];
